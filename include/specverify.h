@@ -108,7 +108,7 @@ extern "C" {
 #define SPEC_API
 #endif
 
-#define SPEC_ABI_VERSION 5
+#define SPEC_ABI_VERSION 6
 #define SPEC_MAX_DRAFT 16        /* chain drafts per request */
 #define SPEC_MAX_TREE_NODES 32   /* token-tree nodes per request, root included */
 
@@ -117,7 +117,8 @@ typedef enum spec_status {
   SPEC_ERR_INVALID_ARG = 1,   /* a null pointer, size, stride or tree that breaks the contract */
   SPEC_ERR_UNSUPPORTED = 2,   /* valid but not built: head_dim not 64/128, a dtype/shape combination */
   SPEC_ERR_WORKSPACE = 3,     /* workspace or staging too small or misaligned */
-  SPEC_ERR_HIP = 4            /* a HIP runtime call failed (launch, copy) */
+  SPEC_ERR_HIP = 4,           /* a HIP runtime call failed (launch, copy) */
+  SPEC_ERR_NO_PAGES = 5       /* no free page left (speccache.h) */
 } spec_status_t;
 
 typedef enum spec_tree_rule {

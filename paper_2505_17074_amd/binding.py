@@ -12,7 +12,8 @@ import os
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libspecverify.so")
 
-SPEC_OK, SPEC_ERR_INVALID_ARG, SPEC_ERR_UNSUPPORTED, SPEC_ERR_WORKSPACE, SPEC_ERR_HIP = range(5)
+SPEC_OK, SPEC_ERR_INVALID_ARG, SPEC_ERR_UNSUPPORTED, SPEC_ERR_WORKSPACE, SPEC_ERR_HIP, \
+    SPEC_ERR_NO_PAGES = range(6)
 SPEC_F32, SPEC_BF16 = 0, 1
 SPEC_TREE_INDEPENDENT, SPEC_TREE_SEQUENTIAL = 0, 1
 SPEC_MAX_DRAFT = 16
@@ -24,6 +25,10 @@ EXPORTS = ("spec_workspace_bytes", "spec_verify_attn", "spec_accept", "spec_veri
            "spec_status_str", "spec_abi_version", "spec_stream_read_probe", "spec_accept_floor_probe",
            "spec_accept_floor_probe_bytes", "spec_verify_noalloc",
            "spec_lm_head_accept", "spec_lm_head_workspace_bytes",
+           "spec_chunk_workspace_bytes", "spec_chunk_attn", "spec_cache_append", "spec_cache_commit",
+           "spec_cache_copy_pages", "spec_pages_create", "spec_pages_destroy", "spec_pages_open",
+           "spec_pages_resize", "spec_pages_fork", "spec_pages_close", "spec_pages_table", "spec_pages_compact",
+           "spec_pages_free_count",
            "spec_sched_create", "spec_sched_destroy", "spec_sched_submit", "spec_sched_next",
            "spec_sched_report", "spec_sched_query", "spec_sched_simulate")
 
@@ -94,6 +99,55 @@ class SpecLmHeadArgs(C.Structure):
                 ("weight_stride", C.c_int64),
                 ("event_begin", C.c_void_p),
                 ("event_end", C.c_void_p)]
+
+
+class SpecCache(C.Structure):
+    _fields_ = [("num_layers", C.c_int32),
+                ("num_kv_heads", C.c_int32),
+                ("head_dim", C.c_int32),
+                ("dtype", C.c_int),
+                ("num_pages", C.c_int32),
+                ("page_tokens", C.c_int32),
+                ("k", C.c_void_p),
+                ("v", C.c_void_p),
+                ("layer_stride", C.c_int64),
+                ("kv_stride_tok", C.c_int64),
+                ("kv_stride_head", C.c_int64),
+                ("block_table", C.c_void_p),
+                ("block_stride", C.c_int32),
+                ("pad0", C.c_int32)]
+
+
+class SpecChunks(C.Structure):
+    _fields_ = [("num_requests", C.c_int32),
+                ("pad0", C.c_int32),
+                ("ctx_len", C.POINTER(C.c_int32)),
+                ("new_len", C.POINTER(C.c_int32))]
+
+
+class SpecChunkAttnArgs(C.Structure):
+    _fields_ = [("num_q_heads", C.c_int32),
+                ("layer", C.c_int32),
+                ("scale", C.c_float),
+                ("out_dtype", C.c_int),
+                ("q", C.c_void_p),
+                ("q_stride_tok", C.c_int64),
+                ("q_stride_head", C.c_int64),
+                ("out", C.c_void_p)]
+
+
+class SpecAppendArgs(C.Structure):
+    _fields_ = [("layer", C.c_int32),
+                ("num_layers", C.c_int32),
+                ("k_new", C.c_void_p),
+                ("v_new", C.c_void_p),
+                ("new_stride_layer", C.c_int64),
+                ("new_stride_tok", C.c_int64),
+                ("new_stride_head", C.c_int64)]
+
+
+class SpecPageCopy(C.Structure):
+    _fields_ = [("src", C.c_int32), ("dst", C.c_int32), ("tokens", C.c_int32)]
 
 
 class SpecSchedParams(C.Structure):
@@ -193,6 +247,36 @@ def load(path: str = LIB_PATH) -> C.CDLL:
     lib.spec_accept_floor_probe.argtypes = [C.c_void_p, C.c_int64, C.c_int32, C.c_int32, C.c_int32, C.c_int32,
                                             C.c_void_p, C.c_size_t, C.c_void_p, C.c_void_p]
     lib.spec_accept_floor_probe.restype = C.c_int
+    lib.spec_chunk_workspace_bytes.argtypes = [P(SpecChunks), P(SpecCache), P(SpecChunkAttnArgs), P(C.c_size_t),
+                                               P(C.c_size_t)]
+    lib.spec_chunk_workspace_bytes.restype = C.c_int
+    lib.spec_chunk_attn.argtypes = [P(SpecChunks), P(SpecCache), P(SpecChunkAttnArgs), C.c_void_p, C.c_size_t,
+                                    C.c_void_p, C.c_size_t, C.c_void_p]
+    lib.spec_chunk_attn.restype = C.c_int
+    lib.spec_cache_append.argtypes = [P(SpecChunks), P(SpecCache), P(SpecAppendArgs), C.c_void_p]
+    lib.spec_cache_append.restype = C.c_int
+    lib.spec_cache_commit.argtypes = [P(SpecRequests), P(SpecCache), C.c_void_p, C.c_void_p]
+    lib.spec_cache_commit.restype = C.c_int
+    lib.spec_cache_copy_pages.argtypes = [P(SpecCache), C.c_void_p, C.c_int32, C.c_void_p]
+    lib.spec_cache_copy_pages.restype = C.c_int
+    lib.spec_pages_create.argtypes = [C.c_int32, C.c_int32, P(C.c_void_p)]
+    lib.spec_pages_create.restype = C.c_int
+    lib.spec_pages_destroy.argtypes = [C.c_void_p]
+    lib.spec_pages_destroy.restype = None
+    lib.spec_pages_open.argtypes = [C.c_void_p, P(C.c_int32)]
+    lib.spec_pages_open.restype = C.c_int
+    lib.spec_pages_resize.argtypes = [C.c_void_p, C.c_int32, C.c_int32, P(SpecPageCopy)]
+    lib.spec_pages_resize.restype = C.c_int
+    lib.spec_pages_fork.argtypes = [C.c_void_p, C.c_int32, P(C.c_int32)]
+    lib.spec_pages_fork.restype = C.c_int
+    lib.spec_pages_close.argtypes = [C.c_void_p, C.c_int32]
+    lib.spec_pages_close.restype = C.c_int
+    lib.spec_pages_table.argtypes = [C.c_void_p, C.c_int32, C.c_void_p, C.c_int32, P(C.c_int32)]
+    lib.spec_pages_table.restype = C.c_int
+    lib.spec_pages_compact.argtypes = [C.c_void_p, C.c_void_p, C.c_int32, P(C.c_int32)]
+    lib.spec_pages_compact.restype = C.c_int
+    lib.spec_pages_free_count.argtypes = [C.c_void_p]
+    lib.spec_pages_free_count.restype = C.c_int32
     lib.spec_sched_create.argtypes = [C.c_int32, P(SpecSchedParams), C.c_int32, P(C.c_void_p)]
     lib.spec_sched_create.restype = C.c_int
     lib.spec_sched_destroy.argtypes = [C.c_void_p]
@@ -274,6 +358,45 @@ def spec_accept_floor_probe_bytes(V, num_rows, B):
 
 def spec_accept_floor_probe(rows, row_stride, elem_bytes, V, num_rows, B, ws, ws_bytes, out, stream):
     return load().spec_accept_floor_probe(rows, row_stride, elem_bytes, V, num_rows, B, ws, ws_bytes, out, stream)
+
+
+def spec_chunk_workspace_bytes(chunks: SpecChunks, cache: SpecCache, args: SpecChunkAttnArgs):
+    """Returns (status, device_bytes, host_bytes)."""
+    dev, host = C.c_size_t(0), C.c_size_t(0)
+    st = load().spec_chunk_workspace_bytes(_ref(chunks), _ref(cache), _ref(args), C.byref(dev), C.byref(host))
+    return st, dev.value, host.value
+
+
+def spec_chunk_attn(chunks, cache, args, ws: int, ws_bytes: int, staging: int, staging_bytes: int, stream: int) -> int:
+    return load().spec_chunk_attn(_ref(chunks), _ref(cache), _ref(args), ws, ws_bytes, staging, staging_bytes, stream)
+
+
+def spec_cache_append(chunks, cache, args, stream: int) -> int:
+    return load().spec_cache_append(_ref(chunks), _ref(cache), _ref(args), stream)
+
+
+def spec_cache_commit(req, cache, accepted_node: int, stream: int) -> int:
+    return load().spec_cache_commit(_ref(req), _ref(cache), accepted_node, stream)
+
+
+def spec_cache_copy_pages(cache, copies: int, n: int, stream: int) -> int:
+    return load().spec_cache_copy_pages(_ref(cache), copies, n, stream)
+
+
+def make_chunks(ctx_len, new_len) -> SpecChunks:
+    """SpecChunks over host int32 arrays; the arrays are kept alive on the struct."""
+    import numpy as np
+    ctx = np.ascontiguousarray(ctx_len, dtype=np.int32)
+    new = np.ascontiguousarray(new_len, dtype=np.int32)
+    if ctx.shape != new.shape or ctx.ndim != 1:
+        raise ValueError("ctx_len and new_len are one number a request")
+    r = SpecChunks()
+    r.num_requests = int(ctx.shape[0])
+    r.ctx_len = ctx.ctypes.data_as(C.POINTER(C.c_int32))
+    r.new_len = new.ctypes.data_as(C.POINTER(C.c_int32))
+    r._keep = [ctx, new]
+    r.rows = int(new.sum())
+    return r
 
 
 def make_requests(ctx_len, draft_len=None, tree_parent=None, tree_parents=None):

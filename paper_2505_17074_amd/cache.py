@@ -1,0 +1,238 @@
+"""The paged KV cache around the verify step (speccache.h): page pools, the
+operators on them, and the page bookkeeping.  Argument marshalling only; the
+operators run in the library's HIP kernels, the bookkeeping in its C++.
+"""
+from __future__ import annotations
+
+import ctypes as C
+from typing import Optional, Sequence
+
+import numpy as np
+import torch
+
+from . import binding as B
+from .batch import Verifier
+
+_DTYPE = {torch.bfloat16: B.SPEC_BF16, torch.float32: B.SPEC_F32}
+
+
+class Pages:
+    """Which sequence holds which page (spec_pages_*)."""
+
+    def __init__(self, num_pages: int, page_tokens: int):
+        self._h = C.c_void_p()
+        self._lib = B.load()
+        B.check(self._lib.spec_pages_create(num_pages, page_tokens, C.byref(self._h)), "spec_pages_create")
+        self.num_pages, self.page_tokens = num_pages, page_tokens
+
+    def __del__(self):
+        if getattr(self, "_h", None):
+            self._lib.spec_pages_destroy(self._h)
+            self._h = None
+
+    def open(self) -> int:
+        s = C.c_int32()
+        B.check(self._lib.spec_pages_open(self._h, C.byref(s)), "spec_pages_open")
+        return s.value
+
+    def resize(self, sequence: int, tokens: int):
+        """The sequence has `tokens` rows from now on.  Returns the page copy
+        (src, dst, tokens) to make before rows are written, or None."""
+        c = B.SpecPageCopy()
+        B.check(self._lib.spec_pages_resize(self._h, sequence, tokens, C.byref(c)), "spec_pages_resize")
+        return (c.src, c.dst, c.tokens) if c.tokens else None
+
+    def fork(self, sequence: int) -> int:
+        s = C.c_int32()
+        B.check(self._lib.spec_pages_fork(self._h, sequence, C.byref(s)), "spec_pages_fork")
+        return s.value
+
+    def close(self, sequence: int) -> None:
+        B.check(self._lib.spec_pages_close(self._h, sequence), "spec_pages_close")
+
+    def table(self, sequence: int) -> np.ndarray:
+        n = C.c_int32()
+        out = np.empty(self.num_pages, np.int32)
+        B.check(self._lib.spec_pages_table(self._h, sequence, out.ctypes.data, out.size, C.byref(n)),
+                "spec_pages_table")
+        return out[:n.value].copy()
+
+    def block_table(self, sequences: Sequence[int], block_stride: Optional[int] = None) -> np.ndarray:
+        """The sequences' page ids [len(sequences), block_stride], zeros behind them."""
+        rows = [self.table(s) for s in sequences]
+        width = block_stride or max([r.size for r in rows] + [1])
+        out = np.zeros((len(rows), width), np.int32)
+        for i, r in enumerate(rows):
+            out[i, :r.size] = r
+        return out
+
+    def compact(self) -> np.ndarray:
+        """Moves used pages to the front of the pool: the copies [n, 3] to make."""
+        n = C.c_int32()
+        out = np.empty((self.num_pages // 2 + 1, 3), np.int32)
+        B.check(self._lib.spec_pages_compact(self._h, out.ctypes.data, out.shape[0], C.byref(n)),
+                "spec_pages_compact")
+        return out[:n.value].copy()
+
+    @property
+    def free(self) -> int:
+        return int(self._lib.spec_pages_free_count(self._h))
+
+
+class PagedCache:
+    """Page pools k, v [layers, num_pages, page_tokens, Hkv, d] (bf16 or fp32,
+    last dimension contiguous, a page's rows apart by one stride), and the
+    block table int32 [requests, block_stride] on the same device (it may be
+    replaced: `table`)."""
+
+    def __init__(self, k: torch.Tensor, v: torch.Tensor, table: Optional[torch.Tensor] = None):
+        if k.dim() != 5 or k.shape != v.shape or k.dtype != v.dtype or k.device != v.device or k.stride() != v.stride():
+            raise ValueError("k and v are [layers, num_pages, page_tokens, Hkv, d] of the same type, strides and device")
+        if k.dtype not in _DTYPE:
+            raise ValueError("bf16 or fp32 pools")
+        if k.stride(4) != 1 or k.stride(1) != k.shape[2] * k.stride(2):
+            raise ValueError("rows are contiguous and pages follow each other")
+        self.k, self.v, self.device = k, v, k.device
+        c = self.c = B.SpecCache()
+        c.num_layers, c.num_pages, c.page_tokens, c.num_kv_heads, c.head_dim = k.shape
+        c.dtype = _DTYPE[k.dtype]
+        c.k, c.v = k.data_ptr(), v.data_ptr()
+        c.layer_stride, c.kv_stride_tok, c.kv_stride_head = k.stride(0), k.stride(2), k.stride(3)
+        self.table = table
+
+    @property
+    def table(self) -> Optional[torch.Tensor]:
+        return self._table
+
+    @table.setter
+    def table(self, t: Optional[torch.Tensor]) -> None:
+        if t is not None:
+            if t.dim() != 2 or t.dtype != torch.int32 or t.device != self.device or t.stride(1) != 1:
+                raise ValueError("the block table is int32 [requests, block_stride] on the pools' device")
+            if t.shape[0] > 1 and t.stride(0) < t.shape[1]:
+                raise ValueError("the block table's rows overlap")
+        self._table = t
+        self.c.block_table = t.data_ptr() if t is not None else None
+        # one row's stride is its width (a table of one row may have any)
+        self.c.block_stride = 0 if t is None else (t.stride(0) if t.shape[0] > 1 else t.shape[1])
+
+    def _stream(self, stream) -> int:
+        return (stream or torch.cuda.current_stream(self.device)).cuda_stream
+
+    def _requests(self, n: int) -> None:
+        if self._table is None or n > self._table.shape[0]:
+            raise ValueError("the block table has no row for every request")
+
+    def append(self, chunks: B.SpecChunks, k_new: torch.Tensor, v_new: torch.Tensor, layer: int = 0,
+               stream: Optional[torch.cuda.Stream] = None) -> None:
+        """Rows k_new, v_new [layers, rows, Hkv, d] (or [rows, Hkv, d]: one layer)
+        to the ends of the requests, in the cache's layers from `layer` on."""
+        if k_new.dim() == 3:
+            k_new, v_new = k_new[None], v_new[None]
+        c = self.c
+        if k_new.shape != v_new.shape or k_new.stride() != v_new.stride() or k_new.dim() != 4 or \
+                tuple(k_new.shape[2:]) != (c.num_kv_heads, c.head_dim) or k_new.shape[1] < chunks.rows or \
+                (k_new.numel() and k_new.stride(3) != 1):
+            raise ValueError("k_new and v_new are [layers, rows, Hkv, d], a row for every new token")
+        if k_new.dtype != self.k.dtype or v_new.dtype != self.k.dtype or k_new.device != self.device or \
+                v_new.device != self.device:
+            raise ValueError("k_new and v_new have the pools' type and device")
+        self._requests(chunks.num_requests)
+        a = B.SpecAppendArgs()
+        a.layer, a.num_layers = layer, k_new.shape[0]
+        a.k_new, a.v_new = k_new.data_ptr(), v_new.data_ptr()
+        a.new_stride_layer, a.new_stride_tok, a.new_stride_head = (max(1, x) for x in k_new.stride()[:3])
+        with torch.cuda.device(self.device):
+            B.check(B.spec_cache_append(chunks, c, a, self._stream(stream)), "spec_cache_append")
+
+    def commit(self, req: B.SpecRequests, accepted_node: torch.Tensor,
+               stream: Optional[torch.cuda.Stream] = None) -> None:
+        """Moves the accepted paths' rows behind the contexts, in every layer."""
+        if accepted_node.dtype != torch.int32 or accepted_node.device != self.device or \
+                accepted_node.dim() != 1 or accepted_node.shape[0] < req.num_requests or \
+                not accepted_node.is_contiguous():
+            raise ValueError("accepted_node is int32 [requests] on the pools' device")
+        self._requests(req.num_requests)
+        with torch.cuda.device(self.device):
+            B.check(B.spec_cache_commit(req, self.c, accepted_node.data_ptr(), self._stream(stream)),
+                    "spec_cache_commit")
+
+    def copy_pages(self, copies, stream: Optional[torch.cuda.Stream] = None) -> None:
+        """Copies (src, dst, tokens) [n, 3], in every layer."""
+        a = np.ascontiguousarray(copies, dtype=np.int32).reshape(-1, 3)
+        with torch.cuda.device(self.device):
+            B.check(B.spec_cache_copy_pages(self.c, a.ctypes.data if a.size else None, a.shape[0],
+                                            self._stream(stream)), "spec_cache_copy_pages")
+
+
+class ChunkAttention(Verifier):
+    """Runs spec_chunk_attn on a PagedCache.  Owns a device workspace, which
+    grows with the batches, and a ring of pinned staging buffers, handled as
+    Verifier's: calls may be issued back to back, calls on another stream wait
+    for the previous call's, and calls that should run at the same time need
+    objects of their own.  A graph is captured from B.spec_chunk_attn with a
+    workspace and staging of its own, not from here: a replay reads the staging
+    it was captured with, and the ring reuses its slots."""
+
+    def __init__(self, cache: PagedCache, num_q_heads: int, scale: float = 0.0, ring: int = 32, event_every: int = 8):
+        if event_every < 1 or ring < event_every:
+            raise ValueError("need ring >= event_every >= 1")
+        self.cache = cache
+        a = self.args = B.SpecChunkAttnArgs()
+        a.num_q_heads, a.scale = num_q_heads, scale
+        self.ws_bytes = self.staging_bytes = 0
+        self.ws_ptr = None
+        self._staging = [None] * ring
+        self._every = event_every
+        self._slot_ev = [None] * ring
+        self._pending = []
+        self._pending_stream = None
+        self._i = 0
+        self._last_stream = None
+
+    def _grow(self, chunks, stream) -> None:
+        st, dev, host = B.spec_chunk_workspace_bytes(chunks, self.cache.c, self.args)
+        B.check(st, "spec_chunk_workspace_bytes")
+        if dev > self.ws_bytes:
+            if self.ws_bytes:
+                stream.synchronize()          # earlier calls' workspace goes back to the allocator
+            self.ws_bytes = dev + dev // 4
+            self._ws = torch.empty(self.ws_bytes + 256, dtype=torch.uint8, device=self.cache.device)
+            self.ws_ptr = (self._ws.data_ptr() + 255) // 256 * 256
+        if host > self.staging_bytes:
+            if self.staging_bytes:
+                stream.synchronize()          # and their staging
+            self.staging_bytes = host + host // 4
+            size = (self.staging_bytes + 255) // 256 * 256
+            self._pinned = torch.empty(size * len(self._staging), dtype=torch.uint8, pin_memory=True)
+            self._staging = [self._pinned.data_ptr() + i * size for i in range(len(self._staging))]
+
+    def run(self, chunks: B.SpecChunks, q: torch.Tensor, out: torch.Tensor, layer: int = 0,
+            stream: Optional[torch.cuda.Stream] = None) -> None:
+        """Attention of q [rows, Hq, d] into out [rows, Hq, d] (bf16 or fp32)."""
+        cache, a = self.cache, self.args
+        shape = (chunks.rows, a.num_q_heads, cache.c.head_dim)
+        if q.dim() != 3 or out.dim() != 3 or q.shape[0] < shape[0] or out.shape[0] < shape[0] or \
+                tuple(q.shape[1:]) != shape[1:] or tuple(out.shape[1:]) != shape[1:]:
+            raise ValueError("q and out are [rows, Hq, d], a row for every new token")
+        if q.dtype != cache.k.dtype or out.dtype not in _DTYPE or q.device != cache.device or \
+                out.device != cache.device or not out.is_contiguous() or (q.numel() and q.stride(2) != 1):
+            raise ValueError("q has the cache's type, out is contiguous bf16 or fp32, both on its device")
+        cache._requests(chunks.num_requests)
+        a.layer, a.out_dtype = layer, _DTYPE[out.dtype]
+        a.q, a.out = q.data_ptr(), out.data_ptr()
+        a.q_stride_tok, a.q_stride_head = max(1, q.stride(0)), max(1, q.stride(1))
+        with torch.cuda.device(cache.device):
+            stream = stream or torch.cuda.current_stream(cache.device)
+            self._order(stream)
+            for grown in (False, True):
+                s = self._slot(stream)
+                try:
+                    st = B.spec_chunk_attn(chunks, cache.c, a, self.ws_ptr, self.ws_bytes, self._staging[s],
+                                           self.staging_bytes, stream.cuda_stream)
+                finally:
+                    self._done(s, stream)
+                if st != B.SPEC_ERR_WORKSPACE or grown:
+                    break
+                self._grow(chunks, stream)
+        B.check(st, "spec_chunk_attn")

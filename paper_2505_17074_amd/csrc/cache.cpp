@@ -1,0 +1,430 @@
+// C ABI of the paged cache's operators (speccache.h): argument checks, the
+// chunk attention's plan, and the row movers' launches.  Every check runs
+// before the first HIP call.
+#include "../../include/speccache.h"
+
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+#include <cstring>
+#include <new>
+#include <unordered_set>
+#include <vector>
+
+#include "sv_chunk.h"
+#include "sv_rules.h"
+
+namespace {
+
+using sv::ChunkItem;
+using sv::ChunkJoin;
+
+constexpr size_t kAlign = 256;
+inline size_t align_up(size_t x) { return (x + kAlign - 1) / kAlign * kAlign; }
+inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+
+// No exception leaves the library: one from the standard containers is memory
+// that the host does not have.
+template <typename F>
+spec_status_t guarded(F&& f) noexcept {
+  try {
+    return f();
+  } catch (...) {
+    return SPEC_ERR_WORKSPACE;
+  }
+}
+
+int elem_bytes(spec_dtype_t t) { return t == SPEC_F32 ? 4 : 2; }
+
+spec_status_t check_cache(const spec_cache_t* c, bool table) {
+  if (!c) return SPEC_ERR_INVALID_ARG;
+  if (c->dtype != SPEC_F32 && c->dtype != SPEC_BF16) return SPEC_ERR_INVALID_ARG;
+  if (c->num_layers < 1 || c->num_kv_heads < 1 || c->head_dim < 1 || c->num_pages < 1) return SPEC_ERR_INVALID_ARG;
+  if (c->page_tokens < 32 || c->page_tokens % 32) return SPEC_ERR_INVALID_ARG;
+  if (!c->k || !c->v || !aligned16(c->k) || !aligned16(c->v)) return SPEC_ERR_INVALID_ARG;
+  const int64_t vec = 16 / elem_bytes(c->dtype);
+  if (c->head_dim % vec) return SPEC_ERR_UNSUPPORTED;
+  if (c->kv_stride_tok < 1 || c->kv_stride_head < 1 || c->kv_stride_tok % vec || c->kv_stride_head % vec)
+    return SPEC_ERR_INVALID_ARG;
+  if (c->num_layers > 1 && (c->layer_stride < 1 || c->layer_stride % vec)) return SPEC_ERR_INVALID_ARG;
+  // a token row holds every head, heads apart
+  if (c->num_kv_heads > 1 && c->kv_stride_head < c->head_dim) return SPEC_ERR_INVALID_ARG;
+  if (c->kv_stride_head > INT32_MAX || c->kv_stride_tok > INT32_MAX ||
+      c->kv_stride_head * (c->num_kv_heads - 1) + c->head_dim > c->kv_stride_tok)
+    return SPEC_ERR_INVALID_ARG;
+  // one page's rows are addressed with 32-bit offsets; a launch's second dimension holds K and V of every layer
+  if ((int64_t)c->page_tokens * c->kv_stride_tok * elem_bytes(c->dtype) >= INT32_MAX || c->num_layers > 32767)
+    return SPEC_ERR_UNSUPPORTED;
+  if (table) {
+    if (!c->block_table || reinterpret_cast<uintptr_t>(c->block_table) % 4 || c->block_stride < 1)
+      return SPEC_ERR_INVALID_ARG;
+  }
+  return SPEC_OK;
+}
+
+// Lengths that fit the block table; the number of new rows.
+spec_status_t check_chunks(const spec_chunks_t* r, const spec_cache_t* c, int64_t* rows) {
+  if (!r || r->num_requests < 1 || !r->ctx_len || !r->new_len) return SPEC_ERR_INVALID_ARG;
+  int64_t nq = 0;
+  for (int i = 0; i < r->num_requests; ++i) {
+    if (r->ctx_len[i] < 0 || r->new_len[i] < 0) return SPEC_ERR_INVALID_ARG;
+    nq += r->new_len[i];
+    const int64_t len = (int64_t)r->ctx_len[i] + r->new_len[i];
+    if (r->new_len[i] > 0 && (len > INT32_MAX / 2 || (len + c->page_tokens - 1) / c->page_tokens > c->block_stride))
+      return SPEC_ERR_INVALID_ARG;
+  }
+  if (nq >= INT32_MAX / 2) return SPEC_ERR_INVALID_ARG;
+  *rows = nq;
+  return SPEC_OK;
+}
+
+int compute_units() {
+  static int cus[64];
+  int dev = 0, n = 0;
+  if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= 64) {
+    (void)hipGetLastError();
+    return 256;
+  }
+  if (cus[dev]) return cus[dev];
+  if (hipDeviceGetAttribute(&n, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess || n <= 0) {
+    (void)hipGetLastError();
+    n = 256;
+  }
+  return cus[dev] = n;
+}
+
+struct ChunkPlan {
+  std::vector<ChunkItem> items;
+  std::vector<ChunkJoin> joins;
+  int rows_per_item = sv::kChunkLowRows;
+  int64_t parts = 0;
+  size_t off_joins = 0, plan_bytes = 0;
+  size_t off_part_o = 0, off_part_ml = 0, device_bytes = 0;
+};
+
+spec_status_t plan_chunk(const spec_chunks_t* r, const spec_cache_t* c, const spec_chunk_attn_args_t* a,
+                         ChunkPlan& P) {
+  spec_status_t st = check_cache(c, true);
+  if (st != SPEC_OK) return st;
+  if (!a || a->num_q_heads < 1 || a->num_q_heads % c->num_kv_heads) return SPEC_ERR_INVALID_ARG;
+  if (a->layer < 0 || a->layer >= c->num_layers) return SPEC_ERR_INVALID_ARG;
+  if (a->out_dtype != SPEC_F32 && a->out_dtype != SPEC_BF16) return SPEC_ERR_INVALID_ARG;
+  if (c->dtype != SPEC_BF16 || (c->head_dim != 64 && c->head_dim != 128)) return SPEC_ERR_UNSUPPORTED;
+  int64_t nq = 0;
+  if ((st = check_chunks(r, c, &nq)) != SPEC_OK) return st;
+  if (nq > 0 && (!a->q || !a->out)) return SPEC_ERR_INVALID_ARG;
+  if (!aligned16(a->q) || !aligned16(a->out)) return SPEC_ERR_INVALID_ARG;
+  if (a->q_stride_tok < 1 || a->q_stride_head < 1 || a->q_stride_tok % 8 || a->q_stride_head % 8)
+    return SPEC_ERR_INVALID_ARG;
+  const int Hkv = c->num_kv_heads, G = a->num_q_heads / Hkv;
+  if (nq * G >= INT32_MAX / 2) return SPEC_ERR_UNSUPPORTED;
+
+  int most = 0;
+  for (int i = 0; i < r->num_requests; ++i) most = std::max(most, r->new_len[i]);
+  const int RT = (int64_t)most * G > sv::kChunkLowRows ? sv::kChunkTallRows : sv::kChunkLowRows;
+  P.rows_per_item = RT;
+  // the row tiles and the keys that each sees
+  struct RowTile { int32_t req, r0, rows, keys; int64_t q0; };
+  std::vector<RowTile> tiles;
+  int64_t q0 = 0, total = 0;
+  for (int i = 0; i < r->num_requests; ++i) {
+    const int n = r->new_len[i], rows = n * G;
+    for (int r0 = 0; r0 < rows; r0 += RT) {
+      const int nr = std::min(RT, rows - r0);
+      const int keys = r->ctx_len[i] + (r0 + nr - 1) / G + 1;
+      tiles.push_back({i, r0, nr, keys, q0});
+      total += (keys + sv::kChunkTile - 1) / sv::kChunkTile;
+    }
+    q0 += n;
+  }
+  total *= Hkv;
+  const int64_t slots = 2 * (int64_t)compute_units();
+  const int64_t least = RT == sv::kChunkTallRows ? 8 : 4;
+  const int64_t target = std::max<int64_t>(least, (total + slots - 1) / slots);
+  int64_t n_items = 0;
+  for (const RowTile& t : tiles) n_items += ((t.keys + sv::kChunkTile - 1) / sv::kChunkTile + target - 1) / target * Hkv;
+  if (n_items >= INT32_MAX / 64) return SPEC_ERR_UNSUPPORTED;
+  P.items.reserve((size_t)n_items);
+  for (const RowTile& t : tiles) {
+    const int64_t kt = (t.keys + sv::kChunkTile - 1) / sv::kChunkTile;
+    const int64_t pieces = (kt + target - 1) / target;
+    const int64_t len = (kt + pieces - 1) / pieces * sv::kChunkTile;
+    const int np = (int)((t.keys + len - 1) / len);
+    for (int h = 0; h < Hkv; ++h) {
+      if (np > 1) {
+        ChunkJoin j{h, t.r0, t.rows, np, P.parts, (int32_t)t.q0, 0};
+        P.joins.push_back(j);
+      }
+      for (int s = 0; s < np; ++s) {
+        ChunkItem it;
+        it.req = t.req;
+        it.kvh = h;
+        it.r0 = t.r0;
+        it.rows = t.rows;
+        it.kb = (int32_t)(s * len);
+        it.ke = (int32_t)std::min<int64_t>(t.keys, (s + 1) * len);
+        it.ctx = r->ctx_len[t.req];
+        it.q0 = (int32_t)t.q0;
+        it.part = np > 1 ? P.parts + (int64_t)s * t.rows : -1;
+        it.pad = 0;
+        P.items.push_back(it);
+      }
+      if (np > 1) P.parts += (int64_t)np * t.rows;
+    }
+  }
+  // longest first (a stable counting sort): the last to start are the shortest
+  {
+    int longest = 0;
+    auto len = [](const ChunkItem& it) { return (it.ke - it.kb + sv::kChunkTile - 1) / sv::kChunkTile; };
+    for (const ChunkItem& it : P.items) longest = std::max(longest, len(it));
+    std::vector<int> start(longest + 2, 0);
+    for (const ChunkItem& it : P.items) ++start[longest - len(it) + 1];
+    for (int t = 1; t <= longest + 1; ++t) start[t] += start[t - 1];
+    std::vector<ChunkItem> sorted(P.items.size());
+    for (const ChunkItem& it : P.items) sorted[start[longest - len(it)]++] = it;
+    P.items.swap(sorted);
+  }
+
+  P.off_joins = align_up(sizeof(ChunkItem) * P.items.size());
+  P.plan_bytes = P.off_joins + align_up(sizeof(ChunkJoin) * P.joins.size());
+  P.off_part_o = P.plan_bytes;
+  P.off_part_ml = align_up(P.off_part_o + sizeof(float) * (size_t)P.parts * c->head_dim);
+  P.device_bytes = align_up(P.off_part_ml + sizeof(float2) * (size_t)P.parts);
+  return SPEC_OK;
+}
+
+// The row movers' view of `layers` layers from `layer` on.  Heads that follow
+// each other without a gap on both sides (apart: their strides) move as one.
+sv::CachePools pools(const spec_cache_t* c, int layer, int layers, bool one_run) {
+  const int64_t eb = elem_bytes(c->dtype);
+  sv::CachePools p;
+  p.layer_bytes = c->num_layers > 1 ? c->layer_stride * eb : 0;
+  p.k = static_cast<char*>(c->k) + layer * p.layer_bytes;
+  p.v = static_cast<char*>(c->v) + layer * p.layer_bytes;
+  p.st_bytes = (int32_t)(c->kv_stride_tok * eb);
+  p.sh_bytes = (int32_t)(c->kv_stride_head * eb);
+  p.page_bytes = (int64_t)c->page_tokens * p.st_bytes;
+  p.num_pages = c->num_pages;
+  p.page_tokens = c->page_tokens;
+  p.layers = layers;
+  p.heads = c->num_kv_heads;
+  p.row_units = (int32_t)(c->head_dim * eb / 16);
+  if (one_run) {
+    p.row_units *= p.heads;
+    p.heads = 1;
+  }
+  return p;
+}
+bool heads_touch(const spec_cache_t* c) { return c->num_kv_heads == 1 || c->kv_stride_head == c->head_dim; }
+
+}  // namespace
+
+extern "C" {
+
+spec_status_t spec_chunk_workspace_bytes(const spec_chunks_t* chunks, const spec_cache_t* cache,
+                                         const spec_chunk_attn_args_t* args, size_t* device_bytes,
+                                         size_t* host_bytes) {
+  return guarded([&]() -> spec_status_t {
+    if (!device_bytes || !host_bytes) return SPEC_ERR_INVALID_ARG;
+    ChunkPlan P;
+    const spec_status_t st = plan_chunk(chunks, cache, args, P);
+    if (st != SPEC_OK) return st;
+    *device_bytes = P.device_bytes;
+    *host_bytes = P.plan_bytes;
+    return SPEC_OK;
+  });
+}
+
+spec_status_t spec_chunk_attn(const spec_chunks_t* chunks, const spec_cache_t* cache,
+                              const spec_chunk_attn_args_t* args, void* workspace, size_t workspace_bytes,
+                              void* host_staging, size_t host_staging_bytes, void* stream) {
+  return guarded([&]() -> spec_status_t {
+    ChunkPlan P;
+    const spec_status_t st = plan_chunk(chunks, cache, args, P);
+    if (st != SPEC_OK) return st;
+    if (P.items.empty()) return SPEC_OK;
+    if (!workspace || reinterpret_cast<uintptr_t>(workspace) % kAlign || workspace_bytes < P.device_bytes ||
+        !host_staging || host_staging_bytes < P.plan_bytes)
+      return SPEC_ERR_WORKSPACE;
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    char* d = static_cast<char*>(workspace);
+    char* h = static_cast<char*>(host_staging);
+    std::memcpy(h, P.items.data(), sizeof(ChunkItem) * P.items.size());
+    if (!P.joins.empty()) std::memcpy(h + P.off_joins, P.joins.data(), sizeof(ChunkJoin) * P.joins.size());
+    // the kernels read the plan where it was staged when that is device-mapped
+    // memory; otherwise it is copied into the workspace first
+    const char* plan = d;
+    void* mapped = nullptr;
+    if (hipHostGetDevicePointer(&mapped, h, 0) == hipSuccess && mapped && aligned16(mapped)) {
+      plan = static_cast<const char*>(mapped);
+    } else {
+      (void)hipGetLastError();
+      if (hipMemcpyAsync(d, h, P.plan_bytes, hipMemcpyHostToDevice, s) != hipSuccess) return SPEC_ERR_HIP;
+    }
+    sv::ChunkParams p{};
+    p.q = args->q;
+    const int64_t lb = cache->num_layers > 1 ? args->layer * cache->layer_stride * 2 : 0;
+    p.k = static_cast<const char*>(cache->k) + lb;
+    p.v = static_cast<const char*>(cache->v) + lb;
+    p.out = args->out;
+    p.part_o = reinterpret_cast<float*>(d + P.off_part_o);
+    p.part_ml = reinterpret_cast<float2*>(d + P.off_part_ml);
+    p.items = reinterpret_cast<const ChunkItem*>(plan);
+    p.joins = reinterpret_cast<const ChunkJoin*>(plan + P.off_joins);
+    p.bt = cache->block_table;
+    p.q_st = args->q_stride_tok;
+    p.q_sh = args->q_stride_head;
+    p.kv_st = cache->kv_stride_tok;
+    p.kv_sh = cache->kv_stride_head;
+    p.bt_stride = cache->block_stride;
+    p.n_items = (int32_t)P.items.size();
+    p.n_joins = (int32_t)P.joins.size();
+    p.page_tokens = cache->page_tokens;
+    p.num_pages = cache->num_pages;
+    p.Hq = args->num_q_heads;
+    p.G = args->num_q_heads / cache->num_kv_heads;
+    p.D = cache->head_dim;
+    p.out_f32 = args->out_dtype == SPEC_F32;
+    p.tall = P.rows_per_item;
+    const float scale = args->scale > 0.f ? args->scale : 1.f / std::sqrt((float)cache->head_dim);
+    p.scale_log2 = scale * 1.4426950408889634f;
+    return sv::launch_chunk(p, s) == hipSuccess ? SPEC_OK : SPEC_ERR_HIP;
+  });
+}
+
+spec_status_t spec_cache_append(const spec_chunks_t* chunks, const spec_cache_t* cache, const spec_append_args_t* args,
+                                void* stream) {
+  spec_status_t st = check_cache(cache, true);
+  if (st != SPEC_OK) return st;
+  int64_t nq = 0;
+  if ((st = check_chunks(chunks, cache, &nq)) != SPEC_OK) return st;
+  if (!args || args->layer < 0 || args->num_layers < 1 || args->layer > cache->num_layers - args->num_layers)
+    return SPEC_ERR_INVALID_ARG;
+  if (nq > 0 && (!args->k_new || !args->v_new)) return SPEC_ERR_INVALID_ARG;
+  if (!aligned16(args->k_new) || !aligned16(args->v_new)) return SPEC_ERR_INVALID_ARG;
+  const int64_t eb = elem_bytes(cache->dtype), vec = 16 / eb;
+  if (args->new_stride_tok < 1 || args->new_stride_head < 1 || args->new_stride_tok % vec ||
+      args->new_stride_head % vec)
+    return SPEC_ERR_INVALID_ARG;
+  if (args->num_layers > 1 && (args->new_stride_layer < 1 || args->new_stride_layer % vec)) return SPEC_ERR_INVALID_ARG;
+
+  const bool touch = heads_touch(cache) && (cache->num_kv_heads == 1 || args->new_stride_head == cache->head_dim);
+  sv::AppendParams p{};
+  p.c = pools(cache, args->layer, args->num_layers, touch);
+  p.k_new = static_cast<const char*>(args->k_new);
+  p.v_new = static_cast<const char*>(args->v_new);
+  p.new_sl = args->num_layers > 1 ? args->new_stride_layer * eb : 0;
+  p.new_st = args->new_stride_tok * eb;
+  p.new_sh = args->new_stride_head * eb;
+  p.bt_stride = cache->block_stride;
+  int64_t row = 0;
+  for (int i0 = 0; i0 < chunks->num_requests; i0 += sv::kMoveRequests) {
+    p.n_req = std::min(sv::kMoveRequests, chunks->num_requests - i0);
+    p.bt = cache->block_table + (int64_t)i0 * cache->block_stride;
+    p.row0 = (int32_t)row;
+    int32_t end = 0;
+    for (int i = 0; i < p.n_req; ++i) {
+      p.ctx[i] = chunks->ctx_len[i0 + i];
+      p.end[i] = end += chunks->new_len[i0 + i];
+    }
+    p.rows = end;
+    row += end;
+    if (end > 0 && sv::launch_append(p, static_cast<hipStream_t>(stream)) != hipSuccess) return SPEC_ERR_HIP;
+  }
+  return SPEC_OK;
+}
+
+spec_status_t spec_cache_commit(const spec_requests_t* req, const spec_cache_t* cache, const int32_t* accepted_node,
+                                void* stream) {
+  spec_status_t st = check_cache(cache, true);
+  if (st != SPEC_OK) return st;
+  if (!req || req->num_requests < 1 || !req->ctx_len || !accepted_node ||
+      reinterpret_cast<uintptr_t>(accepted_node) % 4)
+    return SPEC_ERR_INVALID_ARG;
+  if (req->tree_nodes < 0 || req->tree_nodes > SPEC_MAX_TREE_NODES) return SPEC_ERR_INVALID_ARG;
+  const bool per_req = req->node_count != nullptr;
+  if (per_req && (req->tree_nodes != 0 || !req->tree_parents)) return SPEC_ERR_INVALID_ARG;
+  if (!per_req && req->tree_nodes == 0 && !req->draft_len) return SPEC_ERR_INVALID_ARG;
+  auto tree_ok = [](const int32_t* parent, int n) {
+    if (n < 1 || n > SPEC_MAX_TREE_NODES || !parent || parent[0] != -1) return false;
+    for (int x = 1; x < n; ++x)
+      if (parent[x] < 0 || parent[x] >= x) return false;
+    return true;
+  };
+  if (req->tree_nodes > 0 && !tree_ok(req->tree_parent, req->tree_nodes)) return SPEC_ERR_INVALID_ARG;
+  int64_t o = 0;
+  for (int i = 0; i < req->num_requests; ++i) {
+    int n = req->tree_nodes;
+    if (per_req) {
+      n = req->node_count[i];
+      if (!tree_ok(req->tree_parents + o, n)) return SPEC_ERR_INVALID_ARG;
+      o += n;
+    } else if (n == 0) {
+      if (req->draft_len[i] < 0 || req->draft_len[i] > SPEC_MAX_DRAFT) return SPEC_ERR_INVALID_ARG;
+      n = req->draft_len[i] + 1;
+    }
+    const int64_t len = (int64_t)req->ctx_len[i] + n;
+    if (req->ctx_len[i] < 0 || len > INT32_MAX / 2 ||
+        (len + cache->page_tokens - 1) / cache->page_tokens > cache->block_stride)
+      return SPEC_ERR_INVALID_ARG;
+  }
+  if (!per_req && req->tree_nodes == 0) return SPEC_OK;      // chains are in place
+  if ((int64_t)cache->num_kv_heads * cache->head_dim * elem_bytes(cache->dtype) / 1024 >= 65535)
+    return SPEC_ERR_UNSUPPORTED;
+
+  sv::CommitParams p{};
+  p.c = pools(cache, 0, cache->num_layers, heads_touch(cache));
+  p.bt_stride = cache->block_stride;
+  p.shared = !per_req;
+  o = 0;
+  for (int i0 = 0; i0 < req->num_requests; i0 += sv::kMoveTrees) {
+    p.n_req = std::min(sv::kMoveTrees, req->num_requests - i0);
+    p.bt = cache->block_table + (int64_t)i0 * cache->block_stride;
+    p.accepted = accepted_node + i0;
+    for (int i = 0; i < p.n_req; ++i) {
+      p.ctx[i] = req->ctx_len[i0 + i];
+      if (i > 0 && !per_req) continue;
+      const int n = per_req ? req->node_count[i0 + i] : req->tree_nodes;
+      const int32_t* parent = per_req ? req->tree_parents + o : req->tree_parent;
+      p.nodes[i] = (int8_t)n;
+      for (int x = 0; x < n; ++x) p.parent[i][x] = (int8_t)std::max(parent[x], 0);
+      o += n;
+    }
+    if (sv::launch_commit(p, static_cast<hipStream_t>(stream)) != hipSuccess) return SPEC_ERR_HIP;
+  }
+  return SPEC_OK;
+}
+
+spec_status_t spec_cache_copy_pages(const spec_cache_t* cache, const spec_page_copy_t* copies, int32_t num_copies,
+                                    void* stream) {
+  return guarded([&]() -> spec_status_t {
+    spec_status_t st = check_cache(cache, false);
+    if (st != SPEC_OK) return st;
+    if (num_copies < 0 || (num_copies > 0 && !copies)) return SPEC_ERR_INVALID_ARG;
+    std::unordered_set<int32_t> written;
+    written.reserve(num_copies);
+    for (int i = 0; i < num_copies; ++i) {
+      const spec_page_copy_t& x = copies[i];
+      if (x.src < 0 || x.src >= cache->num_pages || x.dst < 0 || x.dst >= cache->num_pages || x.tokens < 1 ||
+          x.tokens > cache->page_tokens || !written.insert(x.dst).second)
+        return SPEC_ERR_INVALID_ARG;
+    }
+    for (int i = 0; i < num_copies; ++i)
+      if (written.count(copies[i].src)) return SPEC_ERR_INVALID_ARG;
+    sv::PageCopyParams p{};
+    p.c = pools(cache, 0, cache->num_layers, heads_touch(cache));
+    for (int i0 = 0; i0 < num_copies; i0 += sv::kMoveRequests) {
+      p.n = std::min(sv::kMoveRequests, num_copies - i0);
+      for (int i = 0; i < p.n; ++i) {
+        p.src[i] = copies[i0 + i].src;
+        p.dst[i] = copies[i0 + i].dst;
+        p.tokens[i] = copies[i0 + i].tokens;
+      }
+      if (sv::launch_page_copy(p, static_cast<hipStream_t>(stream)) != hipSuccess) return SPEC_ERR_HIP;
+    }
+    return SPEC_OK;
+  });
+}
+
+}  // extern "C"

@@ -937,6 +937,7 @@ const char* spec_status_str(spec_status_t status) {
     case SPEC_ERR_UNSUPPORTED: return "unsupported shape or dtype";
     case SPEC_ERR_WORKSPACE: return "workspace or staging buffer too small or misaligned";
     case SPEC_ERR_HIP: return "HIP runtime error";
+    case SPEC_ERR_NO_PAGES: return "no free page left";
   }
   return "unknown status";
 }

@@ -1,0 +1,121 @@
+// Internal declarations of the paged cache's operators: chunk attention's
+// plan items and kernel parameters, and the row movers' arguments.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+namespace sv {
+
+// One work item of the chunk attention: the keys [kb, ke) of one (request, KV
+// head) for `rows` query rows from row r0 on.  Query row r of a request and KV
+// head is new token r / G under the group's query head r % G, so that a run of
+// rows sees a run of key ranges.
+struct ChunkItem {
+  int32_t req;      // block table row
+  int32_t kvh;
+  int32_t r0, rows;
+  int32_t kb, ke;   // kb a multiple of 64
+  int32_t ctx;
+  int32_t q0;       // the request's first row of q and out
+  int64_t part;     // first partial row of this piece, -1: the item writes out itself
+  int64_t pad;
+};
+static_assert(sizeof(ChunkItem) == 48, "ChunkItem is read as 16-byte units");
+
+// One query-row tile whose key range was cut: its pieces' partial rows follow
+// each other, `rows` apart.
+struct ChunkJoin {
+  int32_t kvh;
+  int32_t r0, rows;
+  int32_t pieces;
+  int64_t part;
+  int32_t q0;
+  int32_t pad;
+};
+static_assert(sizeof(ChunkJoin) == 32, "ChunkJoin is read as 16-byte units");
+
+struct ChunkParams {
+  const void* q;
+  const void* k;        // the layer's pools
+  const void* v;
+  void* out;
+  float* part_o;        // [partial rows, d], not normalised
+  float2* part_ml;      // running maximum (log2 units) and sum
+  const ChunkItem* items;
+  const ChunkJoin* joins;
+  const int32_t* bt;
+  int64_t q_st, q_sh;
+  int64_t kv_st, kv_sh;
+  int64_t bt_stride;
+  int32_t n_items, n_joins;
+  int32_t page_tokens, num_pages;
+  int32_t Hq, G, D;
+  int32_t out_f32;
+  int32_t tall;         // rows per item: kChunkTallRows or kChunkLowRows
+  float scale_log2;
+};
+
+constexpr int kChunkLowRows = 32;
+constexpr int kChunkTallRows = 128;
+constexpr int kChunkTile = 64;         // pieces are cut at multiples of this many keys
+
+hipError_t launch_chunk(const ChunkParams& p, hipStream_t s);
+
+// One kernel argument block of the row movers holds this many requests or
+// pages (kernel arguments end at 4 KB).
+constexpr int kMoveRequests = 256;
+constexpr int kMoveTrees = 64;
+
+struct CachePools {
+  char* k;
+  char* v;
+  int64_t layer_bytes, page_bytes;
+  int32_t st_bytes, sh_bytes;          // token and head strides inside a page
+  int32_t num_pages, page_tokens;
+  int32_t layers;                      // moved by this call, from k / v on
+  int32_t heads, row_units;            // a head's row in 16-byte units
+};
+
+struct AppendParams {
+  CachePools c;
+  const char* k_new;
+  const char* v_new;
+  int64_t new_sl, new_st, new_sh;      // bytes
+  const int32_t* bt;                   // of the block's first request
+  int64_t bt_stride;
+  int32_t n_req;
+  int32_t row0;                        // the block's first row of the new arrays
+  int32_t rows;                        // its rows
+  int32_t ctx[kMoveRequests];
+  int32_t end[kMoveRequests];          // running sum of new_len within the block
+};
+
+struct CommitParams {
+  CachePools c;
+  const int32_t* bt;
+  int64_t bt_stride;
+  const int32_t* accepted;             // of the block's first request
+  int32_t n_req;
+  int32_t shared;                      // one topology: parent[0], nodes[0] for every request
+  int32_t ctx[kMoveTrees];
+  int8_t nodes[kMoveTrees];
+  int8_t parent[kMoveTrees][32];
+};
+
+struct PageCopyParams {
+  CachePools c;
+  int32_t n;
+  int32_t src[kMoveRequests];
+  int32_t dst[kMoveRequests];
+  int32_t tokens[kMoveRequests];
+};
+
+static_assert(sizeof(AppendParams) <= 4096 && sizeof(CommitParams) <= 4096 && sizeof(PageCopyParams) <= 4096,
+              "kernel arguments");
+
+hipError_t launch_append(const AppendParams& p, hipStream_t s);
+hipError_t launch_commit(const CommitParams& p, hipStream_t s);
+hipError_t launch_page_copy(const PageCopyParams& p, hipStream_t s);
+
+}  // namespace sv
