@@ -116,25 +116,48 @@ struct Rows {
 // + (m & 3) of its 32 keys: the C layout then leaves lane half h the keys 16 x
 // + 8 h + 0 .. 7 of its row in registers 8 x .. 8 x + 7, which is the B operand
 // of the second product as it is.
+// Stage j of the ring holds K of tile j and V of tile j - 1: step t takes the
+// scores of tile t + 1 (matrix cores) beside the softmax of tile t (vector
+// units), then the product with V of tile t.
 // PARTS: bf16 parts a probability is carried in (1 for a bf16 output, 3 for
 // an fp32 one: 24 bits).
 // ---------------------------------------------------------------------------
-template <int D, int NW, int TK, int NS, int PARTS>
+template <int D, int NW, int TK, int PARTS>
 struct Chunk {
   using TL = Tile<D, TK>;
   using DL = Deal<D, TK, NW>;
   static constexpr int KS = D / 16, ET = D / 32, KB = TK / 32;
+  static_assert(DL::U == 1 || KB == 1, "a wave's units are one, or K and V of a 32-key tile");
+  struct Scores {
+    f32x16 s[KB];
+  };
+  // The addresses of a lane's reads and transfers.
+  struct Lane {
+    uint32_t koff[KS];         // K operand: chunk 2 ks + lane half of the lane's key row (keys 32.. : + HALF)
+    uint32_t voff[ET];         // V operand: the transposing read's place (keys 16 kk ..: + 16 kk rows)
+    uint32_t off[TL::T];       // transfers: row and swizzled chunk (one matrix a wave, or K and V by `flip`)
+    uint32_t flip[DL::U > 1 ? TL::T : 1];
+  };
 
-  // The wave's units of the tile starting at key t0 (its pages' ids in pg).
-  static __device__ __forceinline__ void issue(lds_char* stage, const Fetch& f, int t0, const int (&pg)[DL::U], int w,
-                                               const uint32_t (&off)[TL::T], const uint32_t (&offv)[TL::T], int lane) {
+  // Unit u of wave w: V after K, the halves in order.
+  static __device__ __forceinline__ bool unit_is_v(int w, int u) { return w * DL::U + u >= KB; }
+  static __device__ __forceinline__ int unit_half(int w, int u) {
+    const int x = w * DL::U + u;
+    return x >= KB ? x - KB : x;
+  }
+
+  // The wave's units of stage j: K of tile j, V of tile j - 1, whichever of
+  // them the item has (tiles begin at key kb).
+  static __device__ __forceinline__ void issue(lds_char* stage, const Fetch& f, int j, int kb, int ntiles,
+                                               const int (&pg)[DL::U], int w, const Lane& A, int lane) {
 #if defined(__HIP_DEVICE_COMPILE__)
 #pragma unroll
     for (int u = 0; u < DL::U; ++u) {
-      const int unit = w * DL::U + u;
-      const bool isv = unit >= KB;
-      const int half = isv ? unit - KB : unit;
-      const int t = t0 + 32 * half;
+      const bool isv = unit_is_v(w, u);
+      const int half = unit_half(w, u);
+      const int tile = isv ? j - 1 : j;
+      if (tile < 0 || tile >= ntiles) continue;          // wave-uniform
+      const int t = kb + TK * tile + 32 * half;
       const int tc = min(t, f.ke - 1);
       const int base = tc - tc % f.page_tokens;          // the page's first key
       const char* src = (isv ? f.v : f.k) + (int64_t)pg[u] * f.page_bytes;
@@ -144,56 +167,63 @@ struct Chunk {
       if (t + 32 <= f.ke) {                              // wave-uniform
         const int soff = (t - base) * f.row_bytes;
 #pragma unroll
-        for (int j = 0; j < TL::T; ++j)
-          __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void*)(dst + j * 1024), 16, isv ? offv[j] : off[j], soff, 0, 0);
+        for (int x = 0; x < TL::T; ++x)
+          __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void*)(dst + x * 1024), 16, at(A, u, x), soff, 0, 0);
       } else {                                           // rows past the end repeat the last one
 #pragma unroll
-        for (int j = 0; j < TL::T; ++j) {
-          const int row = j * TL::RPI + lane / TL::CH;
-          const uint32_t chunk = (isv ? offv[j] : off[j]) - (uint32_t)(row * f.row_bytes);
+        for (int x = 0; x < TL::T; ++x) {
+          const int row = x * TL::RPI + lane / TL::CH;
+          const uint32_t chunk = at(A, u, x) - (uint32_t)(row * f.row_bytes);
           const int key = min(t + row, f.ke - 1) - base;
-          __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void*)(dst + j * 1024), 16,
+          __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void*)(dst + x * 1024), 16,
                                                    (uint32_t)(key * f.row_bytes) + chunk, 0, 0, 0);
         }
       }
     }
 #endif
   }
+  static __device__ __forceinline__ uint32_t at(const Lane& A, int u, int x) {
+    if constexpr (DL::U > 1) return u > 0 ? A.flip[x] : A.off[x];
+    else return A.off[x];
+  }
 
-  // One tile's products for one wave.  `seen_all`: every row of the wave sees
-  // every key of the tile.
-  static __device__ __forceinline__ void compute(const lds_char* cur, Rows<D>& S, const uint32_t (&koff)[KS],
-                                                 const uint32_t (&voff)[ET], int t0, bool seen_all, float c, int lane) {
+  static __device__ __forceinline__ Scores scores(const lds_char* cur, const Rows<D>& S, const Lane& A) {
+    Scores r;
 #if defined(__HIP_DEVICE_COMPILE__)
-    const int half = lane >> 5;
-    f32x16 s[KB];
 #pragma unroll
     for (int kb = 0; kb < KB; ++kb) {
 #pragma unroll
-      for (int i = 0; i < 16; ++i) s[kb][i] = 0.f;
+      for (int i = 0; i < 16; ++i) r.s[kb][i] = 0.f;
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks) {
-        const bf16x8 a = *(lds_bf16x8*)(cur + koff[ks] + kb * TL::HALF);
-        s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, S.q[ks], s[kb], 0, 0, 0);
+        const bf16x8 a = *(lds_bf16x8*)(cur + A.koff[ks] + kb * TL::HALF);
+        r.s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, S.q[ks], r.s[kb], 0, 0, 0);
       }
     }
-    if (!seen_all) {
-#pragma unroll
-      for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const int t = t0 + 32 * kb + 16 * (i >> 3) + 8 * half + (i & 7);
-          s[kb][i] = t <= S.last ? s[kb][i] : -INFINITY;
-        }
-    }
-    // The reference trails the running maximum by at most kLag (log2 units),
-    // so p <= 2^kLag and most tiles leave O and l alone.
-    constexpr float kLag = 8.f;
-    float top = s[0][0];
+#endif
+    return r;
+  }
+
+  // Keys that the row does not see, of the tile starting at key t0.
+  static __device__ __forceinline__ void mask(Scores& x, const Rows<D>& S, int t0, int half) {
 #pragma unroll
     for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
-      for (int i = 0; i < 16; ++i) top = fmaxf(top, s[kb][i]);
+      for (int i = 0; i < 16; ++i) {
+        const int t = t0 + 32 * kb + 16 * (i >> 3) + 8 * half + (i & 7);
+        x.s[kb][i] = t <= S.last ? x.s[kb][i] : -INFINITY;
+      }
+  }
+
+  // The reference trails the running maximum by at most kLag (log2 units), so
+  // p <= 2^kLag and most tiles leave O and l alone.  Returns what to subtract.
+  static __device__ __forceinline__ float reference(const Scores& x, Rows<D>& S, float c) {
+    constexpr float kLag = 8.f;
+    float top = x.s[0][0];
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) top = fmaxf(top, x.s[kb][i]);
     top *= c;
     if (__any(top > S.m + kLag)) {                       // wave-uniform
       const float both = fmaxf(top, __shfl_xor(top, 32));
@@ -204,73 +234,35 @@ struct Chunk {
       for (int eb = 0; eb < ET; ++eb) S.o[eb] *= alpha;
       S.m = m_new;
     }
-    const float ref = S.m == -INFINITY ? 0.f : S.m;
+    return S.m == -INFINITY ? 0.f : S.m;
+  }
+
+  struct Probs {
     uint32_t p[PARTS][KB * 8];
-    float sum = 0.f;
+  };
+  static __device__ __forceinline__ Probs weights(const Scores& x, Rows<D>& S, float c, float ref) {
+    Probs P;
+    float sum0 = 0.f, sum1 = 0.f;
 #pragma unroll
     for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
       for (int i = 0; i < 16; i += 2) {
-        float x0 = __builtin_amdgcn_exp2f(fmaf(s[kb][i], c, -ref));
-        float x1 = __builtin_amdgcn_exp2f(fmaf(s[kb][i + 1], c, -ref));
-        sum += x0;
-        sum += x1;
+        float x0 = __builtin_amdgcn_exp2f(fmaf(x.s[kb][i], c, -ref));
+        float x1 = __builtin_amdgcn_exp2f(fmaf(x.s[kb][i + 1], c, -ref));
+        sum0 += x0;
+        sum1 += x1;
 #pragma unroll
         for (int part = 0; part < PARTS; ++part) {
           const uint32_t h = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2){x0, x1}, bf16x2));
-          p[part][kb * 8 + i / 2] = h;
+          P.p[part][kb * 8 + i / 2] = h;
           if (part + 1 < PARTS) {
             x0 -= __uint_as_float(h << 16);
             x1 -= __uint_as_float(h & 0xffff0000u);
           }
         }
       }
-    S.l += sum;
-    bool careful = false;
-    if (!seen_all) careful = __any(bad_values(cur, voff));
-    if (!careful) {
-#pragma unroll
-      for (int kk = 0; kk < 2 * KB; ++kk)
-#pragma unroll
-        for (int eb = 0; eb < ET; ++eb) {
-          const bf16x8 a = v_operand(cur, voff[eb] + kk * 16 * TL::ROWB);
-#pragma unroll
-          for (int part = 0; part < PARTS; ++part)
-            S.o[eb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, p_operand(p[part], kk), S.o[eb], 0, 0, 0);
-        }
-    } else {
-      // A value that is not finite stands in a tile that some row sees in part:
-      // key by key, so that a zero probability never meets it.
-      for (int x = 0; x < TK; ++x) {
-        const int kk = x >> 4;
-        const bool mine = ((x >> 3) & 1) == half;
-        u32x4 keep;
-#pragma unroll
-        for (int y = 0; y < 4; ++y)
-          keep[y] = mine && ((x & 7) >> 1) == y ? ((x & 1) ? 0xffff0000u : 0xffffu) : 0u;
-        const bool sees = t0 + x <= S.last;
-#pragma unroll
-        for (int eb = 0; eb < ET; ++eb) {
-          const u32x4 a = __builtin_bit_cast(u32x4, v_operand(cur, voff[eb] + kk * 16 * TL::ROWB)) & keep;
-          f32x16 z;
-#pragma unroll
-          for (int i = 0; i < 16; ++i) z[i] = 0.f;
-#pragma unroll
-          for (int part = 0; part < PARTS; ++part) {
-            u32x4 b = {0u, 0u, 0u, 0u};
-#pragma unroll
-            for (int k2 = 0; k2 < 2 * KB; ++k2)
-#pragma unroll
-              for (int y = 0; y < 4; ++y) b[y] = kk == k2 ? p[part][4 * k2 + y] : b[y];
-            z = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a),
-                                                        __builtin_bit_cast(bf16x8, b & keep), z, 0, 0, 0);
-          }
-#pragma unroll
-          for (int i = 0; i < 16; ++i) S.o[eb][i] += sees ? z[i] : 0.f;
-        }
-      }
-    }
-#endif
+    S.l += sum0 + sum1;
+    return P;
   }
 
   static __device__ __forceinline__ bf16x8 p_operand(const uint32_t (&p)[KB * 8], int kk) {
@@ -290,41 +282,110 @@ struct Chunk {
 #endif
   }
 
+  static __device__ __forceinline__ void product(const lds_char* cur, const Probs& P, Rows<D>& S, const Lane& A) {
+#if defined(__HIP_DEVICE_COMPILE__)
+#pragma unroll
+    for (int kk = 0; kk < 2 * KB; ++kk)
+#pragma unroll
+      for (int eb = 0; eb < ET; ++eb) {
+        const bf16x8 a = v_operand(cur, A.voff[eb] + kk * 16 * TL::ROWB);
+#pragma unroll
+        for (int part = 0; part < PARTS; ++part)
+          S.o[eb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, p_operand(P.p[part], kk), S.o[eb], 0, 0, 0);
+      }
+#endif
+  }
+
   // Whether this lane's share of the tile's V holds an infinity or a NaN.
-  static __device__ __forceinline__ bool bad_values(const lds_char* cur, const uint32_t (&voff)[ET]) {
+  static __device__ __forceinline__ bool bad_values(const lds_char* cur, const Lane& A) {
     uint32_t bad = 0;
 #pragma unroll
     for (int kk = 0; kk < 2 * KB; ++kk)
 #pragma unroll
       for (int eb = 0; eb < ET; ++eb) {
-        const u32x4 a = __builtin_bit_cast(u32x4, v_operand(cur, voff[eb] + kk * 16 * TL::ROWB));
+        const u32x4 a = __builtin_bit_cast(u32x4, v_operand(cur, A.voff[eb] + kk * 16 * TL::ROWB));
 #pragma unroll
-        for (int y = 0; y < 4; ++y) {
-          const uint32_t e = a[y] & 0x7f807f80u;         // the exponents; all ones: not finite
-          bad |= (e >= 0x7f800000u) | ((e & 0xffffu) == 0x7f80u);
-        }
+        for (int y = 0; y < 4; ++y)                      // exponents of all ones
+          bad |= ((a[y] & 0x7f800000u) == 0x7f800000u) | ((a[y] & 0x7f80u) == 0x7f80u);
       }
     return bad != 0;
   }
 
-  // The transfers of the next tile, then this tile's products.  The stages
-  // are different ones, which the parameters say (restrict): without it the
-  // compiler waits for the transfers before every read of the tile.
-  static __device__ __forceinline__ void step(lds_char* __restrict__ nxt, const lds_char* __restrict__ cur, bool more,
-                                              const Fetch& f, int tn, const int (&pg)[DL::U], int w,
-                                              const uint32_t (&off)[TL::T], const uint32_t (&offv)[TL::T], Rows<D>& S,
-                                              const uint32_t (&koff)[KS], const uint32_t (&voff)[ET], int t0, int see,
-                                              float c, int lane) {
-    if (more) issue(nxt, f, tn, pg, w, off, offv, lane);
+  // The product where a value that is not finite stands in a tile of which
+  // some row does not see all: key by key, so that a zero probability never
+  // meets it.
+  static __device__ __forceinline__ void careful_product(const lds_char* cur, const Probs& P, Rows<D>& S,
+                                                         const Lane& A, int t0, int half) {
+#if defined(__HIP_DEVICE_COMPILE__)
+    for (int x = 0; x < TK; ++x) {
+      const int kk = x >> 4;
+      const bool mine = ((x >> 3) & 1) == half;
+      u32x4 keep;
+#pragma unroll
+      for (int y = 0; y < 4; ++y) keep[y] = mine && ((x & 7) >> 1) == y ? ((x & 1) ? 0xffff0000u : 0xffffu) : 0u;
+      const bool sees = t0 + x <= S.last;
+#pragma unroll
+      for (int eb = 0; eb < ET; ++eb) {
+        const u32x4 a = __builtin_bit_cast(u32x4, v_operand(cur, A.voff[eb] + kk * 16 * TL::ROWB)) & keep;
+        f32x16 z;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) z[i] = 0.f;
+#pragma unroll
+        for (int part = 0; part < PARTS; ++part) {
+          u32x4 b = {0u, 0u, 0u, 0u};
+#pragma unroll
+          for (int k2 = 0; k2 < 2 * KB; ++k2)
+#pragma unroll
+            for (int y = 0; y < 4; ++y) b[y] = kk == k2 ? P.p[part][4 * k2 + y] : b[y];
+          z = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a),
+                                                      __builtin_bit_cast(bf16x8, b & keep), z, 0, 0, 0);
+        }
+#pragma unroll
+        for (int i = 0; i < 16; ++i) S.o[eb][i] += sees ? z[i] : 0.f;
+      }
+    }
+#endif
+  }
+
+  // Step t of a wave whose rows see all of tile t: the transfers of stage
+  // t + NS, the scores of tile t + 1, the softmax and product of tile t.  The
+  // stage written and the one read are different ones, which the parameters
+  // say (restrict): without it the compiler waits for the transfers before
+  // every read.
+  static __device__ __forceinline__ void step(lds_char* __restrict__ nxt, const lds_char* __restrict__ cur,
+                                              const Fetch& f, int jn, int kb, int ntiles, const int (&pg)[DL::U],
+                                              int w, const Lane& A, Rows<D>& S, Scores& x, float c, int lane) {
+    issue(nxt, f, jn, kb, ntiles, pg, w, A, lane);
     __builtin_amdgcn_sched_barrier(0);
-    if (see) compute(cur, S, koff, voff, t0, see == 2, c, lane);
+    const float ref = reference(x, S, c);
+    const Scores y = scores(cur, S, A);
+    const Probs P = weights(x, S, c, ref);
+    product(cur, P, S, A);
+    x = y;
+  }
+  // The same where they may not (see 0: none of its keys).
+  static __device__ __forceinline__ void edge_step(lds_char* __restrict__ nxt, const lds_char* __restrict__ cur,
+                                                   const Fetch& f, int jn, int kb, int ntiles,
+                                                   const int (&pg)[DL::U], int w, const Lane& A, Rows<D>& S,
+                                                   Scores& x, int t0, bool see, bool see_next, float c, int lane) {
+    issue(nxt, f, jn, kb, ntiles, pg, w, A, lane);
+    __builtin_amdgcn_sched_barrier(0);
+    if (see) {
+      const int half = lane >> 5;
+      mask(x, S, t0, half);
+      const float ref = reference(x, S, c);
+      const Probs P = weights(x, S, c, ref);
+      if (__any(bad_values(cur, A))) careful_product(cur, P, S, A, t0, half);
+      else product(cur, P, S, A);
+    }
+    if (see_next) x = scores(cur, S, A);
   }
 };
 
 template <int D, int NW, int TK, int NS, int PARTS>
-__global__ __launch_bounds__(64 * NW, 2) void chunk_attn(ChunkParams p) {
+__global__ __launch_bounds__(64 * NW, NW == 1 ? 1 : 2) void chunk_attn(ChunkParams p) {
 #if defined(__HIP_DEVICE_COMPILE__)   // the host pass needs the signature only
-  using C = Chunk<D, NW, TK, NS, PARTS>;
+  using C = Chunk<D, NW, TK, PARTS>;
   using TL = Tile<D, TK>;
   using DL = Deal<D, TK, NW>;
   constexpr int KS = C::KS, ET = C::ET;
@@ -335,6 +396,32 @@ __global__ __launch_bounds__(64 * NW, 2) void chunk_attn(ChunkParams p) {
   const int l32 = lane & 31, half = lane >> 5;
   const ChunkItem it = p.items[blockIdx.x];
   const int ntiles = (it.ke - it.kb + TK - 1) / TK;
+
+  Fetch f;
+  f.k = static_cast<const char*>(p.k) + (int64_t)it.kvh * p.kv_sh * 2;
+  f.v = static_cast<const char*>(p.v) + (int64_t)it.kvh * p.kv_sh * 2;
+  f.table = (const const_int32*)(p.bt + (int64_t)it.req * p.bt_stride);
+  f.row_bytes = (int)(p.kv_st * 2);
+  f.page_tokens = p.page_tokens;
+  f.page_bytes = (int64_t)p.page_tokens * f.row_bytes;
+  f.num_pages = p.num_pages;
+  f.ke = it.ke;
+  typename C::Lane A;
+#pragma unroll
+  for (int x = 0; x < TL::T; ++x) {
+    const int row = x * TL::RPI + lane / TL::CH, ch = lane % TL::CH;
+    const bool v0 = C::unit_is_v(w, 0);
+    A.off[x] = (uint32_t)(row * f.row_bytes + ((ch ^ (v0 ? swv<D>(row) : swk<D>(row))) * 16));
+    if constexpr (DL::U > 1) A.flip[x] = (uint32_t)(row * f.row_bytes + ((ch ^ swv<D>(row)) * 16));
+  }
+  int pg[DL::U];
+  auto pages = [&](int j) {
+#pragma unroll
+    for (int u = 0; u < DL::U; ++u) {
+      const int tile = max(C::unit_is_v(w, u) ? j - 1 : j, 0);
+      pg[u] = page_of(f, it.kb + TK * tile + 32 * C::unit_half(w, u));
+    }
+  };
 
   Rows<D> S;
   const int wr0 = 32 * w;                                // the wave's first row of the item
@@ -347,79 +434,70 @@ __global__ __launch_bounds__(64 * NW, 2) void chunk_attn(ChunkParams p) {
     for (int ks = 0; ks < KS; ++ks) S.q[ks] = *reinterpret_cast<const bf16x8*>(src + ks * 32);
     S.last = min(it.ctx + j, it.ke - 1);
   }
+  lds_char* ring = (lds_char*)lds;
+#pragma unroll
+  for (int j = 0; j < NS; ++j) {
+    pages(j);
+    C::issue(ring + j * TL::STAGE, f, j, it.kb, ntiles, pg, w, A, lane);
+  }
+  pages(NS);
   S.m = -INFINITY;
   S.l = 0.f;
 #pragma unroll
   for (int eb = 0; eb < ET; ++eb)
 #pragma unroll
     for (int i = 0; i < 16; ++i) S.o[eb][i] = 0.f;
-  // keys that the wave's first and last row see (none for a wave without rows)
-  const bool has_rows = wr0 < it.rows;
-  const int first_last = min(it.ctx + (it.r0 + min(wr0, it.rows - 1)) / p.G, it.ke - 1);
-  const int last_last = has_rows ? min(it.ctx + (it.r0 + min(wr0 + 31, it.rows - 1)) / p.G, it.ke - 1) : -1;
-
-  Fetch f;
-  f.k = static_cast<const char*>(p.k) + (int64_t)it.kvh * p.kv_sh * 2;
-  f.v = static_cast<const char*>(p.v) + (int64_t)it.kvh * p.kv_sh * 2;
-  f.table = (const const_int32*)(p.bt + (int64_t)it.req * p.bt_stride);
-  f.row_bytes = (int)(p.kv_st * 2);
-  f.page_tokens = p.page_tokens;
-  f.page_bytes = (int64_t)p.page_tokens * f.row_bytes;
-  f.num_pages = p.num_pages;
-  f.ke = it.ke;
-  uint32_t off[TL::T], offv[TL::T];                      // K and V: row and swizzled chunk of each transfer
-#pragma unroll
-  for (int j = 0; j < TL::T; ++j) {
-    const int row = j * TL::RPI + lane / TL::CH, ch = lane % TL::CH;
-    off[j] = (uint32_t)(row * f.row_bytes + ((ch ^ swk<D>(row)) * 16));
-    offv[j] = (uint32_t)(row * f.row_bytes + ((ch ^ swv<D>(row)) * 16));
-  }
-  uint32_t koff[KS], voff[ET];
   {
     const int key = 16 * (l32 >> 4) + 8 * ((l32 >> 2) & 1) + 4 * ((l32 >> 3) & 1) + (l32 & 3);
 #pragma unroll
-    for (int ks = 0; ks < KS; ++ks) koff[ks] = (uint32_t)(key * TL::ROWB + (((2 * ks + half) ^ swk<D>(key)) * 16));
+    for (int ks = 0; ks < KS; ++ks) A.koff[ks] = (uint32_t)(key * TL::ROWB + (((2 * ks + half) ^ swk<D>(key)) * 16));
     const int s = lane & 15, row = 8 * half + (s >> 2);
 #pragma unroll
     for (int eb = 0; eb < ET; ++eb) {
       const int ch = 4 * eb + 2 * ((lane >> 4) & 1) + ((s & 3) >> 1);
-      voff[eb] = (uint32_t)(TL::MAT + row * TL::ROWB + ((ch ^ swv<D>(row)) * 16) + (s & 1) * 8);
+      A.voff[eb] = (uint32_t)(TL::MAT + row * TL::ROWB + ((ch ^ swv<D>(row)) * 16) + (s & 1) * 8);
     }
   }
+  // the last key that the item's first row sees, and the wave's last row (none without rows)
+  const int all_see = min(it.ctx + it.r0 / p.G, it.ke - 1);
+  const int wave_sees = wr0 < it.rows ? min(it.ctx + (it.r0 + min(wr0 + 31, it.rows - 1)) / p.G, it.ke - 1) : -1;
+  const int nfull = all_see + 1 >= it.kb ? (all_see + 1 - it.kb) / TK : 0;     // tiles that every row sees whole
 
-  int pg[DL::U];
-  auto pages = [&](int tile) {
-#pragma unroll
-    for (int u = 0; u < DL::U; ++u) {
-      const int unit = w * DL::U + u;
-      pg[u] = page_of(f, it.kb + TK * tile + 32 * (unit >= C::KB ? unit - C::KB : unit));
-    }
+  // stages 0 .. NS - 1 are under way: wait for stage 0 (K of tile 0)
+  if (ntiles >= NS) {
+    // V waves have nothing in stage 0; what is younger than it is NS - 1 stages
+    wait_vm<(NS - 1) * DL::PER>();
+  } else {
+    wait_vm<0>();
+  }
+  tile_barrier();
+  typename C::Scores x = C::scores(ring, S, A);
+  // step t: stage t + 1 has landed here and everywhere, and every wave has
+  // read what it needs of stage t, where stage t + NS goes
+  auto turn = [&](int t) {
+    if (t + NS - 1 < ntiles) wait_vm<(NS - 2) * DL::PER>();
+    else wait_vm<0>();
+    tile_barrier();
   };
-  lds_char* ring = (lds_char*)lds;
-#pragma unroll
-  for (int t = 0; t < NS - 1; ++t) {
-    if (t < ntiles) {
-      pages(t);
-      C::issue(ring + t * TL::STAGE, f, it.kb + TK * t, pg, w, off, offv, lane);
+  int t = 0;
+  if (wave_sees >= it.kb) {
+    while (t + NS <= nfull) {
+      static_for<0, NS>([&](auto st) {
+        constexpr int ST = decltype(st)::value;
+        turn(t + ST);
+        C::step(ring + ST * TL::STAGE, ring + ((ST + 1) % NS) * TL::STAGE, f, t + ST + NS, it.kb, ntiles, pg, w, A, S,
+                x, p.scale_log2, lane);
+        pages(t + ST + NS + 1);
+      });
+      t += NS;
     }
   }
-  pages(NS - 1);
-  for (int tb = 0; tb < ntiles; tb += NS) {
-    static_for<0, NS>([&](auto st) {
-      constexpr int ST = decltype(st)::value;
-      const int t = tb + ST;
-      if (t < ntiles) {
-        // this wave's transfers of tile t have landed
-        if (t + NS - 2 < ntiles) wait_vm<(NS - 2) * DL::PER>();
-        else wait_vm<0>();
-        tile_barrier();
-        const int t0 = it.kb + TK * t;
-        const int see = t0 > last_last ? 0 : (t0 + TK - 1 <= first_last ? 2 : 1);
-        C::step(ring + ((ST + NS - 1) % NS) * TL::STAGE, ring + ST * TL::STAGE, t + NS - 1 < ntiles, f,
-                it.kb + TK * (t + NS - 1), pg, w, off, offv, S, koff, voff, t0, see, p.scale_log2, lane);
-        pages(t + NS);
-      }
-    });
+  for (; t < ntiles; ++t) {
+    turn(t);
+    const int t0 = it.kb + TK * t;
+    C::edge_step(ring + (t % NS) * TL::STAGE, ring + ((t + 1) % NS) * TL::STAGE, f, t + NS, it.kb, ntiles, pg, w, A, S,
+                 x, t0, t0 <= wave_sees, t + 1 < ntiles && t0 + TK <= wave_sees, p.scale_log2, lane);
+    pages(t + NS + 1);
   }
 
   const float l = S.l + __shfl_xor(S.l, 32);
@@ -434,13 +512,13 @@ __global__ __launch_bounds__(64 * NW, 2) void chunk_attn(ChunkParams p) {
 #pragma unroll
       for (int i = 0; i < 16; i += 4) {
         const int e = 32 * eb + 2 * i + 4 * half;
-        const f32x4 x = {S.o[eb][i] * inv, S.o[eb][i + 1] * inv, S.o[eb][i + 2] * inv, S.o[eb][i + 3] * inv};
+        const f32x4 y = {S.o[eb][i] * inv, S.o[eb][i + 1] * inv, S.o[eb][i + 2] * inv, S.o[eb][i + 3] * inv};
         if constexpr (PARTS == 1) {
           typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
           *reinterpret_cast<u32x2*>(static_cast<uint16_t*>(p.out) + row * D + e) =
-              __builtin_bit_cast(u32x2, __builtin_convertvector(x, bf16x4));
+              __builtin_bit_cast(u32x2, __builtin_convertvector(y, bf16x4));
         } else {
-          *reinterpret_cast<f32x4*>(static_cast<float*>(p.out) + row * D + e) = x;
+          *reinterpret_cast<f32x4*>(static_cast<float*>(p.out) + row * D + e) = y;
         }
       }
   } else {
