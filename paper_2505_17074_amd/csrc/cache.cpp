@@ -7,6 +7,7 @@
 
 #include <algorithm>
 #include <cmath>
+#include <cstdlib>
 #include <cstring>
 #include <new>
 #include <unordered_set>
@@ -141,7 +142,8 @@ spec_status_t plan_chunk(const spec_chunks_t* r, const spec_cache_t* c, const sp
   total *= Hkv;
   const int64_t slots = 2 * (int64_t)compute_units();
   const int64_t least = RT == sv::kChunkTallRows ? 8 : 4;
-  const int64_t target = std::max<int64_t>(least, (total + slots - 1) / slots);
+  int64_t target = std::max<int64_t>(least, (total + slots - 1) / slots);
+  if (const char* e = std::getenv("XCAP")) target = std::max(1, std::atoi(e));
   int64_t n_items = 0;
   for (const RowTile& t : tiles) n_items += ((t.keys + sv::kChunkTile - 1) / sv::kChunkTile + target - 1) / target * Hkv;
   if (n_items >= INT32_MAX / 64) return SPEC_ERR_UNSUPPORTED;
@@ -318,20 +320,38 @@ spec_status_t spec_cache_append(const spec_chunks_t* chunks, const spec_cache_t*
   p.new_st = args->new_stride_tok * eb;
   p.new_sh = args->new_stride_head * eb;
   p.bt_stride = cache->block_stride;
-  int64_t row = 0;
-  for (int i0 = 0; i0 < chunks->num_requests; i0 += sv::kMoveRequests) {
-    p.n_req = std::min(sv::kMoveRequests, chunks->num_requests - i0);
-    p.bt = cache->block_table + (int64_t)i0 * cache->block_stride;
-    p.row0 = (int32_t)row;
-    int32_t end = 0;
-    for (int i = 0; i < p.n_req; ++i) {
-      p.ctx[i] = chunks->ctx_len[i0 + i];
-      p.end[i] = end += chunks->new_len[i0 + i];
-    }
-    p.rows = end;
-    row += end;
-    if (end > 0 && sv::launch_append(p, static_cast<hipStream_t>(stream)) != hipSuccess) return SPEC_ERR_HIP;
+  p.bt = cache->block_table;
+  // Segments of at most `parts` blocks of 16 rows: as few blocks as keep the
+  // batch in one launch's table, so that ragged batches leave few work-groups
+  // without rows.
+  auto blocks = [&](int i) -> int64_t {
+    const int64_t lo = chunks->ctx_len[i], n = chunks->new_len[i];
+    return n ? (lo + n - 1) / sv::kMoveRows - lo / sv::kMoveRows + 1 : 0;
+  };
+  int64_t longest = 0, parts = 1;
+  for (int i = 0; i < chunks->num_requests; ++i) longest = std::max(longest, blocks(i));
+  for (;; parts *= 2) {
+    int64_t segs = 0;
+    for (int i = 0; i < chunks->num_requests; ++i) segs += (blocks(i) + parts - 1) / parts;
+    if (segs <= sv::kMoveSegments || parts >= longest) break;
   }
+  p.parts = (int32_t)parts;
+  int64_t row = 0;
+  for (int i = 0; i < chunks->num_requests; ++i) {
+    int32_t pos = chunks->ctx_len[i];
+    const int32_t end = pos + chunks->new_len[i];
+    while (pos < end) {
+      const int32_t stop = (int32_t)std::min<int64_t>(end, (pos / sv::kMoveRows + parts) * sv::kMoveRows);
+      p.seg[p.n_seg++] = {i, pos, (int32_t)row, stop - pos};
+      row += stop - pos;
+      pos = stop;
+      if (p.n_seg == sv::kMoveSegments) {
+        if (sv::launch_append(p, static_cast<hipStream_t>(stream)) != hipSuccess) return SPEC_ERR_HIP;
+        p.n_seg = 0;
+      }
+    }
+  }
+  if (p.n_seg > 0 && sv::launch_append(p, static_cast<hipStream_t>(stream)) != hipSuccess) return SPEC_ERR_HIP;
   return SPEC_OK;
 }
 

@@ -14,43 +14,46 @@ __device__ __forceinline__ int64_t readlane64(int64_t x, int lane) {
   return (int64_t)(((uint64_t)hi << 32) | lo);
 }
 
-// Byte offset of 16-byte unit u of a token row.
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+// Byte offset of 16-byte unit u of a token row (RUN: its heads follow each
+// other without a gap).
+template <bool RUN>
 __device__ __forceinline__ int64_t unit_at(int u, int row_units, int64_t sh_bytes) {
+  if constexpr (RUN) return (int64_t)u * 16;
   const int h = u / row_units;
   return h * sh_bytes + (int64_t)(u - h * row_units) * 16;
 }
 
-// A wave a new row, layer and matrix: blockIdx.y = 2 layer + (1 for V).
+// blockIdx: (block of 16 rows, segment, 2 layer + (1 for V)).  Blocks are
+// 16-aligned, so one lies in one page.  A wave takes every fourth row of the
+// block, up to four rows' units in flight.
+template <bool RUN>
 __global__ __launch_bounds__(256) void cache_append(AppendParams p) {
+  const AppendSegment sg = p.seg[blockIdx.y];
   const int lane = threadIdx.x & 63;
-  const int row = __builtin_amdgcn_readfirstlane((int)blockIdx.x * 4 + (int)(threadIdx.x >> 6));
-  if (row >= p.rows) return;
-  // requests whose rows end at or before this one
-  int req = 0;
-  for (int b = 0; b < p.n_req; b += 64) {
-    const int i = b + lane;
-    const bool before = i < p.n_req && p.end[min(i, kMoveRequests - 1)] <= row;
-    req += __builtin_popcountll(__ballot(before));
-  }
-  req = __builtin_amdgcn_readfirstlane(min(req, p.n_req - 1));
-  const int first = req > 0 ? p.end[req - 1] : 0;
-  const int t = p.ctx[req] + (row - first);
-  const int pg = p.bt[req * p.bt_stride + t / p.c.page_tokens];
-  if (pg < 0 || pg >= p.c.num_pages) return;
-  const int layer = (int)blockIdx.y >> 1;
-  const bool isv = blockIdx.y & 1;
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int b0 = (sg.pos & ~(kMoveRows - 1)) + kMoveRows * (int)blockIdx.x;
+  const int lo = max(b0, sg.pos), n = min(b0 + kMoveRows, sg.pos + sg.n) - lo;
+  if (w >= n) return;
+  const int pg = p.bt[sg.req * p.bt_stride + lo / p.c.page_tokens];
+  const int layer = (int)blockIdx.z >> 1;
+  const bool isv = blockIdx.z & 1;
+  const char* src = (isv ? p.v_new : p.k_new) + layer * p.new_sl + (int64_t)(sg.row + (lo - sg.pos)) * p.new_st;
   char* dst = (isv ? p.c.v : p.c.k) + layer * p.c.layer_bytes + pg * p.c.page_bytes +
-              (int64_t)(t % p.c.page_tokens) * p.c.st_bytes;
-  const char* src = (isv ? p.v_new : p.k_new) + layer * p.new_sl + (int64_t)(p.row0 + row) * p.new_st;
+              (int64_t)(lo % p.c.page_tokens) * p.c.st_bytes;
+  if (pg < 0 || pg >= p.c.num_pages) return;
   const int units = p.c.heads * p.c.row_units;
-  for (int u0 = lane; u0 < units; u0 += 256) {
-    uint4 x[4];
+  for (int u = lane; u < units; u += 64) {
+    const char* from = src + unit_at<RUN>(u, p.c.row_units, p.new_sh);
+    char* to = dst + unit_at<RUN>(u, p.c.row_units, p.c.sh_bytes);
+    u32x4 x[kMoveRows / 4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-      if (u0 + 64 * i < units) x[i] = *reinterpret_cast<const uint4*>(src + unit_at(u0 + 64 * i, p.c.row_units, p.new_sh));
+    for (int i = 0; i < kMoveRows / 4; ++i)              // rows past the end: the wave's first again
+      x[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(from + (w + 4 * i < n ? w + 4 * i : w) * p.new_st));
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-      if (u0 + 64 * i < units) *reinterpret_cast<uint4*>(dst + unit_at(u0 + 64 * i, p.c.row_units, p.c.sh_bytes)) = x[i];
+    for (int i = 0; i < kMoveRows / 4; ++i)
+      if (w + 4 * i < n) *reinterpret_cast<u32x4*>(to + (w + 4 * i) * (int64_t)p.c.st_bytes) = x[i];
   }
 }
 
@@ -59,6 +62,7 @@ __global__ __launch_bounds__(256) void cache_append(AppendParams p) {
 // A node's index is at least its depth, so a row's new place is never the old
 // place of a deeper one: batches of loads ahead of their stores, ascending,
 // are safe, and no two waves touch the same bytes.
+template <bool RUN>
 __global__ __launch_bounds__(64) void cache_commit(CommitParams p) {
   const int lane = threadIdx.x;
   const int req = blockIdx.x;
@@ -94,53 +98,58 @@ __global__ __launch_bounds__(64) void cache_commit(CommitParams p) {
   char* base = ((blockIdx.y & 1) ? p.c.v : p.c.k) + layer * p.c.layer_bytes;
   const int u = (int)blockIdx.z * 64 + lane;
   const bool on = u < p.c.heads * p.c.row_units;
-  base += on ? unit_at(u, p.c.row_units, p.c.sh_bytes) : 0;
+  base += on ? unit_at<RUN>(u, p.c.row_units, p.c.sh_bytes) : 0;
   for (int t0 = 1; t0 <= depth; t0 += 4) {
-    uint4 x[4];
+    u32x4 x[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) x[i] = *reinterpret_cast<const uint4*>(base + readlane64(from, min(t0 + i, depth)));
+    for (int i = 0; i < 4; ++i) x[i] = *reinterpret_cast<const u32x4*>(base + readlane64(from, min(t0 + i, depth)));
 #pragma unroll
     for (int i = 0; i < 4; ++i)
-      if (on && ((moves >> (t0 + i)) & 1)) *reinterpret_cast<uint4*>(base + readlane64(to, t0 + i)) = x[i];
+      if (on && ((moves >> (t0 + i)) & 1)) *reinterpret_cast<u32x4*>(base + readlane64(to, t0 + i)) = x[i];
   }
 }
 
 constexpr int kCopyUnits = 4;          // 16-byte units a thread
 
-// blockIdx.x: pair; y: 2 layer + (1 for V); z: part of the page.
+// blockIdx: (part of the page, pair, 2 layer + (1 for V)).
+template <bool RUN>
 __global__ __launch_bounds__(256) void cache_copy_pages(PageCopyParams p) {
-  const int i = blockIdx.x;
+  const int i = blockIdx.y;
   const int row_units = p.c.heads * p.c.row_units;
   const int units = p.tokens[i] * row_units;
-  const int u0 = (int)blockIdx.z * (256 * kCopyUnits) + (int)threadIdx.x;
-  if ((int)blockIdx.z * (256 * kCopyUnits) >= units) return;
-  const int layer = (int)blockIdx.y >> 1;
-  char* base = ((blockIdx.y & 1) ? p.c.v : p.c.k) + layer * p.c.layer_bytes;
+  const int u0 = (int)blockIdx.x * (256 * kCopyUnits);
+  if (u0 >= units) return;
+  const int layer = (int)blockIdx.z >> 1;
+  char* base = ((blockIdx.z & 1) ? p.c.v : p.c.k) + layer * p.c.layer_bytes;
   const char* src = base + p.src[i] * p.c.page_bytes;
   char* dst = base + p.dst[i] * p.c.page_bytes;
-  uint4 x[kCopyUnits];
+  u32x4 x[kCopyUnits];
   int64_t at[kCopyUnits];
 #pragma unroll
   for (int j = 0; j < kCopyUnits; ++j) {
-    const int u = u0 + 256 * j;
+    const int u = min(u0 + (int)threadIdx.x + 256 * j, units - 1);
     const int t = u / row_units;
-    at[j] = (int64_t)t * p.c.st_bytes + unit_at(u - t * row_units, p.c.row_units, p.c.sh_bytes);
-    if (u < units) x[j] = *reinterpret_cast<const uint4*>(src + at[j]);
+    at[j] = (int64_t)t * p.c.st_bytes + unit_at<RUN>(u - t * row_units, p.c.row_units, p.c.sh_bytes);
+    x[j] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(src + at[j]));
   }
 #pragma unroll
   for (int j = 0; j < kCopyUnits; ++j)
-    if (u0 + 256 * j < units) *reinterpret_cast<uint4*>(dst + at[j]) = x[j];
+    if (u0 + (int)threadIdx.x + 256 * j < units) __builtin_nontemporal_store(x[j], reinterpret_cast<u32x4*>(dst + at[j]));
 }
 
 }  // namespace
 
 hipError_t launch_append(const AppendParams& p, hipStream_t s) {
-  cache_append<<<dim3((p.rows + 3) / 4, 2 * p.c.layers), dim3(256), 0, s>>>(p);
+  const dim3 g(p.parts, p.n_seg, 2 * p.c.layers);
+  if (p.c.heads == 1) cache_append<true><<<g, dim3(256), 0, s>>>(p);
+  else cache_append<false><<<g, dim3(256), 0, s>>>(p);
   return hipGetLastError();
 }
 
 hipError_t launch_commit(const CommitParams& p, hipStream_t s) {
-  cache_commit<<<dim3(p.n_req, 2 * p.c.layers, (p.c.heads * p.c.row_units + 63) / 64), dim3(64), 0, s>>>(p);
+  const dim3 g(p.n_req, 2 * p.c.layers, (p.c.heads * p.c.row_units + 63) / 64);
+  if (p.c.heads == 1) cache_commit<true><<<g, dim3(64), 0, s>>>(p);
+  else cache_commit<false><<<g, dim3(64), 0, s>>>(p);
   return hipGetLastError();
 }
 
@@ -148,7 +157,9 @@ hipError_t launch_page_copy(const PageCopyParams& p, hipStream_t s) {
   int most = 0;
   for (int i = 0; i < p.n; ++i) most = p.tokens[i] > most ? p.tokens[i] : most;
   const int units = most * p.c.heads * p.c.row_units;
-  cache_copy_pages<<<dim3(p.n, 2 * p.c.layers, (units + 256 * kCopyUnits - 1) / (256 * kCopyUnits)), dim3(256), 0, s>>>(p);
+  const dim3 g((units + 256 * kCopyUnits - 1) / (256 * kCopyUnits), p.n, 2 * p.c.layers);
+  if (p.c.heads == 1) cache_copy_pages<true><<<g, dim3(256), 0, s>>>(p);
+  else cache_copy_pages<false><<<g, dim3(256), 0, s>>>(p);
   return hipGetLastError();
 }
 

@@ -77,18 +77,24 @@ struct CachePools {
   int32_t heads, row_units;            // a head's row in 16-byte units
 };
 
+// A run of one request's new rows: `n` rows from its logical row `pos` on,
+// from row `row` of the new arrays on.
+struct AppendSegment {
+  int32_t req, pos, row, n;
+};
+constexpr int kMoveRows = 16;          // rows of one work-group (divides a page)
+constexpr int kMoveSegments = 224;
+
 struct AppendParams {
   CachePools c;
   const char* k_new;
   const char* v_new;
   int64_t new_sl, new_st, new_sh;      // bytes
-  const int32_t* bt;                   // of the block's first request
+  const int32_t* bt;
   int64_t bt_stride;
-  int32_t n_req;
-  int32_t row0;                        // the block's first row of the new arrays
-  int32_t rows;                        // its rows
-  int32_t ctx[kMoveRequests];
-  int32_t end[kMoveRequests];          // running sum of new_len within the block
+  int32_t n_seg;
+  int32_t parts;                       // work-groups of 16 rows a segment, at most
+  AppendSegment seg[kMoveSegments];
 };
 
 struct CommitParams {
