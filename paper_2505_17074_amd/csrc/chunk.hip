@@ -12,6 +12,7 @@ namespace {
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
@@ -56,6 +57,7 @@ struct Tile {
   static constexpr int STAGE = 2 * MAT;
   static constexpr int RPI = 1024 / ROWB;     // rows of one transfer (64 lanes x 16 bytes)
   static constexpr int T = 32 / RPI;          // transfers of a 32-row half
+  static constexpr int NOFF = D == 128 ? 4 : 2;   // transfers after which K's swizzle comes round
 };
 template <int D>
 __device__ __forceinline__ int swk(int r) {
@@ -80,16 +82,32 @@ struct Deal {
 struct Fetch {
   const char* k;             // this KV head's rows of page 0
   const char* v;
-  const const_int32* table;  // the request's page ids
+  const int32_t* pages;      // the request's page ids
   int64_t page_bytes;
   int32_t page_tokens, num_pages, row_bytes;
   int32_t ke;
 };
 
-// The page of the 32-row half that starts at key t (clamped to the item).
+// Lane l's 32-key block b + l of the item (from key kb on): its page, and the
+// place in it of its first key (of the item's last one for blocks behind it).
+// One load and one division serve 64 blocks; a step reads its block's by lane.
+// (A scalar load a step had its latency in every step.)
+struct Window {
+  int b;
+  int pg, place;
+};
+__device__ __forceinline__ void look(Window& x, const Fetch& f, int kb, int b, int lane) {
+  const int t = min(kb + 32 * (b + lane), f.ke - 1);
+  const int i = t / f.page_tokens;
+  x.b = b;
+  x.place = t - i * f.page_tokens;
+  x.pg = min(max(f.pages[i], 0), f.num_pages - 1);
+}
+
+// The page of key t.
 __device__ __forceinline__ int page_of(const Fetch& f, int t) {
   const int i = __builtin_amdgcn_readfirstlane(min(t, f.ke - 1) / f.page_tokens);
-  const int pg = f.table[i];
+  const int pg = ((const const_int32*)f.pages)[i];
   return __builtin_amdgcn_readfirstlane(min(max(pg, 0), f.num_pages - 1));
 }
 
@@ -127,6 +145,10 @@ struct Chunk {
   using TL = Tile<D, TK>;
   using DL = Deal<D, TK, NW>;
   static constexpr int KS = D / 16, ET = D / 32, KB = TK / 32;
+  // Cache policy of the transfers.  One wave's rows are all that read these keys:
+  // nt, the streaming hint (64 single tokens over 512-8192 rows 217 -> 190 us);
+  // larger tiles' keys are read again by the request's other tiles.
+  static constexpr int CPOL = NW == 1 ? 2 : 0;
   static_assert(DL::U == 1 || KB == 1, "a wave's units are one, or K and V of a 32-key tile");
   struct Scores {
     f32x16 s[KB];
@@ -135,8 +157,8 @@ struct Chunk {
   struct Lane {
     uint32_t koff[KS];         // K operand: chunk 2 ks + lane half of the lane's key row (keys 32.. : + HALF)
     uint32_t voff[ET];         // V operand: the transposing read's place (keys 16 kk ..: + 16 kk rows)
-    uint32_t off[TL::T];       // transfers: row and swizzled chunk (one matrix a wave, or K and V by `flip`)
-    uint32_t flip[DL::U > 1 ? TL::T : 1];
+    uint32_t off[TL::NOFF];    // transfer x of a half: lane's row among its RPI and its swizzled chunk, by x % NOFF
+    uint32_t offv;             // the same for V where a wave fetches both
   };
 
   // Unit u of wave w: V after K, the halves in order.
@@ -146,45 +168,59 @@ struct Chunk {
     return x >= KB ? x - KB : x;
   }
 
+  // The block (of 32 keys from the item's first on) that unit 0 fetches for
+  // stage j; a second unit is V of the tile before.
+  static __device__ __forceinline__ int block_of(int j, int w) {
+    return KB * max(unit_is_v(w, 0) ? j - 1 : j, 0) + unit_half(w, 0);
+  }
+
   // The wave's units of stage j: K of tile j, V of tile j - 1, whichever of
-  // them the item has (tiles begin at key kb).
-  static __device__ __forceinline__ void issue(lds_char* stage, const Fetch& f, int j, int kb, int ntiles,
-                                               const int (&pg)[DL::U], int w, const Lane& A, int lane) {
+  // them the item has (tiles begin at key kb).  Then the window for the next
+  // stage: where a load is due it lands with the transfers.
+  static __device__ __forceinline__ void issue(lds_char* stage, const Fetch& f, int j, int kb, int ntiles, Window& win,
+                                               int2& before, int w, const Lane& A, int lane) {
 #if defined(__HIP_DEVICE_COMPILE__)
+    const int bl = block_of(j, w) - win.b;
+    const int2 now = make_int2(__builtin_amdgcn_readlane(win.pg, bl), __builtin_amdgcn_readlane(win.place, bl));
 #pragma unroll
     for (int u = 0; u < DL::U; ++u) {
       const bool isv = unit_is_v(w, u);
       const int half = unit_half(w, u);
       const int tile = isv ? j - 1 : j;
       if (tile < 0 || tile >= ntiles) continue;          // wave-uniform
+      const int2 at_page = u == 0 ? now : before;
       const int t = kb + TK * tile + 32 * half;
-      const int tc = min(t, f.ke - 1);
-      const int base = tc - tc % f.page_tokens;          // the page's first key
-      const char* src = (isv ? f.v : f.k) + (int64_t)pg[u] * f.page_bytes;
+      const char* src = (isv ? f.v : f.k) + (int64_t)at_page.x * f.page_bytes;
       const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc(
           (void*)src, 0, (f.page_tokens - 1) * f.row_bytes + TL::ROWB, 0x00020000);
       lds_char* dst = stage + (isv ? TL::MAT : 0) + half * TL::HALF;
+      const int soff = at_page.y * f.row_bytes;
       if (t + 32 <= f.ke) {                              // wave-uniform
-        const int soff = (t - base) * f.row_bytes;
 #pragma unroll
         for (int x = 0; x < TL::T; ++x)
-          __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void*)(dst + x * 1024), 16, at(A, u, x), soff, 0, 0);
+          __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void*)(dst + x * 1024), 16, at(A, u, x),
+                                                   soff + x * TL::RPI * f.row_bytes, 0, CPOL);
       } else {                                           // rows past the end repeat the last one
+        int ln = lane;
+        asm("" : "+v"(ln));                              // nothing of this branch before the loop
+        const int lrow = ln / TL::CH, last = f.ke - 1 - t;
 #pragma unroll
         for (int x = 0; x < TL::T; ++x) {
-          const int row = x * TL::RPI + lane / TL::CH;
-          const uint32_t chunk = at(A, u, x) - (uint32_t)(row * f.row_bytes);
-          const int key = min(t + row, f.ke - 1) - base;
+          const uint32_t chunk = at(A, u, x) - (uint32_t)(lrow * f.row_bytes);
+          const int row = max(min(x * TL::RPI + lrow, last), 0);
           __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void*)(dst + x * 1024), 16,
-                                                   (uint32_t)(key * f.row_bytes) + chunk, 0, 0, 0);
+                                                   (uint32_t)(row * f.row_bytes) + chunk, soff, 0, CPOL);
         }
       }
     }
+    before = now;
+    const int next = block_of(j + 1, w);
+    if (next >= win.b + 64) look(win, f, kb, next, lane);
 #endif
   }
   static __device__ __forceinline__ uint32_t at(const Lane& A, int u, int x) {
-    if constexpr (DL::U > 1) return u > 0 ? A.flip[x] : A.off[x];
-    else return A.off[x];
+    if constexpr (DL::U > 1) return u > 0 ? A.offv : A.off[x % TL::NOFF];
+    else return A.off[x % TL::NOFF];
   }
 
   static __device__ __forceinline__ Scores scores(const lds_char* cur, const Rows<D>& S, const Lane& A) {
@@ -206,13 +242,11 @@ struct Chunk {
 
   // Keys that the row does not see, of the tile starting at key t0.
   static __device__ __forceinline__ void mask(Scores& x, const Rows<D>& S, int t0, int half) {
+    const int lim = S.last - t0 - 8 * half;
 #pragma unroll
     for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const int t = t0 + 32 * kb + 16 * (i >> 3) + 8 * half + (i & 7);
-        x.s[kb][i] = t <= S.last ? x.s[kb][i] : -INFINITY;
-      }
+      for (int i = 0; i < 16; ++i) x.s[kb][i] = 32 * kb + 16 * (i >> 3) + (i & 7) <= lim ? x.s[kb][i] : -INFINITY;
   }
 
   // The reference trails the running maximum by at most kLag (log2 units), so
@@ -296,66 +330,15 @@ struct Chunk {
 #endif
   }
 
-  // Whether this lane's share of the tile's V holds an infinity or a NaN.
-  static __device__ __forceinline__ bool bad_values(const lds_char* cur, const Lane& A) {
-    uint32_t bad = 0;
-#pragma unroll
-    for (int kk = 0; kk < 2 * KB; ++kk)
-#pragma unroll
-      for (int eb = 0; eb < ET; ++eb) {
-        const u32x4 a = __builtin_bit_cast(u32x4, v_operand(cur, A.voff[eb] + kk * 16 * TL::ROWB));
-#pragma unroll
-        for (int y = 0; y < 4; ++y)                      // exponents of all ones
-          bad |= ((a[y] & 0x7f800000u) == 0x7f800000u) | ((a[y] & 0x7f80u) == 0x7f80u);
-      }
-    return bad != 0;
-  }
-
-  // The product where a value that is not finite stands in a tile of which
-  // some row does not see all: key by key, so that a zero probability never
-  // meets it.
-  static __device__ __forceinline__ void careful_product(const lds_char* cur, const Probs& P, Rows<D>& S,
-                                                         const Lane& A, int t0, int half) {
-#if defined(__HIP_DEVICE_COMPILE__)
-    for (int x = 0; x < TK; ++x) {
-      const int kk = x >> 4;
-      const bool mine = ((x >> 3) & 1) == half;
-      u32x4 keep;
-#pragma unroll
-      for (int y = 0; y < 4; ++y) keep[y] = mine && ((x & 7) >> 1) == y ? ((x & 1) ? 0xffff0000u : 0xffffu) : 0u;
-      const bool sees = t0 + x <= S.last;
-#pragma unroll
-      for (int eb = 0; eb < ET; ++eb) {
-        const u32x4 a = __builtin_bit_cast(u32x4, v_operand(cur, A.voff[eb] + kk * 16 * TL::ROWB)) & keep;
-        f32x16 z;
-#pragma unroll
-        for (int i = 0; i < 16; ++i) z[i] = 0.f;
-#pragma unroll
-        for (int part = 0; part < PARTS; ++part) {
-          u32x4 b = {0u, 0u, 0u, 0u};
-#pragma unroll
-          for (int k2 = 0; k2 < 2 * KB; ++k2)
-#pragma unroll
-            for (int y = 0; y < 4; ++y) b[y] = kk == k2 ? P.p[part][4 * k2 + y] : b[y];
-          z = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a),
-                                                      __builtin_bit_cast(bf16x8, b & keep), z, 0, 0, 0);
-        }
-#pragma unroll
-        for (int i = 0; i < 16; ++i) S.o[eb][i] += sees ? z[i] : 0.f;
-      }
-    }
-#endif
-  }
-
   // Step t of a wave whose rows see all of tile t: the transfers of stage
   // t + NS, the scores of tile t + 1, the softmax and product of tile t.  The
   // stage written and the one read are different ones, which the parameters
   // say (restrict): without it the compiler waits for the transfers before
   // every read.
   static __device__ __forceinline__ void step(lds_char* __restrict__ nxt, const lds_char* __restrict__ cur,
-                                              const Fetch& f, int jn, int kb, int ntiles, const int (&pg)[DL::U],
+                                              const Fetch& f, int jn, int kb, int ntiles, Window& win, int2& before,
                                               int w, const Lane& A, Rows<D>& S, Scores& x, float c, int lane) {
-    issue(nxt, f, jn, kb, ntiles, pg, w, A, lane);
+    issue(nxt, f, jn, kb, ntiles, win, before, w, A, lane);
     __builtin_amdgcn_sched_barrier(0);
     const float ref = reference(x, S, c);
     const Scores y = scores(cur, S, A);
@@ -365,25 +348,64 @@ struct Chunk {
   }
   // The same where they may not (see 0: none of its keys).
   static __device__ __forceinline__ void edge_step(lds_char* __restrict__ nxt, const lds_char* __restrict__ cur,
-                                                   const Fetch& f, int jn, int kb, int ntiles,
-                                                   const int (&pg)[DL::U], int w, const Lane& A, Rows<D>& S,
-                                                   Scores& x, int t0, bool see, bool see_next, float c, int lane) {
-    issue(nxt, f, jn, kb, ntiles, pg, w, A, lane);
+                                                   const Fetch& f, int jn, int kb, int ntiles, Window& win,
+                                                   int2& before, int w, const Lane& A, Rows<D>& S, Scores& x, int t0,
+                                                   bool see, bool see_next, float c, int lane) {
+    issue(nxt, f, jn, kb, ntiles, win, before, w, A, lane);
     __builtin_amdgcn_sched_barrier(0);
     if (see) {
-      const int half = lane >> 5;
-      mask(x, S, t0, half);
+      mask(x, S, t0, lane >> 5);
       const float ref = reference(x, S, c);
       const Probs P = weights(x, S, c, ref);
-      if (__any(bad_values(cur, A))) careful_product(cur, P, S, A, t0, half);
-      else product(cur, P, S, A);
+      product(cur, P, S, A);
     }
     if (see_next) x = scores(cur, S, A);
   }
 };
 
+// A wave's rows again, key by key from the cache, by the rows' own visibility:
+// a value of a key that a row does not see never meets the row, not even as a
+// product with zero.  Run where the matrix products left a NaN (an infinity or
+// a NaN somewhere in the item's V, or a score that is one).
+template <int D>
+__device__ __forceinline__ void one_by_one(const Fetch& f, Rows<D>& S, int kb, int last, float c, int half) {
+  S.m = -INFINITY;
+  float l = 0.f;
+#pragma unroll
+  for (int eb = 0; eb < D / 32; ++eb)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) S.o[eb][i] = 0.f;
+  for (int t = kb; t <= last; ++t) {
+    const int64_t at = page_of(f, t) * f.page_bytes + (int64_t)(t % f.page_tokens) * f.row_bytes;
+    const bf16x8* k = reinterpret_cast<const bf16x8*>(f.k + at) + half;
+    const bf16x4* v = reinterpret_cast<const bf16x4*>(f.v + at) + half;
+    float s = 0.f;
+#pragma unroll
+    for (int ks = 0; ks < D / 16; ++ks) {
+      const bf16x8 y = k[2 * ks];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) s = fmaf((float)S.q[ks][i], (float)y[i], s);
+    }
+    s = (s + __shfl_xor(s, 32)) * c;
+    const bool sees = t <= S.last;
+    const float m = sees ? fmaxf(S.m, s) : S.m, ref = m == -INFINITY ? 0.f : m;
+    const float alpha = __builtin_amdgcn_exp2f(S.m - ref), w = sees ? __builtin_amdgcn_exp2f(s - ref) : 0.f;
+    S.m = m;
+    l = l * alpha + w;
+#pragma unroll
+    for (int eb = 0; eb < D / 32; ++eb)
+#pragma unroll
+      for (int i = 0; i < 16; i += 4) {
+        const bf16x4 y = v[(32 * eb + 2 * i) / 4];
+#pragma unroll
+        for (int n = 0; n < 4; ++n) S.o[eb][i + n] = S.o[eb][i + n] * alpha + (sees ? w * (float)y[n] : 0.f);
+      }
+  }
+  S.l = half ? 0.f : l;
+}
+
 template <int D, int NW, int TK, int NS, int PARTS>
-__global__ __launch_bounds__(64 * NW, NW == 1 ? 1 : 2) void chunk_attn(ChunkParams p) {
+__global__ __launch_bounds__(64 * NW, 2) void chunk_attn(ChunkParams p) {
 #if defined(__HIP_DEVICE_COMPILE__)   // the host pass needs the signature only
   using C = Chunk<D, NW, TK, PARTS>;
   using TL = Tile<D, TK>;
@@ -400,7 +422,7 @@ __global__ __launch_bounds__(64 * NW, NW == 1 ? 1 : 2) void chunk_attn(ChunkPara
   Fetch f;
   f.k = static_cast<const char*>(p.k) + (int64_t)it.kvh * p.kv_sh * 2;
   f.v = static_cast<const char*>(p.v) + (int64_t)it.kvh * p.kv_sh * 2;
-  f.table = (const const_int32*)(p.bt + (int64_t)it.req * p.bt_stride);
+  f.pages = p.bt + (int64_t)it.req * p.bt_stride;
   f.row_bytes = (int)(p.kv_st * 2);
   f.page_tokens = p.page_tokens;
   f.page_bytes = (int64_t)p.page_tokens * f.row_bytes;
@@ -408,20 +430,15 @@ __global__ __launch_bounds__(64 * NW, NW == 1 ? 1 : 2) void chunk_attn(ChunkPara
   f.ke = it.ke;
   typename C::Lane A;
 #pragma unroll
-  for (int x = 0; x < TL::T; ++x) {
+  for (int x = 0; x < TL::NOFF; ++x) {
     const int row = x * TL::RPI + lane / TL::CH, ch = lane % TL::CH;
-    const bool v0 = C::unit_is_v(w, 0);
-    A.off[x] = (uint32_t)(row * f.row_bytes + ((ch ^ (v0 ? swv<D>(row) : swk<D>(row))) * 16));
-    if constexpr (DL::U > 1) A.flip[x] = (uint32_t)(row * f.row_bytes + ((ch ^ swv<D>(row)) * 16));
+    const int sw = C::unit_is_v(w, 0) ? swv<D>(row) : swk<D>(row);
+    A.off[x] = (uint32_t)(lane / TL::CH * f.row_bytes + ((ch ^ sw) * 16));
+    A.offv = (uint32_t)(lane / TL::CH * f.row_bytes + ((ch ^ swv<D>(row)) * 16));   // the same for every x
   }
-  int pg[DL::U];
-  auto pages = [&](int j) {
-#pragma unroll
-    for (int u = 0; u < DL::U; ++u) {
-      const int tile = max(C::unit_is_v(w, u) ? j - 1 : j, 0);
-      pg[u] = page_of(f, it.kb + TK * tile + 32 * C::unit_half(w, u));
-    }
-  };
+  Window win;
+  look(win, f, it.kb, 0, lane);
+  int2 before = make_int2(0, 0);                         // a second unit's: what the first had last
 
   Rows<D> S;
   const int wr0 = 32 * w;                                // the wave's first row of the item
@@ -436,11 +453,7 @@ __global__ __launch_bounds__(64 * NW, NW == 1 ? 1 : 2) void chunk_attn(ChunkPara
   }
   lds_char* ring = (lds_char*)lds;
 #pragma unroll
-  for (int j = 0; j < NS; ++j) {
-    pages(j);
-    C::issue(ring + j * TL::STAGE, f, j, it.kb, ntiles, pg, w, A, lane);
-  }
-  pages(NS);
+  for (int j = 0; j < NS; ++j) C::issue(ring + j * TL::STAGE, f, j, it.kb, ntiles, win, before, w, A, lane);
   S.m = -INFINITY;
   S.l = 0.f;
 #pragma unroll
@@ -485,9 +498,8 @@ __global__ __launch_bounds__(64 * NW, NW == 1 ? 1 : 2) void chunk_attn(ChunkPara
       static_for<0, NS>([&](auto st) {
         constexpr int ST = decltype(st)::value;
         turn(t + ST);
-        C::step(ring + ST * TL::STAGE, ring + ((ST + 1) % NS) * TL::STAGE, f, t + ST + NS, it.kb, ntiles, pg, w, A, S,
+        C::step(ring + ST * TL::STAGE, ring + ((ST + 1) % NS) * TL::STAGE, f, t + ST + NS, it.kb, ntiles, win, before, w, A, S,
                 x, p.scale_log2, lane);
-        pages(t + ST + NS + 1);
       });
       t += NS;
     }
@@ -495,10 +507,16 @@ __global__ __launch_bounds__(64 * NW, NW == 1 ? 1 : 2) void chunk_attn(ChunkPara
   for (; t < ntiles; ++t) {
     turn(t);
     const int t0 = it.kb + TK * t;
-    C::edge_step(ring + (t % NS) * TL::STAGE, ring + ((t + 1) % NS) * TL::STAGE, f, t + NS, it.kb, ntiles, pg, w, A, S,
+    C::edge_step(ring + (t % NS) * TL::STAGE, ring + ((t + 1) % NS) * TL::STAGE, f, t + NS, it.kb, ntiles, win, before, w, A, S,
                  x, t0, t0 <= wave_sees, t + 1 < ntiles && t0 + TK <= wave_sees, p.scale_log2, lane);
-    pages(t + NS + 1);
   }
+
+  bool bad = false;
+#pragma unroll
+  for (int eb = 0; eb < ET; ++eb)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) bad |= S.o[eb][i] != S.o[eb][i];
+  if (__any(bad)) one_by_one<D>(f, S, it.kb, wave_sees, p.scale_log2, half);
 
   const float l = S.l + __shfl_xor(S.l, 32);
   if (wr0 + l32 >= it.rows) return;
@@ -514,7 +532,6 @@ __global__ __launch_bounds__(64 * NW, NW == 1 ? 1 : 2) void chunk_attn(ChunkPara
         const int e = 32 * eb + 2 * i + 4 * half;
         const f32x4 y = {S.o[eb][i] * inv, S.o[eb][i + 1] * inv, S.o[eb][i + 2] * inv, S.o[eb][i + 3] * inv};
         if constexpr (PARTS == 1) {
-          typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
           *reinterpret_cast<u32x2*>(static_cast<uint16_t*>(p.out) + row * D + e) =
               __builtin_bit_cast(u32x2, __builtin_convertvector(y, bf16x4));
         } else {
@@ -537,42 +554,49 @@ __global__ __launch_bounds__(64 * NW, NW == 1 ? 1 : 2) void chunk_attn(ChunkPara
 // The pieces of one cut row tile, a wave a row:
 //   O = sum_s 2^(m_s - M) O_s / sum_s 2^(m_s - M) l_s,  M = max_s m_s,
 // the pieces in order.  A piece none of whose keys the row sees has m = -inf.
+// A lane four columns, a work-group as many rows as that takes; the pieces'
+// weights first, so that the rows' loads follow each other.
 template <int D, bool F32>
 __global__ __launch_bounds__(256) void chunk_join(ChunkParams p, int groups) {
+  constexpr int LPR = D / 4, RPG = 256 / LPR;            // lanes a row, rows a work-group
   const int x = (int)blockIdx.x / groups;
   const ChunkJoin jn = p.joins[x];
-  const int lane = threadIdx.x & 63;
-  const int rr = __builtin_amdgcn_readfirstlane(((int)blockIdx.x - x * groups) * 4 + (int)(threadIdx.x >> 6));
+  const int rr = ((int)blockIdx.x - x * groups) * RPG + (int)threadIdx.x / LPR;
   if (rr >= jn.rows) return;
-  constexpr int E = D / 64;                              // a lane's columns
+  const int e = ((int)threadIdx.x % LPR) * 4;
+  const float2* ml = p.part_ml + jn.part + rr;
+  const float* po = p.part_o + (jn.part + rr) * D + e;
   float M = -INFINITY;
-  for (int s = 0; s < jn.pieces; ++s) M = fmaxf(M, p.part_ml[jn.part + (int64_t)s * jn.rows + rr].x);
-  float L = 0.f, o[E] = {};
+  for (int s = 0; s < jn.pieces; ++s) M = fmaxf(M, ml[(int64_t)s * jn.rows].x);
+  float L = 0.f;
+  f32x4 o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
   for (int s = 0; s < jn.pieces; ++s) {
-    const int64_t row = jn.part + (int64_t)s * jn.rows + rr;
-    const float2 ml = p.part_ml[row];
-    const float wgt = ml.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml.x - M);
-    L += ml.y * wgt;
+    const float2 y = ml[(int64_t)s * jn.rows];
+    const f32x4 v = *reinterpret_cast<const f32x4*>(po + (int64_t)s * jn.rows * D);
+    const float wgt = y.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(y.x - M);
+    L += y.y * wgt;
 #pragma unroll
-    for (int e = 0; e < E; ++e) o[e] += wgt * p.part_o[row * D + lane * E + e];
+    for (int i = 0; i < 4; ++i) o[i] += wgt * v[i];
   }
+  const float inv = 1.f / L;
   const int r = jn.r0 + rr, j = r / p.G;
-  const int64_t row = (jn.q0 + (int64_t)j) * p.Hq + jn.kvh * p.G + (r - j * p.G);
-#pragma unroll
-  for (int e = 0; e < E; ++e) {
-    const float y = o[e] / L;
-    if constexpr (F32) static_cast<float*>(p.out)[row * D + lane * E + e] = y;
-    else static_cast<__bf16*>(p.out)[row * D + lane * E + e] = (__bf16)y;
-  }
+  const int64_t at = ((jn.q0 + (int64_t)j) * p.Hq + jn.kvh * p.G + (r - j * p.G)) * D + e;
+  const f32x4 y = o * inv;
+  if constexpr (F32) *reinterpret_cast<f32x4*>(static_cast<float*>(p.out) + at) = y;
+  else *reinterpret_cast<u32x2*>(static_cast<uint16_t*>(p.out) + at) = __builtin_bit_cast(u32x2, __builtin_convertvector(y, bf16x4));
 }
 
 template <int D, int PARTS>
 static hipError_t launch_d(const ChunkParams& p, hipStream_t s) {
-  if (p.tall == kChunkTallRows) chunk_attn<D, 4, 64, 2, PARTS><<<dim3(p.n_items), dim3(256), 0, s>>>(p);
-  else chunk_attn<D, 1, 32, 4, PARTS><<<dim3(p.n_items), dim3(64), 0, s>>>(p);
+  ChunkParams q = p;
+  if (p.n_low > 0) chunk_attn<D, 1, 32, 2, PARTS><<<dim3(p.n_low), dim3(64), 0, s>>>(q);
+  q.items += p.n_low;
+  if (p.n_items > p.n_low) chunk_attn<D, 4, 64, 2, PARTS><<<dim3(p.n_items - p.n_low), dim3(256), 0, s>>>(q);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.n_joins == 0) return e;
-  const int groups = (p.tall + 3) / 4;
+  constexpr int RPG = 1024 / D;
+  const int groups = (p.join_rows + RPG - 1) / RPG;
   chunk_join<D, PARTS != 1><<<dim3(p.n_joins * groups), dim3(256), 0, s>>>(p, groups);
   return hipGetLastError();
 }
