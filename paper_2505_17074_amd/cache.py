@@ -4,6 +4,7 @@ operators run in the library's HIP kernels, the bookkeeping in its C++.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes as C
 from typing import Optional, Sequence
 
@@ -14,6 +15,15 @@ from . import binding as B
 from .batch import Verifier
 
 _DTYPE = {torch.bfloat16: B.SPEC_BF16, torch.float32: B.SPEC_F32}
+_HERE = contextlib.nullcontext()
+
+
+def _current_raw_stream(index: int) -> int:
+    return torch.cuda.current_stream(index).cuda_stream
+
+
+# torch's own short way to the handle, where it has it (2 us less a call)
+_current_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", _current_raw_stream)
 
 
 class Pages:
@@ -92,8 +102,14 @@ class PagedCache:
             raise ValueError("bf16 or fp32 pools")
         if k.stride(4) != 1 or k.stride(1) != k.shape[2] * k.stride(2):
             raise ValueError("rows are contiguous and pages follow each other")
-        self.k, self.v, self.device = k, v, k.device
+        self.k, self.v, self.device, self.dtype = k, v, k.device, k.dtype
+        self._index = k.device.index
+        self._head = k.shape[3:]
+        self._lib = B.load()
         c = self.c = B.SpecCache()
+        self._ref = C.byref(c)
+        self._append = B.SpecAppendArgs()
+        self._append_ref = C.byref(self._append)
         c.num_layers, c.num_pages, c.page_tokens, c.num_kv_heads, c.head_dim = k.shape
         c.dtype = _DTYPE[k.dtype]
         c.k, c.v = k.data_ptr(), v.data_ptr()
@@ -112,57 +128,61 @@ class PagedCache:
             if t.shape[0] > 1 and t.stride(0) < t.shape[1]:
                 raise ValueError("the block table's rows overlap")
         self._table = t
+        self._rows = 0 if t is None else t.shape[0]
         self.c.block_table = t.data_ptr() if t is not None else None
         # one row's stride is its width (a table of one row may have any)
         self.c.block_stride = 0 if t is None else (t.stride(0) if t.shape[0] > 1 else t.shape[1])
 
+    def _enter(self):
+        """The pools' device made current for a call (a context)."""
+        return _HERE if torch.cuda.current_device() == self._index else torch.cuda.device(self._index)
+
     def _stream(self, stream) -> int:
-        return (stream or torch.cuda.current_stream(self.device)).cuda_stream
+        return _current_raw_stream(self._index) if stream is None else stream.cuda_stream
 
     def _requests(self, n: int) -> None:
-        if self._table is None or n > self._table.shape[0]:
+        if self._table is None or n > self._rows:
             raise ValueError("the block table has no row for every request")
 
     def append(self, chunks: B.SpecChunks, k_new: torch.Tensor, v_new: torch.Tensor, layer: int = 0,
                stream: Optional[torch.cuda.Stream] = None) -> None:
         """Rows k_new, v_new [layers, rows, Hkv, d] (or [rows, Hkv, d]: one layer)
         to the ends of the requests, in the cache's layers from `layer` on."""
-        if k_new.dim() == 3:
-            k_new, v_new = k_new[None], v_new[None]
-        c = self.c
-        if k_new.shape != v_new.shape or k_new.stride() != v_new.stride() or k_new.dim() != 4 or \
-                tuple(k_new.shape[2:]) != (c.num_kv_heads, c.head_dim) or k_new.shape[1] < chunks.rows or \
-                (k_new.numel() and k_new.stride(3) != 1):
+        shape, st = k_new.shape, k_new.stride()
+        if shape != v_new.shape or st != v_new.stride() or len(shape) not in (3, 4) or \
+                shape[-2:] != self._head or shape[-3] < chunks.rows or (st[-1] != 1 and k_new.numel()):
             raise ValueError("k_new and v_new are [layers, rows, Hkv, d], a row for every new token")
-        if k_new.dtype != self.k.dtype or v_new.dtype != self.k.dtype or k_new.device != self.device or \
+        if k_new.dtype != self.dtype or v_new.dtype != self.dtype or k_new.device != self.device or \
                 v_new.device != self.device:
             raise ValueError("k_new and v_new have the pools' type and device")
         self._requests(chunks.num_requests)
-        a = B.SpecAppendArgs()
-        a.layer, a.num_layers = layer, k_new.shape[0]
+        a = self._append
+        a.layer, a.num_layers = layer, shape[0] if len(shape) == 4 else 1
         a.k_new, a.v_new = k_new.data_ptr(), v_new.data_ptr()
-        a.new_stride_layer, a.new_stride_tok, a.new_stride_head = (max(1, x) for x in k_new.stride()[:3])
-        with torch.cuda.device(self.device):
-            B.check(B.spec_cache_append(chunks, c, a, self._stream(stream)), "spec_cache_append")
+        a.new_stride_layer = max(1, st[0])
+        a.new_stride_tok, a.new_stride_head = max(1, st[-3]), max(1, st[-2])
+        with self._enter():
+            B.check(self._lib.spec_cache_append(chunks, self._ref, self._append_ref, self._stream(stream)),
+                    "spec_cache_append")
 
     def commit(self, req: B.SpecRequests, accepted_node: torch.Tensor,
                stream: Optional[torch.cuda.Stream] = None) -> None:
         """Moves the accepted paths' rows behind the contexts, in every layer."""
+        n = req.num_requests
         if accepted_node.dtype != torch.int32 or accepted_node.device != self.device or \
-                accepted_node.dim() != 1 or accepted_node.shape[0] < req.num_requests or \
-                not accepted_node.is_contiguous():
+                accepted_node.dim() != 1 or accepted_node.shape[0] < n or not accepted_node.is_contiguous():
             raise ValueError("accepted_node is int32 [requests] on the pools' device")
-        self._requests(req.num_requests)
-        with torch.cuda.device(self.device):
-            B.check(B.spec_cache_commit(req, self.c, accepted_node.data_ptr(), self._stream(stream)),
+        self._requests(n)
+        with self._enter():
+            B.check(self._lib.spec_cache_commit(req, self._ref, accepted_node.data_ptr(), self._stream(stream)),
                     "spec_cache_commit")
 
     def copy_pages(self, copies, stream: Optional[torch.cuda.Stream] = None) -> None:
         """Copies (src, dst, tokens) [n, 3], in every layer."""
         a = np.ascontiguousarray(copies, dtype=np.int32).reshape(-1, 3)
-        with torch.cuda.device(self.device):
-            B.check(B.spec_cache_copy_pages(self.c, a.ctypes.data if a.size else None, a.shape[0],
-                                            self._stream(stream)), "spec_cache_copy_pages")
+        with self._enter():
+            B.check(self._lib.spec_cache_copy_pages(self._ref, a.ctypes.data if a.size else None, a.shape[0],
+                                                    self._stream(stream)), "spec_cache_copy_pages")
 
 
 class ChunkAttention(Verifier):
@@ -180,6 +200,8 @@ class ChunkAttention(Verifier):
         self.cache = cache
         a = self.args = B.SpecChunkAttnArgs()
         a.num_q_heads, a.scale = num_q_heads, scale
+        self._args_ref = C.byref(a)
+        self._head = torch.Size((num_q_heads, cache.c.head_dim))
         self.ws_bytes = self.staging_bytes = 0
         self.ws_ptr = None
         self._staging = [None] * ring
@@ -211,25 +233,26 @@ class ChunkAttention(Verifier):
             stream: Optional[torch.cuda.Stream] = None) -> None:
         """Attention of q [rows, Hq, d] into out [rows, Hq, d] (bf16 or fp32)."""
         cache, a = self.cache, self.args
-        shape = (chunks.rows, a.num_q_heads, cache.c.head_dim)
-        if q.dim() != 3 or out.dim() != 3 or q.shape[0] < shape[0] or out.shape[0] < shape[0] or \
-                tuple(q.shape[1:]) != shape[1:] or tuple(out.shape[1:]) != shape[1:]:
+        rows, head = chunks.rows, self._head
+        qs, os, st = q.shape, out.shape, q.stride()
+        if len(qs) != 3 or len(os) != 3 or qs[0] < rows or os[0] < rows or qs[1:] != head or os[1:] != head:
             raise ValueError("q and out are [rows, Hq, d], a row for every new token")
-        if q.dtype != cache.k.dtype or out.dtype not in _DTYPE or q.device != cache.device or \
-                out.device != cache.device or not out.is_contiguous() or (q.numel() and q.stride(2) != 1):
+        kind = _DTYPE.get(out.dtype)
+        if q.dtype != cache.dtype or kind is None or q.device != cache.device or out.device != cache.device or \
+                not out.is_contiguous() or (st[2] != 1 and q.numel()):
             raise ValueError("q has the cache's type, out is contiguous bf16 or fp32, both on its device")
         cache._requests(chunks.num_requests)
-        a.layer, a.out_dtype = layer, _DTYPE[out.dtype]
+        a.layer, a.out_dtype = layer, kind
         a.q, a.out = q.data_ptr(), out.data_ptr()
-        a.q_stride_tok, a.q_stride_head = max(1, q.stride(0)), max(1, q.stride(1))
-        with torch.cuda.device(cache.device):
-            stream = stream or torch.cuda.current_stream(cache.device)
+        a.q_stride_tok, a.q_stride_head = max(1, st[0]), max(1, st[1])
+        with cache._enter():
+            stream = stream or torch.cuda.current_stream(cache._index)
             self._order(stream)
             for grown in (False, True):
                 s = self._slot(stream)
                 try:
-                    st = B.spec_chunk_attn(chunks, cache.c, a, self.ws_ptr, self.ws_bytes, self._staging[s],
-                                           self.staging_bytes, stream.cuda_stream)
+                    st = cache._lib.spec_chunk_attn(chunks, cache._ref, self._args_ref, self.ws_ptr, self.ws_bytes,
+                                                    self._staging[s], self.staging_bytes, stream.cuda_stream)
                 finally:
                     self._done(s, stream)
                 if st != B.SPEC_ERR_WORKSPACE or grown:
