@@ -97,7 +97,8 @@ int compute_units() {
 struct ChunkPlan {
   std::vector<ChunkItem> items;
   std::vector<ChunkJoin> joins;
-  int32_t n_low = 0, join_rows = 0;
+  bool tall = false;
+  int32_t join_rows = 0;
   int64_t parts = 0;
   size_t off_joins = 0, plan_bytes = 0;
   size_t off_part_o = 0, off_part_ml = 0, device_bytes = 0;
@@ -120,97 +121,92 @@ spec_status_t plan_chunk(const spec_chunks_t* r, const spec_cache_t* c, const sp
   const int Hkv = c->num_kv_heads, G = a->num_q_heads / Hkv;
   if (nq * G >= INT32_MAX / 2) return SPEC_ERR_UNSUPPORTED;
 
-  // Row tiles: requests of few rows a KV head (decoding) on one wave each, the
-  // others on work-groups of 128 rows.
+  // Row tiles of one height for the batch: 32 rows on one wave each where no
+  // request has more (decoding), else 128 on a work-group of four.
+  int64_t most = 0;
+  for (int i = 0; i < r->num_requests; ++i) most = std::max<int64_t>(most, (int64_t)r->new_len[i] * G);
+  P.tall = most > sv::kChunkLowRows;
+  const int RT = P.tall ? sv::kChunkTallRows : sv::kChunkLowRows;
   struct RowTile { int32_t req, r0, rows, keys, q0; };
-  std::vector<RowTile> low, tall;
-  int64_t q0 = 0;
+  std::vector<RowTile> tiles;
+  int64_t q0 = 0, total = 0, longest = 0;
   for (int i = 0; i < r->num_requests; ++i) {
     const int n = r->new_len[i], rows = n * G;
-    const int RT = rows <= sv::kChunkLowRows ? sv::kChunkLowRows : sv::kChunkTallRows;
-    std::vector<RowTile>& to = rows <= sv::kChunkLowRows ? low : tall;
     for (int r0 = 0; r0 < rows; r0 += RT) {
       const int nr = std::min(RT, rows - r0);
-      to.push_back({i, r0, nr, r->ctx_len[i] + (r0 + nr - 1) / G + 1, (int32_t)q0});
+      tiles.push_back({i, r0, nr, r->ctx_len[i] + (r0 + nr - 1) / G + 1, (int32_t)q0});
+      const int64_t kt = (tiles.back().keys + sv::kChunkTile - 1) / sv::kChunkTile;
+      total += kt * Hkv;
+      longest = std::max(longest, kt);
     }
     q0 += n;
   }
   const int cus = compute_units();
-  // items of `tiles`, a row tile's keys in equal pieces of at most `cap` 64-key tiles
-  auto lay = [&](const std::vector<RowTile>& tiles, int64_t cap) -> spec_status_t {
-    const size_t first = P.items.size();
-    int longest = 0;
-    for (const RowTile& t : tiles) {
-      const int64_t kt = (t.keys + sv::kChunkTile - 1) / sv::kChunkTile;
-      const int64_t pieces = (kt + cap - 1) / cap;
-      const int64_t len = (kt + pieces - 1) / pieces;
-      const int np = (int)((kt + len - 1) / len);
-      longest = std::max<int>(longest, (int)len);
-      for (int h = 0; h < Hkv; ++h) {
-        if (np > 1) {
-          P.joins.push_back({h, t.r0, t.rows, np, P.parts, t.q0, 0});
-          P.join_rows = std::max(P.join_rows, t.rows);
-        }
-        for (int s = 0; s < np; ++s) {
-          ChunkItem it;
-          it.req = t.req;
-          it.kvh = h;
-          it.r0 = t.r0;
-          it.rows = t.rows;
-          it.kb = (int32_t)(s * len * sv::kChunkTile);
-          it.ke = (int32_t)std::min<int64_t>(t.keys, (s + 1) * len * sv::kChunkTile);
-          it.ctx = r->ctx_len[t.req];
-          it.q0 = t.q0;
-          it.part = np > 1 ? P.parts + (int64_t)s * t.rows : -1;
-          it.pad = 0;
-          P.items.push_back(it);
-        }
-        if (np > 1) P.parts += (int64_t)np * t.rows;
-      }
-      if (P.items.size() >= INT32_MAX / 64) return SPEC_ERR_UNSUPPORTED;
-    }
-    // longest first (a stable counting sort): the last to start are the shortest
-    auto len = [](const ChunkItem& it) { return (it.ke - it.kb + sv::kChunkTile - 1) / sv::kChunkTile; };
-    std::vector<size_t> start(longest + 2, first);
-    for (size_t i = first; i < P.items.size(); ++i) ++start[longest - len(P.items[i]) + 1];
-    for (int t = 1; t <= longest + 1; ++t) start[t] += start[t - 1] - first;
-    std::vector<ChunkItem> sorted(P.items.begin() + first, P.items.end());
-    for (const ChunkItem& it : sorted) P.items[start[longest - len(it)]++] = it;
-    return SPEC_OK;
-  };
-  auto sum_of = [&](const std::vector<RowTile>& tiles) {
-    int64_t n = 0;
-    for (const RowTile& t : tiles) n += (t.keys + sv::kChunkTile - 1) / sv::kChunkTile;
-    return n * Hkv;
-  };
-  if (!low.empty()) {
+  // A row tile's keys in equal pieces of at most so many 64-key tiles.
+  int64_t cap;
+  if (!P.tall) {
     // Few rows: the keys stream past them at HBM's rate whatever the pieces, so
     // they are cut to about 4 / 3 rounds of the work-groups that run at once
-    // (five a compute unit), where the last ones to end lose least, down to 128
+    // (four a compute unit), where the last ones to end lose least, down to 128
     // keys.  64 single tokens over 512-8192 rows: pieces of 1280 keys 190 us,
     // 512 207, 4096 214; one over 1000 rows: 64 keys 18.7, 128 16.9, 256 19.3.
-    const int64_t slots = 5 * (int64_t)cus;
-    const int64_t cap = std::max<int64_t>(2, (3 * sum_of(low) + 4 * slots - 1) / (4 * slots));
-    if ((st = lay(low, cap)) != SPEC_OK) return st;
-  }
-  P.n_low = (int32_t)P.items.size();
-  if (!tall.empty()) {
+    const int64_t slots = 4 * (int64_t)cus;
+    cap = std::max<int64_t>(2, (3 * total + 4 * slots - 1) / (4 * slots));
+  } else {
     // Many rows: a compute unit takes a 64-key tile in about a microsecond,
     // whether one work-group runs on it or two, so the longest item bounds the
     // kernel only where it is longer than a unit's mean share.  Only then is
     // it cut, and where that saves more than the joins cost (about eight
     // tiles).  2048 new tokens, the longest 32 tiles of a mean of 33: whole
-    // 54 us, pieces of 24 tiles 62, 16 64, 8 79.
-    int64_t longest = 0;
-    for (const RowTile& t : tall) longest = std::max<int64_t>(longest, (t.keys + sv::kChunkTile - 1) / sv::kChunkTile);
-    const int64_t mean = (sum_of(tall) + cus - 1) / cus;
-    const int64_t cap = longest <= mean + 8 ? longest : std::max<int64_t>(8, mean);
-    if ((st = lay(tall, cap)) != SPEC_OK) return st;
-    // Work-groups b and b + cus share a compute unit at first: the longest with
-    // the shortest of the first two rounds.
-    const int64_t n = (int64_t)P.items.size() - P.n_low;
-    if (n > cus)
-      std::reverse(P.items.begin() + P.n_low + cus, P.items.begin() + P.n_low + std::min<int64_t>(n, 2 * cus));
+    // 54 us, pieces of 24 tiles 62, 16 64, 8 79.  Decoding requests beside a
+    // chunk run in the same launch (beside 8 chunks of 33-700 tokens, 16 single
+    // ones: 181 us, in a launch of their own before it 198).
+    const int64_t mean = (total + cus - 1) / cus;
+    cap = longest <= mean + 8 ? longest : std::max<int64_t>(8, mean);
+  }
+  longest = 0;
+  for (const RowTile& t : tiles) {
+    const int64_t kt = (t.keys + sv::kChunkTile - 1) / sv::kChunkTile;
+    const int64_t pieces = (kt + cap - 1) / cap;
+    const int64_t len = (kt + pieces - 1) / pieces;
+    const int np = (int)((kt + len - 1) / len);
+    longest = std::max(longest, len);
+    for (int h = 0; h < Hkv; ++h) {
+      if (np > 1) {
+        P.joins.push_back({h, t.r0, t.rows, np, P.parts, t.q0, 0});
+        P.join_rows = std::max(P.join_rows, t.rows);
+      }
+      for (int s = 0; s < np; ++s) {
+        ChunkItem it;
+        it.req = t.req;
+        it.kvh = h;
+        it.r0 = t.r0;
+        it.rows = t.rows;
+        it.kb = (int32_t)(s * len * sv::kChunkTile);
+        it.ke = (int32_t)std::min<int64_t>(t.keys, (s + 1) * len * sv::kChunkTile);
+        it.ctx = r->ctx_len[t.req];
+        it.q0 = t.q0;
+        it.part = np > 1 ? P.parts + (int64_t)s * t.rows : -1;
+        it.pad = 0;
+        P.items.push_back(it);
+      }
+      if (np > 1) P.parts += (int64_t)np * t.rows;
+    }
+    if (P.items.size() >= INT32_MAX / 64) return SPEC_ERR_UNSUPPORTED;
+  }
+  // longest first (a stable counting sort): the last to start are the shortest
+  {
+    auto len = [](const ChunkItem& it) { return (it.ke - it.kb + sv::kChunkTile - 1) / sv::kChunkTile; };
+    std::vector<size_t> start((size_t)longest + 2, 0);
+    for (const ChunkItem& it : P.items) ++start[longest - len(it) + 1];
+    for (int64_t t = 1; t <= longest + 1; ++t) start[t] += start[t - 1];
+    std::vector<ChunkItem> sorted(P.items.size());
+    for (const ChunkItem& it : P.items) sorted[start[longest - len(it)]++] = it;
+    P.items.swap(sorted);
+    // work-groups b and b + cus of the tall kernel share a compute unit at
+    // first: the longest with the shortest of the first two rounds
+    const int64_t n = (int64_t)P.items.size();
+    if (P.tall && n > cus) std::reverse(P.items.begin() + cus, P.items.begin() + std::min<int64_t>(n, 2 * cus));
   }
 
   P.off_joins = align_up(sizeof(ChunkItem) * P.items.size());
@@ -313,7 +309,7 @@ spec_status_t spec_chunk_attn(const spec_chunks_t* chunks, const spec_cache_t* c
     p.G = args->num_q_heads / cache->num_kv_heads;
     p.D = cache->head_dim;
     p.out_f32 = args->out_dtype == SPEC_F32;
-    p.n_low = P.n_low;
+    p.tall = P.tall;
     p.join_rows = P.join_rows;
     const float scale = args->scale > 0.f ? args->scale : 1.f / std::sqrt((float)cache->head_dim);
     p.scale_log2 = scale * 1.4426950408889634f;

@@ -589,10 +589,8 @@ __global__ __launch_bounds__(256) void chunk_join(ChunkParams p, int groups) {
 
 template <int D, int PARTS>
 static hipError_t launch_d(const ChunkParams& p, hipStream_t s) {
-  ChunkParams q = p;
-  if (p.n_low > 0) chunk_attn<D, 1, 32, 2, PARTS><<<dim3(p.n_low), dim3(64), 0, s>>>(q);
-  q.items += p.n_low;
-  if (p.n_items > p.n_low) chunk_attn<D, 4, 64, 2, PARTS><<<dim3(p.n_items - p.n_low), dim3(256), 0, s>>>(q);
+  if (p.tall) chunk_attn<D, 4, 64, 2, PARTS><<<dim3(p.n_items), dim3(256), 0, s>>>(p);
+  else chunk_attn<D, 1, 32, 2, PARTS><<<dim3(p.n_items), dim3(64), 0, s>>>(p);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.n_joins == 0) return e;
   constexpr int RPG = 1024 / D;

@@ -52,7 +52,7 @@ struct ChunkParams {
   int32_t page_tokens, num_pages;
   int32_t Hq, G, D;
   int32_t out_f32;
-  int32_t n_low;        // items of up to kChunkLowRows rows, first in the list
+  int32_t tall;         // items of up to kChunkTallRows rows on four waves, else kChunkLowRows on one
   int32_t join_rows;    // rows of the tallest joined tile
   float scale_log2;
 };
