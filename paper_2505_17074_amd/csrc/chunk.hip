@@ -174,11 +174,11 @@ struct Chunk {
     return KB * max(unit_is_v(w, 0) ? j - 1 : j, 0) + unit_half(w, 0);
   }
 
-  // The wave's units of stage j: K of tile j, V of tile j - 1, whichever of
-  // them the item has (tiles begin at key kb).  Then the window for the next
-  // stage: where a load is due it lands with the transfers.
-  static __device__ __forceinline__ void issue(lds_char* stage, const Fetch& f, int j, int kb, int ntiles, Window& win,
-                                               int2& before, int w, const Lane& A, int lane) {
+  // The wave's units of stage j: K of tile j, V of tile j - 1 (tiles begin at
+  // key kb).  Rows past the item's end, and tiles that it does not have, are
+  // past the buffer's records: they come as zeros.
+  static __device__ __forceinline__ void issue(lds_char* stage, const Fetch& f, int j, int kb, const Window& win,
+                                               int2& before, int w, const Lane& A) {
 #if defined(__HIP_DEVICE_COMPILE__)
     const int bl = block_of(j, w) - win.b;
     const int2 now = make_int2(__builtin_amdgcn_readlane(win.pg, bl), __builtin_amdgcn_readlane(win.place, bl));
@@ -187,35 +187,19 @@ struct Chunk {
       const bool isv = unit_is_v(w, u);
       const int half = unit_half(w, u);
       const int tile = isv ? j - 1 : j;
-      if (tile < 0 || tile >= ntiles) continue;          // wave-uniform
       const int2 at_page = u == 0 ? now : before;
-      const int t = kb + TK * tile + 32 * half;
+      const int rows = tile < 0 ? 0 : min(f.ke - (kb + TK * tile + 32 * half), 32);
       const char* src = (isv ? f.v : f.k) + (int64_t)at_page.x * f.page_bytes;
-      const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc(
-          (void*)src, 0, (f.page_tokens - 1) * f.row_bytes + TL::ROWB, 0x00020000);
-      lds_char* dst = stage + (isv ? TL::MAT : 0) + half * TL::HALF;
       const int soff = at_page.y * f.row_bytes;
-      if (t + 32 <= f.ke) {                              // wave-uniform
+      const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc(
+          (void*)src, 0, rows > 0 ? soff + (rows - 1) * f.row_bytes + TL::ROWB : 0, 0x00020000);
+      lds_char* dst = stage + (isv ? TL::MAT : 0) + half * TL::HALF;
 #pragma unroll
-        for (int x = 0; x < TL::T; ++x)
-          __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void*)(dst + x * 1024), 16, at(A, u, x),
-                                                   soff + x * TL::RPI * f.row_bytes, 0, CPOL);
-      } else {                                           // rows past the end repeat the last one
-        int ln = lane;
-        asm("" : "+v"(ln));                              // nothing of this branch before the loop
-        const int lrow = ln / TL::CH, last = f.ke - 1 - t;
-#pragma unroll
-        for (int x = 0; x < TL::T; ++x) {
-          const uint32_t chunk = at(A, u, x) - (uint32_t)(lrow * f.row_bytes);
-          const int row = max(min(x * TL::RPI + lrow, last), 0);
-          __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void*)(dst + x * 1024), 16,
-                                                   (uint32_t)(row * f.row_bytes) + chunk, soff, 0, CPOL);
-        }
-      }
+      for (int x = 0; x < TL::T; ++x)
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void*)(dst + x * 1024), 16, at(A, u, x),
+                                                 soff + x * TL::RPI * f.row_bytes, 0, CPOL);
     }
     before = now;
-    const int next = block_of(j + 1, w);
-    if (next >= win.b + 64) look(win, f, kb, next, lane);
 #endif
   }
   static __device__ __forceinline__ uint32_t at(const Lane& A, int u, int x) {
@@ -249,15 +233,19 @@ struct Chunk {
       for (int i = 0; i < 16; ++i) x.s[kb][i] = 32 * kb + 16 * (i >> 3) + (i & 7) <= lim ? x.s[kb][i] : -INFINITY;
   }
 
-  // The reference trails the running maximum by at most kLag (log2 units), so
-  // p <= 2^kLag and most tiles leave O and l alone.  Returns what to subtract.
-  static __device__ __forceinline__ float reference(const Scores& x, Rows<D>& S, float c) {
-    constexpr float kLag = 8.f;
+  static __device__ __forceinline__ float largest(const Scores& x) {
     float top = x.s[0][0];
 #pragma unroll
     for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
       for (int i = 0; i < 16; ++i) top = fmaxf(top, x.s[kb][i]);
+    return top;
+  }
+  // The reference trails the running maximum by at most kLag (log2 units), so
+  // p <= 2^kLag and most tiles leave O and l alone.  Returns what to subtract
+  // for a tile whose largest score in this lane is `top`.
+  static __device__ __forceinline__ float reference(float top, Rows<D>& S, float c) {
+    constexpr float kLag = 8.f;
     top *= c;
     if (__any(top > S.m + kLag)) {                       // wave-uniform
       const float both = fmaxf(top, __shfl_xor(top, 32));
@@ -331,31 +319,31 @@ struct Chunk {
   }
 
   // Step t of a wave whose rows see all of tile t: the transfers of stage
-  // t + NS, the scores of tile t + 1, the softmax and product of tile t.  The
-  // stage written and the one read are different ones, which the parameters
-  // say (restrict): without it the compiler waits for the transfers before
-  // every read.
+  // t + NS, the scores of tile t + 1 and their largest, the softmax and product
+  // of tile t.  The stage written and the one read are different ones, which
+  // the parameters say (restrict): without it the compiler waits for the
+  // transfers before every read.
   static __device__ __forceinline__ void step(lds_char* __restrict__ nxt, const lds_char* __restrict__ cur,
-                                              const Fetch& f, int jn, int kb, int ntiles, Window& win, int2& before,
-                                              int w, const Lane& A, Rows<D>& S, Scores& x, float c, int lane) {
-    issue(nxt, f, jn, kb, ntiles, win, before, w, A, lane);
-    __builtin_amdgcn_sched_barrier(0);
-    const float ref = reference(x, S, c);
+                                              const Fetch& f, int jn, int kb, const Window& win, int2& before, int w,
+                                              const Lane& A, Rows<D>& S, Scores& x, float& top, float c) {
+    const float ref = reference(top, S, c);
+    issue(nxt, f, jn, kb, win, before, w, A);
     const Scores y = scores(cur, S, A);
     const Probs P = weights(x, S, c, ref);
     product(cur, P, S, A);
+    top = largest(y);
     x = y;
   }
   // The same where they may not (see 0: none of its keys).
   static __device__ __forceinline__ void edge_step(lds_char* __restrict__ nxt, const lds_char* __restrict__ cur,
-                                                   const Fetch& f, int jn, int kb, int ntiles, Window& win,
-                                                   int2& before, int w, const Lane& A, Rows<D>& S, Scores& x, int t0,
-                                                   bool see, bool see_next, float c, int lane) {
-    issue(nxt, f, jn, kb, ntiles, win, before, w, A, lane);
+                                                   bool more, const Fetch& f, int jn, int kb, const Window& win,
+                                                   int2& before, int w, const Lane& A, Rows<D>& S, Scores& x,
+                                                   float& top, int t0, bool see, bool see_next, float c, int lane) {
+    if (more) issue(nxt, f, jn, kb, win, before, w, A);
     __builtin_amdgcn_sched_barrier(0);
     if (see) {
       mask(x, S, t0, lane >> 5);
-      const float ref = reference(x, S, c);
+      const float ref = reference(largest(x), S, c);
       const Probs P = weights(x, S, c, ref);
       product(cur, P, S, A);
     }
@@ -453,7 +441,7 @@ __global__ __launch_bounds__(64 * NW, 2) void chunk_attn(ChunkParams p) {
   }
   lds_char* ring = (lds_char*)lds;
 #pragma unroll
-  for (int j = 0; j < NS; ++j) C::issue(ring + j * TL::STAGE, f, j, it.kb, ntiles, win, before, w, A, lane);
+  for (int j = 0; j < NS; ++j) C::issue(ring + j * TL::STAGE, f, j, it.kb, win, before, w, A);
   S.m = -INFINITY;
   S.l = 0.f;
 #pragma unroll
@@ -477,39 +465,36 @@ __global__ __launch_bounds__(64 * NW, 2) void chunk_attn(ChunkParams p) {
   const int nfull = all_see + 1 >= it.kb ? (all_see + 1 - it.kb) / TK : 0;     // tiles that every row sees whole
 
   // stages 0 .. NS - 1 are under way: wait for stage 0 (K of tile 0)
-  if (ntiles >= NS) {
-    // V waves have nothing in stage 0; what is younger than it is NS - 1 stages
-    wait_vm<(NS - 1) * DL::PER>();
-  } else {
-    wait_vm<0>();
-  }
+  wait_vm<(NS - 1) * DL::PER>();
   tile_barrier();
   typename C::Scores x = C::scores(ring, S, A);
-  // step t: stage t + 1 has landed here and everywhere, and every wave has
-  // read what it needs of stage t, where stage t + NS goes
-  auto turn = [&](int t) {
-    if (t + NS - 1 < ntiles) wait_vm<(NS - 2) * DL::PER>();
-    else wait_vm<0>();
-    tile_barrier();
-  };
+  float top = C::largest(x);
+  // Step t: stage t + 1 has landed here and everywhere, and every wave has read
+  // what it needs of stage t, where stage t + NS goes.
   int t = 0;
   if (wave_sees >= it.kb) {
     while (t + NS <= nfull) {
+      if (C::block_of(t + 2 * NS - 1, w) >= win.b + 64) look(win, f, it.kb, C::block_of(t + NS, w), lane);
       static_for<0, NS>([&](auto st) {
         constexpr int ST = decltype(st)::value;
-        turn(t + ST);
-        C::step(ring + ST * TL::STAGE, ring + ((ST + 1) % NS) * TL::STAGE, f, t + ST + NS, it.kb, ntiles, win, before, w, A, S,
-                x, p.scale_log2, lane);
+        wait_vm<(NS - 2) * DL::PER>();
+        tile_barrier();
+        C::step(ring + ST * TL::STAGE, ring + ((ST + 1) % NS) * TL::STAGE, f, t + ST + NS, it.kb, win, before, w, A, S,
+                x, top, p.scale_log2);
       });
       t += NS;
     }
   }
   for (; t < ntiles; ++t) {
-    turn(t);
+    wait_vm<0>();
+    tile_barrier();
+    if (C::block_of(t + NS, w) >= win.b + 64) look(win, f, it.kb, C::block_of(t + NS, w), lane);
     const int t0 = it.kb + TK * t;
-    C::edge_step(ring + (t % NS) * TL::STAGE, ring + ((t + 1) % NS) * TL::STAGE, f, t + NS, it.kb, ntiles, win, before, w, A, S,
-                 x, t0, t0 <= wave_sees, t + 1 < ntiles && t0 + TK <= wave_sees, p.scale_log2, lane);
+    C::edge_step(ring + (t % NS) * TL::STAGE, ring + ((t + 1) % NS) * TL::STAGE, t + NS <= ntiles, f, t + NS, it.kb,
+                 win, before, w, A, S, x, top, t0, t0 <= wave_sees, t + 1 < ntiles && t0 + TK <= wave_sees,
+                 p.scale_log2, lane);
   }
+  wait_vm<0>();                                          // no transfer outlives the work-group's LDS
 
   bool bad = false;
 #pragma unroll
