@@ -98,7 +98,7 @@ struct ChunkPlan {
   std::vector<ChunkItem> items;
   std::vector<ChunkJoin> joins;
   bool tall = false;
-  int32_t join_rows = 0;
+  int32_t join_rows = 0, join_pieces = 0;
   int64_t parts = 0;
   size_t off_joins = 0, plan_bytes = 0;
   size_t off_part_o = 0, off_part_ml = 0, device_bytes = 0;
@@ -175,6 +175,7 @@ spec_status_t plan_chunk(const spec_chunks_t* r, const spec_cache_t* c, const sp
       if (np > 1) {
         P.joins.push_back({h, t.r0, t.rows, np, P.parts, t.q0, 0});
         P.join_rows = std::max(P.join_rows, t.rows);
+        P.join_pieces = std::max(P.join_pieces, np);
       }
       for (int s = 0; s < np; ++s) {
         ChunkItem it;
@@ -311,6 +312,7 @@ spec_status_t spec_chunk_attn(const spec_chunks_t* chunks, const spec_cache_t* c
     p.out_f32 = args->out_dtype == SPEC_F32;
     p.tall = P.tall;
     p.join_rows = P.join_rows;
+    p.join_pieces = P.join_pieces;
     const float scale = args->scale > 0.f ? args->scale : 1.f / std::sqrt((float)cache->head_dim);
     p.scale_log2 = scale * 1.4426950408889634f;
     return sv::launch_chunk(p, s) == hipSuccess ? SPEC_OK : SPEC_ERR_HIP;

@@ -536,38 +536,52 @@ __global__ __launch_bounds__(64 * NW, 2) void chunk_attn(ChunkParams p) {
 #endif
 }
 
-// The pieces of one cut row tile, a wave a row:
-//   O = sum_s 2^(m_s - M) O_s / sum_s 2^(m_s - M) l_s,  M = max_s m_s,
-// the pieces in order.  A piece none of whose keys the row sees has m = -inf.
-// A lane four columns, a work-group as many rows as that takes; the pieces'
-// weights first, so that the rows' loads follow each other.
-template <int D, bool F32>
-__global__ __launch_bounds__(256) void chunk_join(ChunkParams p, int groups) {
-  constexpr int LPR = D / 4, RPG = 256 / LPR;            // lanes a row, rows a work-group
-  const int x = (int)blockIdx.x / groups;
-  const ChunkJoin jn = p.joins[x];
-  const int rr = ((int)blockIdx.x - x * groups) * RPG + (int)threadIdx.x / LPR;
-  if (rr >= jn.rows) return;
-  const int e = ((int)threadIdx.x % LPR) * 4;
-  const float2* ml = p.part_ml + jn.part + rr;
-  const float* po = p.part_o + (jn.part + rr) * D + e;
-  float M = -INFINITY;
-  for (int s = 0; s < jn.pieces; ++s) M = fmaxf(M, ml[(int64_t)s * jn.rows].x);
-  float L = 0.f;
-  f32x4 o = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 4
-  for (int s = 0; s < jn.pieces; ++s) {
-    const float2 y = ml[(int64_t)s * jn.rows];
-    const f32x4 v = *reinterpret_cast<const f32x4*>(po + (int64_t)s * jn.rows * D);
-    const float wgt = y.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(y.x - M);
-    L += y.y * wgt;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) o[i] += wgt * v[i];
+// A running join of pieces: O = sum_s 2^(m_s - M) O_s, l alike, M = max_s m_s.
+// A piece none of whose keys the row sees has m = -inf and adds nothing.
+struct Joined {
+  f32x4 o;
+  float m, l;
+  __device__ __forceinline__ void add(float m1, float l1, f32x4 o1) {
+    const float M = fmaxf(m, m1), ref = M == -INFINITY ? 0.f : M;
+    const float a = __builtin_amdgcn_exp2f(m - ref), b = __builtin_amdgcn_exp2f(m1 - ref);
+    o = o * a + o1 * b;
+    l = l * a + l1 * b;
+    m = M;
   }
-  const float inv = 1.f / L;
-  const int r = jn.r0 + rr, j = r / p.G;
-  const int64_t at = ((jn.q0 + (int64_t)j) * p.Hq + jn.kvh * p.G + (r - j * p.G)) * D + e;
-  const f32x4 y = o * inv;
+};
+
+// The joins of cut row tiles, NG groups of D / 4 lanes a work-group: a row each
+// where the tiles have few pieces (ROWS), else a row's pieces dealt to the
+// groups, whose sums meet in LDS.  (A join by the last piece to end, in the
+// kernel above, measured the same for one token over 1000 rows and 3 % slower
+// for 64 of them: its stores and loads past the L2s cost what the launch does.)
+template <int D, bool F32, bool ROWS>
+__global__ __launch_bounds__(256) void chunk_join(ChunkParams p) {
+  constexpr int LPR = D / 4, NG = 256 / LPR;
+  const ChunkJoin jn = p.joins[blockIdx.x];
+  const int g = threadIdx.x / LPR, x = threadIdx.x % LPR;
+  const int rr = ROWS ? (int)blockIdx.y * NG + g : (int)blockIdx.y;
+  if (!ROWS && rr >= jn.rows) return;
+  Joined j = {f32x4{0.f, 0.f, 0.f, 0.f}, -INFINITY, 0.f};
+  const float2* ml = p.part_ml + jn.part + min(rr, jn.rows - 1);
+  const float* po = p.part_o + (jn.part + min(rr, jn.rows - 1)) * D + 4 * x;
+#pragma unroll 4
+  for (int s = ROWS ? 0 : g; s < jn.pieces; s += ROWS ? 1 : NG) {
+    const float2 y = ml[(int64_t)s * jn.rows];
+    j.add(y.x, y.y, *reinterpret_cast<const f32x4*>(po + (int64_t)s * jn.rows * D));
+  }
+  if constexpr (!ROWS) {
+    __shared__ Joined lds[NG][LPR];
+    lds[g][x] = j;
+    __syncthreads();
+    if (g > 0) return;
+    for (int k = 1; k < NG; ++k) j.add(lds[k][x].m, lds[k][x].l, lds[k][x].o);
+  } else if (rr >= jn.rows) {
+    return;
+  }
+  const int r = jn.r0 + rr, tok = r / p.G;
+  const int64_t at = ((jn.q0 + (int64_t)tok) * p.Hq + jn.kvh * p.G + (r - tok * p.G)) * D + 4 * x;
+  const f32x4 y = j.o * (1.f / j.l);
   if constexpr (F32) *reinterpret_cast<f32x4*>(static_cast<float*>(p.out) + at) = y;
   else *reinterpret_cast<u32x2*>(static_cast<uint16_t*>(p.out) + at) = __builtin_bit_cast(u32x2, __builtin_convertvector(y, bf16x4));
 }
@@ -578,9 +592,11 @@ static hipError_t launch_d(const ChunkParams& p, hipStream_t s) {
   else chunk_attn<D, 1, 32, 2, PARTS><<<dim3(p.n_items), dim3(64), 0, s>>>(p);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.n_joins == 0) return e;
-  constexpr int RPG = 1024 / D;
-  const int groups = (p.join_rows + RPG - 1) / RPG;
-  chunk_join<D, PARTS != 1><<<dim3(p.n_joins * groups), dim3(256), 0, s>>>(p, groups);
+  constexpr int NG = 1024 / D;
+  if (p.join_pieces <= 2 * NG)
+    chunk_join<D, PARTS != 1, true><<<dim3(p.n_joins, (p.join_rows + NG - 1) / NG), dim3(256), 0, s>>>(p);
+  else
+    chunk_join<D, PARTS != 1, false><<<dim3(p.n_joins, p.join_rows), dim3(256), 0, s>>>(p);
   return hipGetLastError();
 }
 

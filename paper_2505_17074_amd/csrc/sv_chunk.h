@@ -54,6 +54,7 @@ struct ChunkParams {
   int32_t out_f32;
   int32_t tall;         // items of up to kChunkTallRows rows on four waves, else kChunkLowRows on one
   int32_t join_rows;    // rows of the tallest joined tile
+  int32_t join_pieces;  // pieces of the longest
   float scale_log2;
 };
 
