@@ -218,9 +218,10 @@ spec_status_t plan_chunk(const spec_chunks_t* r, const spec_cache_t* c, const sp
   return SPEC_OK;
 }
 
-// The row movers' view of `layers` layers from `layer` on.  Heads that follow
+// The row movers' view of `layers` layers from `layer` on, `rows` token rows
+// written in each.  Heads that follow
 // each other without a gap on both sides (apart: their strides) move as one.
-sv::CachePools pools(const spec_cache_t* c, int layer, int layers, bool one_run) {
+sv::CachePools pools(const spec_cache_t* c, int layer, int layers, bool one_run, int64_t rows) {
   const int64_t eb = elem_bytes(c->dtype);
   sv::CachePools p;
   p.layer_bytes = c->num_layers > 1 ? c->layer_stride * eb : 0;
@@ -238,6 +239,7 @@ sv::CachePools pools(const spec_cache_t* c, int layer, int layers, bool one_run)
     p.row_units *= p.heads;
     p.heads = 1;
   }
+  p.stream = rows * p.heads * p.row_units * 16 * 2 * layers >= sv::kMoveStream;
   return p;
 }
 bool heads_touch(const spec_cache_t* c) { return c->num_kv_heads == 1 || c->kv_stride_head == c->head_dim; }
@@ -337,7 +339,7 @@ spec_status_t spec_cache_append(const spec_chunks_t* chunks, const spec_cache_t*
 
   const bool touch = heads_touch(cache) && (cache->num_kv_heads == 1 || args->new_stride_head == cache->head_dim);
   sv::AppendParams p{};
-  p.c = pools(cache, args->layer, args->num_layers, touch);
+  p.c = pools(cache, args->layer, args->num_layers, touch, nq);
   p.k_new = static_cast<const char*>(args->k_new);
   p.v_new = static_cast<const char*>(args->v_new);
   p.new_sl = args->num_layers > 1 ? args->new_stride_layer * eb : 0;
@@ -418,7 +420,7 @@ spec_status_t spec_cache_commit(const spec_requests_t* req, const spec_cache_t* 
     return SPEC_ERR_UNSUPPORTED;
 
   sv::CommitParams p{};
-  p.c = pools(cache, 0, cache->num_layers, heads_touch(cache));
+  p.c = pools(cache, 0, cache->num_layers, heads_touch(cache), 0);
   p.bt_stride = cache->block_stride;
   p.shared = !per_req;
   o = 0;
@@ -456,8 +458,10 @@ spec_status_t spec_cache_copy_pages(const spec_cache_t* cache, const spec_page_c
     }
     for (int i = 0; i < num_copies; ++i)
       if (written.count(copies[i].src)) return SPEC_ERR_INVALID_ARG;
+    int64_t rows = 0;
+    for (int i = 0; i < num_copies; ++i) rows += copies[i].tokens;
     sv::PageCopyParams p{};
-    p.c = pools(cache, 0, cache->num_layers, heads_touch(cache));
+    p.c = pools(cache, 0, cache->num_layers, heads_touch(cache), rows);
     for (int i0 = 0; i0 < num_copies; i0 += sv::kMoveRequests) {
       p.n = std::min(sv::kMoveRequests, num_copies - i0);
       for (int i = 0; i < p.n; ++i) {

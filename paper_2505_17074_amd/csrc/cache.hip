@@ -25,10 +25,18 @@ __device__ __forceinline__ int64_t unit_at(int u, int row_units, int64_t sh_byte
   return h * sh_bytes + (int64_t)(u - h * row_units) * 16;
 }
 
+// A unit's store: with the streaming hint in calls that write more than the
+// Infinity Cache would keep for whoever reads it next (kMoveStream).
+template <bool STREAM>
+__device__ __forceinline__ void store(char* to, u32x4 x) {
+  if constexpr (STREAM) __builtin_nontemporal_store(x, reinterpret_cast<u32x4*>(to));
+  else *reinterpret_cast<u32x4*>(to) = x;
+}
+
 // blockIdx: (block of 16 rows, segment, 2 layer + (1 for V)).  Blocks are
 // 16-aligned, so one lies in one page.  A wave takes every fourth row of the
 // block, up to four rows' units in flight.
-template <bool RUN>
+template <bool RUN, bool STREAM>
 __global__ __launch_bounds__(256) void cache_append(AppendParams p) {
   const AppendSegment sg = p.seg[blockIdx.y];
   const int lane = threadIdx.x & 63;
@@ -53,7 +61,7 @@ __global__ __launch_bounds__(256) void cache_append(AppendParams p) {
       x[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(from + (w + 4 * i < n ? w + 4 * i : w) * p.new_st));
 #pragma unroll
     for (int i = 0; i < kMoveRows / 4; ++i)
-      if (w + 4 * i < n) *reinterpret_cast<u32x4*>(to + (w + 4 * i) * (int64_t)p.c.st_bytes) = x[i];
+      if (w + 4 * i < n) store<STREAM>(to + (w + 4 * i) * (int64_t)p.c.st_bytes, x[i]);
   }
 }
 
@@ -112,7 +120,7 @@ __global__ __launch_bounds__(64) void cache_commit(CommitParams p) {
 constexpr int kCopyUnits = 4;          // 16-byte units a thread
 
 // blockIdx: (part of the page, pair, 2 layer + (1 for V)).
-template <bool RUN>
+template <bool RUN, bool STREAM>
 __global__ __launch_bounds__(256) void cache_copy_pages(PageCopyParams p) {
   const int i = blockIdx.y;
   const int row_units = p.c.heads * p.c.row_units;
@@ -134,15 +142,16 @@ __global__ __launch_bounds__(256) void cache_copy_pages(PageCopyParams p) {
   }
 #pragma unroll
   for (int j = 0; j < kCopyUnits; ++j)
-    if (u0 + (int)threadIdx.x + 256 * j < units) __builtin_nontemporal_store(x[j], reinterpret_cast<u32x4*>(dst + at[j]));
+    if (u0 + (int)threadIdx.x + 256 * j < units) store<STREAM>(dst + at[j], x[j]);
 }
 
 }  // namespace
 
 hipError_t launch_append(const AppendParams& p, hipStream_t s) {
   const dim3 g(p.parts, p.n_seg, 2 * p.c.layers);
-  if (p.c.heads == 1) cache_append<true><<<g, dim3(256), 0, s>>>(p);
-  else cache_append<false><<<g, dim3(256), 0, s>>>(p);
+  const bool run = p.c.heads == 1;
+  if (p.c.stream) (run ? cache_append<true, true> : cache_append<false, true>)<<<g, dim3(256), 0, s>>>(p);
+  else (run ? cache_append<true, false> : cache_append<false, false>)<<<g, dim3(256), 0, s>>>(p);
   return hipGetLastError();
 }
 
@@ -158,8 +167,9 @@ hipError_t launch_page_copy(const PageCopyParams& p, hipStream_t s) {
   for (int i = 0; i < p.n; ++i) most = p.tokens[i] > most ? p.tokens[i] : most;
   const int units = most * p.c.heads * p.c.row_units;
   const dim3 g((units + 256 * kCopyUnits - 1) / (256 * kCopyUnits), p.n, 2 * p.c.layers);
-  if (p.c.heads == 1) cache_copy_pages<true><<<g, dim3(256), 0, s>>>(p);
-  else cache_copy_pages<false><<<g, dim3(256), 0, s>>>(p);
+  const bool run = p.c.heads == 1;
+  if (p.c.stream) (run ? cache_copy_pages<true, true> : cache_copy_pages<false, true>)<<<g, dim3(256), 0, s>>>(p);
+  else (run ? cache_copy_pages<true, false> : cache_copy_pages<false, false>)<<<g, dim3(256), 0, s>>>(p);
   return hipGetLastError();
 }
 

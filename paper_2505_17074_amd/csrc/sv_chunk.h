@@ -77,7 +77,12 @@ struct CachePools {
   int32_t num_pages, page_tokens;
   int32_t layers;                      // moved by this call, from k / v on
   int32_t heads, row_units;            // a head's row in 16-byte units
+  int32_t stream;                      // the call writes kMoveStream bytes or more
 };
+// Where the streaming hint on the stores begins to pay (the Infinity Cache
+// holds 256 MB): 276 MB of new rows 94 us with it against 107 without, 126 MB
+// whose accepted paths are moved next 62 against 60.
+constexpr int64_t kMoveStream = (int64_t)192 << 20;
 
 // A run of one request's new rows: `n` rows from its logical row `pos` on,
 // from row `row` of the new arrays on.
