@@ -83,43 +83,29 @@ class DeviceBatch:
         return a
 
 
-class Verifier:
-    """Runs spec_verify / spec_verify_attn / spec_accept on one DeviceBatch.
+class StagingRing:
+    """The staging of calls that share one device workspace: a ring of pinned
+    buffers, one per call in turn, and the order of the calls.
 
-    Owns the device workspace and a ring of `ring` pinned staging buffers,
-    one per call in turn.  The slots used since the last event are covered by
-    one event, recorded after every `event_every`-th call (and before a call
-    on a different stream): each event is a marker packet on the stream, and
-    one per call cost the steps 4-7 us.  Before a slot is rewritten, the
-    event covering its last use is polled until it completes (a spin, not a
-    sleeping wait, so the host never wakes late).  A slot's last use is
-    `ring` >= `event_every` calls back, so it is always covered by then.
-    Calls may be issued back to back without a device sync.
+    The slots used since the last event are covered by one event, recorded
+    after every `event_every`-th call (and before a call on a different
+    stream): each event is a marker packet on the stream, and one per call
+    cost the steps 4-7 us.  Before a slot is rewritten, the event covering its
+    last use is polled until it completes (a spin, not a sleeping wait, so the
+    host never wakes late).  A slot's last use is `ring` >= `event_every` calls
+    back, so it is always covered by then.  Calls may be issued back to back
+    without a device sync.
 
-    Every call uses the one device workspace (split partials, acceptance
-    statistics, tickets), so calls are serialised: before a call on a stream
-    other than the previous call's, that stream waits on an event recorded
-    on the previous call's stream after that call.  Calls that should run
-    concurrently need Verifiers of their own.
+    Calls are serialised: before a call on a stream other than the previous
+    call's, that stream waits on an event recorded on the previous call's
+    stream after that call.  Calls that should run concurrently need objects
+    of their own.
     """
 
-    def __init__(self, batch: DeviceBatch, split_kv: int = 0, ring: int = 32, event_every: int = 8,
-                 attn: Optional[B.SpecAttnArgs] = None):
-        if event_every < 1 or ring < event_every:
-            raise ValueError("need ring >= event_every >= 1")
-        self.batch = batch
-        self.req = batch.requests()
-        self.attn = attn if attn is not None else batch.attn_args(split_kv)
-        self.acc = batch.accept_args()
-        st, dev, host = B.spec_workspace_bytes(self.req, self.attn, self.acc)
-        B.check(st, "spec_workspace_bytes")
-        self.ws_bytes = dev
-        self._ws = torch.empty(dev + 256, dtype=torch.uint8, device=batch.device)
-        self.ws_ptr = (self._ws.data_ptr() + 255) // 256 * 256
-        self.staging_bytes = host
-        self._staging = [torch.empty(max(host, 1), dtype=torch.uint8, pin_memory=True) for _ in range(ring)]
+    def _ring(self, slots: list, event_every: int) -> None:
+        self._staging = slots
         self._every = event_every
-        self._slot_ev = [None] * ring      # the event covering each slot's last use
+        self._slot_ev = [None] * len(slots)   # the event covering each slot's last use
         self._pending = []                 # slots used since the last event
         self._pending_stream = None
         self._i = 0                        # calls issued
@@ -162,6 +148,29 @@ class Verifier:
         self._pending_stream = stream
         if len(self._pending) >= self._every:
             self._cover()
+
+
+class Verifier(StagingRing):
+    """Runs spec_verify / spec_verify_attn / spec_accept on one DeviceBatch.
+
+    Owns the device workspace and `ring` pinned staging buffers (StagingRing).
+    """
+
+    def __init__(self, batch: DeviceBatch, split_kv: int = 0, ring: int = 32, event_every: int = 8,
+                 attn: Optional[B.SpecAttnArgs] = None):
+        if event_every < 1 or ring < event_every:
+            raise ValueError("need ring >= event_every >= 1")
+        self.batch = batch
+        self.req = batch.requests()
+        self.attn = attn if attn is not None else batch.attn_args(split_kv)
+        self.acc = batch.accept_args()
+        st, dev, host = B.spec_workspace_bytes(self.req, self.attn, self.acc)
+        B.check(st, "spec_workspace_bytes")
+        self.ws_bytes = dev
+        self._ws = torch.empty(dev + 256, dtype=torch.uint8, device=batch.device)
+        self.ws_ptr = (self._ws.data_ptr() + 255) // 256 * 256
+        self.staging_bytes = host
+        self._ring([torch.empty(max(host, 1), dtype=torch.uint8, pin_memory=True) for _ in range(ring)], event_every)
 
     def run(self, which: str = "verify", stream: Optional[torch.cuda.Stream] = None) -> None:
         stream = stream or torch.cuda.current_stream(self.batch.device)

@@ -12,10 +12,17 @@ import numpy as np
 import torch
 
 from . import binding as B
-from .batch import Verifier
+from .batch import StagingRing
 
 _DTYPE = {torch.bfloat16: B.SPEC_BF16, torch.float32: B.SPEC_F32}
 _HERE = contextlib.nullcontext()
+
+
+def _stride(t: torch.Tensor, dim: int, otherwise: int) -> int:
+    """A dimension's stride; of a dimension that holds one entry (or none) any
+    will do, and torch may have any."""
+    return t.stride(dim) if t.shape[dim] > 1 else otherwise
+
 
 
 def _current_raw_stream(index: int) -> int:
@@ -100,11 +107,12 @@ class PagedCache:
             raise ValueError("k and v are [layers, num_pages, page_tokens, Hkv, d] of the same type, strides and device")
         if k.dtype not in _DTYPE:
             raise ValueError("bf16 or fp32 pools")
-        if k.stride(4) != 1 or k.stride(1) != k.shape[2] * k.stride(2):
+        if k.stride(4) != 1 or (k.shape[1] > 1 and k.stride(1) != k.shape[2] * k.stride(2)):
             raise ValueError("rows are contiguous and pages follow each other")
         self.k, self.v, self.device, self.dtype = k, v, k.device, k.dtype
         self._index = k.device.index
         self._head = k.shape[3:]
+        self._width = k.shape[3] * k.shape[4]
         self._lib = B.load()
         c = self.c = B.SpecCache()
         self._ref = C.byref(c)
@@ -113,7 +121,8 @@ class PagedCache:
         c.num_layers, c.num_pages, c.page_tokens, c.num_kv_heads, c.head_dim = k.shape
         c.dtype = _DTYPE[k.dtype]
         c.k, c.v = k.data_ptr(), v.data_ptr()
-        c.layer_stride, c.kv_stride_tok, c.kv_stride_head = k.stride(0), k.stride(2), k.stride(3)
+        c.layer_stride, c.kv_stride_tok = k.stride(0), k.stride(2)
+        c.kv_stride_head = _stride(k, 3, c.head_dim)
         self.table = table
 
     @property
@@ -150,7 +159,7 @@ class PagedCache:
         to the ends of the requests, in the cache's layers from `layer` on."""
         shape, st = k_new.shape, k_new.stride()
         if shape != v_new.shape or st != v_new.stride() or len(shape) not in (3, 4) or \
-                shape[-2:] != self._head or shape[-3] < chunks.rows or (st[-1] != 1 and k_new.numel()):
+                shape[-2:] != self._head or shape[-3] < chunks.rows or (st[-1] != 1 and shape[-1] > 1):
             raise ValueError("k_new and v_new are [layers, rows, Hkv, d], a row for every new token")
         if k_new.dtype != self.dtype or v_new.dtype != self.dtype or k_new.device != self.device or \
                 v_new.device != self.device:
@@ -159,8 +168,10 @@ class PagedCache:
         a = self._append
         a.layer, a.num_layers = layer, shape[0] if len(shape) == 4 else 1
         a.k_new, a.v_new = k_new.data_ptr(), v_new.data_ptr()
-        a.new_stride_layer = max(1, st[0])
-        a.new_stride_tok, a.new_stride_head = max(1, st[-3]), max(1, st[-2])
+        width = self._width
+        a.new_stride_layer = st[0]
+        a.new_stride_tok = st[-3] if shape[-3] > 1 else width
+        a.new_stride_head = st[-2] if shape[-2] > 1 else shape[-1]
         with self._enter():
             B.check(self._lib.spec_cache_append(chunks, self._ref, self._append_ref, self._stream(stream)),
                     "spec_cache_append")
@@ -185,12 +196,9 @@ class PagedCache:
                                                     self._stream(stream)), "spec_cache_copy_pages")
 
 
-class ChunkAttention(Verifier):
+class ChunkAttention(StagingRing):
     """Runs spec_chunk_attn on a PagedCache.  Owns a device workspace, which
-    grows with the batches, and a ring of pinned staging buffers, handled as
-    Verifier's: calls may be issued back to back, calls on another stream wait
-    for the previous call's, and calls that should run at the same time need
-    objects of their own.  A graph is captured from B.spec_chunk_attn with a
+    grows with the batches, and `ring` pinned staging buffers (StagingRing).  A graph is captured from B.spec_chunk_attn with a
     workspace and staging of its own, not from here: a replay reads the staging
     it was captured with, and the ring reuses its slots."""
 
@@ -204,13 +212,7 @@ class ChunkAttention(Verifier):
         self._head = torch.Size((num_q_heads, cache.c.head_dim))
         self.ws_bytes = self.staging_bytes = 0
         self.ws_ptr = None
-        self._staging = [None] * ring
-        self._every = event_every
-        self._slot_ev = [None] * ring
-        self._pending = []
-        self._pending_stream = None
-        self._i = 0
-        self._last_stream = None
+        self._ring([None] * ring, event_every)
 
     def _grow(self, chunks, stream) -> None:
         st, dev, host = B.spec_chunk_workspace_bytes(chunks, self.cache.c, self.args)
@@ -239,12 +241,13 @@ class ChunkAttention(Verifier):
             raise ValueError("q and out are [rows, Hq, d], a row for every new token")
         kind = _DTYPE.get(out.dtype)
         if q.dtype != cache.dtype or kind is None or q.device != cache.device or out.device != cache.device or \
-                not out.is_contiguous() or (st[2] != 1 and q.numel()):
+                not out.is_contiguous() or st[2] != 1:
             raise ValueError("q has the cache's type, out is contiguous bf16 or fp32, both on its device")
         cache._requests(chunks.num_requests)
         a.layer, a.out_dtype = layer, kind
         a.q, a.out = q.data_ptr(), out.data_ptr()
-        a.q_stride_tok, a.q_stride_head = max(1, st[0]), max(1, st[1])
+        a.q_stride_tok = st[0] if qs[0] > 1 else qs[1] * qs[2]
+        a.q_stride_head = st[1] if qs[1] > 1 else qs[2]
         with cache._enter():
             stream = stream or torch.cuda.current_stream(cache._index)
             self._order(stream)

@@ -127,14 +127,14 @@ spec_status_t plan_chunk(const spec_chunks_t* r, const spec_cache_t* c, const sp
   for (int i = 0; i < r->num_requests; ++i) most = std::max<int64_t>(most, (int64_t)r->new_len[i] * G);
   P.tall = most > sv::kChunkLowRows;
   const int RT = P.tall ? sv::kChunkTallRows : sv::kChunkLowRows;
-  struct RowTile { int32_t req, r0, rows, keys, q0; };
+  struct RowTile { int32_t req, r0, rows, keys, q0, len, pieces; };
   std::vector<RowTile> tiles;
   int64_t q0 = 0, total = 0, longest = 0;
   for (int i = 0; i < r->num_requests; ++i) {
     const int n = r->new_len[i], rows = n * G;
     for (int r0 = 0; r0 < rows; r0 += RT) {
       const int nr = std::min(RT, rows - r0);
-      tiles.push_back({i, r0, nr, r->ctx_len[i] + (r0 + nr - 1) / G + 1, (int32_t)q0});
+      tiles.push_back({i, r0, nr, r->ctx_len[i] + (r0 + nr - 1) / G + 1, (int32_t)q0, 0, 0});
       const int64_t kt = (tiles.back().keys + sv::kChunkTile - 1) / sv::kChunkTile;
       total += kt * Hkv;
       longest = std::max(longest, kt);
@@ -164,51 +164,73 @@ spec_status_t plan_chunk(const spec_chunks_t* r, const spec_cache_t* c, const sp
     const int64_t mean = (total + cus - 1) / cus;
     cap = longest <= mean + 8 ? longest : std::max<int64_t>(8, mean);
   }
-  longest = 0;
-  for (const RowTile& t : tiles) {
+  int64_t n_items = 0;
+  for (RowTile& t : tiles) {
     const int64_t kt = (t.keys + sv::kChunkTile - 1) / sv::kChunkTile;
     const int64_t pieces = (kt + cap - 1) / cap;
-    const int64_t len = (kt + pieces - 1) / pieces;
-    const int np = (int)((kt + len - 1) / len);
-    longest = std::max(longest, len);
-    for (int h = 0; h < Hkv; ++h) {
-      if (np > 1) {
-        P.joins.push_back({h, t.r0, t.rows, np, P.parts, t.q0, 0});
-        P.join_rows = std::max(P.join_rows, t.rows);
-        P.join_pieces = std::max(P.join_pieces, np);
+    t.len = (int32_t)((kt + pieces - 1) / pieces);
+    t.pieces = (int32_t)((kt + t.len - 1) / t.len);
+    n_items += (int64_t)t.pieces * Hkv;
+  }
+  if (n_items >= (int64_t)1 << 24) return SPEC_ERR_UNSUPPORTED;      // a launch's work-items are 32 bits
+  // The longest first, so that the last to start are the shortest; after each,
+  // its request's neighbouring row tiles down to 7 / 8 of its length, which
+  // read the same keys: with the heads innermost they run on the same XCD
+  // (work-group b on XCD b % 8) at the same time (64 requests of 64 tokens over
+  // 4000 rows 357 us, by length alone 419).  Single tokens share nothing, and
+  // there a head's pieces follow each other (64 of them 192 us, heads
+  // innermost 199).
+  std::vector<int32_t> order, sorted(tiles.size());
+  order.reserve(tiles.size());
+  for (size_t i = 0; i < tiles.size(); ++i) sorted[i] = (int32_t)i;
+  std::stable_sort(sorted.begin(), sorted.end(), [&](int32_t x, int32_t y) { return tiles[x].len > tiles[y].len; });
+  std::vector<bool> placed(tiles.size(), false);
+  for (const int32_t x : sorted) {
+    if (placed[x]) continue;
+    const RowTile& t = tiles[x];
+    auto with = [&](int64_t y) {
+      return y >= 0 && y < (int64_t)tiles.size() && !placed[y] && tiles[y].req == t.req &&
+             8 * (int64_t)tiles[y].len >= 7 * (int64_t)t.len;
+    };
+    placed[x] = true;
+    order.push_back(x);
+    for (int step : {-1, 1})
+      for (int64_t y = (int64_t)x + step; with(y); y += step) {
+        placed[y] = true;
+        order.push_back((int32_t)y);
       }
-      for (int s = 0; s < np; ++s) {
-        ChunkItem it;
-        it.req = t.req;
-        it.kvh = h;
-        it.r0 = t.r0;
-        it.rows = t.rows;
-        it.kb = (int32_t)(s * len * sv::kChunkTile);
-        it.ke = (int32_t)std::min<int64_t>(t.keys, (s + 1) * len * sv::kChunkTile);
-        it.ctx = r->ctx_len[t.req];
-        it.q0 = t.q0;
-        it.part = np > 1 ? P.parts + (int64_t)s * t.rows : -1;
-        it.pad = 0;
-        P.items.push_back(it);
-      }
-      if (np > 1) P.parts += (int64_t)np * t.rows;
+  }
+  P.items.reserve((size_t)n_items);
+  for (const int32_t x : order) {
+    const RowTile& t = tiles[x];
+    const int64_t part = P.parts;
+    if (t.pieces > 1) {
+      for (int h = 0; h < Hkv; ++h)
+        P.joins.push_back({h, t.r0, t.rows, t.pieces, part + (int64_t)h * t.pieces * t.rows, t.q0, 0});
+      P.join_rows = std::max(P.join_rows, t.rows);
+      P.join_pieces = std::max(P.join_pieces, t.pieces);
+      P.parts += (int64_t)Hkv * t.pieces * t.rows;
     }
-    if (P.items.size() >= INT32_MAX / 64) return SPEC_ERR_UNSUPPORTED;
+    for (int i = 0; i < t.pieces * Hkv; ++i) {
+      const int h = P.tall ? i % Hkv : i / t.pieces, s = P.tall ? i / Hkv : i % t.pieces;
+      ChunkItem it;
+      it.req = t.req;
+      it.kvh = h;
+      it.r0 = t.r0;
+      it.rows = t.rows;
+      it.kb = (int32_t)((int64_t)s * t.len * sv::kChunkTile);
+      it.ke = (int32_t)std::min<int64_t>(t.keys, (int64_t)(s + 1) * t.len * sv::kChunkTile);
+      it.ctx = r->ctx_len[t.req];
+      it.q0 = t.q0;
+      it.part = t.pieces > 1 ? part + ((int64_t)h * t.pieces + s) * t.rows : -1;
+      it.pad = 0;
+      P.items.push_back(it);
+    }
   }
-  // longest first (a stable counting sort): the last to start are the shortest
-  {
-    auto len = [](const ChunkItem& it) { return (it.ke - it.kb + sv::kChunkTile - 1) / sv::kChunkTile; };
-    std::vector<size_t> start((size_t)longest + 2, 0);
-    for (const ChunkItem& it : P.items) ++start[longest - len(it) + 1];
-    for (int64_t t = 1; t <= longest + 1; ++t) start[t] += start[t - 1];
-    std::vector<ChunkItem> sorted(P.items.size());
-    for (const ChunkItem& it : P.items) sorted[start[longest - len(it)]++] = it;
-    P.items.swap(sorted);
-    // work-groups b and b + cus of the tall kernel share a compute unit at
-    // first: the longest with the shortest of the first two rounds
-    const int64_t n = (int64_t)P.items.size();
-    if (P.tall && n > cus) std::reverse(P.items.begin() + cus, P.items.begin() + std::min<int64_t>(n, 2 * cus));
-  }
+  // work-groups b and b + cus of the tall kernel share a compute unit at first:
+  // the longest with the shortest of the first two rounds
+  if (P.tall && n_items > cus)
+    std::reverse(P.items.begin() + cus, P.items.begin() + std::min<int64_t>(n_items, 2 * cus));
 
   P.off_joins = align_up(sizeof(ChunkItem) * P.items.size());
   P.plan_bytes = P.off_joins + align_up(sizeof(ChunkJoin) * P.joins.size());
