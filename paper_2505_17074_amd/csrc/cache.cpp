@@ -148,21 +148,24 @@ spec_status_t plan_chunk(const spec_chunks_t* r, const spec_cache_t* c, const sp
     // Few rows: the keys stream past them at HBM's rate whatever the pieces, so
     // they are cut to about 4 / 3 rounds of the work-groups that run at once
     // (four a compute unit), where the last ones to end lose least, down to 128
-    // keys.  64 single tokens over 512-8192 rows: pieces of 1280 keys 190 us,
-    // 512 207, 4096 214; one over 1000 rows: 64 keys 18.7, 128 16.9, 256 19.3.
+    // keys (64 where that leaves no compute unit two).  64 single tokens over
+    // 512-8192 rows: pieces of 1280 keys 190 us, 512 207, 4096 214; one over 2000
+    // rows of 8 KV heads: 64 keys 12.9, 128 14.9; over 4000: 15.2 and 14.6.
     const int64_t slots = 4 * (int64_t)cus;
-    cap = std::max<int64_t>(2, (3 * total + 4 * slots - 1) / (4 * slots));
+    cap = std::max<int64_t>(total <= cus ? 1 : 2, (3 * total + 4 * slots - 1) / (4 * slots));
   } else {
     // Many rows: a compute unit takes a 64-key tile in about a microsecond,
     // whether one work-group runs on it or two, so the longest item bounds the
     // kernel only where it is longer than a unit's mean share.  Only then is
-    // it cut, and where that saves more than the joins cost (about eight
+    // it cut, and where that saves more than the join costs (about seven
     // tiles).  2048 new tokens, the longest 32 tiles of a mean of 33: whole
-    // 54 us, pieces of 24 tiles 62, 16 64, 8 79.  Decoding requests beside a
-    // chunk run in the same launch (beside 8 chunks of 33-700 tokens, 16 single
-    // ones: 181 us, in a launch of their own before it 198).
+    // 48 us, pieces of 24 tiles 62, 16 64, 8 79; 1024, 16 of 9: whole 25, cut
+    // 27; 64 over 2000 rows, 33 of 3: whole 40, pieces of 12 tiles 22, 8 20,
+    // 4 17.  Decoding requests beside a chunk run in the same launch (beside 8
+    // chunks of 33-700 tokens, 16 single ones: 181 us, in a launch of their own
+    // before it 198).
     const int64_t mean = (total + cus - 1) / cus;
-    cap = longest <= mean + 8 ? longest : std::max<int64_t>(8, mean);
+    cap = longest <= mean + 7 ? longest : std::max<int64_t>(4, mean);
   }
   int64_t n_items = 0;
   for (RowTile& t : tiles) {
