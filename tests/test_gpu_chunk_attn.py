@@ -197,3 +197,95 @@ def test_page_ids_outside_the_pool(gpu_lib):
     p.table[0, 1], p.table[0, 2] = -5, 1 << 30
     got = _run(p, q, BF16)
     assert torch.equal(got[40:], good[40:])
+
+
+def _device_case(B_, n, ctx, hkv, G, d, page, seed):
+    """Large pools made on the device; returns (cache, table, ctx, q)."""
+    from paper_2505_17074_amd.cache import PagedCache
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    per = -(-(ctx + n) // page)
+    order = torch.randperm(B_ * per + 2, generator=g, device="cuda")[:B_ * per].to(torch.int32).view(B_, per)
+    k, v = (torch.randn((1, B_ * per + 2, page, hkv, d), generator=g, device="cuda", dtype=BF16) for _ in range(2))
+    q = torch.randn((B_ * n, hkv * G, d), generator=g, device="cuda", dtype=BF16)
+    return PagedCache(k, v, order.contiguous()), q
+
+
+@pytest.mark.parametrize("B_,n,ctx,hkv,G,d", [(43, 1, 2111, 32, 1, 64), (64, 32, 2500, 8, 4, 128)],
+                         ids=["one_wave", "four_waves"])
+def test_items_of_more_than_2048_keys(gpu_lib, B_, n, ctx, hkv, G, d):
+    """Batches whose items are not cut at all: the page ids of an item come in
+    several windows.  A few requests against the definition, on the device."""
+    print(f"[case] chunk long items {B_} {n} {ctx}", flush=True)
+    cache, q = _device_case(B_, n, ctx, hkv, G, d, 96, 5)
+    out = torch.empty((B_ * n, hkv * G, d), dtype=F32, device="cuda")
+    ChunkAttention(cache, hkv * G).run(B.make_chunks([ctx] * B_, [n] * B_), q, out)
+    seen = torch.arange(ctx + n, device="cuda")[None] <= ctx + torch.arange(n, device="cuda")[:, None]
+    for i in (0, B_ // 2, B_ - 1):
+        kk, vv = (x[0, cache.table[i].long()].reshape(-1, hkv, d)[:ctx + n].double() for x in (cache.k, cache.v))
+        for h in range(hkv * G):
+            qq = q[i * n:(i + 1) * n, h].double()
+            s = torch.where(seen, (qq @ kk[:, h // G].t().contiguous()) / d ** 0.5, -float("inf"))
+            w = torch.softmax(s, -1)
+            ref, size = w @ vv[:, h // G], w @ vv[:, h // G].abs()
+            e = (d + 6) * 2.0 ** -24 * 1.4427 * float(qq.abs().max() * kk.abs().max()) * d ** 0.5
+            bound = size * (2 * e + 2.0 ** -24 + (2 * (ctx + n) + 16) * 2.0 ** -24) + 2.0 ** -24 * ref.abs()
+            assert ((out[i * n:(i + 1) * n, h].double() - ref).abs() <= bound * 1.01).all(), (i, h)
+
+
+def test_keys_and_values_in_one_tensor(gpu_lib):
+    """K and V interleaved by token: views of one [.., 2, Hkv, d] allocation."""
+    from paper_2505_17074_amd.cache import PagedCache
+    print("[case] chunk interleaved", flush=True)
+    p = Paged([200, 40], [60, 1], 2, 64, 32, layers=2, seed=9).write()
+    both = torch.full((2, p.num_pages, 32, 2, 2, 64), float("nan"), dtype=BF16, device="cuda")
+    both[:, :, :, 0], both[:, :, :, 1] = p.k, p.v
+    cache = PagedCache(both[:, :, :, 0], both[:, :, :, 1], p.table)
+    q = queries(61, 8, 64, seed=9)
+    out = torch.empty((61, 8, 64), dtype=F32, device="cuda")
+    ChunkAttention(cache, 8).run(p.chunks(), q.cuda(), out, layer=1)
+    check_close(out, *reference(p, q, layer=1, out=F32))
+    k_new, v_new = (torch.randn((2, 61, 2, 64)).to(BF16).cuda() for _ in range(2))
+    cache.append(p.chunks(), k_new, v_new)
+    torch.cuda.synchronize()
+    q0 = 0
+    for i in range(2):
+        c, n = int(p.ctx[i]), int(p.new[i])
+        pg, pl = (torch.from_numpy(x).cuda() for x in p.where(i, np.arange(c, c + n)))
+        assert torch.equal(both[:, pg, pl, 0], k_new[:, q0:q0 + n]) and torch.equal(both[:, pg, pl, 1], v_new[:, q0:q0 + n])
+        q0 += n
+
+
+@pytest.mark.parametrize("seed", range(12))
+def test_random_batches(gpu_lib, seed):
+    rng = np.random.default_rng(100 + seed)
+    b = int(rng.integers(1, 7))
+    ctx = [int(x) for x in rng.integers(0, rng.choice([3, 70, 600]), b)]
+    new = [int(x) for x in rng.integers(0, rng.choice([2, 9, 150]), b)]
+    new[0] = max(new[0], 1)
+    hkv, G = int(rng.choice([1, 2, 3])), int(rng.choice([1, 2, 4, 5, 8]))
+    d, page, out = int(rng.choice([64, 128])), int(rng.choice([32, 64, 96, 256])), [BF16, F32][seed % 2]
+    print(f"[case] chunk random {seed} ctx {ctx} new {new} heads {hkv * G}/{hkv} d {d} page {page}", flush=True)
+    p = Paged(ctx, new, hkv, d, page, seed=seed, layers=1 + seed % 2).write()
+    q = queries(sum(new), hkv * G, d, seed=seed)
+    check_close(_run(p, q, out, layer=seed % 2), *reference(p, q, layer=seed % 2, out=out))
+
+
+def test_one_object_for_growing_batches(gpu_lib):
+    """Workspace and staging grow with the batches; a large one between small
+    ones, back to back."""
+    print("[case] chunk growing", flush=True)
+    p = Paged([900, 3000, 5, 77], [1, 1, 130, 64], 2, 128, seed=30).write()
+    att = ChunkAttention(p.cache, 8)
+    table = p.table.clone()
+    want, outs = [], []
+    for sel in ([0], [2, 3], [0, 1, 2, 3], [0], [1], [0, 1, 2, 3]):
+        q = queries(int(p.new[sel].sum()), 8, 128, seed=len(sel))
+        out = torch.empty((q.shape[0], 8, 128), dtype=BF16, device="cuda")
+        p.cache.table = table[sel].contiguous()
+        outs.append((p.cache.table, q.cuda(), out))
+        att.run(B.make_chunks(p.ctx[sel], p.new[sel]), outs[-1][1], out)
+        sub = Paged.__new__(Paged)
+        sub.ctx, sub.new, sub.hkv, sub.rows = p.ctx[sel], p.new[sel], 2, [p.rows[i] for i in sel]
+        want.append(reference(sub, q))
+    for (_, _, out), (ref, bound) in zip(outs, want):
+        check_close(out, ref, bound)
