@@ -6,14 +6,13 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <atomic>
 #include <cmath>
 #include <cstring>
-#include <new>
 #include <unordered_set>
 #include <vector>
 
 #include "sv_chunk.h"
-#include "sv_rules.h"
 
 namespace {
 
@@ -80,25 +79,26 @@ spec_status_t check_chunks(const spec_chunks_t* r, const spec_cache_t* c, int64_
 }
 
 int compute_units() {
-  static int cus[64];
+  static std::atomic<int> cus[64];
   int dev = 0, n = 0;
   if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= 64) {
     (void)hipGetLastError();
     return 256;
   }
-  if (cus[dev]) return cus[dev];
+  if (const int known = cus[dev].load(std::memory_order_relaxed)) return known;
   if (hipDeviceGetAttribute(&n, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess || n <= 0) {
     (void)hipGetLastError();
     n = 256;
   }
-  return cus[dev] = n;
+  cus[dev].store(n, std::memory_order_relaxed);
+  return n;
 }
 
 struct ChunkPlan {
   std::vector<ChunkItem> items;
   std::vector<ChunkJoin> joins;
   bool tall = false;
-  int32_t join_rows = 0, join_pieces = 0;
+  int32_t join_rows = 0, join_pieces = 0, turn0 = 0, turn1 = 0;
   int64_t parts = 0;
   size_t off_joins = 0, plan_bytes = 0;
   size_t off_part_o = 0, off_part_ml = 0, device_bytes = 0;
@@ -173,9 +173,9 @@ spec_status_t plan_chunk(const spec_chunks_t* r, const spec_cache_t* c, const sp
     const int64_t pieces = (kt + cap - 1) / cap;
     t.len = (int32_t)((kt + pieces - 1) / pieces);
     t.pieces = (int32_t)((kt + t.len - 1) / t.len);
-    n_items += (int64_t)t.pieces * Hkv;
+    n_items += t.pieces;
   }
-  if (n_items >= (int64_t)1 << 24) return SPEC_ERR_UNSUPPORTED;      // a launch's work-items are 32 bits
+  if (n_items * Hkv >= (int64_t)1 << 24) return SPEC_ERR_UNSUPPORTED;      // a launch's work-items are 32 bits
   // The longest first, so that the last to start are the shortest; after each,
   // its request's neighbouring row tiles down to 7 / 8 of its length, which
   // read the same keys: with the heads innermost they run on the same XCD
@@ -206,34 +206,22 @@ spec_status_t plan_chunk(const spec_chunks_t* r, const spec_cache_t* c, const sp
   P.items.reserve((size_t)n_items);
   for (const int32_t x : order) {
     const RowTile& t = tiles[x];
-    const int64_t part = P.parts;
+    const int32_t len = t.len * sv::kChunkTile;
+    for (int32_t s = 0; s < t.pieces; ++s)
+      P.items.push_back({t.req, t.r0, t.rows, t.keys, len, s, t.pieces, r->ctx_len[t.req], P.parts, t.q0, 0});
     if (t.pieces > 1) {
-      for (int h = 0; h < Hkv; ++h)
-        P.joins.push_back({h, t.r0, t.rows, t.pieces, part + (int64_t)h * t.pieces * t.rows, t.q0, 0});
+      P.joins.push_back({t.r0, t.rows, t.pieces, t.q0, P.parts, 0});
       P.join_rows = std::max(P.join_rows, t.rows);
       P.join_pieces = std::max(P.join_pieces, t.pieces);
       P.parts += (int64_t)Hkv * t.pieces * t.rows;
     }
-    for (int i = 0; i < t.pieces * Hkv; ++i) {
-      const int h = P.tall ? i % Hkv : i / t.pieces, s = P.tall ? i / Hkv : i % t.pieces;
-      ChunkItem it;
-      it.req = t.req;
-      it.kvh = h;
-      it.r0 = t.r0;
-      it.rows = t.rows;
-      it.kb = (int32_t)((int64_t)s * t.len * sv::kChunkTile);
-      it.ke = (int32_t)std::min<int64_t>(t.keys, (int64_t)(s + 1) * t.len * sv::kChunkTile);
-      it.ctx = r->ctx_len[t.req];
-      it.q0 = t.q0;
-      it.part = t.pieces > 1 ? part + ((int64_t)h * t.pieces + s) * t.rows : -1;
-      it.pad = 0;
-      P.items.push_back(it);
-    }
   }
   // work-groups b and b + cus of the tall kernel share a compute unit at first:
   // the longest with the shortest of the first two rounds
-  if (P.tall && n_items > cus)
-    std::reverse(P.items.begin() + cus, P.items.begin() + std::min<int64_t>(n_items, 2 * cus));
+  if (P.tall && n_items * Hkv > cus) {
+    P.turn0 = cus;
+    P.turn1 = (int32_t)std::min<int64_t>(n_items * Hkv, 2 * (int64_t)cus);
+  }
 
   P.off_joins = align_up(sizeof(ChunkItem) * P.items.size());
   P.plan_bytes = P.off_joins + align_up(sizeof(ChunkJoin) * P.joins.size());
@@ -244,8 +232,8 @@ spec_status_t plan_chunk(const spec_chunks_t* r, const spec_cache_t* c, const sp
 }
 
 // The row movers' view of `layers` layers from `layer` on, `rows` token rows
-// written in each.  Heads that follow
-// each other without a gap on both sides (apart: their strides) move as one.
+// written in each.  one_run: the heads follow each other without a gap on both
+// sides, and move as one.
 sv::CachePools pools(const spec_cache_t* c, int layer, int layers, bool one_run, int64_t rows) {
   const int64_t eb = elem_bytes(c->dtype);
   sv::CachePools p;
@@ -333,7 +321,10 @@ spec_status_t spec_chunk_attn(const spec_chunks_t* chunks, const spec_cache_t* c
     p.n_joins = (int32_t)P.joins.size();
     p.page_tokens = cache->page_tokens;
     p.num_pages = cache->num_pages;
+    p.turn0 = P.turn0;
+    p.turn1 = P.turn1;
     p.Hq = args->num_q_heads;
+    p.Hkv = cache->num_kv_heads;
     p.G = args->num_q_heads / cache->num_kv_heads;
     p.D = cache->head_dim;
     p.out_f32 = args->out_dtype == SPEC_F32;
@@ -473,6 +464,7 @@ spec_status_t spec_cache_copy_pages(const spec_cache_t* cache, const spec_page_c
     spec_status_t st = check_cache(cache, false);
     if (st != SPEC_OK) return st;
     if (num_copies < 0 || (num_copies > 0 && !copies)) return SPEC_ERR_INVALID_ARG;
+    if (num_copies > cache->num_pages) return SPEC_ERR_INVALID_ARG;      // some page is written twice
     std::unordered_set<int32_t> written;
     written.reserve(num_copies);
     for (int i = 0; i < num_copies; ++i) {

@@ -392,6 +392,27 @@ __device__ __forceinline__ void one_by_one(const Fetch& f, Rows<D>& S, int kb, i
   S.l = half ? 0.f : l;
 }
 
+// Work-group b's work: keys [kb, ke) of one request and KV head, `rows` query
+// rows from r0 on, the partial rows from `part` on (-1: it writes out itself).
+struct Piece {
+  int32_t req, kvh, r0, rows, kb, ke, ctx, q0;
+  int64_t part;
+};
+// A row tile's work-groups are next to each other, those of a piece (HEADS: the
+// XCDs read different heads) or of a head (a head's keys stream past in order).
+template <bool HEADS>
+__device__ __forceinline__ Piece piece_of(const ChunkParams& p, int b) {
+  if (b >= p.turn0 && b < p.turn1) b = p.turn0 + p.turn1 - 1 - b;
+  const int i = b / p.Hkv;
+  const ChunkItem x = p.items[i];                        // some piece of the tile
+  const int g = b - (i - x.piece) * p.Hkv;               // the work-group's place among the tile's
+  const int h = HEADS ? b - i * p.Hkv : g / x.pieces;
+  const int s = HEADS ? x.piece : g - h * x.pieces;
+  const int kb = s * x.len;
+  return {x.req, h, x.r0, x.rows, kb, min(x.keys, kb + x.len), x.ctx, x.q0,
+          x.pieces > 1 ? x.part + ((int64_t)h * x.pieces + s) * x.rows : -1};
+}
+
 template <int D, int NW, int TK, int NS, int PARTS>
 __global__ __launch_bounds__(64 * NW, 2) void chunk_attn(ChunkParams p) {
 #if defined(__HIP_DEVICE_COMPILE__)   // the host pass needs the signature only
@@ -404,7 +425,7 @@ __global__ __launch_bounds__(64 * NW, 2) void chunk_attn(ChunkParams p) {
   const int lane = threadIdx.x & 63;
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int l32 = lane & 31, half = lane >> 5;
-  const ChunkItem it = p.items[blockIdx.x];
+  const Piece it = piece_of<NW != 1>(p, blockIdx.x);
   const int ntiles = (it.ke - it.kb + TK - 1) / TK;
 
   Fetch f;
@@ -558,13 +579,15 @@ struct Joined {
 template <int D, bool F32, bool ROWS>
 __global__ __launch_bounds__(256) void chunk_join(ChunkParams p) {
   constexpr int LPR = D / 4, NG = 256 / LPR;
-  const ChunkJoin jn = p.joins[blockIdx.x];
+  const int tile = (int)blockIdx.x / p.Hkv, kvh = (int)blockIdx.x - tile * p.Hkv;
+  const ChunkJoin jn = p.joins[tile];
+  const int64_t part = jn.part + (int64_t)kvh * jn.pieces * jn.rows;
   const int g = threadIdx.x / LPR, x = threadIdx.x % LPR;
   const int rr = ROWS ? (int)blockIdx.y * NG + g : (int)blockIdx.y;
   if (!ROWS && rr >= jn.rows) return;
   Joined j = {f32x4{0.f, 0.f, 0.f, 0.f}, -INFINITY, 0.f};
-  const float2* ml = p.part_ml + jn.part + min(rr, jn.rows - 1);
-  const float* po = p.part_o + (jn.part + min(rr, jn.rows - 1)) * D + 4 * x;
+  const float2* ml = p.part_ml + part + min(rr, jn.rows - 1);
+  const float* po = p.part_o + (part + min(rr, jn.rows - 1)) * D + 4 * x;
 #pragma unroll 4
   for (int s = ROWS ? 0 : g; s < jn.pieces; s += ROWS ? 1 : NG) {
     const float2 y = ml[(int64_t)s * jn.rows];
@@ -580,7 +603,7 @@ __global__ __launch_bounds__(256) void chunk_join(ChunkParams p) {
     return;
   }
   const int r = jn.r0 + rr, tok = r / p.G;
-  const int64_t at = ((jn.q0 + (int64_t)tok) * p.Hq + jn.kvh * p.G + (r - tok * p.G)) * D + 4 * x;
+  const int64_t at = ((jn.q0 + (int64_t)tok) * p.Hq + kvh * p.G + (r - tok * p.G)) * D + 4 * x;
   const f32x4 y = j.o * (1.f / j.l);
   if constexpr (F32) *reinterpret_cast<f32x4*>(static_cast<float*>(p.out) + at) = y;
   else *reinterpret_cast<u32x2*>(static_cast<uint16_t*>(p.out) + at) = __builtin_bit_cast(u32x2, __builtin_convertvector(y, bf16x4));
@@ -588,15 +611,15 @@ __global__ __launch_bounds__(256) void chunk_join(ChunkParams p) {
 
 template <int D, int PARTS>
 static hipError_t launch_d(const ChunkParams& p, hipStream_t s) {
-  if (p.tall) chunk_attn<D, 4, 64, 2, PARTS><<<dim3(p.n_items), dim3(256), 0, s>>>(p);
-  else chunk_attn<D, 1, 32, 2, PARTS><<<dim3(p.n_items), dim3(64), 0, s>>>(p);
+  if (p.tall) chunk_attn<D, 4, 64, 2, PARTS><<<dim3(p.n_items * p.Hkv), dim3(256), 0, s>>>(p);
+  else chunk_attn<D, 1, 32, 2, PARTS><<<dim3(p.n_items * p.Hkv), dim3(64), 0, s>>>(p);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.n_joins == 0) return e;
   constexpr int NG = 1024 / D;
   if (p.join_pieces <= 2 * NG)
-    chunk_join<D, PARTS != 1, true><<<dim3(p.n_joins, (p.join_rows + NG - 1) / NG), dim3(256), 0, s>>>(p);
+    chunk_join<D, PARTS != 1, true><<<dim3(p.n_joins * p.Hkv, (p.join_rows + NG - 1) / NG), dim3(256), 0, s>>>(p);
   else
-    chunk_join<D, PARTS != 1, false><<<dim3(p.n_joins, p.join_rows), dim3(256), 0, s>>>(p);
+    chunk_join<D, PARTS != 1, false><<<dim3(p.n_joins * p.Hkv, p.join_rows), dim3(256), 0, s>>>(p);
   return hipGetLastError();
 }
 

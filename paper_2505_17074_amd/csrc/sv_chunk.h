@@ -7,31 +7,32 @@
 
 namespace sv {
 
-// One work item of the chunk attention: the keys [kb, ke) of one (request, KV
-// head) for `rows` query rows from row r0 on.  Query row r of a request and KV
-// head is new token r / G under the group's query head r % G, so that a run of
-// rows sees a run of key ranges.
+// One piece of the chunk attention's work, the same for every KV head: keys
+// [piece * len, (piece + 1) * len) of the first `keys` keys of a request, for
+// `rows` query rows from row r0 on.  Query row r of a request and KV head is new
+// token r / G under the group's query head r % G, so that a run of rows sees a
+// run of key ranges.  A row tile's pieces follow each other in the list.
 struct ChunkItem {
   int32_t req;      // block table row
-  int32_t kvh;
   int32_t r0, rows;
-  int32_t kb, ke;   // kb a multiple of 64
+  int32_t keys;
+  int32_t len;      // a multiple of kChunkTile
+  int32_t piece, pieces;
   int32_t ctx;
+  int64_t part;     // the tile's first partial row (pieces > 1): head h's piece s from (h pieces + s) rows on
   int32_t q0;       // the request's first row of q and out
-  int64_t part;     // first partial row of this piece, -1: the item writes out itself
-  int64_t pad;
+  int32_t pad;
 };
 static_assert(sizeof(ChunkItem) == 48, "ChunkItem is read as 16-byte units");
 
-// One query-row tile whose key range was cut: its pieces' partial rows follow
-// each other, `rows` apart.
+// One query-row tile whose key range was cut: a head's pieces' partial rows
+// follow each other, `rows` apart, the heads `pieces * rows` apart.
 struct ChunkJoin {
-  int32_t kvh;
   int32_t r0, rows;
   int32_t pieces;
-  int64_t part;
   int32_t q0;
-  int32_t pad;
+  int64_t part;
+  int64_t pad;
 };
 static_assert(sizeof(ChunkJoin) == 32, "ChunkJoin is read as 16-byte units");
 
@@ -48,9 +49,10 @@ struct ChunkParams {
   int64_t q_st, q_sh;
   int64_t kv_st, kv_sh;
   int64_t bt_stride;
-  int32_t n_items, n_joins;
+  int32_t n_items, n_joins;            // of one KV head
+  int32_t turn0, turn1;                // work-groups [turn0, turn1) take their places from the end
   int32_t page_tokens, num_pages;
-  int32_t Hq, G, D;
+  int32_t Hq, Hkv, G, D;
   int32_t out_f32;
   int32_t tall;         // items of up to kChunkTallRows rows on four waves, else kChunkLowRows on one
   int32_t join_rows;    // rows of the tallest joined tile
