@@ -16,6 +16,7 @@ from .batch import StagingRing
 
 _DTYPE = {torch.bfloat16: B.SPEC_BF16, torch.float32: B.SPEC_F32}
 _HERE = contextlib.nullcontext()
+_kept = []                             # what objects that ended inside a graph capture held
 
 
 def _stride(t: torch.Tensor, dim: int, otherwise: int) -> int:
@@ -23,6 +24,11 @@ def _stride(t: torch.Tensor, dim: int, otherwise: int) -> int:
     will do, and torch may have any."""
     return t.stride(dim) if t.shape[dim] > 1 else otherwise
 
+
+def _alike(a: torch.Tensor, b: torch.Tensor) -> bool:
+    """The same shape, and the same strides where these matter."""
+    return a.shape == b.shape and (a.stride() == b.stride() or all(
+        x == y for n, x, y in zip(a.shape, a.stride(), b.stride()) if n > 1))
 
 
 def _current_raw_stream(index: int) -> int:
@@ -100,14 +106,14 @@ class PagedCache:
     """Page pools k, v [layers, num_pages, page_tokens, Hkv, d] (bf16 or fp32,
     last dimension contiguous, a page's rows apart by one stride), and the
     block table int32 [requests, block_stride] on the same device (it may be
-    replaced: `table`)."""
+    replaced: `table`).  An object is used by one thread at a time."""
 
     def __init__(self, k: torch.Tensor, v: torch.Tensor, table: Optional[torch.Tensor] = None):
-        if k.dim() != 5 or k.shape != v.shape or k.dtype != v.dtype or k.device != v.device or k.stride() != v.stride():
+        if k.dim() != 5 or k.dtype != v.dtype or k.device != v.device or not _alike(k, v):
             raise ValueError("k and v are [layers, num_pages, page_tokens, Hkv, d] of the same type, strides and device")
         if k.dtype not in _DTYPE:
             raise ValueError("bf16 or fp32 pools")
-        if k.stride(4) != 1 or (k.shape[1] > 1 and k.stride(1) != k.shape[2] * k.stride(2)):
+        if _stride(k, 4, 1) != 1 or (k.shape[1] > 1 and k.stride(1) != k.shape[2] * k.stride(2)):
             raise ValueError("rows are contiguous and pages follow each other")
         self.k, self.v, self.device, self.dtype = k, v, k.device, k.dtype
         self._index = k.device.index
@@ -132,7 +138,7 @@ class PagedCache:
     @table.setter
     def table(self, t: Optional[torch.Tensor]) -> None:
         if t is not None:
-            if t.dim() != 2 or t.dtype != torch.int32 or t.device != self.device or t.stride(1) != 1:
+            if t.dim() != 2 or t.dtype != torch.int32 or t.device != self.device or _stride(t, 1, 1) != 1:
                 raise ValueError("the block table is int32 [requests, block_stride] on the pools' device")
             if t.shape[0] > 1 and t.stride(0) < t.shape[1]:
                 raise ValueError("the block table's rows overlap")
@@ -144,6 +150,8 @@ class PagedCache:
 
     def _enter(self):
         """The pools' device made current for a call (a context)."""
+        if self._index is None:
+            raise ValueError("the pools are not in device memory")
         return _HERE if torch.cuda.current_device() == self._index else torch.cuda.device(self._index)
 
     def _stream(self, stream) -> int:
@@ -158,7 +166,7 @@ class PagedCache:
         """Rows k_new, v_new [layers, rows, Hkv, d] (or [rows, Hkv, d]: one layer)
         to the ends of the requests, in the cache's layers from `layer` on."""
         shape, st = k_new.shape, k_new.stride()
-        if shape != v_new.shape or st != v_new.stride() or len(shape) not in (3, 4) or \
+        if not _alike(k_new, v_new) or len(shape) not in (3, 4) or \
                 shape[-2:] != self._head or shape[-3] < chunks.rows or (st[-1] != 1 and shape[-1] > 1):
             raise ValueError("k_new and v_new are [layers, rows, Hkv, d], a row for every new token")
         if k_new.dtype != self.dtype or v_new.dtype != self.dtype or k_new.device != self.device or \
@@ -198,9 +206,10 @@ class PagedCache:
 
 class ChunkAttention(StagingRing):
     """Runs spec_chunk_attn on a PagedCache.  Owns a device workspace, which
-    grows with the batches, and `ring` pinned staging buffers (StagingRing).  A graph is captured from B.spec_chunk_attn with a
-    workspace and staging of its own, not from here: a replay reads the staging
-    it was captured with, and the ring reuses its slots."""
+    grows with the batches, and `ring` pinned staging buffers (StagingRing).  A
+    graph is captured from B.spec_chunk_attn with a workspace and staging of its
+    own, not from here: a replay reads the staging it was captured with, and the
+    ring reuses its slots.  An object is used by one thread at a time."""
 
     def __init__(self, cache: PagedCache, num_q_heads: int, scale: float = 0.0, ring: int = 32, event_every: int = 8):
         if event_every < 1 or ring < event_every:
@@ -211,8 +220,22 @@ class ChunkAttention(StagingRing):
         self._args_ref = C.byref(a)
         self._head = torch.Size((num_q_heads, cache.c.head_dim))
         self.ws_bytes = self.staging_bytes = 0
-        self.ws_ptr = None
+        self.ws_ptr = self._ws = self._pinned = None
         self._ring([None] * ring, event_every)
+
+    def __del__(self):
+        # the last call may still read the staging and write the workspace, and
+        # both go back to torch's allocators, which know of neither
+        last = getattr(self, "_last_stream", None)
+        if last is None:
+            return
+        try:
+            if torch.cuda.is_current_stream_capturing():     # no synchronization in a capture
+                _kept.append((self._ws, self._pinned))
+            else:
+                last.synchronize()
+        except Exception:                     # the interpreter or the device is going away
+            pass
 
     def _grow(self, chunks, stream) -> None:
         st, dev, host = B.spec_chunk_workspace_bytes(chunks, self.cache.c, self.args)
@@ -221,7 +244,8 @@ class ChunkAttention(StagingRing):
             if self.ws_bytes:
                 stream.synchronize()          # earlier calls' workspace goes back to the allocator
             self.ws_bytes = dev + dev // 4
-            self._ws = torch.empty(self.ws_bytes + 256, dtype=torch.uint8, device=self.cache.device)
+            with torch.cuda.stream(stream):       # a block that no other stream's pending work has
+                self._ws = torch.empty(self.ws_bytes + 256, dtype=torch.uint8, device=self.cache.device)
             self.ws_ptr = (self._ws.data_ptr() + 255) // 256 * 256
         if host > self.staging_bytes:
             if self.staging_bytes:

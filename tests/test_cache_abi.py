@@ -216,3 +216,34 @@ def test_python_refusals():
             att.run(chunks, qq, oo)
     with pytest.raises(ValueError):
         B.make_chunks([1, 2], [1])
+
+
+def test_pools_in_host_memory():
+    """Every call on pools that no GPU holds is refused before the library sees it."""
+    k = torch.zeros((1, 4, 32, 2, 64), dtype=torch.bfloat16)
+    c = PagedCache(k, k.clone(), torch.zeros((2, 2), dtype=torch.int32))
+    chunks, rows = B.make_chunks([0, 0], [3, 2]), torch.zeros((5, 2, 64), dtype=torch.bfloat16)
+    q, o = torch.zeros((5, 4, 64), dtype=torch.bfloat16), torch.zeros((5, 4, 64))
+    for call in (lambda: c.append(chunks, rows, rows), lambda: c.copy_pages([(0, 1, 3)]),
+                 lambda: c.commit(B.make_requests([0, 0], None, [-1, 0]), torch.zeros(2, dtype=torch.int32)),
+                 lambda: ChunkAttention(c, 4).run(chunks, q, o)):
+        with pytest.raises(ValueError, match="device memory"):
+            call()
+
+
+def test_strides_of_single_entries():
+    """A dimension of one entry may have any stride, and K and V different ones."""
+    k = torch.zeros((4, 32, 2, 64)).as_strided((1, 4, 32, 2, 64), (7, 4096, 128, 64, 1))
+    v = torch.zeros((1, 4, 32, 2, 64))
+    c = PagedCache(k, v, torch.zeros((2, 5), dtype=torch.int32)[:, :1])
+    assert (c.c.kv_stride_tok, c.c.kv_stride_head, c.c.block_stride) == (128, 64, 5)
+    c.table = torch.zeros(2, dtype=torch.int32).as_strided((2, 1), (1, 3))
+    with pytest.raises(ValueError, match="device memory"):             # and not their strides
+        c.append(B.make_chunks([3], [1]), torch.zeros((1, 2, 64)), torch.zeros((1, 9, 64))[:, :2])
+    with pytest.raises(ValueError, match="a row for every new token"):
+        c.append(B.make_chunks([3], [2]), torch.zeros((2, 2, 64)), torch.zeros((2, 9, 64))[:, :2])
+
+
+def test_more_copies_than_pages():
+    """Refused before anything as long as the list is read."""
+    assert B.spec_cache_copy_pages(_cache(), np.zeros(3, np.int32).ctypes.data, 2**31 - 1, 0) == INV

@@ -289,3 +289,30 @@ def test_one_object_for_growing_batches(gpu_lib):
         want.append(reference(sub, q))
     for (_, _, out), (ref, bound) in zip(outs, want):
         check_close(out, ref, bound)
+
+
+def test_objects_that_end_with_work_pending(gpu_lib):
+    """Staging and workspace stay until the call that uses them has ended,
+    whoever takes their memory next."""
+    print("[case] chunk objects ending early", flush=True)
+    p = Paged([900, 3000, 5, 77], [1, 1, 130, 64], 2, 128, seed=31).write()
+    q = queries(196, 8, 128, seed=31).cuda()
+    ref, out = (torch.empty((196, 8, 128), dtype=BF16, device="cuda") for _ in range(2))
+    ChunkAttention(p.cache, 8).run(p.chunks(), q, ref)
+    side = torch.cuda.Stream()
+    a = torch.randn((4096, 4096), device="cuda")
+    torch.cuda.synchronize()
+    for _ in range(4):
+        out.zero_()
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            for _ in range(8):
+                torch.mm(a, a)                            # the call below waits behind these
+        att = ChunkAttention(p.cache, 8)
+        att.run(p.chunks(), q, out, stream=side)
+        sizes = att._pinned.numel(), att._ws.numel()
+        del att
+        torch.empty(sizes[0], dtype=torch.uint8, pin_memory=True).fill_(0)
+        torch.empty(sizes[1], dtype=torch.uint8, device="cuda").fill_(255)
+        torch.cuda.synchronize()
+        assert torch.equal(out, ref)
