@@ -101,7 +101,7 @@ struct ChunkPlan {
   int32_t join_rows = 0, join_pieces = 0, turn0 = 0, turn1 = 0;
   int64_t parts = 0;
   size_t off_joins = 0, plan_bytes = 0;
-  size_t off_part_o = 0, off_part_ml = 0, device_bytes = 0;
+  size_t off_part = 0, device_bytes = 0;
 };
 
 spec_status_t plan_chunk(const spec_chunks_t* r, const spec_cache_t* c, const spec_chunk_attn_args_t* a,
@@ -225,9 +225,8 @@ spec_status_t plan_chunk(const spec_chunks_t* r, const spec_cache_t* c, const sp
 
   P.off_joins = align_up(sizeof(ChunkItem) * P.items.size());
   P.plan_bytes = P.off_joins + align_up(sizeof(ChunkJoin) * P.joins.size());
-  P.off_part_o = P.plan_bytes;
-  P.off_part_ml = align_up(P.off_part_o + sizeof(float) * (size_t)P.parts * c->head_dim);
-  P.device_bytes = align_up(P.off_part_ml + sizeof(float2) * (size_t)P.parts);
+  P.off_part = align_up(P.plan_bytes + sizeof(float2) * (size_t)P.parts);
+  P.device_bytes = align_up(P.off_part + sizeof(float) * (size_t)P.parts * c->head_dim);
   return SPEC_OK;
 }
 
@@ -307,33 +306,32 @@ spec_status_t spec_chunk_attn(const spec_chunks_t* chunks, const spec_cache_t* c
     p.k = static_cast<const char*>(cache->k) + lb;
     p.v = static_cast<const char*>(cache->v) + lb;
     p.out = args->out;
-    p.part_o = reinterpret_cast<float*>(d + P.off_part_o);
-    p.part_ml = reinterpret_cast<float2*>(d + P.off_part_ml);
+    p.part = reinterpret_cast<float*>(d + P.off_part);
     p.items = reinterpret_cast<const ChunkItem*>(plan);
-    p.joins = reinterpret_cast<const ChunkJoin*>(plan + P.off_joins);
     p.bt = cache->block_table;
     p.q_st = args->q_stride_tok;
     p.q_sh = args->q_stride_head;
-    p.kv_st = cache->kv_stride_tok;
-    p.kv_sh = cache->kv_stride_head;
+    p.kv_st = (int32_t)cache->kv_stride_tok;
+    p.kv_sh = (int32_t)cache->kv_stride_head;
     p.bt_stride = cache->block_stride;
-    p.n_items = (int32_t)P.items.size();
-    p.n_joins = (int32_t)P.joins.size();
     p.page_tokens = cache->page_tokens;
     p.num_pages = cache->num_pages;
-    p.turn0 = P.turn0;
-    p.turn1 = P.turn1;
-    p.Hq = args->num_q_heads;
     p.Hkv = cache->num_kv_heads;
     p.G = args->num_q_heads / cache->num_kv_heads;
-    p.D = cache->head_dim;
-    p.out_f32 = args->out_dtype == SPEC_F32;
-    p.tall = P.tall;
-    p.join_rows = P.join_rows;
-    p.join_pieces = P.join_pieces;
+    p.turn0 = P.turn0;
+    p.turn1 = P.turn1;
     const float scale = args->scale > 0.f ? args->scale : 1.f / std::sqrt((float)cache->head_dim);
     p.scale_log2 = scale * 1.4426950408889634f;
-    return sv::launch_chunk(p, s) == hipSuccess ? SPEC_OK : SPEC_ERR_HIP;
+    sv::JoinParams j{};
+    j.out = p.out;
+    j.part = p.part;
+    j.Hkv = p.Hkv;
+    j.G = p.G;
+    if (P.joins.size() == 1) j.one = P.joins[0];
+    else j.joins = reinterpret_cast<const ChunkJoin*>(plan + P.off_joins);
+    const sv::ChunkLaunch l = {(int32_t)P.items.size(), (int32_t)P.joins.size(), cache->head_dim,
+                               args->out_dtype == SPEC_F32, P.tall, P.join_rows, P.join_pieces};
+    return sv::launch_chunk(p, j, l, s) == hipSuccess ? SPEC_OK : SPEC_ERR_HIP;
   });
 }
 

@@ -432,7 +432,7 @@ __global__ __launch_bounds__(64 * NW, 2) void chunk_attn(ChunkParams p) {
   f.k = static_cast<const char*>(p.k) + (int64_t)it.kvh * p.kv_sh * 2;
   f.v = static_cast<const char*>(p.v) + (int64_t)it.kvh * p.kv_sh * 2;
   f.pages = p.bt + (int64_t)it.req * p.bt_stride;
-  f.row_bytes = (int)(p.kv_st * 2);
+  f.row_bytes = p.kv_st * 2;
   f.page_tokens = p.page_tokens;
   f.page_bytes = (int64_t)p.page_tokens * f.row_bytes;
   f.num_pages = p.num_pages;
@@ -529,7 +529,7 @@ __global__ __launch_bounds__(64 * NW, 2) void chunk_attn(ChunkParams p) {
   const int r = it.r0 + wr0 + l32;
   if (it.part < 0) {
     const int j = r / p.G;
-    const int64_t row = (it.q0 + (int64_t)j) * p.Hq + it.kvh * p.G + (r - j * p.G);
+    const int64_t row = (it.q0 + (int64_t)j) * (p.Hkv * p.G) + it.kvh * p.G + (r - j * p.G);
     const float inv = 1.f / l;
 #pragma unroll
     for (int eb = 0; eb < ET; ++eb)
@@ -550,9 +550,9 @@ __global__ __launch_bounds__(64 * NW, 2) void chunk_attn(ChunkParams p) {
     for (int eb = 0; eb < ET; ++eb)
 #pragma unroll
       for (int i = 0; i < 16; i += 4)
-        *reinterpret_cast<f32x4*>(p.part_o + row * D + 32 * eb + 2 * i + 4 * half) =
+        *reinterpret_cast<f32x4*>(p.part + row * D + 32 * eb + 2 * i + 4 * half) =
             f32x4{S.o[eb][i], S.o[eb][i + 1], S.o[eb][i + 2], S.o[eb][i + 3]};
-    if (half == 0) p.part_ml[row] = make_float2(S.m, l);
+    if (half == 0) reinterpret_cast<float2*>(p.part)[-1 - row] = make_float2(S.m, l);
   }
 #endif
 }
@@ -577,20 +577,21 @@ struct Joined {
 // kernel above, measured the same for one token over 1000 rows and 3 % slower
 // for 64 of them: its stores and loads past the L2s cost what the launch does.)
 template <int D, bool F32, bool ROWS>
-__global__ __launch_bounds__(256) void chunk_join(ChunkParams p) {
+__global__ __launch_bounds__(256) void chunk_join(JoinParams p) {
   constexpr int LPR = D / 4, NG = 256 / LPR;
   const int tile = (int)blockIdx.x / p.Hkv, kvh = (int)blockIdx.x - tile * p.Hkv;
-  const ChunkJoin jn = p.joins[tile];
+  const ChunkJoin jn = p.joins ? p.joins[tile] : p.one;
   const int64_t part = jn.part + (int64_t)kvh * jn.pieces * jn.rows;
   const int g = threadIdx.x / LPR, x = threadIdx.x % LPR;
   const int rr = ROWS ? (int)blockIdx.y * NG + g : (int)blockIdx.y;
   if (!ROWS && rr >= jn.rows) return;
   Joined j = {f32x4{0.f, 0.f, 0.f, 0.f}, -INFINITY, 0.f};
-  const float2* ml = p.part_ml + part + min(rr, jn.rows - 1);
-  const float* po = p.part_o + (part + min(rr, jn.rows - 1)) * D + 4 * x;
+  const int64_t first = part + min(rr, jn.rows - 1);
+  const float2* ml = reinterpret_cast<const float2*>(p.part) - 1 - first;
+  const float* po = p.part + first * D + 4 * x;
 #pragma unroll 4
   for (int s = ROWS ? 0 : g; s < jn.pieces; s += ROWS ? 1 : NG) {
-    const float2 y = ml[(int64_t)s * jn.rows];
+    const float2 y = ml[-(int64_t)s * jn.rows];
     j.add(y.x, y.y, *reinterpret_cast<const f32x4*>(po + (int64_t)s * jn.rows * D));
   }
   if constexpr (!ROWS) {
@@ -603,29 +604,29 @@ __global__ __launch_bounds__(256) void chunk_join(ChunkParams p) {
     return;
   }
   const int r = jn.r0 + rr, tok = r / p.G;
-  const int64_t at = ((jn.q0 + (int64_t)tok) * p.Hq + kvh * p.G + (r - tok * p.G)) * D + 4 * x;
+  const int64_t at = ((jn.q0 + (int64_t)tok) * (p.Hkv * p.G) + kvh * p.G + (r - tok * p.G)) * D + 4 * x;
   const f32x4 y = j.o * (1.f / j.l);
   if constexpr (F32) *reinterpret_cast<f32x4*>(static_cast<float*>(p.out) + at) = y;
   else *reinterpret_cast<u32x2*>(static_cast<uint16_t*>(p.out) + at) = __builtin_bit_cast(u32x2, __builtin_convertvector(y, bf16x4));
 }
 
 template <int D, int PARTS>
-static hipError_t launch_d(const ChunkParams& p, hipStream_t s) {
-  if (p.tall) chunk_attn<D, 4, 64, 2, PARTS><<<dim3(p.n_items * p.Hkv), dim3(256), 0, s>>>(p);
-  else chunk_attn<D, 1, 32, 2, PARTS><<<dim3(p.n_items * p.Hkv), dim3(64), 0, s>>>(p);
+static hipError_t launch_d(const ChunkParams& p, const JoinParams& j, const ChunkLaunch& l, hipStream_t s) {
+  if (l.tall) chunk_attn<D, 4, 64, 2, PARTS><<<dim3(l.n_items * p.Hkv), dim3(256), 0, s>>>(p);
+  else chunk_attn<D, 1, 32, 2, PARTS><<<dim3(l.n_items * p.Hkv), dim3(64), 0, s>>>(p);
   hipError_t e = hipGetLastError();
-  if (e != hipSuccess || p.n_joins == 0) return e;
+  if (e != hipSuccess || l.n_joins == 0) return e;
   constexpr int NG = 1024 / D;
-  if (p.join_pieces <= 2 * NG)
-    chunk_join<D, PARTS != 1, true><<<dim3(p.n_joins * p.Hkv, (p.join_rows + NG - 1) / NG), dim3(256), 0, s>>>(p);
+  if (l.join_pieces <= 2 * NG)
+    chunk_join<D, PARTS != 1, true><<<dim3(l.n_joins * p.Hkv, (l.join_rows + NG - 1) / NG), dim3(256), 0, s>>>(j);
   else
-    chunk_join<D, PARTS != 1, false><<<dim3(p.n_joins * p.Hkv, p.join_rows), dim3(256), 0, s>>>(p);
+    chunk_join<D, PARTS != 1, false><<<dim3(l.n_joins * p.Hkv, l.join_rows), dim3(256), 0, s>>>(j);
   return hipGetLastError();
 }
 
-hipError_t launch_chunk(const ChunkParams& p, hipStream_t s) {
-  if (p.D == 128) return p.out_f32 ? launch_d<128, 3>(p, s) : launch_d<128, 1>(p, s);
-  return p.out_f32 ? launch_d<64, 3>(p, s) : launch_d<64, 1>(p, s);
+hipError_t launch_chunk(const ChunkParams& p, const JoinParams& j, const ChunkLaunch& l, hipStream_t s) {
+  if (l.D == 128) return l.out_f32 ? launch_d<128, 3>(p, j, l, s) : launch_d<128, 1>(p, j, l, s);
+  return l.out_f32 ? launch_d<64, 3>(p, j, l, s) : launch_d<64, 1>(p, j, l, s);
 }
 
 }  // namespace sv

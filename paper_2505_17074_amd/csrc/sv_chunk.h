@@ -36,35 +36,53 @@ struct ChunkJoin {
 };
 static_assert(sizeof(ChunkJoin) == 32, "ChunkJoin is read as 16-byte units");
 
+// Kernel arguments of 128 bytes and more cost the host 1.1 us a launch (2.8 us
+// with less, 3.9 from there to 2 KB, 4.1 with 4 KB), which is what the smallest
+// calls wait for: the arguments end below that where they can.
+constexpr size_t kSmallArgs = 127;
+
 struct ChunkParams {
   const void* q;
   const void* k;        // the layer's pools
   const void* v;
   void* out;
-  float* part_o;        // [partial rows, d], not normalised
-  float2* part_ml;      // running maximum (log2 units) and sum
+  float* part;          // partial row i, not normalised, at part + i d; its running maximum (log2
+                        // units) and sum at (float2*)part - 1 - i
   const ChunkItem* items;
-  const ChunkJoin* joins;
   const int32_t* bt;
   int64_t q_st, q_sh;
-  int64_t kv_st, kv_sh;
-  int64_t bt_stride;
-  int32_t n_items, n_joins;            // of one KV head
-  int32_t turn0, turn1;                // work-groups [turn0, turn1) take their places from the end
+  int32_t kv_st, kv_sh;
+  int32_t bt_stride;
   int32_t page_tokens, num_pages;
-  int32_t Hq, Hkv, G, D;
-  int32_t out_f32;
-  int32_t tall;         // items of up to kChunkTallRows rows on four waves, else kChunkLowRows on one
+  int32_t Hkv, G;
+  int32_t turn0, turn1; // work-groups [turn0, turn1) take their places from the end
+  float scale_log2;
+};
+
+struct JoinParams {
+  void* out;
+  const float* part;
+  const ChunkJoin* joins;              // null: `one` is all
+  int32_t Hkv, G;
+  ChunkJoin one;
+};
+static_assert(sizeof(ChunkParams) <= kSmallArgs && sizeof(JoinParams) <= kSmallArgs, "small arguments");
+
+// What the launches go by.
+struct ChunkLaunch {
+  int32_t n_items, n_joins;            // of one KV head
+  int32_t D;
+  bool out_f32;
+  bool tall;            // items of up to kChunkTallRows rows on four waves, else kChunkLowRows on one
   int32_t join_rows;    // rows of the tallest joined tile
   int32_t join_pieces;  // pieces of the longest
-  float scale_log2;
 };
 
 constexpr int kChunkLowRows = 32;
 constexpr int kChunkTallRows = 128;
 constexpr int kChunkTile = 64;         // pieces are cut at multiples of this many keys
 
-hipError_t launch_chunk(const ChunkParams& p, hipStream_t s);
+hipError_t launch_chunk(const ChunkParams& p, const JoinParams& j, const ChunkLaunch& l, hipStream_t s);
 
 // One kernel argument block of the row movers holds this many requests or
 // pages (kernel arguments end at 4 KB).
