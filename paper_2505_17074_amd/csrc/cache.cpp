@@ -230,10 +230,9 @@ spec_status_t plan_chunk(const spec_chunks_t* r, const spec_cache_t* c, const sp
   return SPEC_OK;
 }
 
-// The row movers' view of `layers` layers from `layer` on, `rows` token rows
-// written in each.  one_run: the heads follow each other without a gap on both
-// sides, and move as one.
-sv::CachePools pools(const spec_cache_t* c, int layer, int layers, bool one_run, int64_t rows) {
+// The row movers' view of the layers from `layer` on.  one_run: the heads
+// follow each other without a gap on both sides, and move as one.
+sv::CachePools pools(const spec_cache_t* c, int layer, bool one_run) {
   const int64_t eb = elem_bytes(c->dtype);
   sv::CachePools p;
   p.layer_bytes = c->num_layers > 1 ? c->layer_stride * eb : 0;
@@ -241,18 +240,19 @@ sv::CachePools pools(const spec_cache_t* c, int layer, int layers, bool one_run,
   p.v = static_cast<char*>(c->v) + layer * p.layer_bytes;
   p.st_bytes = (int32_t)(c->kv_stride_tok * eb);
   p.sh_bytes = (int32_t)(c->kv_stride_head * eb);
-  p.page_bytes = (int64_t)c->page_tokens * p.st_bytes;
   p.num_pages = c->num_pages;
   p.page_tokens = c->page_tokens;
-  p.layers = layers;
   p.heads = c->num_kv_heads;
   p.row_units = (int32_t)(c->head_dim * eb / 16);
   if (one_run) {
     p.row_units *= p.heads;
     p.heads = 1;
   }
-  p.stream = rows * p.heads * p.row_units * 16 * 2 * layers >= sv::kMoveStream;
   return p;
+}
+// `rows` token rows written in each of `layers` layers.
+sv::MoveLaunch move_launch(const sv::CachePools& p, int layers, int64_t rows) {
+  return {layers, rows * p.heads * p.row_units * 16 * 2 * layers >= sv::kMoveStream};
 }
 bool heads_touch(const spec_cache_t* c) { return c->num_kv_heads == 1 || c->kv_stride_head == c->head_dim; }
 
@@ -352,46 +352,53 @@ spec_status_t spec_cache_append(const spec_chunks_t* chunks, const spec_cache_t*
   if (args->num_layers > 1 && (args->new_stride_layer < 1 || args->new_stride_layer % vec)) return SPEC_ERR_INVALID_ARG;
 
   const bool touch = heads_touch(cache) && (cache->num_kv_heads == 1 || args->new_stride_head == cache->head_dim);
-  sv::AppendParams p{};
-  p.c = pools(cache, args->layer, args->num_layers, touch, nq);
+  if (!touch && args->new_stride_head * eb / 16 > INT32_MAX) return SPEC_ERR_UNSUPPORTED;
+  sv::AppendParams<sv::kMoveSegments> p{};
+  p.c = pools(cache, args->layer, touch);
+  const sv::MoveLaunch l = move_launch(p.c, args->num_layers, nq);
   p.k_new = static_cast<const char*>(args->k_new);
   p.v_new = static_cast<const char*>(args->v_new);
   p.new_sl = args->num_layers > 1 ? args->new_stride_layer * eb : 0;
   p.new_st = args->new_stride_tok * eb;
-  p.new_sh = args->new_stride_head * eb;
+  p.new_sh = touch ? 0 : (int32_t)(args->new_stride_head * eb / 16);
   p.bt_stride = cache->block_stride;
   p.bt = cache->block_table;
   // Segments of at most `parts` blocks of 16 rows: as few blocks as keep the
   // batch in one launch's table, so that ragged batches leave few work-groups
-  // without rows.
+  // without rows; a single request's rows are one segment.
   auto blocks = [&](int i) -> int64_t {
     const int64_t lo = chunks->ctx_len[i], n = chunks->new_len[i];
     return n ? (lo + n - 1) / sv::kMoveRows - lo / sv::kMoveRows + 1 : 0;
   };
-  int64_t longest = 0, parts = 1;
-  for (int i = 0; i < chunks->num_requests; ++i) longest = std::max(longest, blocks(i));
+  int64_t longest = 0, all = 0;
+  for (int i = 0; i < chunks->num_requests; ++i) {
+    longest = std::max(longest, blocks(i));
+    all += blocks(i);
+  }
+  int64_t parts = longest == all && all < 1 << 16 ? std::max<int64_t>(longest, 1) : 1;
   for (;; parts *= 2) {
     int64_t segs = 0;
     for (int i = 0; i < chunks->num_requests; ++i) segs += (blocks(i) + parts - 1) / parts;
     if (segs <= sv::kMoveSegments || parts >= longest) break;
   }
-  p.parts = (int32_t)parts;
+  hipStream_t s = static_cast<hipStream_t>(stream);
   int64_t row = 0;
+  int n_seg = 0;
   for (int i = 0; i < chunks->num_requests; ++i) {
     int32_t pos = chunks->ctx_len[i];
     const int32_t end = pos + chunks->new_len[i];
     while (pos < end) {
       const int32_t stop = (int32_t)std::min<int64_t>(end, (pos / sv::kMoveRows + parts) * sv::kMoveRows);
-      p.seg[p.n_seg++] = {i, pos, (int32_t)row, stop - pos};
+      p.seg[n_seg++] = {i, pos, (int32_t)row, stop - pos};
       row += stop - pos;
       pos = stop;
-      if (p.n_seg == sv::kMoveSegments) {
-        if (sv::launch_append(p, static_cast<hipStream_t>(stream)) != hipSuccess) return SPEC_ERR_HIP;
-        p.n_seg = 0;
+      if (n_seg == sv::kMoveSegments) {
+        if (sv::launch_append(p, n_seg, (int)parts, l, s) != hipSuccess) return SPEC_ERR_HIP;
+        n_seg = 0;
       }
     }
   }
-  if (p.n_seg > 0 && sv::launch_append(p, static_cast<hipStream_t>(stream)) != hipSuccess) return SPEC_ERR_HIP;
+  if (n_seg > 0 && sv::launch_append(p, n_seg, (int)parts, l, s) != hipSuccess) return SPEC_ERR_HIP;
   return SPEC_OK;
 }
 
@@ -433,16 +440,17 @@ spec_status_t spec_cache_commit(const spec_requests_t* req, const spec_cache_t* 
   if ((int64_t)cache->num_kv_heads * cache->head_dim * elem_bytes(cache->dtype) / 1024 >= 65535)
     return SPEC_ERR_UNSUPPORTED;
 
-  sv::CommitParams p{};
-  p.c = pools(cache, 0, cache->num_layers, heads_touch(cache), 0);
+  sv::CommitParams<sv::kMoveTrees> p{};
+  p.c = pools(cache, 0, heads_touch(cache));
+  const sv::MoveLaunch l = move_launch(p.c, cache->num_layers, 0);
   p.bt_stride = cache->block_stride;
   p.shared = !per_req;
   o = 0;
   for (int i0 = 0; i0 < req->num_requests; i0 += sv::kMoveTrees) {
-    p.n_req = std::min(sv::kMoveTrees, req->num_requests - i0);
+    const int n_req = std::min(sv::kMoveTrees, req->num_requests - i0);
     p.bt = cache->block_table + (int64_t)i0 * cache->block_stride;
     p.accepted = accepted_node + i0;
-    for (int i = 0; i < p.n_req; ++i) {
+    for (int i = 0; i < n_req; ++i) {
       p.ctx[i] = req->ctx_len[i0 + i];
       if (i > 0 && !per_req) continue;
       const int n = per_req ? req->node_count[i0 + i] : req->tree_nodes;
@@ -451,7 +459,7 @@ spec_status_t spec_cache_commit(const spec_requests_t* req, const spec_cache_t* 
       for (int x = 0; x < n; ++x) p.parent[i][x] = (int8_t)std::max(parent[x], 0);
       o += n;
     }
-    if (sv::launch_commit(p, static_cast<hipStream_t>(stream)) != hipSuccess) return SPEC_ERR_HIP;
+    if (sv::launch_commit(p, n_req, l, static_cast<hipStream_t>(stream)) != hipSuccess) return SPEC_ERR_HIP;
   }
   return SPEC_OK;
 }
@@ -475,16 +483,13 @@ spec_status_t spec_cache_copy_pages(const spec_cache_t* cache, const spec_page_c
       if (written.count(copies[i].src)) return SPEC_ERR_INVALID_ARG;
     int64_t rows = 0;
     for (int i = 0; i < num_copies; ++i) rows += copies[i].tokens;
-    sv::PageCopyParams p{};
-    p.c = pools(cache, 0, cache->num_layers, heads_touch(cache), rows);
-    for (int i0 = 0; i0 < num_copies; i0 += sv::kMoveRequests) {
-      p.n = std::min(sv::kMoveRequests, num_copies - i0);
-      for (int i = 0; i < p.n; ++i) {
-        p.src[i] = copies[i0 + i].src;
-        p.dst[i] = copies[i0 + i].dst;
-        p.tokens[i] = copies[i0 + i].tokens;
-      }
-      if (sv::launch_page_copy(p, static_cast<hipStream_t>(stream)) != hipSuccess) return SPEC_ERR_HIP;
+    sv::PageCopyParams<sv::kMovePages> p{};
+    p.c = pools(cache, 0, heads_touch(cache));
+    const sv::MoveLaunch l = move_launch(p.c, cache->num_layers, rows);
+    for (int i0 = 0; i0 < num_copies; i0 += sv::kMovePages) {
+      const int n = std::min(sv::kMovePages, num_copies - i0);
+      for (int i = 0; i < n; ++i) p.pair[i] = {copies[i0 + i].src, copies[i0 + i].dst, copies[i0 + i].tokens};
+      if (sv::launch_page_copy(p, n, l, static_cast<hipStream_t>(stream)) != hipSuccess) return SPEC_ERR_HIP;
     }
     return SPEC_OK;
   });

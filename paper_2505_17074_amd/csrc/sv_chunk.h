@@ -84,20 +84,21 @@ constexpr int kChunkTile = 64;         // pieces are cut at multiples of this ma
 
 hipError_t launch_chunk(const ChunkParams& p, const JoinParams& j, const ChunkLaunch& l, hipStream_t s);
 
-// One kernel argument block of the row movers holds this many requests or
-// pages (kernel arguments end at 4 KB).
-constexpr int kMoveRequests = 256;
-constexpr int kMoveTrees = 64;
-
+// The row movers' arguments hold what the host knows of a batch: N entries of a
+// table that ends at 4 KB, or as many as stay under kSmallArgs.
 struct CachePools {
   char* k;
   char* v;
-  int64_t layer_bytes, page_bytes;
+  int64_t layer_bytes;
   int32_t st_bytes, sh_bytes;          // token and head strides inside a page
   int32_t num_pages, page_tokens;
-  int32_t layers;                      // moved by this call, from k / v on
   int32_t heads, row_units;            // a head's row in 16-byte units
-  int32_t stream;                      // the call writes kMoveStream bytes or more
+};
+
+// What the launches go by.
+struct MoveLaunch {
+  int32_t layers;                      // moved by this call, from k / v on
+  bool stream;                         // the call writes kMoveStream bytes or more
 };
 // Where the streaming hint on the stores begins to pay (the Infinity Cache
 // holds 256 MB): 276 MB of new rows 94 us with it against 107 without, 126 MB
@@ -110,45 +111,54 @@ struct AppendSegment {
   int32_t req, pos, row, n;
 };
 constexpr int kMoveRows = 16;          // rows of one work-group (divides a page)
-constexpr int kMoveSegments = 224;
+constexpr int kMoveSegments = 240;
 
+template <int N>
 struct AppendParams {
   CachePools c;
   const char* k_new;
   const char* v_new;
-  int64_t new_sl, new_st, new_sh;      // bytes
   const int32_t* bt;
-  int64_t bt_stride;
-  int32_t n_seg;
-  int32_t parts;                       // work-groups of 16 rows a segment, at most
-  AppendSegment seg[kMoveSegments];
+  int64_t new_sl, new_st;              // bytes
+  int32_t new_sh;                      // 16-byte units
+  int32_t bt_stride;
+  AppendSegment seg[N];
 };
 
+constexpr int kMoveTrees = 64;
+
+template <int N>
 struct CommitParams {
   CachePools c;
   const int32_t* bt;
-  int64_t bt_stride;
   const int32_t* accepted;             // of the block's first request
-  int32_t n_req;
+  int32_t bt_stride;
   int32_t shared;                      // one topology: parent[0], nodes[0] for every request
-  int32_t ctx[kMoveTrees];
-  int8_t nodes[kMoveTrees];
-  int8_t parent[kMoveTrees][32];
+  int32_t ctx[N];
+  int8_t parent[N][32];
+  int8_t nodes[N];
 };
 
+struct PagePair {
+  int32_t src, dst, tokens;
+};
+constexpr int kMovePages = 256, kMovePagesSmall = 5;
+
+template <int N>
 struct PageCopyParams {
   CachePools c;
-  int32_t n;
-  int32_t src[kMoveRequests];
-  int32_t dst[kMoveRequests];
-  int32_t tokens[kMoveRequests];
+  PagePair pair[N];
 };
 
-static_assert(sizeof(AppendParams) <= 4096 && sizeof(CommitParams) <= 4096 && sizeof(PageCopyParams) <= 4096,
-              "kernel arguments");
+static_assert(sizeof(AppendParams<kMoveSegments>) <= 4096 && sizeof(CommitParams<kMoveTrees>) <= 4096 &&
+                  sizeof(PageCopyParams<kMovePages>) <= 4096, "kernel arguments");
+static_assert(sizeof(AppendParams<1>) <= kSmallArgs && sizeof(CommitParams<1>) <= kSmallArgs &&
+                  sizeof(PageCopyParams<kMovePagesSmall>) <= kSmallArgs, "small arguments");
 
-hipError_t launch_append(const AppendParams& p, hipStream_t s);
-hipError_t launch_commit(const CommitParams& p, hipStream_t s);
-hipError_t launch_page_copy(const PageCopyParams& p, hipStream_t s);
+// The first n entries of p's table; an append's segments have at most `parts`
+// work-groups of 16 rows.
+hipError_t launch_append(const AppendParams<kMoveSegments>& p, int n, int parts, const MoveLaunch& l, hipStream_t s);
+hipError_t launch_commit(const CommitParams<kMoveTrees>& p, int n, const MoveLaunch& l, hipStream_t s);
+hipError_t launch_page_copy(const PageCopyParams<kMovePages>& p, int n, const MoveLaunch& l, hipStream_t s);
 
 }  // namespace sv
