@@ -280,3 +280,45 @@ def test_fork_and_compaction_keep_every_sequence(gpu_lib):
                 got = k[1, t].reshape(-1, hkv, d)[:len(r), 1, 5].cpu().numpy()
                 assert np.array_equal(got, r), (step, s)
                 assert np.array_equal(-v[0, t].reshape(-1, hkv, d)[:len(r), 0, 63].cpu().numpy(), r)
+
+
+@pytest.mark.parametrize("ctx,new,hkv,d,page,dtype,layers,gap", [
+    (0, 700, 2, 128, 64, BF16, 2, 0), (37, 1, 2, 64, 32, F32, 3, 0), (47, 18, 3, 40, 96, BF16, 1, 8),
+    (1000, 5, 8, 128, 64, BF16, 2, 0), (15, 1, 1, 64, 32, BF16, 1, 0)])
+def test_append_of_one_request(gpu_lib, ctx, new, hkv, d, page, dtype, layers, gap):
+    """Alone, and among others that have nothing new."""
+    print(f"[case] append one request {ctx} {new}", flush=True)
+    p = Paged([3, ctx, 9], [0, new, 0], hkv, d, page, dtype, layers, seed=ctx + new, fill=3.0, gap=gap)
+    p.write(p.ctx)
+    k_new, v_new = p.new_rows()
+    before = p.k.clone(), p.v.clone()
+    p.write()
+    want = p.k.clone(), p.v.clone()
+    table = p.table
+    for chunks, rows in ((p.chunks(), table), (B.make_chunks([ctx], [new]), table[1:2])):
+        p.k.copy_(before[0])
+        p.v.copy_(before[1])
+        p.cache.table = rows
+        p.cache.append(chunks, k_new, v_new)
+        _same(p, *want)
+
+
+@pytest.mark.parametrize("shared", [True, False], ids=["shared", "own"])
+@pytest.mark.parametrize("n,node", [(1, 0), (2, 1), (32, 31), (32, 17), (15, -1)])
+def test_commit_of_one_tree(gpu_lib, n, node, shared):
+    print(f"[case] commit one tree {n} {node}", flush=True)
+    rng = np.random.default_rng(n + node)
+    par = [-1] + [int(rng.integers(max(0, j - 3), j)) for j in range(1, n)]
+    _commit_case([29], [par], [node], 2, 128, 32, BF16, 2, shared)
+
+
+@pytest.mark.parametrize("n", [4, 5, 6])
+def test_copies_of_a_few_pages(gpu_lib, n):
+    print(f"[case] copy {n} pages", flush=True)
+    p = Paged([64 * 20], [0], 2, 128, 64, layers=2, seed=n, spare=0).write()
+    pairs = np.array([[i, 19 - i, 64 - 9 * i] for i in range(n)], np.int32)
+    want = p.k.clone(), p.v.clone()
+    for s, t, rows in pairs.tolist():
+        want[0][:, t, :rows], want[1][:, t, :rows] = p.k[:, s, :rows], p.v[:, s, :rows]
+    p.cache.copy_pages(pairs)
+    _same(p, *want)
