@@ -19,6 +19,8 @@
  *     requests (or pages) than fit runs as several launches in order on the
  *     stream;
  *   - spec_chunk_attn stages its plan as spec_verify_attn does;
+ *   - SPEC_ERR_WORKSPACE is also the answer where the host has no memory left
+ *     for a plan or the bookkeeping;
  *   - nothing reads or writes a page outside the pools: page ids from the
  *     block table (device memory, the caller's contract) are clamped into
  *     [0, num_pages) where rows are read, and rows of a page id outside are
@@ -98,8 +100,9 @@ typedef struct spec_chunks {
  * and infinities included, whether it is a later token's row, a row behind
  * the request's end in its last page, or another request's page.
  * Long key ranges are cut into pieces whose partial outputs a second kernel
- * combines, when the batch alone would leave compute units idle; the cut
- * depends on the lengths and the device alone, and results are deterministic.
+ * joins, where the batch alone would leave compute units idle; the cut depends
+ * on the lengths, the head counts and the device alone, and results are
+ * deterministic.  out overlaps neither q nor the cache.
  */
 typedef struct spec_chunk_attn_args {
   int32_t num_q_heads;
@@ -126,7 +129,8 @@ SPEC_API spec_status_t spec_chunk_attn(const spec_chunks_t* chunks, const spec_c
  * its logical row ctx_len[i] + r, in layers layer .. layer + num_layers - 1.
  *   k_new, v_new  [num_layers][Nq, Hkv, d] in the cache's dtype, strides in
  *                 elements (new_stride_layer ignored for one layer), last dim
- *                 contiguous, 16-byte aligned rows.
+ *                 contiguous, 16-byte aligned rows.  No row of them lies where
+ *                 a row is written.
  * Two requests that name the same page (shared pages of a fork) must not
  * both append to it; spec_pages_resize sees to that.
  */

@@ -65,13 +65,12 @@ spec_status_t check_cache(const spec_cache_t* c, bool table) {
 // Lengths that fit the block table; the number of new rows.
 spec_status_t check_chunks(const spec_chunks_t* r, const spec_cache_t* c, int64_t* rows) {
   if (!r || r->num_requests < 1 || !r->ctx_len || !r->new_len) return SPEC_ERR_INVALID_ARG;
+  const int64_t room = std::min<int64_t>((int64_t)c->block_stride * c->page_tokens, INT32_MAX / 2);
   int64_t nq = 0;
   for (int i = 0; i < r->num_requests; ++i) {
     if (r->ctx_len[i] < 0 || r->new_len[i] < 0) return SPEC_ERR_INVALID_ARG;
     nq += r->new_len[i];
-    const int64_t len = (int64_t)r->ctx_len[i] + r->new_len[i];
-    if (r->new_len[i] > 0 && (len > INT32_MAX / 2 || (len + c->page_tokens - 1) / c->page_tokens > c->block_stride))
-      return SPEC_ERR_INVALID_ARG;
+    if (r->new_len[i] > 0 && (int64_t)r->ctx_len[i] + r->new_len[i] > room) return SPEC_ERR_INVALID_ARG;
   }
   if (nq >= INT32_MAX / 2) return SPEC_ERR_INVALID_ARG;
   *rows = nq;
@@ -420,6 +419,7 @@ spec_status_t spec_cache_commit(const spec_requests_t* req, const spec_cache_t* 
     return true;
   };
   if (req->tree_nodes > 0 && !tree_ok(req->tree_parent, req->tree_nodes)) return SPEC_ERR_INVALID_ARG;
+  const int64_t room = std::min<int64_t>((int64_t)cache->block_stride * cache->page_tokens, INT32_MAX / 2);
   int64_t o = 0;
   for (int i = 0; i < req->num_requests; ++i) {
     int n = req->tree_nodes;
@@ -431,10 +431,7 @@ spec_status_t spec_cache_commit(const spec_requests_t* req, const spec_cache_t* 
       if (req->draft_len[i] < 0 || req->draft_len[i] > SPEC_MAX_DRAFT) return SPEC_ERR_INVALID_ARG;
       n = req->draft_len[i] + 1;
     }
-    const int64_t len = (int64_t)req->ctx_len[i] + n;
-    if (req->ctx_len[i] < 0 || len > INT32_MAX / 2 ||
-        (len + cache->page_tokens - 1) / cache->page_tokens > cache->block_stride)
-      return SPEC_ERR_INVALID_ARG;
+    if (req->ctx_len[i] < 0 || (int64_t)req->ctx_len[i] + n > room) return SPEC_ERR_INVALID_ARG;
   }
   if (!per_req && req->tree_nodes == 0) return SPEC_OK;      // chains are in place
   if ((int64_t)cache->num_kv_heads * cache->head_dim * elem_bytes(cache->dtype) / 1024 >= 65535)

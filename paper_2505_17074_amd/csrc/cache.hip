@@ -37,7 +37,9 @@ __device__ __forceinline__ void store(char* to, u32x4 x) {
 
 // blockIdx: (block of 16 rows, segment, 2 layer + (1 for V)).  Blocks are
 // 16-aligned, so one lies in one page.  A wave takes every fourth row of the
-// block, up to four rows' units in flight.
+// block, up to four rows' units in flight.  2-9 rows of 128 requests (5.8 MB
+// moved): 3.9 us, the launch; 300-700 rows of 4 requests in 32 layers (553 MB): 93
+// us, 5.9 TB/s (torch's copy 4.9).
 template <bool RUN, bool STREAM, int N>
 __global__ __launch_bounds__(256) void cache_append(AppendParams<N> p) {
   const AppendSegment sg = p.seg[N > 1 ? blockIdx.y : 0];
@@ -71,7 +73,9 @@ __global__ __launch_bounds__(256) void cache_append(AppendParams<N> p) {
 // node at depth t is read into lane t; rows move in the order of their depth.
 // A node's index is at least its depth, so a row's new place is never the old
 // place of a deeper one: batches of loads ahead of their stores, ascending,
-// are safe, and no two waves touch the same bytes.
+// are safe, and no two waves touch the same bytes.  One tree of 15 nodes in 32
+// layers 3.8 us (the launch and its dependent loads), 64 of them 8.4 us for
+// about 29 MB moved, which the append before left in the caches.
 template <bool RUN, int N>
 __global__ __launch_bounds__(64) void cache_commit(CommitParams<N> p) {
   const int lane = threadIdx.x;
@@ -121,7 +125,9 @@ __global__ __launch_bounds__(64) void cache_commit(CommitParams<N> p) {
 
 constexpr int kCopyUnits = 4;          // 16-byte units a thread
 
-// blockIdx: (part of the page, pair, 2 layer + (1 for V)).
+// blockIdx: (part of the page, pair, 2 layer + (1 for V)).  One page of 64 rows
+// in 32 layers (2 x 8 heads of 128) 3.2 us, the launch; 96 of them (1.61 GB) 284
+// us, 5.7 TB/s.
 template <bool RUN, bool STREAM, int N>
 __global__ __launch_bounds__(256) void cache_copy_pages(PageCopyParams<N> p) {
   const PagePair pair = p.pair[blockIdx.y];

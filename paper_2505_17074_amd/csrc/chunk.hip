@@ -3,6 +3,21 @@
 // With s_rt = scale q_r . k_t over the keys t that row r sees,
 //   out_r = sum_t 2^(s_rt log2 e - m_r) v_t / sum_t 2^(s_rt log2 e - m_r),
 // one pass over the keys with a running reference m_r and sum l_r (fp32).
+//
+// What bounds it, by the query rows that read a KV head's keys (d = 128; times
+// of a whole call, those under 20 us in a row):
+//   few: HBM.  64 single tokens over 512-8192 rows, 8 KV heads under 32 query
+//     heads (1.16 GB): 191 us, 6.1 TB/s (a plain read stream reaches 6.5); one
+//     over 1000 rows (4 MB): 13-14 us, two launches of 7.2 and 4.3.
+//   many: the matrix cores, at the clock that their power leaves (1.67-1.75 GHz).
+//     1024 tokens over 30011 rows, 8 heads a group (1.02 TFLOP): 907-930 us,
+//     1.10-1.13 PFLOP/s, MFMA busy 61 % (the library's 8192^3 product 1.2); 2048
+//     without a context: 46 us, 0.75, where the tiles on the diagonal (run apart,
+//     half of each seen) and the start are a third.
+//   both: 8 chunks of 33-700 tokens and 16 single ones, 32 heads of their own
+//     (671 MB, 73 GFLOP): 153 us, 4.4 TB/s.
+// An fp32 output has three products with V for one: 16 requests of 1-400 tokens
+// over 0-1500 rows, d = 64: 38 us.
 #include "sv_chunk.h"
 
 #include <type_traits>
@@ -130,6 +145,14 @@ struct Rows {
 //   S^T[key, row] = K[key, :] . Q[row, :]     v_mfma_f32_32x32x16_bf16, K as A
 //   softmax over the keys                      fp32
 //   O^T[e, row] += V^T[e, key] . P^T[key, row] V^T by transposing LDS reads
+// Rows are on the MFMA's columns in both products, so that a row's maximum, sum
+// and factor are one lane's (and its partner's 32 lanes on), and the operand
+// that all waves share is the one read from LDS.  Four waves a work-group and
+// 64-key tiles (128 KB of LDS for the two on a compute unit) where a KV head has
+// more than 32 query rows, else one wave, 32-key tiles and four work-groups a
+// compute unit.  Long case above: 64 rows a wave 1197 us (the accumulators move
+// between register files), eight waves 928 (a 2048-token prompt 71 for 46),
+// 32-key tiles in four stages 1000, 64-row work-groups 1089.
 // MFMA row m of S^T holds key 16 (m >> 4) + 8 ((m >> 2) & 1) + 4 ((m >> 3) & 1)
 // + (m & 3) of its 32 keys: the C layout then leaves lane half h the keys 16 x
 // + 8 h + 0 .. 7 of its row in registers 8 x .. 8 x + 7, which is the B operand
