@@ -316,3 +316,40 @@ def test_objects_that_end_with_work_pending(gpu_lib):
         torch.empty(sizes[1], dtype=torch.uint8, device="cuda").fill_(255)
         torch.cuda.synchronize()
         assert torch.equal(out, ref)
+
+
+FEW = [0, 1, 30, 31, 32, 33, 62, 63, 64, 65, 127, 128, 129, 191, 700, 2047, 4200]
+
+
+@pytest.mark.parametrize("out", [BF16, F32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("new,hkv,G", [(1, 2, 4), (1, 1, 1), (8, 2, 4), (5, 2, 3), (32, 1, 1)])
+def test_few_rows_beside_many(gpu_lib, new, hkv, G, out):
+    """Requests of up to 32 query rows a KV head in a batch with a longer one."""
+    print(f"[case] chunk few beside many {new} {hkv} {G} {out}", flush=True)
+    p = Paged(FEW + [90], [new] * len(FEW) + [150], hkv, 128, 32, seed=new + G).write()
+    q = queries(new * len(FEW) + 150, hkv * G, 128, seed=G)
+    check_close(_run(p, q, out), *reference(p, q, out=out))
+
+
+def test_few_rows_cut_beside_many(gpu_lib):
+    """A request of few rows whose keys are cut into pieces."""
+    print("[case] chunk few rows cut", flush=True)
+    p = Paged([9000, 10], [2, 80], 1, 128, 64, seed=77).write()
+    q = queries(82, 4, 128, seed=5)
+    check_close(_run(p, q, F32), *reference(p, q, out=F32))
+
+
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+@pytest.mark.parametrize("at", [40, 52, 54, 100, 133])
+def test_few_rows_beside_many_not_finite(gpu_lib, at, bad):
+    """A V row that is not finite, by where it falls among the waves' shares:
+    seen by all tokens of the first request, by some, and by none of the second's."""
+    print(f"[case] chunk few rows not finite {at} {bad}", flush=True)
+    p = Paged([50, 128, 3], [6, 7, 70], 2, 128, seed=16)
+    i = 0 if at < 56 else 1
+    p.rows[i][1][:, at] = bad
+    p.write()
+    q = queries(83, 8, 128, seed=1)
+    ref, bound = reference(p, q, out=F32)
+    assert not np.isfinite(ref).all() and np.isfinite(ref[13:]).all()
+    check_close(_run(p, q, F32), ref, bound)
