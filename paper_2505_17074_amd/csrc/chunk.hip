@@ -8,15 +8,15 @@
 // of a whole call, those under 20 us in a row):
 //   few: HBM.  64 single tokens over 512-8192 rows, 8 KV heads under 32 query
 //     heads (1.16 GB): 191 us, 6.1 TB/s (a plain read stream reaches 6.5); one
-//     over 1000 rows (4 MB): 13-14 us, two launches of 7.2 and 4.3.
+//     over 1000 rows (4 MB): 11-15 us, two launches of 7.2 and 4.2.
 //   many: the matrix cores, at the clock that their power leaves (1.67-1.75 GHz).
-//     1024 tokens over 30011 rows, 8 heads a group (1.02 TFLOP): 902-939 us,
-//     1.09-1.13 PFLOP/s, MFMA busy 61-64 % (the library's 8192^3 product 1.2).
+//     1024 tokens over 30011 rows, 8 heads a group (1.02 TFLOP): 902-975 us,
+//     1.05-1.13 PFLOP/s, MFMA busy 61-64 % (the library's 8192^3 product 1.2).
 //     2048 without a context, 4 heads a group (34 GFLOP): 46 us, 0.75 PFLOP/s: the
 //     longest row tile's 32 key tiles, 1.1-1.2 us each on a compute unit that the
 //     shorter ones have left (0.94 where two row tiles share it), and the start.
 //   both: 8 chunks of 33-700 tokens and 16 single ones, 32 heads of their own
-//     (671 MB, 73 GFLOP): 153 us, 4.4 TB/s.
+//     (671 MB, 73 GFLOP): 150 us, 4.5 TB/s.
 // An fp32 output has three products with V for one: 16 requests of 1-400 tokens
 // over 0-1500 rows, d = 64: 38 us.
 #include "sv_chunk.h"
