@@ -383,11 +383,21 @@ def spec_cache_copy_pages(cache, copies: int, n: int, stream: int) -> int:
     return load().spec_cache_copy_pages(_ref(cache), copies, n, stream)
 
 
-def make_chunks(ctx_len, new_len) -> SpecChunks:
-    """SpecChunks over host int32 arrays; the arrays are kept alive on the struct."""
+def int32_copy(x):
+    """An int32 array of x, whose values have to be such numbers."""
     import numpy as np
-    ctx = np.ascontiguousarray(ctx_len, dtype=np.int32)
-    new = np.ascontiguousarray(new_len, dtype=np.int32)
+    given = np.asarray(x)
+    if given.dtype.kind not in "iu" and given.size:
+        raise ValueError("not whole numbers")
+    a = np.array(given, dtype=np.int32, order="C")
+    if given.dtype != np.int32 and not (a == given).all():
+        raise ValueError("whole numbers of more than 32 bits")
+    return a
+
+
+def make_chunks(ctx_len, new_len) -> SpecChunks:
+    """SpecChunks over int32 copies of the lengths, kept alive on the struct."""
+    ctx, new = int32_copy(ctx_len), int32_copy(new_len)
     if ctx.shape != new.shape or ctx.ndim != 1:
         raise ValueError("ctx_len and new_len are one number a request")
     r = SpecChunks()

@@ -198,7 +198,10 @@ class PagedCache:
 
     def copy_pages(self, copies, stream: Optional[torch.cuda.Stream] = None) -> None:
         """Copies (src, dst, tokens) [n, 3], in every layer."""
-        a = np.ascontiguousarray(copies, dtype=np.int32).reshape(-1, 3)
+        a = copies
+        if not (isinstance(a, np.ndarray) and a.dtype == np.int32 and a.flags.c_contiguous):
+            a = B.int32_copy(a)
+        a = a.reshape(-1, 3)
         with self._enter():
             B.check(self._lib.spec_cache_copy_pages(self._ref, a.ctypes.data if a.size else None, a.shape[0],
                                                     self._stream(stream)), "spec_cache_copy_pages")

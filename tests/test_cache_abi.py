@@ -247,3 +247,21 @@ def test_strides_of_single_entries():
 def test_more_copies_than_pages():
     """Refused before anything as long as the list is read."""
     assert B.spec_cache_copy_pages(_cache(), np.zeros(3, np.int32).ctypes.data, 2**31 - 1, 0) == INV
+
+
+def test_lengths_are_copied_and_whole():
+    ctx, new = np.array([4, 5], np.int32), np.array([1, 2], np.int32)
+    chunks = B.make_chunks(ctx, new)
+    ctx += 100
+    new += 100
+    assert [chunks.ctx_len[i] for i in range(2)] == [4, 5] and [chunks.new_len[i] for i in range(2)] == [1, 2]
+    assert chunks.rows == 3
+    for bad in ([1.5, 2], np.array([2**32, 1]), np.array([1, np.nan])):
+        with pytest.raises(ValueError):
+            B.make_chunks(bad, [1, 1])
+        with pytest.raises(ValueError):
+            B.make_chunks([1, 1], bad)
+    k = torch.zeros((1, 4, 32, 2, 64))
+    for bad in ([(0, 1, 2.5)], np.array([[2**32, 1, 3]])):
+        with pytest.raises(ValueError, match="whole numbers"):
+            PagedCache(k, k.clone()).copy_pages(bad)
