@@ -534,6 +534,7 @@ struct Chunk {
     }
     if (see_next) x = scores(cur, S, A);
   }
+  // Where a lane reads its operands of both products (the layouts above).
   static __device__ __forceinline__ void places(Lane& A, int l32, int half, int lane) {
     const int key = 16 * (l32 >> 4) + 8 * ((l32 >> 2) & 1) + 4 * ((l32 >> 3) & 1) + (l32 & 3);
 #pragma unroll
@@ -545,8 +546,8 @@ struct Chunk {
       A.voff[eb] = (uint32_t)(TL::MAT + row * TL::ROWB + ((ch ^ swv<D>(row)) * 16) + (s & 1) * 8);
     }
   }
-  // Step t of a wave that has every second tile's 32 keys at `key0` of the tile
-  // (mine: tile t's, whose scores it has; else it takes the scores of tile t + 1).
+  // Step t of a wave that has 32 keys of every second tile, `cur` moved to them
+  // (mine: of tile t, whose scores it has; else it takes the scores of tile t + 1).
   static __device__ __forceinline__ void shared_step(lds_char* __restrict__ nxt, const lds_char* __restrict__ cur,
                                                      bool more, const Fetch& f, int jn, int kb, const Window& win,
                                                      int2& before, int w, const Lane& A, Rows<D>& S, ScoresOf<1>& x,
@@ -593,7 +594,11 @@ struct Chunk {
                   t + NS, it.kb, win, before, w, A, S, x, (t & 1) == par, it.kb + TK * t + 32 * hb, p.scale_log2, lane);
     }
     wait_vm<0>();
-    // the waves' shares meet in wave 0, the ring their place; a maximum that is NaN tells that O has one
+    // The waves' shares meet in wave 0, the ring their place; a maximum that is NaN
+    // tells that O has one.  (A vote of the work-group by __syncthreads_or has an
+    // LDS variable of its own: with a second one the compiler no longer tells the
+    // stages apart and waits for the transfers before every read, 49 -> 57 us for
+    // a prompt of 2048.)
     bool bad = __any(has_nan(S));
     f32x4* at = reinterpret_cast<f32x4*>(lds) + lane;
     float2* ml = reinterpret_cast<float2*>(lds + (NW - 1) * D * 128) + lane;
