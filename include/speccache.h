@@ -90,11 +90,13 @@ typedef struct spec_chunks {
  *              dim contiguous, 16-byte aligned rows.  Query head h reads KV
  *              head h / (Hq / Hkv).  scale <= 0 selects 1/sqrt(d).
  *   out        [Nq, Hq, d] contiguous, 16-byte aligned, in out_dtype:
- *              SPEC_BF16 (probabilities rounded to bf16 for the second
- *              product) or SPEC_F32 (probabilities carried in three bf16
- *              parts, about fp32's precision).  Scores, maxima, sums and
- *              outputs accumulate in fp32 in both.  Rows past Nq are left
- *              as they are.
+ *              SPEC_BF16 or SPEC_F32.  For SPEC_F32 the probabilities
+ *              enter the second product in three bf16 parts (off by 2^-24 of
+ *              their value at most); for SPEC_BF16 in two (2^-16) where no
+ *              request of the batch has more than 32 query rows a KV head
+ *              (new_len Hq / Hkv), else in one (2^-8, as the output's own
+ *              rounding).  Scores, maxima, sums and outputs accumulate in
+ *              fp32 in all.  Rows past Nq are left as they are.
  *   d in {64, 128}; bf16 caches only (SPEC_ERR_UNSUPPORTED otherwise).
  * A value of K or V that a token does not see never reaches its output, NaN
  * and infinities included, whether it is a later token's row, a row behind

@@ -193,7 +193,7 @@ __device__ __forceinline__ int last_seen(const ChunkParams& p, const Piece& it, 
   return min(it.ctx + (it.r0 + min(wr0 + 31, it.rows - 1)) / p.G, it.ke - 1);
 }
 
-template <int D, int PARTS>
+template <int D, bool F32>
 __device__ __forceinline__ void write_out(const ChunkParams& p, const Piece& it, const Rows<D>& S, int wr0, int l32,
                                           int half) {
   constexpr int ET = D / 32;
@@ -210,11 +210,11 @@ __device__ __forceinline__ void write_out(const ChunkParams& p, const Piece& it,
       for (int i = 0; i < 16; i += 4) {
         const int e = 32 * eb + 2 * i + 4 * half;
         const f32x4 y = {S.o[eb][i] * inv, S.o[eb][i + 1] * inv, S.o[eb][i + 2] * inv, S.o[eb][i + 3] * inv};
-        if constexpr (PARTS == 1) {
+        if constexpr (F32) {
+          *reinterpret_cast<f32x4*>(static_cast<float*>(p.out) + row * D + e) = y;
+        } else {
           *reinterpret_cast<u32x2*>(static_cast<uint16_t*>(p.out) + row * D + e) =
               __builtin_bit_cast(u32x2, __builtin_convertvector(y, bf16x4));
-        } else {
-          *reinterpret_cast<f32x4*>(static_cast<float*>(p.out) + row * D + e) = y;
         }
       }
   } else {
@@ -312,8 +312,18 @@ __device__ __forceinline__ void one_by_one(const Fetch& f, Rows<D>& S, int kb, i
 // Stage j of the ring holds K of tile j and V of tile j - 1: step t takes the
 // scores of tile t + 1 (matrix cores) beside the softmax of tile t (vector
 // units), then the product with V of tile t.
-// PARTS: bf16 parts a probability is carried in (1 for a bf16 output, 3 for
-// an fp32 one: 24 bits).
+// PARTS: bf16 parts a probability is carried in, p = p1 + p2 + p3, each the
+// rounding of what the ones before leave: half a step of bf16 is 2^-8, so one
+// part is off by 2^-8 p at most, two by 2^-16 p, three by 2^-24 p.  An fp32
+// output takes three.  A bf16 output rounds by 2^-8 itself.  With up to 32 rows
+// a KV head (the keys' bytes are what the kernel waits for) it takes two parts,
+// which add nothing to that and cost no time to speak of (64 single tokens over
+// 512-8192 rows 190.0 -> 190.8 us, one over 1000 11.4 -> 11.5).  Beyond, where
+// the matrix cores bound it, a second part is half as much work again (1024
+// tokens over 30011 rows 887 -> 1197 us, 2048 without a context 46.4 -> 56.7, 8
+// chunks beside 16 single tokens 150 -> 169), for an error of 0.0016 of the
+// row's norm in place of 0.0021-0.0024, and it takes one: who needs the better
+// product there asks for an fp32 output.
 // ---------------------------------------------------------------------------
 template <int D, int NW, int TK, int PARTS>
 struct Chunk {
@@ -626,7 +636,7 @@ struct Chunk {
   }
 };
 
-template <int D, int NW, int TK, int NS, int PARTS>
+template <int D, int NW, int TK, int NS, int PARTS, bool F32>
 __global__ __launch_bounds__(64 * NW, 2) void chunk_attn(ChunkParams p) {
 #if defined(__HIP_DEVICE_COMPILE__)   // the host pass needs the signature only
   using C = Chunk<D, NW, TK, PARTS>;
@@ -717,7 +727,7 @@ __global__ __launch_bounds__(64 * NW, 2) void chunk_attn(ChunkParams p) {
     if (w > 0) return;
   }
   if (__any(bad)) one_by_one<D>(f, S, it.kb, wave_sees, p.scale_log2, half);
-  write_out<D, PARTS>(p, it, S, wr0, l32, half);
+  write_out<D, F32>(p, it, S, wr0, l32, half);
 #endif
 }
 
@@ -775,23 +785,23 @@ __global__ __launch_bounds__(256) void chunk_join(JoinParams p) {
       __builtin_bit_cast(u32x2, __builtin_convertvector(y, bf16x4));
 }
 
-template <int D, int PARTS>
+template <int D, bool F32>
 static hipError_t launch_d(const ChunkParams& p, const JoinParams& j, const ChunkLaunch& l, hipStream_t s) {
-  if (l.tall) chunk_attn<D, 4, 64, 2, PARTS><<<dim3(l.n_items * p.Hkv), dim3(256), 0, s>>>(p);
-  else chunk_attn<D, 1, 32, 2, PARTS><<<dim3(l.n_items * p.Hkv), dim3(64), 0, s>>>(p);
+  if (l.tall) chunk_attn<D, 4, 64, 2, F32 ? 3 : 1, F32><<<dim3(l.n_items * p.Hkv), dim3(256), 0, s>>>(p);
+  else chunk_attn<D, 1, 32, 2, F32 ? 3 : 2, F32><<<dim3(l.n_items * p.Hkv), dim3(64), 0, s>>>(p);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || l.n_joins == 0) return e;
   constexpr int NG = 1024 / D;
   if (l.join_pieces <= 2 * NG)
-    chunk_join<D, PARTS != 1, true><<<dim3(l.n_joins * p.Hkv, (l.join_rows + NG - 1) / NG), dim3(256), 0, s>>>(j);
+    chunk_join<D, F32, true><<<dim3(l.n_joins * p.Hkv, (l.join_rows + NG - 1) / NG), dim3(256), 0, s>>>(j);
   else
-    chunk_join<D, PARTS != 1, false><<<dim3(l.n_joins * p.Hkv, l.join_rows), dim3(256), 0, s>>>(j);
+    chunk_join<D, F32, false><<<dim3(l.n_joins * p.Hkv, l.join_rows), dim3(256), 0, s>>>(j);
   return hipGetLastError();
 }
 
 hipError_t launch_chunk(const ChunkParams& p, const JoinParams& j, const ChunkLaunch& l, hipStream_t s) {
-  if (l.D == 128) return l.out_f32 ? launch_d<128, 3>(p, j, l, s) : launch_d<128, 1>(p, j, l, s);
-  return l.out_f32 ? launch_d<64, 3>(p, j, l, s) : launch_d<64, 1>(p, j, l, s);
+  if (l.D == 128) return l.out_f32 ? launch_d<128, true>(p, j, l, s) : launch_d<128, false>(p, j, l, s);
+  return l.out_f32 ? launch_d<64, true>(p, j, l, s) : launch_d<64, false>(p, j, l, s);
 }
 
 }  // namespace sv
