@@ -105,7 +105,10 @@ struct Fetch {
 };
 
 // Lane l's 32-key block b + l of the item (from key kb on): its page, and the
-// place in it of its first key (of the item's last one for blocks behind it).
+// place in it of its first key (those of the item's last block for blocks
+// behind it).  kb and a page's tokens are multiples of 32, so a block's 32 rows
+// lie in one page: whatever of them a transfer's bounds let through is memory of
+// the pool.
 // One load and one division serve 64 blocks; a step reads its block's by lane.
 // (A scalar load a step had its latency in every step.)
 struct Window {
@@ -113,7 +116,7 @@ struct Window {
   int pg, place;
 };
 __device__ __forceinline__ void look(Window& x, const Fetch& f, int kb, int b, int lane) {
-  const int t = min(kb + 32 * (b + lane), f.ke - 1);
+  const int t = min(kb + 32 * (b + lane), (f.ke - 1) & ~31);
   const int i = t / f.page_tokens;
   x.b = b;
   x.place = t - i * f.page_tokens;
@@ -363,7 +366,11 @@ struct Chunk {
 
   // The wave's units of stage j: K of tile j, V of tile j - 1 (tiles begin at
   // key kb).  Rows past the item's end, and tiles that it does not have, are
-  // past the buffer's records: they come as zeros.
+  // past the buffer's records (a raw buffer's bounds check takes the scalar
+  // offset in, measured on gfx950 by loads with the offset below, at and past the
+  // records' end): they come as zeros.  Nothing rests on that but time: without
+  // it they would be rows of the same block, which are masked, and a NaN among
+  // them would send the rows through the fallback below.
   template <int POL = CPOL>
   static __device__ __forceinline__ void issue(lds_char* stage, const Fetch& f, int j, int kb, const Window& win,
                                                int2& before, int w, const Lane& A) {
