@@ -33,6 +33,7 @@ typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef short s16x8 __attribute__((ext_vector_type(8)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef __attribute__((address_space(3))) char lds_char;
@@ -250,19 +251,12 @@ __device__ __forceinline__ void join_rows(Rows<D>& S, float m1, float l1, const 
 }
 
 
-// A wave's rows again, key by key from the cache, by the rows' own visibility:
-// a value of a key that a row does not see never meets the row, not even as a
-// product with zero.  Run where the matrix products left a NaN (an infinity or
-// a NaN somewhere in the item's V, or a score that is one).
+// The wave's rows over keys [t, last] one at a time, by the rows' own
+// visibility: a value of a key that a row does not see never meets the row, not
+// even as a product with zero.
 template <int D>
-__device__ __forceinline__ void one_by_one(const Fetch& f, Rows<D>& S, int kb, int last, float c, int half) {
-  S.m = -INFINITY;
-  float l = 0.f;
-#pragma unroll
-  for (int eb = 0; eb < D / 32; ++eb)
-#pragma unroll
-    for (int i = 0; i < 16; ++i) S.o[eb][i] = 0.f;
-  for (int t = kb; t <= last; ++t) {
+__device__ __forceinline__ void one_by_one(const Fetch& f, Rows<D>& S, int t, int last, float c, int half) {
+  for (; t <= last; ++t) {
     const int64_t at = page_of(f, t) * f.page_bytes + (int64_t)(t % f.page_tokens) * f.row_bytes;
     const bf16x8* k = reinterpret_cast<const bf16x8*>(f.k + at) + half;
     const bf16x4* v = reinterpret_cast<const bf16x4*>(f.v + at) + half;
@@ -278,7 +272,7 @@ __device__ __forceinline__ void one_by_one(const Fetch& f, Rows<D>& S, int kb, i
     const float m = sees ? fmaxf(S.m, s) : S.m, ref = m == -INFINITY ? 0.f : m;
     const float alpha = __builtin_amdgcn_exp2f(S.m - ref), w = sees ? __builtin_amdgcn_exp2f(s - ref) : 0.f;
     S.m = m;
-    l = l * alpha + w;
+    S.l = S.l * alpha + (half ? 0.f : w);
 #pragma unroll
     for (int eb = 0; eb < D / 32; ++eb)
 #pragma unroll
@@ -288,7 +282,6 @@ __device__ __forceinline__ void one_by_one(const Fetch& f, Rows<D>& S, int kb, i
         for (int n = 0; n < 4; ++n) S.o[eb][i + n] = S.o[eb][i + n] * alpha + (sees ? w * (float)y[n] : 0.f);
       }
   }
-  S.l = half ? 0.f : l;
 }
 
 }  // namespace
@@ -551,9 +544,13 @@ struct Chunk {
     }
     if (see_next) x = scores(cur, S, A);
   }
+  // The key of a 32-key block that lane l32 holds for the first product.
+  static __device__ __forceinline__ int key_of(int l32) {
+    return 16 * (l32 >> 4) + 8 * ((l32 >> 2) & 1) + 4 * ((l32 >> 3) & 1) + (l32 & 3);
+  }
   // Where a lane reads its operands of both products (the layouts above).
   static __device__ __forceinline__ void places(Lane& A, int l32, int half, int lane) {
-    const int key = 16 * (l32 >> 4) + 8 * ((l32 >> 2) & 1) + 4 * ((l32 >> 3) & 1) + (l32 & 3);
+    const int key = key_of(l32);
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) A.koff[ks] = (uint32_t)(key * TL::ROWB + (((2 * ks + half) ^ swk<D>(key)) * 16));
     const int s = lane & 15, row = 8 * half + (s >> 2);
@@ -562,6 +559,52 @@ struct Chunk {
       const int ch = 4 * eb + 2 * ((lane >> 4) & 1) + ((s & 3) >> 1);
       A.voff[eb] = (uint32_t)(TL::MAT + row * TL::ROWB + ((ch ^ swv<D>(row)) * 16) + (s & 1) * 8);
     }
+  }
+  // The wave's rows again, straight from the cache, where the products left a NaN
+  // (a value of the item's V that is not finite, or a score that is NaN): an
+  // unseen key's weight is zero, and zero times such a value is NaN.  Blocks that
+  // all rows see whole (the first row does) have no unseen key and go through the
+  // same products; only the rest, up to 31 keys of such a block, the rows' own
+  // tokens and the last block, goes key by key.  1024 tokens over 30011 rows with
+  // one NaN among the first keys, where every wave comes here: 3.9 ms for 0.94
+  // (key by key over all of them 97 ms); 512 over 16000: 0.82 ms for 0.19 (23).
+  static __device__ __forceinline__ void again(const Fetch& f, Rows<D>& S, int kb, int last, float c, int l32, int half) {
+#if defined(__HIP_DEVICE_COMPILE__)
+    const int all = __builtin_amdgcn_readfirstlane(S.last);
+    asm volatile("" : "+v"(l32), "+v"(half));          // none of the addresses below is held in the loops above
+    S.clear();
+    int t = kb;
+    for (; t + 31 <= all; t += 32) {
+      const int64_t at = page_of(f, t) * f.page_bytes + (int64_t)(t % f.page_tokens) * f.row_bytes;
+      const char* k = f.k + at + (int64_t)key_of(l32) * f.row_bytes + half * 16;
+      const char* v = f.v + at + (int64_t)(8 * half) * f.row_bytes + l32 * 2;
+      ScoresOf<1> x;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) x.s[0][i] = 0.f;
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks)
+        x.s[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<const bf16x8*>(k + ks * 32), S.q[ks], x.s[0],
+                                                         0, 0, 0);
+      const float ref = reference(largest(x), S, c);
+      const auto P = weights(x, S, c, ref);
+#pragma unroll
+      for (int kk = 0; kk < 2; ++kk) {
+        __builtin_amdgcn_sched_barrier(0);               // no more loads under way than there are registers
+#pragma unroll
+        for (int eb = 0; eb < ET; ++eb) {
+          s16x8 a;
+#pragma unroll
+          for (int i = 0; i < 8; ++i)
+            a[i] = *reinterpret_cast<const short*>(v + (int64_t)(16 * kk + i) * f.row_bytes + eb * 64);
+#pragma unroll
+          for (int part = 0; part < PARTS; ++part)
+            S.o[eb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), p_operand(P.p[part], kk),
+                                                              S.o[eb], 0, 0, 0);
+        }
+      }
+    }
+    one_by_one<D>(f, S, t, last, c, half);
+#endif
   }
   // Step t of a wave that has 32 keys of every second tile, `cur` moved to them
   // (mine: of tile t, whose scores it has; else it takes the scores of tile t + 1).
@@ -643,8 +686,9 @@ struct Chunk {
   }
 };
 
+// (d = 64: three waves a SIMD.)
 template <int D, int NW, int TK, int NS, int PARTS, bool F32>
-__global__ __launch_bounds__(64 * NW, 2) void chunk_attn(ChunkParams p) {
+__global__ __launch_bounds__(64 * NW, D == 64 ? 3 : 2) void chunk_attn(ChunkParams p) {
 #if defined(__HIP_DEVICE_COMPILE__)   // the host pass needs the signature only
   using C = Chunk<D, NW, TK, PARTS>;
   using TL = Tile<D, TK>;
@@ -733,7 +777,8 @@ __global__ __launch_bounds__(64 * NW, 2) void chunk_attn(ChunkParams p) {
     bad = C::template shared_rows<NS>(p, it, f, A, win, lds, ntiles, w, lane, S);
     if (w > 0) return;
   }
-  if (__any(bad)) one_by_one<D>(f, S, it.kb, wave_sees, p.scale_log2, half);
+  if (__any(bad))
+    C::again(f, S, it.kb, wave_sees, p.scale_log2, l32, half);
   write_out<D, F32>(p, it, S, wr0, l32, half);
 #endif
 }
