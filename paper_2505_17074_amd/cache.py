@@ -39,6 +39,14 @@ def _current_raw_stream(index: int) -> int:
 _current_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", _current_raw_stream)
 
 
+def _capturing(stream: torch.cuda.Stream) -> bool:
+    """Whether a graph is being captured on the stream (of the current device)."""
+    if stream.cuda_stream == _current_raw_stream(stream.device_index):
+        return torch.cuda.is_current_stream_capturing()
+    with torch.cuda.stream(stream):
+        return torch.cuda.is_current_stream_capturing()
+
+
 class Pages:
     """Which sequence holds which page (spec_pages_*)."""
 
@@ -211,8 +219,9 @@ class ChunkAttention(StagingRing):
     """Runs spec_chunk_attn on a PagedCache.  Owns a device workspace, which
     grows with the batches, and `ring` pinned staging buffers (StagingRing).  A
     graph is captured from B.spec_chunk_attn with a workspace and staging of its
-    own, not from here: a replay reads the staging it was captured with, and the
-    ring reuses its slots.  An object is used by one thread at a time."""
+    own: a replay reads the staging it was captured with, and here the ring
+    reuses its slots, so a call on a capturing stream is refused.  An object is
+    used by one thread at a time."""
 
     def __init__(self, cache: PagedCache, num_q_heads: int, scale: float = 0.0, ring: int = 32, event_every: int = 8):
         if event_every < 1 or ring < event_every:
@@ -277,6 +286,8 @@ class ChunkAttention(StagingRing):
         a.q_stride_head = st[1] if qs[1] > 1 else qs[2]
         with cache._enter():
             stream = stream or torch.cuda.current_stream(cache._index)
+            if _capturing(stream):
+                raise RuntimeError("a graph's calls need a workspace and staging of their own: capture B.spec_chunk_attn")
             self._order(stream)
             for grown in (False, True):
                 s = self._slot(stream)
