@@ -48,6 +48,8 @@ extern "C" {
  *                 block_table[i * block_stride + j], its logical row t being
  *                 row t % page_tokens of page block_table[i * block_stride +
  *                 t / page_tokens].  May be NULL for spec_cache_copy_pages.
+ *   block_width   entries of a row that exist (1 .. block_stride; 0:
+ *                 block_stride of them).  Lengths that need more are refused.
  */
 typedef struct spec_cache {
   int32_t num_layers;
@@ -63,7 +65,7 @@ typedef struct spec_cache {
   int64_t kv_stride_head;
   const int32_t* block_table;
   int32_t block_stride;
-  int32_t pad0;
+  int32_t block_width;
 } spec_cache_t;
 
 /*

@@ -108,7 +108,7 @@ extern "C" {
 #define SPEC_API
 #endif
 
-#define SPEC_ABI_VERSION 6
+#define SPEC_ABI_VERSION 7
 #define SPEC_MAX_DRAFT 16        /* chain drafts per request */
 #define SPEC_MAX_TREE_NODES 32   /* token-tree nodes per request, root included */
 

@@ -115,7 +115,7 @@ class SpecCache(C.Structure):
                 ("kv_stride_head", C.c_int64),
                 ("block_table", C.c_void_p),
                 ("block_stride", C.c_int32),
-                ("pad0", C.c_int32)]
+                ("block_width", C.c_int32)]
 
 
 class SpecChunks(C.Structure):

@@ -113,8 +113,9 @@ class Pages:
 class PagedCache:
     """Page pools k, v [layers, num_pages, page_tokens, Hkv, d] (bf16 or fp32,
     last dimension contiguous, a page's rows apart by one stride), and the
-    block table int32 [requests, block_stride] on the same device (it may be
-    replaced: `table`).  An object is used by one thread at a time."""
+    block table int32 [requests, pages of the longest] on the same device, its
+    rows apart by any stride (it may be replaced: `table`).  An object is used
+    by one thread at a time."""
 
     def __init__(self, k: torch.Tensor, v: torch.Tensor, table: Optional[torch.Tensor] = None):
         if k.dim() != 5 or k.dtype != v.dtype or k.device != v.device or not _alike(k, v):
@@ -147,14 +148,15 @@ class PagedCache:
     def table(self, t: Optional[torch.Tensor]) -> None:
         if t is not None:
             if t.dim() != 2 or t.dtype != torch.int32 or t.device != self.device or _stride(t, 1, 1) != 1:
-                raise ValueError("the block table is int32 [requests, block_stride] on the pools' device")
+                raise ValueError("the block table is int32 [requests, pages] on the pools' device")
             if t.shape[0] > 1 and t.stride(0) < t.shape[1]:
                 raise ValueError("the block table's rows overlap")
         self._table = t
         self._rows = 0 if t is None else t.shape[0]
         self.c.block_table = t.data_ptr() if t is not None else None
         # one row's stride is its width (a table of one row may have any)
-        self.c.block_stride = 0 if t is None else (t.stride(0) if t.shape[0] > 1 else t.shape[1])
+        self.c.block_width = 0 if t is None else t.shape[1]
+        self.c.block_stride = 0 if t is None or not t.shape[1] else (t.stride(0) if t.shape[0] > 1 else t.shape[1])
 
     def _enter(self):
         """The pools' device made current for a call (a context)."""

@@ -56,16 +56,23 @@ spec_status_t check_cache(const spec_cache_t* c, bool table) {
   if ((int64_t)c->page_tokens * c->kv_stride_tok * elem_bytes(c->dtype) >= INT32_MAX || c->num_layers > 32767)
     return SPEC_ERR_UNSUPPORTED;
   if (table) {
-    if (!c->block_table || reinterpret_cast<uintptr_t>(c->block_table) % 4 || c->block_stride < 1)
+    if (!c->block_table || reinterpret_cast<uintptr_t>(c->block_table) % 4 || c->block_stride < 1 ||
+        c->block_width < 0 || c->block_width > c->block_stride)
       return SPEC_ERR_INVALID_ARG;
   }
   return SPEC_OK;
 }
 
+// The rows that a request's part of the block table has room for.
+int64_t table_room(const spec_cache_t* c) {
+  const int64_t pages = c->block_width ? c->block_width : c->block_stride;
+  return std::min<int64_t>(pages * c->page_tokens, INT32_MAX / 2);
+}
+
 // Lengths that fit the block table; the number of new rows.
 spec_status_t check_chunks(const spec_chunks_t* r, const spec_cache_t* c, int64_t* rows) {
   if (!r || r->num_requests < 1 || !r->ctx_len || !r->new_len) return SPEC_ERR_INVALID_ARG;
-  const int64_t room = std::min<int64_t>((int64_t)c->block_stride * c->page_tokens, INT32_MAX / 2);
+  const int64_t room = table_room(c);
   int64_t nq = 0;
   for (int i = 0; i < r->num_requests; ++i) {
     if (r->ctx_len[i] < 0 || r->new_len[i] < 0) return SPEC_ERR_INVALID_ARG;
@@ -419,7 +426,7 @@ spec_status_t spec_cache_commit(const spec_requests_t* req, const spec_cache_t* 
     return true;
   };
   if (req->tree_nodes > 0 && !tree_ok(req->tree_parent, req->tree_nodes)) return SPEC_ERR_INVALID_ARG;
-  const int64_t room = std::min<int64_t>((int64_t)cache->block_stride * cache->page_tokens, INT32_MAX / 2);
+  const int64_t room = table_room(cache);
   int64_t o = 0;
   for (int i = 0; i < req->num_requests; ++i) {
     int n = req->tree_nodes;

@@ -1,0 +1,72 @@
+"""Calls of the paged cache that its documentation allows or seems to, on a
+host without a GPU: what they are refused for."""
+import pytest
+import torch
+
+from paper_2505_17074_amd import binding as B
+from paper_2505_17074_amd.cache import PagedCache
+
+FAKE = 1 << 20      # a 256-aligned fake device address; never dereferenced on these paths
+
+
+@pytest.fixture(scope="module", autouse=True)
+def lib():
+    import os
+    if not os.path.exists(B.LIB_PATH):
+        from paper_2505_17074_amd import build
+        build.build()
+    return B.load()
+
+
+def _device(table, dtype=torch.bfloat16):
+    """A cache over pools in host memory whose struct names fake device
+    addresses: for calls that the library's checks end."""
+    k = torch.zeros((1, 8, 32, 2, 64), dtype=dtype)
+    c = PagedCache(k, k.clone(), table)
+    c.c.k = c.c.v = c.c.block_table = FAKE
+    return c
+
+
+def _calls(c, ctx, new):
+    """Every operator that reads the block table, its status."""
+    chunks = B.make_chunks([ctx, 0], [new, 1])
+    a = B.SpecChunkAttnArgs()
+    a.num_q_heads, a.out_dtype, a.q, a.out, a.q_stride_tok, a.q_stride_head = 4, B.SPEC_BF16, FAKE, FAKE, 256, 64
+    p = B.SpecAppendArgs()
+    p.num_layers, p.k_new, p.v_new, p.new_stride_tok, p.new_stride_head = 1, FAKE, FAKE, 128, 64
+    req = B.make_requests([ctx, 0], None, [-1] + list(range(new - 1)))
+    return (B.spec_chunk_workspace_bytes(chunks, c.c, a)[0],
+            B.spec_chunk_attn(chunks, c.c, a, None, 0, None, 0, 0),
+            B.spec_cache_append(chunks, c.c, p, 0), B.spec_cache_commit(req, c.c, FAKE, 0))
+
+
+def test_lengths_behind_the_tables_columns():
+    """A table that is the first columns of a wider one has room for those
+    columns' rows; what lies behind them in a row's stride is not read."""
+    c = _device(torch.zeros((2, 9), dtype=torch.int32)[:, :2])
+    assert (c.c.block_stride, c.c.block_width) == (9, 2)
+    assert set(_calls(c, 60, 5)) == {B.SPEC_ERR_INVALID_ARG}         # 65 rows, two pages of 32
+    one = _device(torch.zeros((1, 9), dtype=torch.int32)[:, :2])
+    assert (one.c.block_stride, one.c.block_width) == (2, 2)
+
+
+def test_table_without_columns():
+    for t in (torch.zeros((2, 9), dtype=torch.int32)[:, :0], torch.zeros((1, 0), dtype=torch.int32)):
+        assert set(_calls(_device(t), 0, 1)) == {B.SPEC_ERR_INVALID_ARG}
+
+
+def test_width_of_the_struct():
+    c = _device(torch.zeros((2, 9), dtype=torch.int32))
+    for width, ctx, want in ((0, 284, B.SPEC_ERR_INVALID_ARG), (9, 284, B.SPEC_ERR_INVALID_ARG), (10, 0, B.SPEC_ERR_INVALID_ARG),
+                             (-1, 0, B.SPEC_ERR_INVALID_ARG), (3, 92, B.SPEC_ERR_INVALID_ARG)):
+        c.c.block_width = width
+        assert set(_calls(c, ctx, 5)) == {want}, width
+    for width, ctx in ((0, 283), (9, 283), (3, 91)):                 # the last rows that there is room for
+        c.c.block_width = width
+        assert _calls_sizes(c, ctx, 5) == B.SPEC_OK, width
+
+
+def _calls_sizes(c, ctx, new):
+    a = B.SpecChunkAttnArgs()
+    a.num_q_heads, a.out_dtype, a.q, a.out, a.q_stride_tok, a.q_stride_head = 4, B.SPEC_BF16, FAKE, FAKE, 256, 64
+    return B.spec_chunk_workspace_bytes(B.make_chunks([ctx, 0], [new, 1]), c.c, a)[0]
