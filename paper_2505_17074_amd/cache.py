@@ -211,9 +211,10 @@ class PagedCache:
         a = copies
         if not (isinstance(a, np.ndarray) and a.dtype == np.int32 and a.flags.c_contiguous):
             a = B.int32_copy(a)
-        a = a.reshape(-1, 3)
+        if a.size and (a.ndim != 2 or a.shape[1] != 3):
+            raise ValueError("copies are [n, 3]: source, destination, tokens")
         with self._enter():
-            B.check(self._lib.spec_cache_copy_pages(self._ref, a.ctypes.data if a.size else None, a.shape[0],
+            B.check(self._lib.spec_cache_copy_pages(self._ref, a.ctypes.data if a.size else None, a.size // 3,
                                                     self._stream(stream)), "spec_cache_copy_pages")
 
 

@@ -1,5 +1,6 @@
 """Calls of the paged cache that its documentation allows or seems to, on a
 host without a GPU: what they are refused for."""
+import numpy as np
 import pytest
 import torch
 
@@ -70,3 +71,15 @@ def _calls_sizes(c, ctx, new):
     a = B.SpecChunkAttnArgs()
     a.num_q_heads, a.out_dtype, a.q, a.out, a.q_stride_tok, a.q_stride_head = 4, B.SPEC_BF16, FAKE, FAKE, 256, 64
     return B.spec_chunk_workspace_bytes(B.make_chunks([ctx, 0], [new, 1]), c.c, a)[0]
+
+
+def test_copies_of_another_shape():
+    """Six numbers that are not two copies, or no list of copies at all."""
+    k = torch.zeros((1, 8, 32, 2, 64))
+    c = PagedCache(k, k.clone())
+    for bad in (np.array([[0, 1], [5, 2], [3, 4]], np.int32), [0, 1, 5], np.zeros((1, 2, 3), np.int32), [[0, 1, 5, 6]]):
+        with pytest.raises(ValueError, match="copies are"):
+            c.copy_pages(bad)
+    for none in ([], np.zeros((0, 3), np.int32), np.zeros(0, np.int32)):
+        with pytest.raises(ValueError, match="device memory"):       # the pools', and not the list's shape
+            c.copy_pages(none)
