@@ -7,6 +7,7 @@ there is no fallback implementation.
 from __future__ import annotations
 
 import ctypes as C
+import operator
 import os
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -381,6 +382,14 @@ def spec_cache_commit(req, cache, accepted_node: int, stream: int) -> int:
 
 def spec_cache_copy_pages(cache, copies: int, n: int, stream: int) -> int:
     return load().spec_cache_copy_pages(_ref(cache), copies, n, stream)
+
+
+def int32(x) -> int:
+    """x, which has to be a whole number of 32 bits (ctypes cuts longer ones)."""
+    x = operator.index(x)
+    if not -2**31 <= x < 2**31:
+        raise ValueError("a whole number of more than 32 bits")
+    return x
 
 
 def int32_copy(x):

@@ -53,7 +53,8 @@ class Pages:
     def __init__(self, num_pages: int, page_tokens: int):
         self._h = C.c_void_p()
         self._lib = B.load()
-        B.check(self._lib.spec_pages_create(num_pages, page_tokens, C.byref(self._h)), "spec_pages_create")
+        B.check(self._lib.spec_pages_create(B.int32(num_pages), B.int32(page_tokens), C.byref(self._h)),
+                "spec_pages_create")
         self.num_pages, self.page_tokens = num_pages, page_tokens
 
     def __del__(self):
@@ -70,21 +71,22 @@ class Pages:
         """The sequence has `tokens` rows from now on.  Returns the page copy
         (src, dst, tokens) to make before rows are written, or None."""
         c = B.SpecPageCopy()
-        B.check(self._lib.spec_pages_resize(self._h, sequence, tokens, C.byref(c)), "spec_pages_resize")
+        B.check(self._lib.spec_pages_resize(self._h, B.int32(sequence), B.int32(tokens), C.byref(c)),
+                "spec_pages_resize")
         return (c.src, c.dst, c.tokens) if c.tokens else None
 
     def fork(self, sequence: int) -> int:
         s = C.c_int32()
-        B.check(self._lib.spec_pages_fork(self._h, sequence, C.byref(s)), "spec_pages_fork")
+        B.check(self._lib.spec_pages_fork(self._h, B.int32(sequence), C.byref(s)), "spec_pages_fork")
         return s.value
 
     def close(self, sequence: int) -> None:
-        B.check(self._lib.spec_pages_close(self._h, sequence), "spec_pages_close")
+        B.check(self._lib.spec_pages_close(self._h, B.int32(sequence)), "spec_pages_close")
 
     def table(self, sequence: int) -> np.ndarray:
         n = C.c_int32()
         out = np.empty(self.num_pages, np.int32)
-        B.check(self._lib.spec_pages_table(self._h, sequence, out.ctypes.data, out.size, C.byref(n)),
+        B.check(self._lib.spec_pages_table(self._h, B.int32(sequence), out.ctypes.data, out.size, C.byref(n)),
                 "spec_pages_table")
         return out[:n.value].copy()
 
@@ -151,12 +153,14 @@ class PagedCache:
                 raise ValueError("the block table is int32 [requests, pages] on the pools' device")
             if t.shape[0] > 1 and t.stride(0) < t.shape[1]:
                 raise ValueError("the block table's rows overlap")
+        # one row's stride is its width (a table of one row may have any)
+        width = 0 if t is None else B.int32(t.shape[1])
+        stride = B.int32(t.stride(0)) if width and t.shape[0] > 1 else width
         self._table = t
         self._rows = 0 if t is None else t.shape[0]
         self.c.block_table = t.data_ptr() if t is not None else None
-        # one row's stride is its width (a table of one row may have any)
-        self.c.block_width = 0 if t is None else t.shape[1]
-        self.c.block_stride = 0 if t is None or not t.shape[1] else (t.stride(0) if t.shape[0] > 1 else t.shape[1])
+        self.c.block_width = width
+        self.c.block_stride = stride
 
     def _enter(self):
         """The pools' device made current for a call (a context)."""
@@ -184,7 +188,7 @@ class PagedCache:
             raise ValueError("k_new and v_new have the pools' type and device")
         self._requests(chunks.num_requests)
         a = self._append
-        a.layer, a.num_layers = layer, shape[0] if len(shape) == 4 else 1
+        a.layer, a.num_layers = B.int32(layer), shape[0] if len(shape) == 4 else 1
         a.k_new, a.v_new = k_new.data_ptr(), v_new.data_ptr()
         width = self._width
         a.new_stride_layer = st[0]
@@ -231,7 +235,7 @@ class ChunkAttention(StagingRing):
             raise ValueError("need ring >= event_every >= 1")
         self.cache = cache
         a = self.args = B.SpecChunkAttnArgs()
-        a.num_q_heads, a.scale = num_q_heads, scale
+        a.num_q_heads, a.scale = B.int32(num_q_heads), scale
         self._args_ref = C.byref(a)
         self._head = torch.Size((num_q_heads, cache.c.head_dim))
         self.ws_bytes = self.staging_bytes = 0
@@ -283,7 +287,7 @@ class ChunkAttention(StagingRing):
                 not out.is_contiguous() or st[2] != 1:
             raise ValueError("q has the cache's type, out is contiguous bf16 or fp32, both on its device")
         cache._requests(chunks.num_requests)
-        a.layer, a.out_dtype = layer, kind
+        a.layer, a.out_dtype = B.int32(layer), kind
         a.q, a.out = q.data_ptr(), out.data_ptr()
         a.q_stride_tok = st[0] if qs[0] > 1 else qs[1] * qs[2]
         a.q_stride_head = st[1] if qs[1] > 1 else qs[2]

@@ -5,7 +5,7 @@ import pytest
 import torch
 
 from paper_2505_17074_amd import binding as B
-from paper_2505_17074_amd.cache import PagedCache
+from paper_2505_17074_amd.cache import ChunkAttention, PagedCache, Pages
 
 FAKE = 1 << 20      # a 256-aligned fake device address; never dereferenced on these paths
 
@@ -83,3 +83,28 @@ def test_copies_of_another_shape():
     for none in ([], np.zeros((0, 3), np.int32), np.zeros(0, np.int32)):
         with pytest.raises(ValueError, match="device memory"):       # the pools', and not the list's shape
             c.copy_pages(none)
+
+
+def test_numbers_of_more_than_32_bits():
+    """Refused, and not cut to what their low bits say."""
+    big = 2**32
+    for args in ((big + 5, 64), (5, big + 64), (2.0, 64)):
+        with pytest.raises((ValueError, TypeError)):
+            Pages(*args)
+    p = Pages(8, 32)
+    s = p.open()
+    p.resize(s, 200)
+    for call in (lambda: p.resize(s, big + 1), lambda: p.resize(big + s, 1), lambda: p.fork(big + s), lambda: p.close(big + s),
+                 lambda: p.table(big + s)):
+        with pytest.raises(ValueError, match="32 bits"):
+            call()
+    assert p.free == 1 and p.table(s).size == 7
+    k = torch.zeros((1, 8, 32, 2, 64), dtype=torch.bfloat16)
+    c = PagedCache(k, k.clone(), torch.zeros((1, 4), dtype=torch.int32))
+    rows, chunks = torch.zeros((1, 2, 64), dtype=torch.bfloat16), B.make_chunks([0], [1])
+    with pytest.raises(ValueError, match="32 bits"):
+        c.append(chunks, rows, rows, layer=big)
+    with pytest.raises(ValueError, match="32 bits"):
+        ChunkAttention(c, big + 4)
+    with pytest.raises(ValueError, match="32 bits"):
+        ChunkAttention(c, 4).run(chunks, torch.zeros((1, 4, 64), dtype=torch.bfloat16), torch.zeros((1, 4, 64)), layer=big)
