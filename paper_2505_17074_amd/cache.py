@@ -117,7 +117,13 @@ class PagedCache:
     last dimension contiguous, a page's rows apart by one stride), and the
     block table int32 [requests, pages of the longest] on the same device, its
     rows apart by any stride (it may be replaced: `table`).  An object is used
-    by one thread at a time."""
+    by one thread at a time.
+
+    A call runs on `stream`, or the current one, after what is on it already.
+    Pools and table are recorded on that stream, so that their memory is not
+    given away under a call; the other tensors of a call (new rows, queries,
+    outputs, accepted nodes) are its caller's to order and to keep, as for any
+    work on a stream that is not their own."""
 
     def __init__(self, k: torch.Tensor, v: torch.Tensor, table: Optional[torch.Tensor] = None):
         if k.dim() != 5 or k.dtype != v.dtype or k.device != v.device or not _alike(k, v):
@@ -157,6 +163,7 @@ class PagedCache:
         width = 0 if t is None else B.int32(t.shape[1])
         stride = B.int32(t.stride(0)) if width and t.shape[0] > 1 else width
         self._table = t
+        self._streams = set()              # handles of the streams that table and pools are recorded on
         self._rows = 0 if t is None else t.shape[0]
         self.c.block_table = t.data_ptr() if t is not None else None
         self.c.block_width = width
@@ -169,7 +176,14 @@ class PagedCache:
         return _HERE if torch.cuda.current_device() == self._index else torch.cuda.device(self._index)
 
     def _stream(self, stream) -> int:
-        return _current_raw_stream(self._index) if stream is None else stream.cuda_stream
+        h = _current_raw_stream(self._index) if stream is None else stream.cuda_stream
+        if h not in self._streams:
+            s = stream or torch.cuda.current_stream(self._index)
+            for t in (self.k, self.v, self._table):
+                if t is not None:
+                    t.record_stream(s)
+            self._streams.add(h)
+        return h
 
     def _requests(self, n: int) -> None:
         if self._table is None or n > self._rows:
@@ -295,12 +309,13 @@ class ChunkAttention(StagingRing):
             stream = stream or torch.cuda.current_stream(cache._index)
             if _capturing(stream):
                 raise RuntimeError("a graph's calls need a workspace and staging of their own: capture B.spec_chunk_attn")
+            h = cache._stream(stream)
             self._order(stream)
             for grown in (False, True):
                 s = self._slot(stream)
                 try:
                     st = cache._lib.spec_chunk_attn(chunks, cache._ref, self._args_ref, self.ws_ptr, self.ws_bytes,
-                                                    self._staging[s], self.staging_bytes, stream.cuda_stream)
+                                                    self._staging[s], self.staging_bytes, h)
                 finally:
                     self._done(s, stream)
                 if st != B.SPEC_ERR_WORKSPACE or grown:
