@@ -84,16 +84,21 @@ class Pages:
         B.check(self._lib.spec_pages_close(self._h, B.int32(sequence)), "spec_pages_close")
 
     def table(self, sequence: int) -> np.ndarray:
-        n = C.c_int32()
-        out = np.empty(self.num_pages, np.int32)
-        B.check(self._lib.spec_pages_table(self._h, B.int32(sequence), out.ctypes.data, out.size, C.byref(n)),
-                "spec_pages_table")
-        return out[:n.value].copy()
+        n, s = C.c_int32(), B.int32(sequence)
+        st = self._lib.spec_pages_table(self._h, s, None, 0, C.byref(n))     # their number
+        out = np.empty(n.value, np.int32)
+        if st == B.SPEC_ERR_WORKSPACE:
+            st = self._lib.spec_pages_table(self._h, s, out.ctypes.data, out.size, C.byref(n))
+        B.check(st, "spec_pages_table")
+        return out
 
     def block_table(self, sequences: Sequence[int], block_stride: Optional[int] = None) -> np.ndarray:
         """The sequences' page ids [len(sequences), block_stride], zeros behind them."""
         rows = [self.table(s) for s in sequences]
-        width = block_stride or max([r.size for r in rows] + [1])
+        longest = max([r.size for r in rows] + [1])
+        width = block_stride or longest
+        if width < longest:
+            raise ValueError("a sequence has more pages than the table has columns")
         out = np.zeros((len(rows), width), np.int32)
         for i, r in enumerate(rows):
             out[i, :r.size] = r

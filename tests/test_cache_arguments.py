@@ -108,3 +108,24 @@ def test_numbers_of_more_than_32_bits():
         ChunkAttention(c, big + 4)
     with pytest.raises(ValueError, match="32 bits"):
         ChunkAttention(c, 4).run(chunks, torch.zeros((1, 4, 64), dtype=torch.bfloat16), torch.zeros((1, 4, 64)), layer=big)
+
+
+def test_tables_of_a_large_pool():
+    """A sequence's table takes its own pages' room, not the pool's."""
+    import tracemalloc
+    p = Pages(1 << 20, 32)
+    seqs = [p.open() for _ in range(20)]
+    for i, s in enumerate(seqs):
+        p.resize(s, 32 * i)
+    p.block_table(seqs)
+    tracemalloc.start()
+    t = p.block_table(seqs)
+    peak = tracemalloc.get_traced_memory()[1]
+    tracemalloc.stop()
+    assert peak < 1 << 16                                # the pool's ids would be 4 MB
+    assert t.shape == (20, 19) and [int((r > 0).sum()) for r in t[2:]] == list(range(2, 20))
+    assert t[1, 0] == 0 and p.table(seqs[0]).size == 0 and p.table(seqs[7]).tolist() == t[7, :7].tolist()
+    with pytest.raises(ValueError, match="columns"):
+        p.block_table(seqs, 18)
+    with pytest.raises(B.SpecError):
+        p.table(20)
