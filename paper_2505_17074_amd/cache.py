@@ -16,7 +16,7 @@ from .batch import StagingRing
 
 _DTYPE = {torch.bfloat16: B.SPEC_BF16, torch.float32: B.SPEC_F32}
 _HERE = contextlib.nullcontext()
-_kept = []                             # what objects that ended inside a graph capture held
+_kept = []                             # what objects that ended inside a graph capture held, until the next object
 
 
 def _stride(t: torch.Tensor, dim: int, otherwise: int) -> int:
@@ -45,6 +45,18 @@ def _capturing(stream: torch.cuda.Stream) -> bool:
         return torch.cuda.is_current_stream_capturing()
     with torch.cuda.stream(stream):
         return torch.cuda.is_current_stream_capturing()
+
+
+def _let_go() -> None:
+    """What ended objects held goes back once their last calls have ended; not
+    in a capture, where nothing may be waited for."""
+    if _kept and not torch.cuda.is_current_stream_capturing():
+        for _ in range(len(_kept)):
+            try:
+                held = _kept.pop()         # other threads' objects end here too
+            except IndexError:
+                return
+            held[0].synchronize()
 
 
 class Pages:
@@ -260,6 +272,7 @@ class ChunkAttention(StagingRing):
         self.ws_bytes = self.staging_bytes = 0
         self.ws_ptr = self._ws = self._pinned = None
         self._ring([None] * ring, event_every)
+        _let_go()
 
     def __del__(self):
         # the last call may still read the staging and write the workspace, and
@@ -268,10 +281,8 @@ class ChunkAttention(StagingRing):
         if last is None:
             return
         try:
-            if torch.cuda.is_current_stream_capturing():     # no synchronization in a capture
-                _kept.append((self._ws, self._pinned))
-            else:
-                last.synchronize()
+            _kept.append((last, self._ws, self._pinned))
+            _let_go()
         except Exception:                     # the interpreter or the device is going away
             pass
 

@@ -40,3 +40,32 @@ def test_a_captured_call_is_refused(gpu_lib, named):
         assert torch.equal(out, ref)
         out.zero_()
     assert (x == 4).all()
+
+
+def test_an_object_that_ends_inside_a_capture(gpu_lib):
+    """Its buffers stay until the capture is over, and not for good."""
+    import gc
+    from paper_2505_17074_amd import cache as module
+    print("[case] chunk object ends in a capture", flush=True)
+    gc.collect()
+    p = Paged([900], [2], 2, 128, seed=5).write()
+    q = queries(2, 8, 128, seed=5).cuda()
+    out, ref = (torch.zeros((2, 8, 128), dtype=BF16, device="cuda") for _ in range(2))
+    ChunkAttention(p.cache, 8).run(p.chunks(), q, ref)
+    assert not module._kept
+    x = torch.zeros(4, device="cuda")
+    att = ChunkAttention(p.cache, 8)
+    att.run(p.chunks(), q, out)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, capture_error_mode="relaxed"):
+        x.add_(1)
+        ws = att._ws.data_ptr()
+        del att
+        assert [w.data_ptr() for _, w, _ in module._kept] == [ws]
+    g.replay()
+    again = ChunkAttention(p.cache, 8)
+    assert not module._kept
+    again.run(p.chunks(), q, out)
+    torch.cuda.synchronize()
+    assert torch.equal(out, ref) and (x == 1).all()
