@@ -35,16 +35,15 @@ def _current_raw_stream(index: int) -> int:
     return torch.cuda.current_stream(index).cuda_stream
 
 
-# torch's own short way to the handle, where it has it (2 us less a call)
+# torch's own short ways, where it has them (2 us less a call)
 _current_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", _current_raw_stream)
+_capturing_here = getattr(torch._C, "_cuda_isCurrentStreamCapturing", torch.cuda.is_current_stream_capturing)
 
 
 def _capturing(stream: torch.cuda.Stream) -> bool:
-    """Whether a graph is being captured on the stream (of the current device)."""
-    if stream.cuda_stream == _current_raw_stream(stream.device_index):
-        return torch.cuda.is_current_stream_capturing()
+    """Whether a graph is being captured on the stream."""
     with torch.cuda.stream(stream):
-        return torch.cuda.is_current_stream_capturing()
+        return _capturing_here()
 
 
 def _let_go() -> None:
@@ -180,7 +179,7 @@ class PagedCache:
         width = 0 if t is None else B.int32(t.shape[1])
         stride = B.int32(t.stride(0)) if width and t.shape[0] > 1 else width
         self._table = t
-        self._streams = set()              # handles of the streams that table and pools are recorded on
+        self._streams = {}                 # the streams that table and pools are recorded on, by their handles
         self._rows = 0 if t is None else t.shape[0]
         self.c.block_table = t.data_ptr() if t is not None else None
         self.c.block_width = width
@@ -195,12 +194,14 @@ class PagedCache:
     def _stream(self, stream) -> int:
         h = _current_raw_stream(self._index) if stream is None else stream.cuda_stream
         if h not in self._streams:
-            s = stream or torch.cuda.current_stream(self._index)
-            for t in (self.k, self.v, self._table):
-                if t is not None:
-                    t.record_stream(s)
-            self._streams.add(h)
+            self._record(h, stream or torch.cuda.current_stream(self._index))
         return h
+
+    def _record(self, h: int, stream: torch.cuda.Stream) -> None:
+        for t in (self.k, self.v, self._table):
+            if t is not None:
+                t.record_stream(stream)
+        self._streams[h] = stream
 
     def _requests(self, n: int) -> None:
         if self._table is None or n > self._rows:
@@ -322,10 +323,10 @@ class ChunkAttention(StagingRing):
         a.q_stride_tok = st[0] if qs[0] > 1 else qs[1] * qs[2]
         a.q_stride_head = st[1] if qs[1] > 1 else qs[2]
         with cache._enter():
-            stream = stream or torch.cuda.current_stream(cache._index)
-            if _capturing(stream):
+            if _capturing_here() if stream is None else _capturing(stream):
                 raise RuntimeError("a graph's calls need a workspace and staging of their own: capture B.spec_chunk_attn")
             h = cache._stream(stream)
+            stream = stream or cache._streams[h]
             self._order(stream)
             for grown in (False, True):
                 s = self._slot(stream)
