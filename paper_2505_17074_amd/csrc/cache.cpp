@@ -152,19 +152,23 @@ spec_status_t plan_chunk(const spec_chunks_t* r, const spec_cache_t* c, const sp
   int64_t cap;
   if (!P.tall) {
     // Few rows: the keys stream past them at HBM's rate whatever the pieces, so
-    // they are cut to about 4 / 3 rounds of the work-groups that run at once
-    // (four a compute unit), where the last ones to end lose least, down to 128
-    // keys (64 where that leaves no compute unit two).  64 single tokens over
-    // 512-8192 rows: pieces of 1280 keys 190 us, 512 207, 4096 214; one over 2000
-    // rows of 8 KV heads: 64 keys 12.9, 128 14.9; over 4000: 15.2 and 14.6.
+    // they are cut to 16 / 3 of them a compute unit, about what runs there at once
+    // for d = 128 (five, by their 32 KB of LDS), where the last ones to end lose
+    // least, down to 128 keys (64 where that leaves no compute unit two).  64
+    // single tokens over 512-8192 rows: pieces of 1280 keys 190 us, 512 207, 4096
+    // 214; one over 2000 rows of 8 KV heads: 64 keys 12.9, 128 14.9; over 4000:
+    // 15.2 and 14.6.  All at d = 128; d = 64 goes by the same rule, though ten would
+    // fit: 64 single tokens over 4000 rows of 8 KV heads (524 MB) 86 us, 6.1 TB/s.
     const int64_t slots = 4 * (int64_t)cus;
     cap = std::max<int64_t>(total <= cus ? 1 : 2, (3 * total + 4 * slots - 1) / (4 * slots));
   } else {
     // Many rows: a compute unit takes a 64-key tile in about a microsecond,
-    // whether one work-group runs on it or two, so the longest item bounds the
-    // kernel only where it is longer than a unit's mean share.  Only then is
-    // it cut, and where that saves more than the join costs (about seven
-    // tiles).  2048 new tokens, the longest 32 tiles of a mean of 33: whole
+    // whether one work-group runs on it or two (1.1-1.2 and 0.94), so the longest
+    // item bounds the kernel only where it is longer than a unit's mean share.
+    // Only then is it cut, and where that saves more than the join costs (about
+    // seven tiles).  Measured at d = 128 with a bf16 output, and used for d = 64
+    // (three work-groups a unit) and fp32 outputs as it is; a tile of few rows
+    // counts like a full one.  2048 new tokens, the longest 32 tiles of a mean of 33: whole
     // 48 us, pieces of 24 tiles 62, 16 64, 8 79; 1024, 16 of 9: whole 25, cut
     // 27; 64 over 2000 rows, 33 of 3: whole 40, pieces of 12 tiles 22, 8 20,
     // 4 17.  Decoding requests beside a chunk run in the same launch (beside 8
@@ -184,11 +188,12 @@ spec_status_t plan_chunk(const spec_chunks_t* r, const spec_cache_t* c, const sp
   if (n_items * Hkv >= (int64_t)1 << 24) return SPEC_ERR_UNSUPPORTED;      // a launch's work-items are 32 bits
   // The longest first, so that the last to start are the shortest; after each,
   // its request's neighbouring row tiles down to 7 / 8 of its length, which
-  // read the same keys: with the heads innermost they run on the same XCD
-  // (work-group b on XCD b % 8) at the same time (64 requests of 64 tokens over
-  // 4000 rows 357 us, by length alone 419).  Single tokens share nothing, and
-  // there a head's pieces follow each other (64 of them 192 us, heads
-  // innermost 199).
+  // read the same keys at the same time.  With the heads innermost they also
+  // run on the same XCD (work-group b on XCD b % 8) where the KV heads are a
+  // multiple of eight (64 requests of 64 tokens over 4000 rows, 8 KV heads, 357
+  // us, by length alone 419); four heads spread a head's tiles over two XCDs, one
+  // over all.  Single tokens share nothing, and there a head's pieces follow
+  // each other (64 of them 192 us, heads innermost 199).
   std::vector<int32_t> order, sorted(tiles.size());
   order.reserve(tiles.size());
   for (size_t i = 0; i < tiles.size(); ++i) sorted[i] = (int32_t)i;
@@ -222,8 +227,9 @@ spec_status_t plan_chunk(const spec_chunks_t* r, const spec_cache_t* c, const sp
       P.parts += (int64_t)Hkv * t.pieces * t.rows;
     }
   }
-  // work-groups b and b + cus of the tall kernel share a compute unit at first:
-  // the longest with the shortest of the first two rounds
+  // work-groups b and b + cus of the tall kernel share a compute unit at first
+  // (d = 128; with d = 64 a third joins them): the longest with the shortest of
+  // the first two rounds
   if (P.tall && n_items * Hkv > cus) {
     P.turn0 = cus;
     P.turn1 = (int32_t)std::min<int64_t>(n_items * Hkv, 2 * (int64_t)cus);

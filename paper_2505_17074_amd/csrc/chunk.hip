@@ -8,7 +8,7 @@
 // of a whole call, those under 20 us in a row):
 //   few: HBM.  64 single tokens over 512-8192 rows, 8 KV heads under 32 query
 //     heads (1.16 GB): 191 us, 6.1 TB/s (a plain read stream reaches 6.5); one
-//     over 1000 rows (4 MB): 11-15 us, two launches of 7.2 and 4.2.
+//     over 1000 rows (4 MB): 11-15 us, two launches of 7.8 and 4.1.
 //   many: the matrix cores, at the clock that their power leaves (1.67-1.75 GHz).
 //     1024 tokens over 30011 rows, 8 heads a group (1.02 TFLOP): 902-975 us,
 //     1.05-1.13 PFLOP/s, MFMA busy 61-64 % (the library's 8192^3 product 1.2).
@@ -16,9 +16,11 @@
 //     longest row tile's 32 key tiles, 1.1-1.2 us each on a compute unit that the
 //     shorter ones have left (0.94 where two row tiles share it), and the start.
 //   both: 8 chunks of 33-700 tokens and 16 single ones, 32 heads of their own
-//     (671 MB, 73 GFLOP): 150 us, 4.5 TB/s.
+//     (671 MB, 73 GFLOP): 151 us, 4.5 TB/s; MFMA busy 33 %, a fifth of it for the
+//     empty rows of partly filled tiles.
 // An fp32 output has three products with V for one: 16 requests of 1-400 tokens
-// over 0-1500 rows, d = 64: 38 us.
+// over 0-1500 rows, d = 64: 38 us, MFMA busy 31 %, 1.2 waves a SIMD on average:
+// the longest items' 28 key tiles (a unit's mean share is 25) outlast the rest.
 #include "sv_chunk.h"
 
 #include <type_traits>
@@ -297,8 +299,8 @@ __device__ __forceinline__ void one_by_one(const Fetch& f, Rows<D>& S, int t, in
 // and factor are one lane's (and its partner's 32 lanes on), and the operand
 // that all waves share is the one read from LDS.  Four waves a work-group and
 // 64-key tiles (128 KB of LDS for the two on a compute unit) where a KV head has
-// more than 32 query rows, else one wave, 32-key tiles and four work-groups a
-// compute unit.  Long case above: 64 rows a wave 1197 us (the accumulators move
+// more than 32 query rows, else one wave, 32-key tiles and five work-groups a
+// compute unit (d = 64: three and ten).  Long case above: 64 rows a wave 1197 us (the accumulators move
 // between register files), eight waves 928 (a 2048-token prompt 71 for 46),
 // 32-key tiles in four stages 1000, 64-row work-groups 1089.
 // MFMA row m of S^T holds key 16 (m >> 4) + 8 ((m >> 2) & 1) + 4 ((m >> 3) & 1)
