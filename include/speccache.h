@@ -104,10 +104,10 @@ typedef struct spec_chunks {
  * and infinities included, whether it is a later token's row, a row behind
  * the request's end in its last page, or another request's page.
  * Where such values lie among keys that are read, the rows concerned are
- * computed a second time: a long call takes about four times as long, a short
- * one up to 0.1 ms more.  The sums over V are not normalised before the last
- * step and may reach 2^8 times the keys' number times V's largest value, which
- * has to stay in fp32's range.
+ * computed a second time: a call takes up to about five times as long, or up
+ * to 0.1 ms more where that is longer.  The sums over V are not normalised
+ * before the last step and may reach 2^8 times the keys' number times V's
+ * largest value, which has to stay in fp32's range.
  * Long key ranges are cut into pieces whose partial outputs a second kernel
  * joins, where the batch alone would leave compute units idle; the cut depends
  * on the lengths, the head counts and the device alone, and results are

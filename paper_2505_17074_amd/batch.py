@@ -154,6 +154,9 @@ class Verifier(StagingRing):
     """Runs spec_verify / spec_verify_attn / spec_accept on one DeviceBatch.
 
     Owns the device workspace and `ring` pinned staging buffers (StagingRing).
+    A graph is captured from the library's calls (binding) with a workspace and
+    staging of its own: a replay reads the staging it was captured with, which
+    later calls of the ring write again.
     """
 
     def __init__(self, batch: DeviceBatch, split_kv: int = 0, ring: int = 32, event_every: int = 8,
