@@ -248,6 +248,9 @@ def load(path: str = LIB_PATH) -> C.CDLL:
     lib.spec_accept_floor_probe.argtypes = [C.c_void_p, C.c_int64, C.c_int32, C.c_int32, C.c_int32, C.c_int32,
                                             C.c_void_p, C.c_size_t, C.c_void_p, C.c_void_p]
     lib.spec_accept_floor_probe.restype = C.c_int
+    # the HIP runtime that the library is linked with
+    lib.hipStreamIsCapturing.argtypes = [C.c_void_p, C.c_void_p]
+    lib.hipStreamIsCapturing.restype = C.c_int
     lib.spec_chunk_workspace_bytes.argtypes = [P(SpecChunks), P(SpecCache), P(SpecChunkAttnArgs), P(C.c_size_t),
                                                P(C.c_size_t)]
     lib.spec_chunk_workspace_bytes.restype = C.c_int
@@ -359,6 +362,16 @@ def spec_accept_floor_probe_bytes(V, num_rows, B):
 
 def spec_accept_floor_probe(rows, row_stride, elem_bytes, V, num_rows, B, ws, ws_bytes, out, stream):
     return load().spec_accept_floor_probe(rows, row_stride, elem_bytes, V, num_rows, B, ws, ws_bytes, out, stream)
+
+
+def stream_capturing(stream: int) -> bool:
+    """Whether a graph is being captured on the stream (a handle; the null
+    stream cannot be captured).  torch asks of the current stream only, and
+    making another one current takes 6 us."""
+    if not stream:
+        return False
+    status = C.c_int()
+    return load().hipStreamIsCapturing(stream, C.byref(status)) == 0 and status.value != 0
 
 
 def spec_chunk_workspace_bytes(chunks: SpecChunks, cache: SpecCache, args: SpecChunkAttnArgs):
