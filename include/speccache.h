@@ -165,6 +165,51 @@ SPEC_API spec_status_t spec_cache_append(const spec_chunks_t* chunks, const spec
                                          const spec_append_args_t* args, void* stream);
 
 /*
+ * The same with the position rotation on the way: each new row of K, and of
+ * the queries beside it, turned by its position, V as it is.  For pair i of
+ * rotary_dim / 2, position p and the angle a = p freq[i] (radians),
+ *   (x, y) -> (x cos a - y sin a, y cos a + x sin a),
+ * the products and sums in fp32 (cos and sin off by 2^-23 at most, whatever p:
+ * the angle and its turns are taken in 64 bits), each result rounded once.
+ *   rotary_dim   the elements of a head that are turned, its first (an even
+ *                number, up to head_dim and 512); the others are copied.  Pairs
+ *                are elements i and i + rotary_dim / 2, or, with interleaved =
+ *                1, 2 i and 2 i + 1.  Both halves (interleaved: rotary_dim) have
+ *                to be whole 16-byte units (SPEC_ERR_UNSUPPORTED otherwise).
+ *   freq         fp32 [rotary_dim / 2] (device): radians a position, whatever
+ *                scaling for long contexts they hold.
+ *   positions    int32 [Nq] (device), one a new row, any value: the nodes of a
+ *                token tree have ctx_len + depth, so that an accepted path's
+ *                rows are right where spec_cache_commit moves them.  NULL: the
+ *                row's place in its request, ctx_len[i] + r.
+ *   q, q_out     [Nq, num_q_heads, d] in the cache's dtype, strides in elements,
+ *                last dim contiguous, 16-byte aligned rows.  q_out is q itself
+ *                (with the same strides) or overlaps nothing that the call reads
+ *                or writes.  num_q_heads 0: no queries (the four strides are
+ *                ignored).  With queries num_layers is 1.
+ * Rows of q_out past Nq, and rows of K and V whose page id is outside the pool,
+ * are left as they are.
+ */
+typedef struct spec_rotation {
+  int32_t rotary_dim;
+  int32_t interleaved;
+  const float* freq;
+  const int32_t* positions;
+  int32_t num_q_heads;
+  int32_t pad0;
+  const void* q;
+  int64_t q_stride_tok;
+  int64_t q_stride_head;
+  void* q_out;
+  int64_t out_stride_tok;
+  int64_t out_stride_head;
+} spec_rotation_t;
+
+SPEC_API spec_status_t spec_cache_append_rotated(const spec_chunks_t* chunks, const spec_cache_t* cache,
+                                                 const spec_append_args_t* args, const spec_rotation_t* rotation,
+                                                 void* stream);
+
+/*
  * After a round: moves the rows of each request's accepted path behind its
  * context, in every layer of the cache.  Request i's verify rows sit at its
  * logical rows ctx_len[i] + node (as spec_verify_attn reads them); the path

@@ -26,7 +26,7 @@ EXPORTS = ("spec_workspace_bytes", "spec_verify_attn", "spec_accept", "spec_veri
            "spec_status_str", "spec_abi_version", "spec_stream_read_probe", "spec_accept_floor_probe",
            "spec_accept_floor_probe_bytes", "spec_verify_noalloc",
            "spec_lm_head_accept", "spec_lm_head_workspace_bytes",
-           "spec_chunk_workspace_bytes", "spec_chunk_attn", "spec_cache_append", "spec_cache_commit",
+           "spec_chunk_workspace_bytes", "spec_chunk_attn", "spec_cache_append", "spec_cache_append_rotated", "spec_cache_commit",
            "spec_cache_copy_pages", "spec_pages_create", "spec_pages_destroy", "spec_pages_open",
            "spec_pages_resize", "spec_pages_fork", "spec_pages_close", "spec_pages_table", "spec_pages_compact",
            "spec_pages_free_count",
@@ -147,6 +147,21 @@ class SpecAppendArgs(C.Structure):
                 ("new_stride_head", C.c_int64)]
 
 
+class SpecRotation(C.Structure):
+    _fields_ = [("rotary_dim", C.c_int32),
+                ("interleaved", C.c_int32),
+                ("freq", C.c_void_p),
+                ("positions", C.c_void_p),
+                ("num_q_heads", C.c_int32),
+                ("pad0", C.c_int32),
+                ("q", C.c_void_p),
+                ("q_stride_tok", C.c_int64),
+                ("q_stride_head", C.c_int64),
+                ("q_out", C.c_void_p),
+                ("out_stride_tok", C.c_int64),
+                ("out_stride_head", C.c_int64)]
+
+
 class SpecPageCopy(C.Structure):
     _fields_ = [("src", C.c_int32), ("dst", C.c_int32), ("tokens", C.c_int32)]
 
@@ -259,6 +274,8 @@ def load(path: str = LIB_PATH) -> C.CDLL:
     lib.spec_chunk_attn.restype = C.c_int
     lib.spec_cache_append.argtypes = [P(SpecChunks), P(SpecCache), P(SpecAppendArgs), C.c_void_p]
     lib.spec_cache_append.restype = C.c_int
+    lib.spec_cache_append_rotated.argtypes = [P(SpecChunks), P(SpecCache), P(SpecAppendArgs), P(SpecRotation), C.c_void_p]
+    lib.spec_cache_append_rotated.restype = C.c_int
     lib.spec_cache_commit.argtypes = [P(SpecRequests), P(SpecCache), C.c_void_p, C.c_void_p]
     lib.spec_cache_commit.restype = C.c_int
     lib.spec_cache_copy_pages.argtypes = [P(SpecCache), C.c_void_p, C.c_int32, C.c_void_p]
@@ -387,6 +404,10 @@ def spec_chunk_attn(chunks, cache, args, ws: int, ws_bytes: int, staging: int, s
 
 def spec_cache_append(chunks, cache, args, stream: int) -> int:
     return load().spec_cache_append(_ref(chunks), _ref(cache), _ref(args), stream)
+
+
+def spec_cache_append_rotated(chunks, cache, args, rotation, stream: int) -> int:
+    return load().spec_cache_append_rotated(_ref(chunks), _ref(cache), _ref(args), _ref(rotation), stream)
 
 
 def spec_cache_commit(req, cache, accepted_node: int, stream: int) -> int:

@@ -150,6 +150,8 @@ class PagedCache:
         self._ref = C.byref(c)
         self._append = B.SpecAppendArgs()
         self._append_ref = C.byref(self._append)
+        self._rotation = B.SpecRotation()
+        self._rotation_ref = C.byref(self._rotation)
         c.num_layers, c.num_pages, c.page_tokens, c.num_kv_heads, c.head_dim = k.shape
         c.dtype = _DTYPE[k.dtype]
         c.k, c.v = k.data_ptr(), v.data_ptr()
@@ -200,10 +202,8 @@ class PagedCache:
         if self._table is None or n > self._rows:
             raise ValueError("the block table has no row for every request")
 
-    def append(self, chunks: B.SpecChunks, k_new: torch.Tensor, v_new: torch.Tensor, layer: int = 0,
-               stream: Optional[torch.cuda.Stream] = None) -> None:
-        """Rows k_new, v_new [layers, rows, Hkv, d] (or [rows, Hkv, d]: one layer)
-        to the ends of the requests, in the cache's layers from `layer` on."""
+    def _new_rows(self, chunks: B.SpecChunks, k_new: torch.Tensor, v_new: torch.Tensor, layer: int) -> int:
+        """The append arguments; the number of layers."""
         shape, st = k_new.shape, k_new.stride()
         if not _alike(k_new, v_new) or len(shape) not in (3, 4) or \
                 shape[-2:] != self._head or shape[-3] < chunks.rows or (st[-1] != 1 and shape[-1] > 1):
@@ -219,9 +219,58 @@ class PagedCache:
         a.new_stride_layer = st[0]
         a.new_stride_tok = st[-3] if shape[-3] > 1 else width
         a.new_stride_head = st[-2] if shape[-2] > 1 else shape[-1]
+        return a.num_layers
+
+    def append(self, chunks: B.SpecChunks, k_new: torch.Tensor, v_new: torch.Tensor, layer: int = 0,
+               stream: Optional[torch.cuda.Stream] = None) -> None:
+        """Rows k_new, v_new [layers, rows, Hkv, d] (or [rows, Hkv, d]: one layer)
+        to the ends of the requests, in the cache's layers from `layer` on."""
+        self._new_rows(chunks, k_new, v_new, layer)
         with self._enter():
             B.check(self._lib.spec_cache_append(chunks, self._ref, self._append_ref, self._stream(stream)),
                     "spec_cache_append")
+
+    def append_rotated(self, chunks: B.SpecChunks, k_new: torch.Tensor, v_new: torch.Tensor, freq: torch.Tensor,
+                       q: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None,
+                       positions: Optional[torch.Tensor] = None, interleaved: bool = False, layer: int = 0,
+                       stream: Optional[torch.cuda.Stream] = None) -> None:
+        """append with K, and the queries q [rows, Hq, d] into q_out (or in place:
+        q_out = q), turned by their positions on the way: pair i of a head's first
+        2 len(freq) elements by position x freq[i] radians.  Pairs are elements i
+        and i + len(freq), or, interleaved, 2 i and 2 i + 1.  freq is fp32;
+        positions int32 [rows], without them a row's place in its request."""
+        layers = self._new_rows(chunks, k_new, v_new, layer)
+        rows = chunks.rows
+        if freq.dtype != torch.float32 or freq.dim() != 1 or freq.device != self.device or _stride(freq, 0, 1) != 1:
+            raise ValueError("freq is fp32 [rotary dim / 2] on the pools' device")
+        if positions is not None and (positions.dtype != torch.int32 or positions.dim() != 1 or
+                                      positions.device != self.device or positions.shape[0] < rows or
+                                      _stride(positions, 0, 1) != 1):
+            raise ValueError("positions are int32 [rows] on the pools' device")
+        r = self._rotation
+        r.rotary_dim, r.interleaved = 2 * freq.shape[0], 1 if interleaved else 0
+        r.freq = freq.data_ptr()
+        r.positions = None if positions is None else positions.data_ptr()
+        r.num_q_heads = 0
+        if (q is None) != (q_out is None):
+            raise ValueError("q and q_out go together")
+        if q is not None:
+            if layers != 1:
+                raise ValueError("queries belong to one layer")
+            for t in (q, q_out):
+                if t.dim() != 3 or t.shape[0] < rows or t.shape[1] != q.shape[1] or t.shape[1] < 1 or \
+                        t.shape[2] != self._head[1] or (t.stride(2) != 1 and t.shape[2] > 1):
+                    raise ValueError("q and q_out are [rows, Hq, d], a row for every new token")
+                if t.dtype != self.dtype or t.device != self.device:
+                    raise ValueError("q and q_out have the pools' type and device")
+            r.num_q_heads = q.shape[1]
+            wide = q.shape[1] * q.shape[2]
+            r.q, r.q_out = q.data_ptr(), q_out.data_ptr()
+            r.q_stride_tok, r.q_stride_head = _stride(q, 0, wide), _stride(q, 1, q.shape[2])
+            r.out_stride_tok, r.out_stride_head = _stride(q_out, 0, wide), _stride(q_out, 1, q.shape[2])
+        with self._enter():
+            B.check(self._lib.spec_cache_append_rotated(chunks, self._ref, self._append_ref, self._rotation_ref,
+                                                        self._stream(stream)), "spec_cache_append_rotated")
 
     def commit(self, req: B.SpecRequests, accepted_node: torch.Tensor,
                stream: Optional[torch.cuda.Stream] = None) -> None:

@@ -266,6 +266,64 @@ sv::CachePools pools(const spec_cache_t* c, int layer, bool one_run) {
 sv::MoveLaunch move_launch(const sv::CachePools& p, int layers, int64_t rows) {
   return {layers, rows * p.heads * p.row_units * 16 * 2 * layers >= sv::kMoveStream};
 }
+// The new rows as segments of at most `parts` blocks of `rows` rows, in launches
+// of up to kMoveSegments of them: as few blocks as keep the batch in one launch's
+// table, so that ragged batches leave few work-groups without rows; a single
+// request's rows are one segment.
+template <typename P, typename F>
+spec_status_t in_segments(const spec_chunks_t* chunks, int rows, P& p, F&& launch) {
+  auto blocks = [&](int i) -> int64_t {
+    const int64_t lo = chunks->ctx_len[i], n = chunks->new_len[i];
+    return n ? (lo + n - 1) / rows - lo / rows + 1 : 0;
+  };
+  int64_t longest = 0, all = 0;
+  for (int i = 0; i < chunks->num_requests; ++i) {
+    longest = std::max(longest, blocks(i));
+    all += blocks(i);
+  }
+  int64_t parts = longest == all && all < 1 << 16 ? std::max<int64_t>(longest, 1) : 1;
+  for (;; parts *= 2) {
+    int64_t segs = 0;
+    for (int i = 0; i < chunks->num_requests; ++i) segs += (blocks(i) + parts - 1) / parts;
+    if (segs <= sv::kMoveSegments || parts >= longest) break;
+  }
+  int64_t row = 0;
+  int n_seg = 0;
+  for (int i = 0; i < chunks->num_requests; ++i) {
+    int32_t pos = chunks->ctx_len[i];
+    const int32_t end = pos + chunks->new_len[i];
+    while (pos < end) {
+      const int32_t stop = (int32_t)std::min<int64_t>(end, (pos / rows + parts) * rows);
+      p.seg[n_seg++] = {i, pos, (int32_t)row, stop - pos};
+      row += stop - pos;
+      pos = stop;
+      if (n_seg == sv::kMoveSegments) {
+        if (launch(n_seg, (int)parts) != hipSuccess) return SPEC_ERR_HIP;
+        n_seg = 0;
+      }
+    }
+  }
+  if (n_seg > 0 && launch(n_seg, (int)parts) != hipSuccess) return SPEC_ERR_HIP;
+  return SPEC_OK;
+}
+
+// The checks of an append: lengths, layers, the new rows' strides.
+spec_status_t check_append(const spec_chunks_t* chunks, const spec_cache_t* cache, const spec_append_args_t* args,
+                           int64_t* rows) {
+  spec_status_t st = check_cache(cache, true);
+  if (st != SPEC_OK) return st;
+  if ((st = check_chunks(chunks, cache, rows)) != SPEC_OK) return st;
+  if (!args || args->layer < 0 || args->num_layers < 1 || args->layer > cache->num_layers - args->num_layers)
+    return SPEC_ERR_INVALID_ARG;
+  if (*rows > 0 && (!args->k_new || !args->v_new)) return SPEC_ERR_INVALID_ARG;
+  if (!aligned16(args->k_new) || !aligned16(args->v_new)) return SPEC_ERR_INVALID_ARG;
+  const int64_t vec = 16 / elem_bytes(cache->dtype);
+  if (args->new_stride_tok < 1 || args->new_stride_head < 1 || args->new_stride_tok % vec ||
+      args->new_stride_head % vec)
+    return SPEC_ERR_INVALID_ARG;
+  if (args->num_layers > 1 && (args->new_stride_layer < 1 || args->new_stride_layer % vec)) return SPEC_ERR_INVALID_ARG;
+  return SPEC_OK;
+}
 bool heads_touch(const spec_cache_t* c) { return c->num_kv_heads == 1 || c->kv_stride_head == c->head_dim; }
 
 }  // namespace
@@ -349,20 +407,10 @@ spec_status_t spec_chunk_attn(const spec_chunks_t* chunks, const spec_cache_t* c
 
 spec_status_t spec_cache_append(const spec_chunks_t* chunks, const spec_cache_t* cache, const spec_append_args_t* args,
                                 void* stream) {
-  spec_status_t st = check_cache(cache, true);
-  if (st != SPEC_OK) return st;
   int64_t nq = 0;
-  if ((st = check_chunks(chunks, cache, &nq)) != SPEC_OK) return st;
-  if (!args || args->layer < 0 || args->num_layers < 1 || args->layer > cache->num_layers - args->num_layers)
-    return SPEC_ERR_INVALID_ARG;
-  if (nq > 0 && (!args->k_new || !args->v_new)) return SPEC_ERR_INVALID_ARG;
-  if (!aligned16(args->k_new) || !aligned16(args->v_new)) return SPEC_ERR_INVALID_ARG;
-  const int64_t eb = elem_bytes(cache->dtype), vec = 16 / eb;
-  if (args->new_stride_tok < 1 || args->new_stride_head < 1 || args->new_stride_tok % vec ||
-      args->new_stride_head % vec)
-    return SPEC_ERR_INVALID_ARG;
-  if (args->num_layers > 1 && (args->new_stride_layer < 1 || args->new_stride_layer % vec)) return SPEC_ERR_INVALID_ARG;
-
+  const spec_status_t st = check_append(chunks, cache, args, &nq);
+  if (st != SPEC_OK) return st;
+  const int64_t eb = elem_bytes(cache->dtype);
   const bool touch = heads_touch(cache) && (cache->num_kv_heads == 1 || args->new_stride_head == cache->head_dim);
   if (!touch && args->new_stride_head * eb / 16 > INT32_MAX) return SPEC_ERR_UNSUPPORTED;
   sv::AppendParams<sv::kMoveSegments> p{};
@@ -375,43 +423,67 @@ spec_status_t spec_cache_append(const spec_chunks_t* chunks, const spec_cache_t*
   p.new_sh = touch ? 0 : (int32_t)(args->new_stride_head * eb / 16);
   p.bt_stride = cache->block_stride;
   p.bt = cache->block_table;
-  // Segments of at most `parts` blocks of 16 rows: as few blocks as keep the
-  // batch in one launch's table, so that ragged batches leave few work-groups
-  // without rows; a single request's rows are one segment.
-  auto blocks = [&](int i) -> int64_t {
-    const int64_t lo = chunks->ctx_len[i], n = chunks->new_len[i];
-    return n ? (lo + n - 1) / sv::kMoveRows - lo / sv::kMoveRows + 1 : 0;
-  };
-  int64_t longest = 0, all = 0;
-  for (int i = 0; i < chunks->num_requests; ++i) {
-    longest = std::max(longest, blocks(i));
-    all += blocks(i);
-  }
-  int64_t parts = longest == all && all < 1 << 16 ? std::max<int64_t>(longest, 1) : 1;
-  for (;; parts *= 2) {
-    int64_t segs = 0;
-    for (int i = 0; i < chunks->num_requests; ++i) segs += (blocks(i) + parts - 1) / parts;
-    if (segs <= sv::kMoveSegments || parts >= longest) break;
-  }
   hipStream_t s = static_cast<hipStream_t>(stream);
-  int64_t row = 0;
-  int n_seg = 0;
-  for (int i = 0; i < chunks->num_requests; ++i) {
-    int32_t pos = chunks->ctx_len[i];
-    const int32_t end = pos + chunks->new_len[i];
-    while (pos < end) {
-      const int32_t stop = (int32_t)std::min<int64_t>(end, (pos / sv::kMoveRows + parts) * sv::kMoveRows);
-      p.seg[n_seg++] = {i, pos, (int32_t)row, stop - pos};
-      row += stop - pos;
-      pos = stop;
-      if (n_seg == sv::kMoveSegments) {
-        if (sv::launch_append(p, n_seg, (int)parts, l, s) != hipSuccess) return SPEC_ERR_HIP;
-        n_seg = 0;
-      }
-    }
+  return in_segments(chunks, sv::kMoveRows, p, [&](int n, int parts) { return sv::launch_append(p, n, parts, l, s); });
+}
+
+spec_status_t spec_cache_append_rotated(const spec_chunks_t* chunks, const spec_cache_t* cache,
+                                        const spec_append_args_t* args, const spec_rotation_t* rot, void* stream) {
+  int64_t nq = 0;
+  const spec_status_t st = check_append(chunks, cache, args, &nq);
+  if (st != SPEC_OK) return st;
+  const int64_t eb = elem_bytes(cache->dtype), vec = 16 / eb;
+  if (!rot || rot->rotary_dim < 2 || rot->rotary_dim % 2 || rot->rotary_dim > cache->head_dim) return SPEC_ERR_INVALID_ARG;
+  if (rot->interleaved != 0 && rot->interleaved != 1) return SPEC_ERR_INVALID_ARG;
+  if (reinterpret_cast<uintptr_t>(rot->freq) % 4 || reinterpret_cast<uintptr_t>(rot->positions) % 4)
+    return SPEC_ERR_INVALID_ARG;
+  if (nq > 0 && !rot->freq) return SPEC_ERR_INVALID_ARG;
+  // whole 16-byte units on both sides of a pair; the angles of a work-group's rows lie in LDS
+  if (rot->rotary_dim % (rot->interleaved ? vec : 2 * vec) || rot->rotary_dim > 2 * sv::kMaxTurned) return SPEC_ERR_UNSUPPORTED;
+  if (rot->num_q_heads < 0) return SPEC_ERR_INVALID_ARG;
+  if (rot->num_q_heads > 0) {
+    if (args->num_layers != 1) return SPEC_ERR_INVALID_ARG;
+    if (nq > 0 && (!rot->q || !rot->q_out)) return SPEC_ERR_INVALID_ARG;
+    if (!aligned16(rot->q) || !aligned16(rot->q_out)) return SPEC_ERR_INVALID_ARG;
+    for (const int64_t x : {rot->q_stride_tok, rot->q_stride_head, rot->out_stride_tok, rot->out_stride_head})
+      if (x < 1 || x % vec) return SPEC_ERR_INVALID_ARG;
+    // rows that are written do not overlap
+    if (rot->num_q_heads > 1 && rot->out_stride_head < cache->head_dim) return SPEC_ERR_INVALID_ARG;
+    if (nq > 1 && rot->out_stride_tok < (rot->num_q_heads - 1) * rot->out_stride_head + cache->head_dim)
+      return SPEC_ERR_INVALID_ARG;
+    if (rot->q == rot->q_out && (rot->q_stride_tok != rot->out_stride_tok || rot->q_stride_head != rot->out_stride_head))
+      return SPEC_ERR_INVALID_ARG;
+    if (std::max(rot->q_stride_head, rot->out_stride_head) * eb / 16 > INT32_MAX) return SPEC_ERR_UNSUPPORTED;
   }
-  if (n_seg > 0 && sv::launch_append(p, n_seg, (int)parts, l, s) != hipSuccess) return SPEC_ERR_HIP;
-  return SPEC_OK;
+  if (args->new_stride_head * eb / 16 > INT32_MAX) return SPEC_ERR_UNSUPPORTED;
+  // a work-group counts its rows' heads and columns in 32 bits
+  if (((int64_t)rot->num_q_heads + 2 * (int64_t)cache->num_kv_heads) * cache->head_dim >= 1 << 26) return SPEC_ERR_UNSUPPORTED;
+  sv::RotateParams<sv::kMoveSegments> p{};
+  p.c = pools(cache, args->layer, false);
+  const sv::MoveLaunch l = move_launch(p.c, args->num_layers, nq);
+  p.k_new = static_cast<const char*>(args->k_new);
+  p.v_new = static_cast<const char*>(args->v_new);
+  p.new_sl = args->num_layers > 1 ? args->new_stride_layer * eb : 0;
+  p.new_st = args->new_stride_tok * eb;
+  p.new_sh = (int32_t)(args->new_stride_head * eb / 16);
+  p.q_heads = rot->num_q_heads;
+  if (p.q_heads > 0) {
+    p.q = static_cast<const char*>(rot->q);
+    p.q_out = static_cast<char*>(rot->q_out);
+    p.q_st = rot->q_stride_tok * eb;
+    p.out_st = rot->out_stride_tok * eb;
+    p.q_sh = (int32_t)(rot->q_stride_head * eb / 16);
+    p.out_sh = (int32_t)(rot->out_stride_head * eb / 16);
+  }
+  p.pairs = rot->rotary_dim / 2;
+  p.freq = rot->freq;
+  p.positions = rot->positions;
+  p.bt = cache->block_table;
+  p.bt_stride = cache->block_stride;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  return in_segments(chunks, sv::kTurnRows, p, [&](int n, int parts) {
+    return sv::launch_rotate(p, n, parts, l, cache->dtype == SPEC_F32, rot->interleaved != 0, s);
+  });
 }
 
 spec_status_t spec_cache_commit(const spec_requests_t* req, const spec_cache_t* cache, const int32_t* accepted_node,

@@ -15,6 +15,8 @@ __device__ __forceinline__ int64_t readlane64(int64_t x, int lane) {
 }
 
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 
 __device__ __forceinline__ int64_t page_bytes(const CachePools& c) { return (int64_t)c.page_tokens * c.st_bytes; }
 
@@ -66,6 +68,174 @@ __global__ __launch_bounds__(256) void cache_append(AppendParams<N> p) {
 #pragma unroll
     for (int i = 0; i < kMoveRows / 4; ++i)
       if (w + 4 * i < n) store<STREAM>(to + (w + 4 * i) * (int64_t)p.c.st_bytes, x[i]);
+  }
+}
+
+// cos and sin of p f, an angle in radians, for a whole number p and an fp32 f:
+// the product and its turns in 64 bits (p f has up to 55 bits, off by 2^-53 of
+// it; an angle of 2^20 turns is off by 2^-32 of one), the rest within an eighth of
+// a turn by the series, whose next terms are below 2^-28.
+__device__ __forceinline__ float2 cos_sin(int32_t p, float f) {
+  const double turns4 = (double)p * (double)f * 0.63661977236758134308;      // quarter turns: 2 / pi
+  const double whole = __builtin_rint(turns4);
+  const float x = (float)((turns4 - whole) * 1.57079632679489661923);
+  const float y = x * x;
+  const float s = x + x * y * fmaf(y, fmaf(y, fmaf(y, 2.7557319e-6f, -1.9841270e-4f), 8.3333333e-3f), -1.6666667e-1f);
+  const float c = fmaf(y, fmaf(y, fmaf(y, fmaf(y, fmaf(y, -2.7557319e-7f, 2.4801587e-5f), -1.3888889e-3f), 4.1666667e-2f), -0.5f), 1.f);
+  // the quadrant: whole mod 4 (whole / 4 may have more than 32 bits)
+  const int q = (int)(whole - 4.0 * __builtin_floor(whole * 0.25));
+  const float a = q & 1 ? s : c, b = q & 1 ? c : s;
+  return make_float2(q == 1 || q == 2 ? -a : a, q >= 2 ? -b : b);
+}
+
+template <bool F32>
+struct Turned {                        // a 16-byte unit's elements in fp32
+  static constexpr int VEC = F32 ? 4 : 8;
+  float x[VEC];
+  __device__ __forceinline__ explicit Turned(u32x4 u) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if constexpr (F32) {
+        x[i] = __uint_as_float(u[i]);
+      } else {
+        x[2 * i] = __uint_as_float(u[i] << 16);
+        x[2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u);
+      }
+    }
+  }
+  __device__ __forceinline__ u32x4 pack() const {
+    u32x4 u;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if constexpr (F32) u[i] = __float_as_uint(x[i]);
+      else u[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2){x[2 * i], x[2 * i + 1]}, bf16x2));
+    }
+    return u;
+  }
+};
+
+// Appended rows, K and the queries rotated on the way: for pair i of a head's
+// first 2 `pairs` elements and angle p f_i,
+//   (x, y) -> (x cos - y sin, y cos + x sin),
+// in fp32, each result rounded once.  Pairs are elements i and i + pairs, or 2 i
+// and 2 i + 1 (INTER).
+// blockIdx: (block of 4 rows, segment, layer).  The block's angles are computed
+// once, into LDS, beside the first loads; a thread keeps its columns of a head
+// (two units, INTER or without a partner one) and goes from head to head and
+// row to row, the queries' heads first, then K's and V's.
+template <bool F32, bool INTER, bool STREAM, int N>
+__global__ __launch_bounds__(256) void cache_append_rotated(RotateParams<N> p) {
+  constexpr int VEC = Turned<F32>::VEC, AHEAD = 4;
+  __shared__ float cs[kTurnRows][2][kMaxTurned];
+  const AppendSegment sg = p.seg[N > 1 ? blockIdx.y : 0];
+  const int b0 = (sg.pos & ~(kTurnRows - 1)) + kTurnRows * (int)blockIdx.x;
+  const int lo = max(b0, sg.pos), n = min(b0 + kTurnRows, sg.pos + sg.n) - lo;
+  if (n <= 0) return;
+  const int pg = p.bt[(int64_t)sg.req * p.bt_stride + lo / p.c.page_tokens];
+  const bool kept = pg >= 0 && pg < p.c.num_pages;
+  const int layer = blockIdx.z;
+  const int64_t at = layer * p.c.layer_bytes + (kept ? pg : 0) * page_bytes(p.c) +
+                     (int64_t)(lo % p.c.page_tokens) * p.c.st_bytes;
+  const int64_t row0 = sg.row + (lo - sg.pos);
+  // columns of a head: its turned ones (a unit and its partner), then the rest
+  const int turned = INTER ? p.pairs * 2 / VEC : p.pairs / VEC;
+  const int cols = p.c.row_units - (INTER ? 0 : turned);
+  const int heads = p.q_heads + 2 * p.c.heads;
+  const int u0 = (int)threadIdx.x % cols, hstep = 256 / cols;
+
+  struct Item {
+    const char* from;
+    char* to;
+    int u, row;
+    bool on, write, turn, two;
+  };
+  // a head narrower than 256 columns: hstep heads at a time; else the block walks the columns too
+  const int wide = hstep ? 1 : (cols + 255) / 256;
+  const int step = hstep ? hstep : 1;
+  const int mine = hstep ? (int)threadIdx.x / cols : 0;
+  const int items = n * heads * wide;
+  auto item = [&](int i) {
+    Item x;
+    x.on = i < items && (hstep == 0 || mine < hstep);
+    const int hw = i / wide, part = i - hw * wide;
+    x.row = min(hw / heads, n - 1);
+    const int h = min(hw - x.row * heads, heads - 1);
+    x.u = hstep ? u0 : part * 256 + (int)threadIdx.x;
+    x.on = x.on && x.u < cols;
+    const int64_t r = row0 + x.row;
+    const int hk = h - p.q_heads, hv = hk - p.c.heads;
+    if (hk < 0) {
+      x.from = p.q + r * p.q_st + (int64_t)h * p.q_sh * 16;
+      x.to = p.q_out + r * p.out_st + (int64_t)h * p.out_sh * 16;
+    } else {
+      const int kh = hv < 0 ? hk : hv;
+      x.from = (hv < 0 ? p.k_new : p.v_new) + layer * p.new_sl + r * p.new_st + (int64_t)kh * p.new_sh * 16;
+      x.to = (hv < 0 ? p.c.k : p.c.v) + at + (int64_t)x.row * p.c.st_bytes + (int64_t)kh * p.c.sh_bytes;
+    }
+    x.write = x.on && (hk < 0 || kept);
+    x.two = !INTER && x.u < turned;
+    x.turn = x.u < turned && hv < 0;
+    // behind the turned columns and their partners
+    x.u += !INTER && x.u >= turned ? turned : 0;
+    x.from += (int64_t)x.u * 16;
+    x.to += (int64_t)x.u * 16;
+    return x;
+  };
+  auto load = [&](const Item& x, u32x4& a, u32x4& b) {
+    if (x.on) {
+      a = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(x.from));
+      if (x.two) b = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(x.from) + turned);
+    }
+  };
+  auto finish = [&](const Item& x, u32x4 a, u32x4 b) {
+    if (!x.write) return;
+    if (x.turn) {
+      const float* c = &cs[x.row][0][0];
+      const float* s = &cs[x.row][1][0];
+      Turned<F32> y(a);
+      if constexpr (INTER) {
+        const int i0 = x.u * (VEC / 2);
+#pragma unroll
+        for (int i = 0; i < VEC; i += 2) {
+          const float u = y.x[i], v = y.x[i + 1], co = c[i0 + i / 2], si = s[i0 + i / 2];
+          y.x[i] = fmaf(u, co, -(v * si));
+          y.x[i + 1] = fmaf(v, co, u * si);
+        }
+      } else {
+        const int i0 = x.u * VEC;
+        Turned<F32> z(b);
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) {
+          const float u = y.x[i], v = z.x[i], co = c[i0 + i], si = s[i0 + i];
+          y.x[i] = fmaf(u, co, -(v * si));
+          z.x[i] = fmaf(v, co, u * si);
+        }
+        b = z.pack();
+      }
+      a = y.pack();
+    }
+    store<STREAM>(x.to, a);
+    if (x.two) store<STREAM>(x.to + (int64_t)turned * 16, b);
+  };
+
+  u32x4 a[AHEAD], b[AHEAD];
+#pragma unroll
+  for (int k = 0; k < AHEAD; ++k) load(item(mine + k * step), a[k], b[k]);
+  for (int i = threadIdx.x; i < n * p.pairs; i += 256) {
+    const int row = i / p.pairs, x = i - row * p.pairs;
+    const int pos = p.positions ? p.positions[row0 + row] : lo + row;
+    const float2 y = cos_sin(pos, p.freq[x]);
+    cs[row][0][x] = y.x;
+    cs[row][1][x] = y.y;
+  }
+  __syncthreads();
+  for (int i = mine; i < items; i += AHEAD * step) {
+#pragma unroll
+    for (int k = 0; k < AHEAD; ++k) finish(item(i + k * step), a[k], b[k]);
+    if (i + AHEAD * step < items) {
+#pragma unroll
+      for (int k = 0; k < AHEAD; ++k) load(item(i + (AHEAD + k) * step), a[k], b[k]);
+    }
   }
 }
 
@@ -163,6 +333,13 @@ static AppendParams<M> small(const AppendParams<N>& p) {
   return q;
 }
 template <int M, int N>
+static RotateParams<M> small(const RotateParams<N>& p) {
+  RotateParams<M> q{p.c,      p.k_new,  p.v_new, p.q,    p.q_out, p.bt,        p.freq,    p.positions, p.new_sl, p.new_st,
+                    p.q_st,   p.out_st, p.new_sh, p.q_sh, p.out_sh, p.bt_stride, p.q_heads, p.pairs,     {}};
+  for (int i = 0; i < M; ++i) q.seg[i] = p.seg[i];
+  return q;
+}
+template <int M, int N>
 static CommitParams<M> small(const CommitParams<N>& p) {
   CommitParams<M> q{p.c, p.bt, p.accepted, p.bt_stride, p.shared, {}, {}, {}};
   for (int i = 0; i < M; ++i) {
@@ -189,6 +366,22 @@ static hipError_t append(const AppendParams<N>& p, dim3 g, bool stream, hipStrea
 hipError_t launch_append(const AppendParams<kMoveSegments>& p, int n, int parts, const MoveLaunch& l, hipStream_t s) {
   const dim3 g(parts, n, 2 * l.layers);
   return n == 1 ? append(small<1>(p), g, l.stream, s) : append(p, g, l.stream, s);
+}
+
+template <bool F32, bool INTER, int N>
+static hipError_t rotate(const RotateParams<N>& p, dim3 g, bool stream, hipStream_t s) {
+  if (stream) cache_append_rotated<F32, INTER, true, N><<<g, dim3(256), 0, s>>>(p);
+  else cache_append_rotated<F32, INTER, false, N><<<g, dim3(256), 0, s>>>(p);
+  return hipGetLastError();
+}
+hipError_t launch_rotate(const RotateParams<kMoveSegments>& p, int n, int parts, const MoveLaunch& l, bool f32,
+                         bool interleaved, hipStream_t s) {
+  const dim3 g(parts, n, l.layers);
+  auto go = [&](const auto& x) {
+    if (f32) return interleaved ? rotate<true, true>(x, g, l.stream, s) : rotate<true, false>(x, g, l.stream, s);
+    return interleaved ? rotate<false, true>(x, g, l.stream, s) : rotate<false, false>(x, g, l.stream, s);
+  };
+  return n == 1 ? go(small<1>(p)) : go(p);
 }
 
 template <int N>

@@ -111,6 +111,8 @@ struct AppendSegment {
   int32_t req, pos, row, n;
 };
 constexpr int kMoveRows = 16;          // rows of one work-group (divides a page)
+constexpr int kTurnRows = 4;           // of one that rotates them
+constexpr int kMaxTurned = 256;        // pairs of a head that it rotates
 constexpr int kMoveSegments = 240;
 
 template <int N>
@@ -122,6 +124,24 @@ struct AppendParams {
   int64_t new_sl, new_st;              // bytes
   int32_t new_sh;                      // 16-byte units
   int32_t bt_stride;
+  AppendSegment seg[N];
+};
+
+// Appended rows with the rotation: the queries' rows beside them (null: none).
+template <int N>
+struct RotateParams {
+  CachePools c;
+  const char* k_new;
+  const char* v_new;
+  const char* q;
+  char* q_out;
+  const int32_t* bt;
+  const float* freq;                   // [pairs]
+  const int32_t* positions;            // of the packed rows; null: their logical rows
+  int64_t new_sl, new_st, q_st, out_st;     // bytes
+  int32_t new_sh, q_sh, out_sh;             // 16-byte units
+  int32_t bt_stride;
+  int32_t q_heads, pairs;
   AppendSegment seg[N];
 };
 
@@ -150,14 +170,16 @@ struct PageCopyParams {
   PagePair pair[N];
 };
 
-static_assert(sizeof(AppendParams<kMoveSegments>) <= 4096 && sizeof(CommitParams<kMoveTrees>) <= 4096 &&
+static_assert(sizeof(AppendParams<kMoveSegments>) <= 4096 && sizeof(RotateParams<kMoveSegments>) <= 4096 && sizeof(CommitParams<kMoveTrees>) <= 4096 &&
                   sizeof(PageCopyParams<kMovePages>) <= 4096, "kernel arguments");
 static_assert(sizeof(AppendParams<1>) <= kSmallArgs && sizeof(CommitParams<1>) <= kSmallArgs &&
                   sizeof(PageCopyParams<kMovePagesSmall>) <= kSmallArgs, "small arguments");
 
 // The first n entries of p's table; an append's segments have at most `parts`
-// work-groups of 16 rows.
+// work-groups of kMoveRows (kTurnRows) rows.
 hipError_t launch_append(const AppendParams<kMoveSegments>& p, int n, int parts, const MoveLaunch& l, hipStream_t s);
+hipError_t launch_rotate(const RotateParams<kMoveSegments>& p, int n, int parts, const MoveLaunch& l, bool f32,
+                         bool interleaved, hipStream_t s);
 hipError_t launch_commit(const CommitParams<kMoveTrees>& p, int n, const MoveLaunch& l, hipStream_t s);
 hipError_t launch_page_copy(const PageCopyParams<kMovePages>& p, int n, const MoveLaunch& l, hipStream_t s);
 
