@@ -142,6 +142,66 @@ SPEC_API spec_status_t spec_chunk_attn(const spec_chunks_t* chunks, const spec_c
                                        void* host_staging, size_t host_staging_bytes, void* stream);
 
 /*
+ * The same attention with a sliding window and sinks: new token j of request i,
+ * at row t = ctx_len[i] + j, sees the rows s <= t with s > t - window or s <
+ * sinks.
+ *   window   rows that a token sees up to its own (>= 1; its own is always one).
+ *   sinks    first rows that all later tokens see (>= 0).
+ * Rows that no new token sees are not read but for some that share a 32-row
+ * block with one that is, and none of them reaches an output; nor are page ids
+ * of other blocks, so that the pages behind a window may have been given away.
+ * Everything else is as for spec_chunk_attn; a window and sinks that hide nothing
+ * give its results bit for bit where the same pieces are cut.
+ */
+typedef struct spec_window {
+  int32_t window;
+  int32_t sinks;
+} spec_window_t;
+
+SPEC_API spec_status_t spec_chunk_window_workspace_bytes(const spec_chunks_t* chunks, const spec_cache_t* cache,
+                                                         const spec_chunk_attn_args_t* args,
+                                                         const spec_window_t* window, size_t* device_bytes,
+                                                         size_t* host_bytes);
+
+SPEC_API spec_status_t spec_chunk_attn_window(const spec_chunks_t* chunks, const spec_cache_t* cache,
+                                              const spec_chunk_attn_args_t* args, const spec_window_t* window,
+                                              void* workspace, size_t workspace_bytes, void* host_staging,
+                                              size_t host_staging_bytes, void* stream);
+
+/*
+ * The same attention (no window) for requests that begin with the same rows:
+ * forks of one prompt, conversations behind one system prompt.  A prefix is read
+ * once for all tokens of its group, and each request's own rows for itself; the
+ * two are joined in fp32.
+ *   group_size  [num_groups] (host): the batch's requests in order, so many a
+ *               group (each >= 1, their sum num_requests).
+ *   prefix_len  [num_groups] (host): rows that the group's requests have in
+ *               common (>= 0), at most the ctx_len of each that has new tokens.
+ *               The rows 0 .. prefix_len - 1 hold the same values for all of
+ *               them; they are read through the block table's row of the group's
+ *               first request, which need not have new tokens but has to have the
+ *               prefix (its pages are as spec_pages_fork leaves them).
+ * Groups of one request with new tokens, and prefixes of less than a few 64-row
+ * tiles, are computed as without.
+ */
+typedef struct spec_prefixes {
+  int32_t num_groups;
+  int32_t pad0;
+  const int32_t* group_size;
+  const int32_t* prefix_len;
+} spec_prefixes_t;
+
+SPEC_API spec_status_t spec_chunk_shared_workspace_bytes(const spec_chunks_t* chunks, const spec_cache_t* cache,
+                                                         const spec_chunk_attn_args_t* args,
+                                                         const spec_prefixes_t* prefixes, size_t* device_bytes,
+                                                         size_t* host_bytes);
+
+SPEC_API spec_status_t spec_chunk_attn_shared(const spec_chunks_t* chunks, const spec_cache_t* cache,
+                                              const spec_chunk_attn_args_t* args, const spec_prefixes_t* prefixes,
+                                              void* workspace, size_t workspace_bytes, void* host_staging,
+                                              size_t host_staging_bytes, void* stream);
+
+/*
  * New K/V rows into the cache's pages: row r of request i's new rows goes to
  * its logical row ctx_len[i] + r, in layers layer .. layer + num_layers - 1.
  *   k_new, v_new  [num_layers][Nq, Hkv, d] in the cache's dtype, strides in

@@ -26,7 +26,8 @@ EXPORTS = ("spec_workspace_bytes", "spec_verify_attn", "spec_accept", "spec_veri
            "spec_status_str", "spec_abi_version", "spec_stream_read_probe", "spec_accept_floor_probe",
            "spec_accept_floor_probe_bytes", "spec_verify_noalloc",
            "spec_lm_head_accept", "spec_lm_head_workspace_bytes",
-           "spec_chunk_workspace_bytes", "spec_chunk_attn", "spec_cache_append", "spec_cache_append_rotated", "spec_cache_commit",
+           "spec_chunk_workspace_bytes", "spec_chunk_attn", "spec_chunk_window_workspace_bytes", "spec_chunk_attn_window",
+           "spec_chunk_shared_workspace_bytes", "spec_chunk_attn_shared", "spec_cache_append", "spec_cache_append_rotated", "spec_cache_commit",
            "spec_cache_copy_pages", "spec_pages_create", "spec_pages_destroy", "spec_pages_open",
            "spec_pages_resize", "spec_pages_fork", "spec_pages_close", "spec_pages_table", "spec_pages_compact",
            "spec_pages_free_count",
@@ -135,6 +136,17 @@ class SpecChunkAttnArgs(C.Structure):
                 ("q_stride_tok", C.c_int64),
                 ("q_stride_head", C.c_int64),
                 ("out", C.c_void_p)]
+
+
+class SpecWindow(C.Structure):
+    _fields_ = [("window", C.c_int32), ("sinks", C.c_int32)]
+
+
+class SpecPrefixes(C.Structure):
+    _fields_ = [("num_groups", C.c_int32),
+                ("pad0", C.c_int32),
+                ("group_size", C.POINTER(C.c_int32)),
+                ("prefix_len", C.POINTER(C.c_int32))]
 
 
 class SpecAppendArgs(C.Structure):
@@ -272,6 +284,12 @@ def load(path: str = LIB_PATH) -> C.CDLL:
     lib.spec_chunk_attn.argtypes = [P(SpecChunks), P(SpecCache), P(SpecChunkAttnArgs), C.c_void_p, C.c_size_t,
                                     C.c_void_p, C.c_size_t, C.c_void_p]
     lib.spec_chunk_attn.restype = C.c_int
+    for name, kind in (("window", SpecWindow), ("shared", SpecPrefixes)):
+        size, run = getattr(lib, f"spec_chunk_{name}_workspace_bytes"), getattr(lib, f"spec_chunk_attn_{name}")
+        size.argtypes = [P(SpecChunks), P(SpecCache), P(SpecChunkAttnArgs), P(kind), P(C.c_size_t), P(C.c_size_t)]
+        run.argtypes = [P(SpecChunks), P(SpecCache), P(SpecChunkAttnArgs), P(kind), C.c_void_p, C.c_size_t,
+                        C.c_void_p, C.c_size_t, C.c_void_p]
+        size.restype = run.restype = C.c_int
     lib.spec_cache_append.argtypes = [P(SpecChunks), P(SpecCache), P(SpecAppendArgs), C.c_void_p]
     lib.spec_cache_append.restype = C.c_int
     lib.spec_cache_append_rotated.argtypes = [P(SpecChunks), P(SpecCache), P(SpecAppendArgs), P(SpecRotation), C.c_void_p]
@@ -402,6 +420,35 @@ def spec_chunk_attn(chunks, cache, args, ws: int, ws_bytes: int, staging: int, s
     return load().spec_chunk_attn(_ref(chunks), _ref(cache), _ref(args), ws, ws_bytes, staging, staging_bytes, stream)
 
 
+def spec_chunk_window_workspace_bytes(chunks: SpecChunks, cache: SpecCache, args: SpecChunkAttnArgs, window: SpecWindow):
+    """Returns (status, device_bytes, host_bytes)."""
+    dev, host = C.c_size_t(0), C.c_size_t(0)
+    st = load().spec_chunk_window_workspace_bytes(_ref(chunks), _ref(cache), _ref(args), _ref(window), C.byref(dev),
+                                                  C.byref(host))
+    return st, dev.value, host.value
+
+
+def spec_chunk_attn_window(chunks, cache, args, window, ws: int, ws_bytes: int, staging: int, staging_bytes: int,
+                           stream: int) -> int:
+    return load().spec_chunk_attn_window(_ref(chunks), _ref(cache), _ref(args), _ref(window), ws, ws_bytes, staging,
+                                         staging_bytes, stream)
+
+
+def spec_chunk_shared_workspace_bytes(chunks: SpecChunks, cache: SpecCache, args: SpecChunkAttnArgs,
+                                      prefixes: SpecPrefixes):
+    """Returns (status, device_bytes, host_bytes)."""
+    dev, host = C.c_size_t(0), C.c_size_t(0)
+    st = load().spec_chunk_shared_workspace_bytes(_ref(chunks), _ref(cache), _ref(args), _ref(prefixes), C.byref(dev),
+                                                  C.byref(host))
+    return st, dev.value, host.value
+
+
+def spec_chunk_attn_shared(chunks, cache, args, prefixes, ws: int, ws_bytes: int, staging: int, staging_bytes: int,
+                           stream: int) -> int:
+    return load().spec_chunk_attn_shared(_ref(chunks), _ref(cache), _ref(args), _ref(prefixes), ws, ws_bytes, staging,
+                                         staging_bytes, stream)
+
+
 def spec_cache_append(chunks, cache, args, stream: int) -> int:
     return load().spec_cache_append(_ref(chunks), _ref(cache), _ref(args), stream)
 
@@ -450,6 +497,20 @@ def make_chunks(ctx_len, new_len) -> SpecChunks:
     r._keep = [ctx, new]
     r.rows = int(new.sum())
     return r
+
+
+def make_prefixes(group_size, prefix_len) -> SpecPrefixes:
+    """SpecPrefixes over int32 copies of the groups' sizes and common rows, kept
+    alive on the struct."""
+    size, rows = int32_copy(group_size), int32_copy(prefix_len)
+    if size.shape != rows.shape or size.ndim != 1:
+        raise ValueError("group_size and prefix_len are one number a group")
+    p = SpecPrefixes()
+    p.num_groups = int(size.shape[0])
+    p.group_size = size.ctypes.data_as(C.POINTER(C.c_int32))
+    p.prefix_len = rows.ctypes.data_as(C.POINTER(C.c_int32))
+    p._keep = [size, rows]
+    return p
 
 
 def make_requests(ctx_len, draft_len=None, tree_parent=None, tree_parents=None):

@@ -297,16 +297,26 @@ class PagedCache:
 
 
 class ChunkAttention(StagingRing):
-    """Runs spec_chunk_attn on a PagedCache.  Owns a device workspace, which
+    """Runs spec_chunk_attn on a PagedCache; with `window`, spec_chunk_attn_window
+    (a token sees the last `window` rows up to its own and the first `sinks`); a
+    call with prefixes, spec_chunk_attn_shared.  Owns a device workspace, which
     grows with the batches, and `ring` pinned staging buffers (StagingRing).  A
     graph is captured from B.spec_chunk_attn with a workspace and staging of its
     own: a replay reads the staging it was captured with, and here the ring
     reuses its slots, so a call on a capturing stream is refused.  An object is
     used by one thread at a time."""
 
-    def __init__(self, cache: PagedCache, num_q_heads: int, scale: float = 0.0, ring: int = 32, event_every: int = 8):
+    def __init__(self, cache: PagedCache, num_q_heads: int, scale: float = 0.0, ring: int = 32, event_every: int = 8,
+                 window: Optional[int] = None, sinks: int = 0):
         if event_every < 1 or ring < event_every:
             raise ValueError("need ring >= event_every >= 1")
+        if window is None and sinks:
+            raise ValueError("sinks belong to a window")
+        self._window = None
+        if window is not None:
+            self._window = B.SpecWindow(B.int32(window), B.int32(sinks))
+            if window < 1 or sinks < 0:
+                raise ValueError("a window has at least a token's own row, sinks are not negative")
         self.cache = cache
         a = self.args = B.SpecChunkAttnArgs()
         a.num_q_heads, a.scale = B.int32(num_q_heads), scale
@@ -329,8 +339,13 @@ class ChunkAttention(StagingRing):
         except Exception:                     # the interpreter or the device is going away
             pass
 
-    def _grow(self, chunks, stream) -> None:
-        st, dev, host = B.spec_chunk_workspace_bytes(chunks, self.cache.c, self.args)
+    def _grow(self, chunks, stream, prefixes) -> None:
+        if self._window is not None:
+            st, dev, host = B.spec_chunk_window_workspace_bytes(chunks, self.cache.c, self.args, self._window)
+        elif prefixes is not None:
+            st, dev, host = B.spec_chunk_shared_workspace_bytes(chunks, self.cache.c, self.args, prefixes)
+        else:
+            st, dev, host = B.spec_chunk_workspace_bytes(chunks, self.cache.c, self.args)
         B.check(st, "spec_chunk_workspace_bytes")
         if dev > self.ws_bytes:
             if self.ws_bytes:
@@ -348,8 +363,12 @@ class ChunkAttention(StagingRing):
             self._staging = [self._pinned.data_ptr() + i * size for i in range(len(self._staging))]
 
     def run(self, chunks: B.SpecChunks, q: torch.Tensor, out: torch.Tensor, layer: int = 0,
-            stream: Optional[torch.cuda.Stream] = None) -> None:
-        """Attention of q [rows, Hq, d] into out [rows, Hq, d] (bf16 or fp32)."""
+            stream: Optional[torch.cuda.Stream] = None, prefixes: Optional[B.SpecPrefixes] = None) -> None:
+        """Attention of q [rows, Hq, d] into out [rows, Hq, d] (bf16 or fp32).
+        prefixes (B.make_prefixes): neighbouring requests that begin with the same
+        rows, which are read once for all of them."""
+        if prefixes is not None and self._window is not None:
+            raise ValueError("shared prefixes have no window")
         cache, a = self.cache, self.args
         rows, head = chunks.rows, self._head
         qs, os, st = q.shape, out.shape, q.stride()
@@ -373,11 +392,16 @@ class ChunkAttention(StagingRing):
             for grown in (False, True):
                 s = self._slot(stream)
                 try:
-                    st = cache._lib.spec_chunk_attn(chunks, cache._ref, self._args_ref, self.ws_ptr, self.ws_bytes,
-                                                    self._staging[s], self.staging_bytes, h)
+                    where = self.ws_ptr, self.ws_bytes, self._staging[s], self.staging_bytes, h
+                    if self._window is not None:
+                        st = cache._lib.spec_chunk_attn_window(chunks, cache._ref, self._args_ref, self._window, *where)
+                    elif prefixes is not None:
+                        st = cache._lib.spec_chunk_attn_shared(chunks, cache._ref, self._args_ref, prefixes, *where)
+                    else:
+                        st = cache._lib.spec_chunk_attn(chunks, cache._ref, self._args_ref, *where)
                 finally:
                     self._done(s, stream)
                 if st != B.SPEC_ERR_WORKSPACE or grown:
                     break
-                self._grow(chunks, stream)
+                self._grow(chunks, stream, prefixes)
         B.check(st, "spec_chunk_attn")

@@ -18,6 +18,7 @@ namespace {
 
 using sv::ChunkItem;
 using sv::ChunkJoin;
+using sv::ChunkMeet;
 
 constexpr size_t kAlign = 256;
 inline size_t align_up(size_t x) { return (x + kAlign - 1) / kAlign * kAlign; }
@@ -103,15 +104,49 @@ int compute_units() {
 struct ChunkPlan {
   std::vector<ChunkItem> items;
   std::vector<ChunkJoin> joins;
-  bool tall = false;
-  int32_t join_rows = 0, join_pieces = 0, turn0 = 0, turn1 = 0;
+  std::vector<ChunkMeet> meets;
+  bool tall = false, some = false;
+  int32_t join_rows = 0, join_pieces = 0, meet_rows = 0, turn0 = 0, turn1 = 0;
+  int32_t window = sv::kNoWindow, sinks = 0;
   int64_t parts = 0;
-  size_t off_joins = 0, plan_bytes = 0;
+  size_t off_joins = 0, off_meets = 0, plan_bytes = 0;
   size_t off_part = 0, device_bytes = 0;
 };
 
+// A row tile of the plan: `rows` query rows from r0 on, keys counted without the
+// `skip` ones that it leaves out.
+struct RowTile {
+  int32_t req, r0, rows, keys, q0, ctx, skip;
+  int32_t run;              // tiles of one run follow each other and read the same keys
+  int32_t len = 0, pieces = 0;
+  int64_t part = -1;
+  bool meets = false;       // joined with another tile's keys, whether cut or not
+};
+
+// A group of requests behind a shared prefix: its tiles of the prefix, and each
+// request's own.
+struct Shared {
+  int32_t first, count, prefix;            // prefix: the shared keys that are read once
+  size_t tile0;                            // its first tile of the prefix
+};
+
+// Shorter prefixes are left with the requests.
+constexpr int32_t kLeastPrefix = 128;
+
+spec_status_t check_prefixes(const spec_chunks_t* r, const spec_prefixes_t* g) {
+  if (g->num_groups < 1 || !g->group_size || !g->prefix_len) return SPEC_ERR_INVALID_ARG;
+  int64_t at = 0;
+  for (int x = 0; x < g->num_groups; ++x) {
+    if (g->group_size[x] < 1 || g->prefix_len[x] < 0 || at + g->group_size[x] > r->num_requests)
+      return SPEC_ERR_INVALID_ARG;
+    for (int i = 0; i < g->group_size[x]; ++i, ++at)
+      if (r->new_len[at] > 0 && r->ctx_len[at] < g->prefix_len[x]) return SPEC_ERR_INVALID_ARG;
+  }
+  return at == r->num_requests ? SPEC_OK : SPEC_ERR_INVALID_ARG;
+}
+
 spec_status_t plan_chunk(const spec_chunks_t* r, const spec_cache_t* c, const spec_chunk_attn_args_t* a,
-                         ChunkPlan& P) {
+                         const spec_window_t* win, const spec_prefixes_t* groups, ChunkPlan& P) {
   spec_status_t st = check_cache(c, true);
   if (st != SPEC_OK) return st;
   if (!a || a->num_q_heads < 1 || a->num_q_heads % c->num_kv_heads) return SPEC_ERR_INVALID_ARG;
@@ -129,21 +164,75 @@ spec_status_t plan_chunk(const spec_chunks_t* r, const spec_cache_t* c, const sp
 
   // Row tiles of one height for the batch: 32 rows on one wave each where no
   // request has more (decoding), else 128 on a work-group of four.
+  if (win && (win->window < 1 || win->sinks < 0)) return SPEC_ERR_INVALID_ARG;
+  if (groups && (st = check_prefixes(r, groups)) != SPEC_OK) return st;
+  // Groups whose prefix is read once, its rows those of all its requests.  Whole
+  // 64-key tiles of it; what is left goes with each request's own keys.
+  std::vector<Shared> shared;
+  std::vector<int32_t> prefix_of(groups ? r->num_requests : 0, 0);
+  if (groups) {
+    int32_t at = 0;
+    for (int x = 0; x < groups->num_groups; at += groups->group_size[x++]) {
+      const int32_t prefix = groups->prefix_len[x] / sv::kChunkTile * sv::kChunkTile;
+      int with_rows = 0;
+      for (int i = at; i < at + groups->group_size[x]; ++i) with_rows += r->new_len[i] > 0;
+      if (with_rows < 2 || prefix < kLeastPrefix) continue;
+      shared.push_back({at, groups->group_size[x], prefix, 0});
+      for (int i = at; i < at + groups->group_size[x]; ++i) prefix_of[i] = prefix;
+    }
+  }
+  P.some = win || !shared.empty();
+  if (win) {
+    P.window = std::min(win->window, sv::kNoWindow);
+    P.sinks = std::min(win->sinks, sv::kNoWindow);
+  }
   int64_t most = 0;
   for (int i = 0; i < r->num_requests; ++i) most = std::max<int64_t>(most, (int64_t)r->new_len[i] * G);
+  for (const Shared& x : shared) {
+    int64_t rows = 0;
+    for (int i = x.first; i < x.first + x.count; ++i) rows += (int64_t)r->new_len[i] * G;
+    most = std::max(most, rows);
+  }
   P.tall = most > sv::kChunkLowRows;
   const int RT = P.tall ? sv::kChunkTallRows : sv::kChunkLowRows;
-  struct RowTile { int32_t req, r0, rows, keys, q0, len, pieces; };
   std::vector<RowTile> tiles;
   int64_t q0 = 0, total = 0, longest = 0;
+  auto place = [&](const RowTile& t) {
+    tiles.push_back(t);
+    const int64_t kt = (t.keys + sv::kChunkTile - 1) / sv::kChunkTile;
+    total += kt * Hkv;
+    longest = std::max(longest, kt);
+  };
+  size_t next = 0;
+  std::vector<size_t> own0;                // each request's first tile of its own, where a prefix is shared
+  if (!shared.empty()) own0.resize(r->num_requests);
   for (int i = 0; i < r->num_requests; ++i) {
+    if (next < shared.size() && shared[next].first == i) {
+      Shared& x = shared[next];
+      int32_t rows = 0;
+      for (int y = i; y < i + x.count; ++y) rows += r->new_len[y] * G;
+      x.tile0 = tiles.size();
+      for (int r0 = 0; r0 < rows; r0 += RT) {
+        RowTile t{i, r0, std::min(RT, rows - r0), x.prefix, (int32_t)q0, x.prefix, 0, r->num_requests + (int32_t)next};
+        t.meets = true;
+        place(t);
+      }
+      ++next;
+    }
     const int n = r->new_len[i], rows = n * G;
+    const int32_t prefix = shared.empty() ? 0 : prefix_of[i];
+    if (!own0.empty()) own0[i] = tiles.size();
     for (int r0 = 0; r0 < rows; r0 += RT) {
       const int nr = std::min(RT, rows - r0);
-      tiles.push_back({i, r0, nr, r->ctx_len[i] + (r0 + nr - 1) / G + 1, (int32_t)q0, 0, 0});
-      const int64_t kt = (tiles.back().keys + sv::kChunkTile - 1) / sv::kChunkTile;
-      total += kt * Hkv;
-      longest = std::max(longest, kt);
+      int32_t skip = prefix;
+      if (win) {
+        // the first key that the tile's first row sees behind the sinks, down to a 32-row border
+        const int32_t sinks = (P.sinks + 31) / 32 * 32;
+        skip = std::max((std::max(r->ctx_len[i] + r0 / G - P.window + 1, 0) & ~31) - sinks, 0);
+      }
+      RowTile t{i, r0, nr, r->ctx_len[i] + (r0 + nr - 1) / G + 1 - skip, (int32_t)q0, r->ctx_len[i] - skip, skip, i};
+      t.meets = prefix > 0;
+      place(t);
     }
     q0 += n;
   }
@@ -203,7 +292,7 @@ spec_status_t plan_chunk(const spec_chunks_t* r, const spec_cache_t* c, const sp
     if (placed[x]) continue;
     const RowTile& t = tiles[x];
     auto with = [&](int64_t y) {
-      return y >= 0 && y < (int64_t)tiles.size() && !placed[y] && tiles[y].req == t.req &&
+      return y >= 0 && y < (int64_t)tiles.size() && !placed[y] && tiles[y].run == t.run &&
              8 * (int64_t)tiles[y].len >= 7 * (int64_t)t.len;
     };
     placed[x] = true;
@@ -216,15 +305,36 @@ spec_status_t plan_chunk(const spec_chunks_t* r, const spec_cache_t* c, const sp
   }
   P.items.reserve((size_t)n_items);
   for (const int32_t x : order) {
-    const RowTile& t = tiles[x];
+    RowTile& t = tiles[x];
     const int32_t len = t.len * sv::kChunkTile;
+    // a plan without keys left out tells cut tiles by their pieces
+    t.part = !P.some || t.pieces > 1 || t.meets ? P.parts : -1;
     for (int32_t s = 0; s < t.pieces; ++s)
-      P.items.push_back({t.req, t.r0, t.rows, t.keys, len, s, t.pieces, r->ctx_len[t.req], P.parts, t.q0, 0});
-    if (t.pieces > 1) {
+      P.items.push_back({t.req, t.r0, t.rows, t.keys, len, s, t.pieces, t.ctx, t.part, t.q0, t.skip});
+    if (t.pieces > 1 && !t.meets) {
       P.joins.push_back({t.r0, t.rows, t.pieces, t.q0, P.parts, 0});
       P.join_rows = std::max(P.join_rows, t.rows);
       P.join_pieces = std::max(P.join_pieces, t.pieces);
-      P.parts += (int64_t)Hkv * t.pieces * t.rows;
+    }
+    if (t.pieces > 1 || t.meets) P.parts += (int64_t)Hkv * t.pieces * t.rows;
+  }
+  // Where a request's tiles and its group's tiles of the prefix have rows in
+  // common, run by run.
+  for (const Shared& x : shared) {
+    int64_t before = 0;                    // the group's rows ahead of the request's
+    for (int i = x.first; i < x.first + x.count; ++i) {
+      const int32_t rows = r->new_len[i] * G;
+      for (int32_t rr = 0; rr < rows;) {
+        const RowTile& own = tiles[own0[i] + rr / RT];
+        const RowTile& pre = tiles[x.tile0 + (before + rr) / RT];
+        const int32_t in_own = rr - own.r0, in_pre = (int32_t)(before + rr) - pre.r0;
+        const int32_t n = std::min(own.rows - in_own, pre.rows - in_pre);
+        P.meets.push_back({{pre.part + in_pre, own.part + in_own}, {pre.pieces, own.pieces}, {pre.rows, own.rows}, own.q0,
+                           rr, n, 0});
+        P.meet_rows = std::max(P.meet_rows, n);
+        rr += n;
+      }
+      before += rows;
     }
   }
   // work-groups b and b + cus of the tall kernel share a compute unit at first
@@ -236,7 +346,8 @@ spec_status_t plan_chunk(const spec_chunks_t* r, const spec_cache_t* c, const sp
   }
 
   P.off_joins = align_up(sizeof(ChunkItem) * P.items.size());
-  P.plan_bytes = P.off_joins + align_up(sizeof(ChunkJoin) * P.joins.size());
+  P.off_meets = P.off_joins + align_up(sizeof(ChunkJoin) * P.joins.size());
+  P.plan_bytes = P.off_meets + align_up(sizeof(ChunkMeet) * P.meets.size());
   P.off_part = align_up(P.plan_bytes + sizeof(float2) * (size_t)P.parts);
   P.device_bytes = align_up(P.off_part + sizeof(float) * (size_t)P.parts * c->head_dim);
   return SPEC_OK;
@@ -326,17 +437,14 @@ spec_status_t check_append(const spec_chunks_t* chunks, const spec_cache_t* cach
 }
 bool heads_touch(const spec_cache_t* c) { return c->num_kv_heads == 1 || c->kv_stride_head == c->head_dim; }
 
-}  // namespace
-
-extern "C" {
-
-spec_status_t spec_chunk_workspace_bytes(const spec_chunks_t* chunks, const spec_cache_t* cache,
-                                         const spec_chunk_attn_args_t* args, size_t* device_bytes,
-                                         size_t* host_bytes) {
+// What the chunk attention's entry points have in common.
+spec_status_t chunk_bytes(const spec_chunks_t* chunks, const spec_cache_t* cache, const spec_chunk_attn_args_t* args,
+                          const spec_window_t* window, const spec_prefixes_t* prefixes, size_t* device_bytes,
+                          size_t* host_bytes) {
   return guarded([&]() -> spec_status_t {
     if (!device_bytes || !host_bytes) return SPEC_ERR_INVALID_ARG;
     ChunkPlan P;
-    const spec_status_t st = plan_chunk(chunks, cache, args, P);
+    const spec_status_t st = plan_chunk(chunks, cache, args, window, prefixes, P);
     if (st != SPEC_OK) return st;
     *device_bytes = P.device_bytes;
     *host_bytes = P.plan_bytes;
@@ -344,12 +452,12 @@ spec_status_t spec_chunk_workspace_bytes(const spec_chunks_t* chunks, const spec
   });
 }
 
-spec_status_t spec_chunk_attn(const spec_chunks_t* chunks, const spec_cache_t* cache,
-                              const spec_chunk_attn_args_t* args, void* workspace, size_t workspace_bytes,
-                              void* host_staging, size_t host_staging_bytes, void* stream) {
+spec_status_t chunk_attn(const spec_chunks_t* chunks, const spec_cache_t* cache, const spec_chunk_attn_args_t* args,
+                         const spec_window_t* window, const spec_prefixes_t* prefixes, void* workspace,
+                         size_t workspace_bytes, void* host_staging, size_t host_staging_bytes, void* stream) {
   return guarded([&]() -> spec_status_t {
     ChunkPlan P;
-    const spec_status_t st = plan_chunk(chunks, cache, args, P);
+    const spec_status_t st = plan_chunk(chunks, cache, args, window, prefixes, P);
     if (st != SPEC_OK) return st;
     if (P.items.empty()) return SPEC_OK;
     if (!workspace || reinterpret_cast<uintptr_t>(workspace) % kAlign || workspace_bytes < P.device_bytes ||
@@ -360,6 +468,7 @@ spec_status_t spec_chunk_attn(const spec_chunks_t* chunks, const spec_cache_t* c
     char* h = static_cast<char*>(host_staging);
     std::memcpy(h, P.items.data(), sizeof(ChunkItem) * P.items.size());
     if (!P.joins.empty()) std::memcpy(h + P.off_joins, P.joins.data(), sizeof(ChunkJoin) * P.joins.size());
+    if (!P.meets.empty()) std::memcpy(h + P.off_meets, P.meets.data(), sizeof(ChunkMeet) * P.meets.size());
     // the kernels read the plan where it was staged when that is device-mapped
     // memory; otherwise it is copied into the workspace first
     const char* plan = d;
@@ -392,6 +501,8 @@ spec_status_t spec_chunk_attn(const spec_chunks_t* chunks, const spec_cache_t* c
     p.turn1 = P.turn1;
     const float scale = args->scale > 0.f ? args->scale : 1.f / std::sqrt((float)cache->head_dim);
     p.scale_log2 = scale * 1.4426950408889634f;
+    p.window = P.window;
+    p.sinks = P.sinks;
     sv::JoinParams j{};
     j.out = p.out;
     j.part = p.part;
@@ -399,10 +510,59 @@ spec_status_t spec_chunk_attn(const spec_chunks_t* chunks, const spec_cache_t* c
     j.G = p.G;
     if (P.joins.size() == 1) j.one = P.joins[0];
     else j.joins = reinterpret_cast<const ChunkJoin*>(plan + P.off_joins);
+    const sv::MeetParams m = {p.out, p.part, reinterpret_cast<const ChunkMeet*>(plan + P.off_meets), p.Hkv, p.G};
     const sv::ChunkLaunch l = {(int32_t)P.items.size(), (int32_t)P.joins.size(), cache->head_dim,
-                               args->out_dtype == SPEC_F32, P.tall, P.join_rows, P.join_pieces};
-    return sv::launch_chunk(p, j, l, s) == hipSuccess ? SPEC_OK : SPEC_ERR_HIP;
+                               args->out_dtype == SPEC_F32, P.tall, P.join_rows, P.join_pieces, P.some,
+                               (int32_t)P.meets.size(), P.meet_rows};
+    return sv::launch_chunk(p, j, m, l, s) == hipSuccess ? SPEC_OK : SPEC_ERR_HIP;
   });
+}
+
+}  // namespace
+
+extern "C" {
+
+spec_status_t spec_chunk_workspace_bytes(const spec_chunks_t* chunks, const spec_cache_t* cache,
+                                         const spec_chunk_attn_args_t* args, size_t* device_bytes,
+                                         size_t* host_bytes) {
+  return chunk_bytes(chunks, cache, args, nullptr, nullptr, device_bytes, host_bytes);
+}
+
+spec_status_t spec_chunk_attn(const spec_chunks_t* chunks, const spec_cache_t* cache,
+                              const spec_chunk_attn_args_t* args, void* workspace, size_t workspace_bytes,
+                              void* host_staging, size_t host_staging_bytes, void* stream) {
+  return chunk_attn(chunks, cache, args, nullptr, nullptr, workspace, workspace_bytes, host_staging,
+                    host_staging_bytes, stream);
+}
+
+spec_status_t spec_chunk_window_workspace_bytes(const spec_chunks_t* chunks, const spec_cache_t* cache,
+                                                const spec_chunk_attn_args_t* args, const spec_window_t* window,
+                                                size_t* device_bytes, size_t* host_bytes) {
+  return window ? chunk_bytes(chunks, cache, args, window, nullptr, device_bytes, host_bytes) : SPEC_ERR_INVALID_ARG;
+}
+
+spec_status_t spec_chunk_attn_window(const spec_chunks_t* chunks, const spec_cache_t* cache,
+                                     const spec_chunk_attn_args_t* args, const spec_window_t* window, void* workspace,
+                                     size_t workspace_bytes, void* host_staging, size_t host_staging_bytes,
+                                     void* stream) {
+  if (!window) return SPEC_ERR_INVALID_ARG;
+  return chunk_attn(chunks, cache, args, window, nullptr, workspace, workspace_bytes, host_staging, host_staging_bytes,
+                    stream);
+}
+
+spec_status_t spec_chunk_shared_workspace_bytes(const spec_chunks_t* chunks, const spec_cache_t* cache,
+                                                const spec_chunk_attn_args_t* args, const spec_prefixes_t* prefixes,
+                                                size_t* device_bytes, size_t* host_bytes) {
+  return prefixes ? chunk_bytes(chunks, cache, args, nullptr, prefixes, device_bytes, host_bytes) : SPEC_ERR_INVALID_ARG;
+}
+
+spec_status_t spec_chunk_attn_shared(const spec_chunks_t* chunks, const spec_cache_t* cache,
+                                     const spec_chunk_attn_args_t* args, const spec_prefixes_t* prefixes,
+                                     void* workspace, size_t workspace_bytes, void* host_staging,
+                                     size_t host_staging_bytes, void* stream) {
+  if (!prefixes) return SPEC_ERR_INVALID_ARG;
+  return chunk_attn(chunks, cache, args, nullptr, prefixes, workspace, workspace_bytes, host_staging,
+                    host_staging_bytes, stream);
 }
 
 spec_status_t spec_cache_append(const spec_chunks_t* chunks, const spec_cache_t* cache, const spec_append_args_t* args,

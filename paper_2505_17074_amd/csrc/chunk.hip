@@ -105,7 +105,14 @@ struct Fetch {
   int64_t page_bytes;
   int32_t page_tokens, num_pages, row_bytes;
   int32_t ke;
+  int32_t first, skip;       // SOME: key t >= first is the request's row t + skip
 };
+// The request's row that is key t of the item.
+template <bool SOME>
+__device__ __forceinline__ int row_of(const Fetch& f, int t) {
+  if constexpr (SOME) return t < f.first ? t : t + f.skip;
+  return t;
+}
 
 // Lane l's 32-key block b + l of the item (from key kb on): its page, and the
 // place in it of its first key (those of the item's last block for blocks
@@ -118,19 +125,23 @@ struct Window {
   int b;
   int pg, place;
 };
+template <bool SOME>
 __device__ __forceinline__ void look(Window& x, const Fetch& f, int kb, int b, int lane) {
-  const int t = min(kb + 32 * (b + lane), (f.ke - 1) & ~31);
+  const int t = row_of<SOME>(f, min(kb + 32 * (b + lane), (f.ke - 1) & ~31));
   const int i = t / f.page_tokens;
   x.b = b;
   x.place = t - i * f.page_tokens;
   x.pg = min(max(f.pages[i], 0), f.num_pages - 1);
 }
 
-// The page of key t.
-__device__ __forceinline__ int page_of(const Fetch& f, int t) {
-  const int i = __builtin_amdgcn_readfirstlane(min(t, f.ke - 1) / f.page_tokens);
+// Byte offset of key t's row in the pools.
+template <bool SOME>
+__device__ __forceinline__ int64_t place_of(const Fetch& f, int t) {
+  const int r = row_of<SOME>(f, min(t, f.ke - 1));
+  const int i = __builtin_amdgcn_readfirstlane(r / f.page_tokens);
   const int pg = ((const const_int32*)f.pages)[i];
-  return __builtin_amdgcn_readfirstlane(min(max(pg, 0), f.num_pages - 1));
+  return __builtin_amdgcn_readfirstlane(min(max(pg, 0), f.num_pages - 1)) * f.page_bytes +
+         (int64_t)(r % f.page_tokens) * f.row_bytes;
 }
 
 // The query rows of one wave: 32 rows, lane l holding row l % 32 (both halves
@@ -141,6 +152,11 @@ struct Rows {
   f32x16 o[D / 32];          // o[eb][i]: column 32 eb + 8 (i / 4) + 4 (l / 32) + i % 4
   float m, l;                // reference (log2 units) and this half's sum
   int32_t last;              // the row's last visible key
+  int32_t low, sinks;        // SOME: it sees keys from low on, and those below sinks
+  template <bool SOME>
+  __device__ __forceinline__ bool sees(int t) const {
+    return t <= last && (!SOME || t >= low || t < sinks);
+  }
   __device__ __forceinline__ void clear() {
     m = -INFINITY;
     l = 0.f;
@@ -165,10 +181,11 @@ __device__ __forceinline__ bool has_nan(const Rows<D>& S) {
 struct Piece {
   int32_t req, kvh, r0, rows, kb, ke, ctx, q0;
   int64_t part;
+  int32_t skip;
 };
 // A row tile's work-groups are next to each other, those of a piece (HEADS: the
 // XCDs read different heads) or of a head (a head's keys stream past in order).
-template <bool HEADS>
+template <bool HEADS, bool SOME>
 __device__ __forceinline__ Piece piece_of(const ChunkParams& p, int b) {
   if (b >= p.turn0 && b < p.turn1) b = p.turn0 + p.turn1 - 1 - b;
   const int i = b / p.Hkv;
@@ -178,11 +195,11 @@ __device__ __forceinline__ Piece piece_of(const ChunkParams& p, int b) {
   const int s = HEADS ? x.piece : g - h * x.pieces;
   const int kb = s * x.len;
   return {x.req, h, x.r0, x.rows, kb, min(x.keys, kb + x.len), x.ctx, x.q0,
-          x.pieces > 1 ? x.part + ((int64_t)h * x.pieces + s) * x.rows : -1};
+          (SOME ? x.part >= 0 : x.pieces > 1) ? x.part + ((int64_t)h * x.pieces + s) * x.rows : -1, x.skip};
 }
 
 // Rows wr0 .. wr0 + 31 of the item (past its last: that one again).
-template <int D>
+template <bool SOME, int D>
 __device__ __forceinline__ void load_rows(Rows<D>& S, const ChunkParams& p, const Piece& it, int wr0, int l32,
                                           int half) {
   const int r = it.r0 + min(wr0 + l32, it.rows - 1);
@@ -193,6 +210,10 @@ __device__ __forceinline__ void load_rows(Rows<D>& S, const ChunkParams& p, cons
 #pragma unroll
   for (int ks = 0; ks < D / 16; ++ks) S.q[ks] = *reinterpret_cast<const bf16x8*>(src + ks * 32);
   S.last = min(it.ctx + j, it.ke - 1);
+  if constexpr (SOME) {
+    S.low = it.ctx + j - p.window + 1;
+    S.sinks = p.sinks;
+  }
 }
 // The last key that one of them sees.
 __device__ __forceinline__ int last_seen(const ChunkParams& p, const Piece& it, int wr0) {
@@ -256,10 +277,10 @@ __device__ __forceinline__ void join_rows(Rows<D>& S, float m1, float l1, const 
 // The wave's rows over keys [t, last] one at a time, by the rows' own
 // visibility: a value of a key that a row does not see never meets the row, not
 // even as a product with zero.
-template <int D>
+template <bool SOME, int D>
 __device__ __forceinline__ void one_by_one(const Fetch& f, Rows<D>& S, int t, int last, float c, int half) {
   for (; t <= last; ++t) {
-    const int64_t at = page_of(f, t) * f.page_bytes + (int64_t)(t % f.page_tokens) * f.row_bytes;
+    const int64_t at = place_of<SOME>(f, t);
     const bf16x8* k = reinterpret_cast<const bf16x8*>(f.k + at) + half;
     const bf16x4* v = reinterpret_cast<const bf16x4*>(f.v + at) + half;
     float s = 0.f;
@@ -270,7 +291,7 @@ __device__ __forceinline__ void one_by_one(const Fetch& f, Rows<D>& S, int t, in
       for (int i = 0; i < 8; ++i) s = fmaf((float)S.q[ks][i], (float)y[i], s);
     }
     s = (s + __shfl_xor(s, 32)) * c;
-    const bool sees = t <= S.last;
+    const bool sees = S.template sees<SOME>(t);
     const float m = sees ? fmaxf(S.m, s) : S.m, ref = m == -INFINITY ? 0.f : m;
     const float alpha = __builtin_amdgcn_exp2f(S.m - ref), w = sees ? __builtin_amdgcn_exp2f(s - ref) : 0.f;
     S.m = m;
@@ -323,7 +344,9 @@ __device__ __forceinline__ void one_by_one(const Fetch& f, Rows<D>& S, int t, in
 // row's norm in place of 0.0021-0.0024, and it takes one: who needs the better
 // product there asks for an fp32 output.
 // ---------------------------------------------------------------------------
-template <int D, int NW, int TK, int PARTS>
+// SOME: items that leave keys out (sv_chunk.h).  What a row does not see at the
+// window's start is masked as behind its own token; whole tiles lie between.
+template <int D, int NW, int TK, int PARTS, bool SOME>
 struct Chunk {
   using TL = Tile<D, TK>;
   using DL = Deal<D, TK, NW>;
@@ -419,10 +442,14 @@ struct Chunk {
   template <int N>
   static __device__ __forceinline__ void mask(ScoresOf<N>& x, const Rows<D>& S, int t0, int half) {
     const int lim = S.last - t0 - 8 * half;
+    const int low = SOME ? S.low - t0 - 8 * half : 0, sinks = SOME ? S.sinks - t0 - 8 * half : 0;
 #pragma unroll
     for (int kb = 0; kb < N; ++kb)
 #pragma unroll
-      for (int i = 0; i < 16; ++i) x.s[kb][i] = 32 * kb + 16 * (i >> 3) + (i & 7) <= lim ? x.s[kb][i] : -INFINITY;
+      for (int i = 0; i < 16; ++i) {
+        const int k = 32 * kb + 16 * (i >> 3) + (i & 7);
+        x.s[kb][i] = k <= lim && (!SOME || k >= low || k < sinks) ? x.s[kb][i] : -INFINITY;
+      }
   }
 
   template <int N>
@@ -573,11 +600,18 @@ struct Chunk {
   static __device__ __forceinline__ void again(const Fetch& f, Rows<D>& S, int kb, int last, float c, int l32, int half) {
 #if defined(__HIP_DEVICE_COMPILE__)
     const int all = __builtin_amdgcn_readfirstlane(S.last);
+    const int low = SOME ? __builtin_amdgcn_readlane(S.low, 31) : 0;       // from here on all of them see a key
     asm volatile("" : "+v"(l32), "+v"(half));          // none of the addresses below is held in the loops above
     S.clear();
     int t = kb;
-    for (; t + 31 <= all; t += 32) {
-      const int64_t at = page_of(f, t) * f.page_bytes + (int64_t)(t % f.page_tokens) * f.row_bytes;
+    for (; SOME ? t <= last : t + 31 <= all; t += 32) {
+      if constexpr (SOME) {
+        if (t + 31 > all || (t < low && t + 31 >= S.sinks)) {
+          one_by_one<SOME, D>(f, S, t, min(t + 31, last), c, half);
+          continue;
+        }
+      }
+      const int64_t at = place_of<SOME>(f, t);
       const char* k = f.k + at + (int64_t)key_of(l32) * f.row_bytes + half * 16;
       const char* v = f.v + at + (int64_t)(8 * half) * f.row_bytes + l32 * 2;
       ScoresOf<1> x;
@@ -605,7 +639,7 @@ struct Chunk {
         }
       }
     }
-    one_by_one<D>(f, S, t, last, c, half);
+    if constexpr (!SOME) one_by_one<SOME, D>(f, S, t, last, c, half);
 #endif
   }
   // Step t of a wave that has 32 keys of every second tile, `cur` moved to them
@@ -639,7 +673,7 @@ struct Chunk {
     const int l32 = lane & 31, half = lane >> 5;
     lds_char* ring = (lds_char*)lds;
     int2 before = make_int2(0, 0);
-    load_rows(S, p, it, 0, l32, half);
+    load_rows<SOME>(S, p, it, 0, l32, half);
 #pragma unroll
     for (int j = 0; j < NS; ++j) issue<2>(ring + j * TL::STAGE, f, j, it.kb, win, before, w, A);
     S.clear();
@@ -651,7 +685,7 @@ struct Chunk {
     for (int t = 0; t < ntiles; ++t) {
       wait_vm<0>();
       tile_barrier();
-      if (block_of(t + NS, w) >= win.b + 64) look(win, f, it.kb, block_of(t + NS, w), lane);
+      if (block_of(t + NS, w) >= win.b + 64) look<SOME>(win, f, it.kb, block_of(t + NS, w), lane);
       shared_step(ring + (t % NS) * TL::STAGE, ring + ((t + 1) % NS) * TL::STAGE + hb * TL::HALF, t + NS <= ntiles, f,
                   t + NS, it.kb, win, before, w, A, S, x, (t & 1) == par, it.kb + TK * t + 32 * hb, p.scale_log2, lane);
     }
@@ -689,10 +723,10 @@ struct Chunk {
 };
 
 // (d = 64: three waves a SIMD.)
-template <int D, int NW, int TK, int NS, int PARTS, bool F32>
+template <int D, int NW, int TK, int NS, int PARTS, bool F32, bool SOME>
 __global__ __launch_bounds__(64 * NW, D == 64 ? 3 : 2) void chunk_attn(ChunkParams p) {
 #if defined(__HIP_DEVICE_COMPILE__)   // the host pass needs the signature only
-  using C = Chunk<D, NW, TK, PARTS>;
+  using C = Chunk<D, NW, TK, PARTS, SOME>;
   using TL = Tile<D, TK>;
   using DL = Deal<D, TK, NW>;
   __shared__ __attribute__((aligned(1024))) char lds[NS * TL::STAGE];
@@ -700,7 +734,7 @@ __global__ __launch_bounds__(64 * NW, D == 64 ? 3 : 2) void chunk_attn(ChunkPara
   const int lane = threadIdx.x & 63;
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int l32 = lane & 31, half = lane >> 5;
-  const Piece it = piece_of<NW != 1>(p, blockIdx.x);
+  const Piece it = piece_of<NW != 1, SOME>(p, blockIdx.x);
   const int ntiles = (it.ke - it.kb + TK - 1) / TK;
 
   Fetch f;
@@ -712,6 +746,10 @@ __global__ __launch_bounds__(64 * NW, D == 64 ? 3 : 2) void chunk_attn(ChunkPara
   f.page_bytes = (int64_t)p.page_tokens * f.row_bytes;
   f.num_pages = p.num_pages;
   f.ke = it.ke;
+  if constexpr (SOME) {
+    f.first = (p.sinks + 31) & ~31;
+    f.skip = it.skip;
+  }
   typename C::Lane A;
 #pragma unroll
   for (int x = 0; x < TL::NOFF; ++x) {
@@ -721,7 +759,7 @@ __global__ __launch_bounds__(64 * NW, D == 64 ? 3 : 2) void chunk_attn(ChunkPara
     A.offv = (uint32_t)(lane / TL::CH * f.row_bytes + ((ch ^ swv<D>(row)) * 16));   // the same for every x
   }
   Window win;
-  look(win, f, it.kb, 0, lane);
+  look<SOME>(win, f, it.kb, 0, lane);
   int2 before = make_int2(0, 0);                         // a second unit's: what the first had last
 
   lds_char* ring = (lds_char*)lds;
@@ -735,7 +773,7 @@ __global__ __launch_bounds__(64 * NW, D == 64 ? 3 : 2) void chunk_attn(ChunkPara
   Rows<D> S;
   bool bad;
   if (!shared) {
-    load_rows(S, p, it, wr0, l32, half);
+    load_rows<SOME>(S, p, it, wr0, l32, half);
 #pragma unroll
     for (int j = 0; j < NS; ++j) C::issue(ring + j * TL::STAGE, f, j, it.kb, win, before, w, A);
     S.clear();
@@ -751,9 +789,28 @@ __global__ __launch_bounds__(64 * NW, D == 64 ? 3 : 2) void chunk_attn(ChunkPara
     // Step t: stage t + 1 has landed here and everywhere, and every wave has read
     // what it needs of stage t, where stage t + NS goes.
     int t = 0;
+    if constexpr (SOME) {
+      // the tiles that begin before the last row's window, and one more where the
+      // ring's stages ask for it
+      const int low = it.ctx + (it.r0 + it.rows - 1) / p.G - p.window + 1;
+      int edge = it.ke <= p.sinks || low <= it.kb ? 0 : min((low - it.kb + TK - 1) / TK, ntiles);
+      edge = min((edge + NS - 1) / NS * NS, ntiles);
+      // the first key in the window of the wave's first row: its tiles before have sinks or nothing
+      const int wave_low = wr0 < it.rows ? it.ctx + (it.r0 + wr0) / p.G - p.window + 1 : INT32_MAX;
+      for (; t < edge; ++t) {
+        wait_vm<0>();
+        tile_barrier();
+        if (C::block_of(t + NS, w) >= win.b + 64) look<SOME>(win, f, it.kb, C::block_of(t + NS, w), lane);
+        const int t0 = it.kb + TK * t, t1 = t0 + TK;
+        C::edge_step(ring + (t % NS) * TL::STAGE, ring + ((t + 1) % NS) * TL::STAGE, t + NS <= ntiles, f, t + NS, it.kb,
+                     win, before, w, A, S, x, top, t0, t0 <= wave_sees && (t1 > wave_low || t0 < p.sinks),
+                     t + 1 < ntiles && t1 <= wave_sees && (t1 + TK > wave_low || t1 < p.sinks), p.scale_log2, lane);
+      }
+      if (t > 0) top = C::largest(x);
+    }
     if (wave_sees >= it.kb) {
       while (t + NS <= nfull) {
-        if (C::block_of(t + 2 * NS - 1, w) >= win.b + 64) look(win, f, it.kb, C::block_of(t + NS, w), lane);
+        if (C::block_of(t + 2 * NS - 1, w) >= win.b + 64) look<SOME>(win, f, it.kb, C::block_of(t + NS, w), lane);
         static_for<0, NS>([&](auto st) {
           constexpr int ST = decltype(st)::value;
           wait_vm<(NS - 2) * DL::PER>();
@@ -767,7 +824,7 @@ __global__ __launch_bounds__(64 * NW, D == 64 ? 3 : 2) void chunk_attn(ChunkPara
     for (; t < ntiles; ++t) {
       wait_vm<0>();
       tile_barrier();
-      if (C::block_of(t + NS, w) >= win.b + 64) look(win, f, it.kb, C::block_of(t + NS, w), lane);
+      if (C::block_of(t + NS, w) >= win.b + 64) look<SOME>(win, f, it.kb, C::block_of(t + NS, w), lane);
       const int t0 = it.kb + TK * t;
       C::edge_step(ring + (t % NS) * TL::STAGE, ring + ((t + 1) % NS) * TL::STAGE, t + NS <= ntiles, f, t + NS, it.kb,
                    win, before, w, A, S, x, top, t0, t0 <= wave_sees, t + 1 < ntiles && t0 + TK <= wave_sees,
@@ -839,13 +896,48 @@ __global__ __launch_bounds__(256) void chunk_join(JoinParams p) {
       __builtin_bit_cast(u32x2, __builtin_convertvector(y, bf16x4));
 }
 
+// Rows behind a shared prefix: the pieces of both their tiles, NG rows a
+// work-group, D / 4 lanes a row.
 template <int D, bool F32>
-static hipError_t launch_d(const ChunkParams& p, const JoinParams& j, const ChunkLaunch& l, hipStream_t s) {
-  if (l.tall) chunk_attn<D, 4, 64, 2, F32 ? 3 : 1, F32><<<dim3(l.n_items * p.Hkv), dim3(256), 0, s>>>(p);
-  else chunk_attn<D, 1, 32, 2, F32 ? 3 : 2, F32><<<dim3(l.n_items * p.Hkv), dim3(64), 0, s>>>(p);
-  hipError_t e = hipGetLastError();
-  if (e != hipSuccess || l.n_joins == 0) return e;
+__global__ __launch_bounds__(256) void chunk_meet(MeetParams p) {
+  constexpr int LPR = D / 4, NG = 256 / LPR;
+  const int run = (int)blockIdx.x / p.Hkv, kvh = (int)blockIdx.x - run * p.Hkv;
+  const ChunkMeet mt = p.meets[run];
+  const int rr = (int)blockIdx.y * NG + (int)threadIdx.x / LPR, x = threadIdx.x % LPR;
+  if (rr >= mt.rows) return;
+  Joined j = {f32x4{0.f, 0.f, 0.f, 0.f}, -INFINITY, 0.f};
+#pragma unroll
+  for (int side = 0; side < 2; ++side) {
+    const int64_t first = mt.part[side] + (int64_t)kvh * mt.pieces[side] * mt.stride[side] + rr;
+    const float2* ml = reinterpret_cast<const float2*>(p.part) - 1 - first;
+    const float* po = p.part + first * D + 4 * x;
+#pragma unroll 4
+    for (int s = 0; s < mt.pieces[side]; ++s) {
+      const int64_t at = (int64_t)s * mt.stride[side];
+      const float2 y = ml[-at];
+      j.add(y.x, y.y, *reinterpret_cast<const f32x4*>(po + at * D));
+    }
+  }
+  const int r = mt.r0 + rr, tok = r / p.G;
+  const int64_t at = ((mt.q0 + (int64_t)tok) * (p.Hkv * p.G) + kvh * p.G + (r - tok * p.G)) * D + 4 * x;
+  const f32x4 y = j.o * (1.f / j.l);
+  if constexpr (F32) *reinterpret_cast<f32x4*>(static_cast<float*>(p.out) + at) = y;
+  else *reinterpret_cast<u32x2*>(static_cast<uint16_t*>(p.out) + at) =
+      __builtin_bit_cast(u32x2, __builtin_convertvector(y, bf16x4));
+}
+
+template <int D, bool F32, bool SOME>
+static hipError_t launch_d(const ChunkParams& p, const JoinParams& j, const MeetParams& m, const ChunkLaunch& l,
+                           hipStream_t s) {
+  if (l.tall) chunk_attn<D, 4, 64, 2, F32 ? 3 : 1, F32, SOME><<<dim3(l.n_items * p.Hkv), dim3(256), 0, s>>>(p);
+  else chunk_attn<D, 1, 32, 2, F32 ? 3 : 2, F32, SOME><<<dim3(l.n_items * p.Hkv), dim3(64), 0, s>>>(p);
   constexpr int NG = 1024 / D;
+  hipError_t e = hipGetLastError();
+  if (e == hipSuccess && SOME && l.n_meets > 0) {
+    chunk_meet<D, F32><<<dim3(l.n_meets * p.Hkv, (l.meet_rows + NG - 1) / NG), dim3(256), 0, s>>>(m);
+    e = hipGetLastError();
+  }
+  if (e != hipSuccess || l.n_joins == 0) return e;
   if (l.join_pieces <= 2 * NG)
     chunk_join<D, F32, true><<<dim3(l.n_joins * p.Hkv, (l.join_rows + NG - 1) / NG), dim3(256), 0, s>>>(j);
   else
@@ -853,9 +945,15 @@ static hipError_t launch_d(const ChunkParams& p, const JoinParams& j, const Chun
   return hipGetLastError();
 }
 
-hipError_t launch_chunk(const ChunkParams& p, const JoinParams& j, const ChunkLaunch& l, hipStream_t s) {
-  if (l.D == 128) return l.out_f32 ? launch_d<128, true>(p, j, l, s) : launch_d<128, false>(p, j, l, s);
-  return l.out_f32 ? launch_d<64, true>(p, j, l, s) : launch_d<64, false>(p, j, l, s);
+hipError_t launch_chunk(const ChunkParams& p, const JoinParams& j, const MeetParams& m, const ChunkLaunch& l,
+                        hipStream_t s) {
+  auto some = [&](auto d, auto f32) {
+    constexpr int D = decltype(d)::value;
+    constexpr bool F32 = decltype(f32)::value;
+    return l.some ? launch_d<D, F32, true>(p, j, m, l, s) : launch_d<D, F32, false>(p, j, m, l, s);
+  };
+  auto out = [&](auto d) { return l.out_f32 ? some(d, std::true_type{}) : some(d, std::false_type{}); };
+  return l.D == 128 ? out(std::integral_constant<int, 128>{}) : out(std::integral_constant<int, 64>{});
 }
 
 }  // namespace sv

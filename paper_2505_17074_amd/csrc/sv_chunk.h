@@ -21,9 +21,18 @@ struct ChunkItem {
   int32_t ctx;
   int64_t part;     // the tile's first partial row (pieces > 1): head h's piece s from (h pieces + s) rows on
   int32_t q0;       // the request's first row of q and out
-  int32_t pad;
+  int32_t skip;     // SOME: keys left out behind the first ones (below), a multiple of 32
 };
 static_assert(sizeof(ChunkItem) == 48, "ChunkItem is read as 16-byte units");
+
+// Items that leave out a run of keys (SOME: windows behind their sinks, requests
+// behind a shared prefix).  Their keys are counted without it: key t of an item is
+// the request's row t where t < first, else t + skip, `first` the sinks rounded up
+// to 32 (ChunkParams::sinks), and `keys` and `ctx` are in these counts (ctx may be
+// negative).  New token j sees the keys t <= ctx + j with t > ctx + j - window
+// or t < sinks.  The run begins and ends on a 32-row border of the request, so
+// that a 32-key block is of one page.  `part` is negative where the item writes
+// out itself.
 
 // One query-row tile whose key range was cut: a head's pieces' partial rows
 // follow each other, `rows` apart, the heads `pieces * rows` apart.
@@ -57,6 +66,25 @@ struct ChunkParams {
   int32_t Hkv, G;
   int32_t turn0, turn1; // work-groups [turn0, turn1) take their places from the end
   float scale_log2;
+  int32_t window, sinks;               // SOME
+};
+
+// Rows whose keys two tiles had, the prefix's and the request's own (a join of
+// requests behind a shared prefix).  Row rr of the run is partial row part + (h
+// pieces + s) stride + rr of each, h the KV head, s the piece.
+struct ChunkMeet {
+  int64_t part[2];
+  int32_t pieces[2], stride[2];
+  int32_t q0, r0, rows;                // the run's rows of the request that begins at row q0
+  int32_t pad;
+};
+static_assert(sizeof(ChunkMeet) == 48, "ChunkMeet is read as 16-byte units");
+
+struct MeetParams {
+  void* out;
+  const float* part;
+  const ChunkMeet* meets;
+  int32_t Hkv, G;
 };
 
 struct JoinParams {
@@ -76,13 +104,17 @@ struct ChunkLaunch {
   bool tall;            // items of up to kChunkTallRows rows on four waves, else kChunkLowRows on one
   int32_t join_rows;    // rows of the tallest joined tile
   int32_t join_pieces;  // pieces of the longest
+  bool some;            // items that leave keys out
+  int32_t n_meets, meet_rows;
 };
 
 constexpr int kChunkLowRows = 32;
 constexpr int kChunkTallRows = 128;
 constexpr int kChunkTile = 64;         // pieces are cut at multiples of this many keys
+constexpr int kNoWindow = 1 << 30;     // wider than any request is long
 
-hipError_t launch_chunk(const ChunkParams& p, const JoinParams& j, const ChunkLaunch& l, hipStream_t s);
+hipError_t launch_chunk(const ChunkParams& p, const JoinParams& j, const MeetParams& m, const ChunkLaunch& l,
+                        hipStream_t s);
 
 // The row movers' arguments hold what the host knows of a batch: N entries of a
 // table that ends at 4 KB, or as many as stay under kSmallArgs.
