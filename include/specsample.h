@@ -1,0 +1,96 @@
+/*
+ * specsample.h -- C ABI of sampling: a token of each row of logits by
+ * temperature, top-k, top-p and min-p from a given uniform, and the distribution
+ * that it was drawn from.
+ *
+ * A drafting step needs both: the tokens are spec_accept's draft_tokens and the
+ * probability rows its draft_probs (specverify.h, the test of Eq. (1) of arXiv
+ * 2505.17074 compares them with the target's).  With SPEC_SAMPLE_LOGITS a target's
+ * rows become the logits of its own truncated distribution, spec_accept's
+ * target_logits.  A row without drafts gets its token here.
+ *
+ * Conventions: those of specverify.h for streams, errors and argument checks.
+ */
+#ifndef SPECSAMPLE_H
+#define SPECSAMPLE_H
+
+#include "specverify.h"
+
+#ifdef __cplusplus
+extern "C" {
+#endif
+
+typedef enum spec_sample_rows {
+  SPEC_SAMPLE_NONE = 0,
+  SPEC_SAMPLE_PROBS = 1,
+  SPEC_SAMPLE_LOGITS = 2
+} spec_sample_rows_t;
+
+/*
+ * One row's tokens in the order of their logits, the largest first and the
+ * lower id first among equals, have the weights w = exp((l - l_max) / T).  What
+ * stays is the shortest of
+ *   top-k   the first top_k of the order;
+ *   top-p   the shortest run from the front whose weight is at least top_p times
+ *           that of the tokens that top-k leaves;
+ *   min-p   the tokens with w >= min_p;
+ * the first token in any case.  The sampled one is the smallest id whose
+ * cumulative weight, over ids ascending among what stays, exceeds u times the
+ * total (spec_accept's convention).
+ *
+ *   num_rows, vocab   >= 1.
+ *   dtype             of the logits: SPEC_F32 or SPEC_BF16.
+ *   logits            [num_rows, vocab] (device), row stride logits_stride
+ *                     elements (>= vocab), aligned to their elements.  Minus
+ *                     infinity is a token that is masked out, NaN the same; of
+ *                     plus infinities each has weight 1 and all else none.
+ *   temperature       fp32 [num_rows] (device) or NULL: 1.  Not above zero (or
+ *                     NaN): the first token alone.
+ *   top_k             int32 [num_rows] or NULL; below one: no limit.
+ *   top_p             fp32 [num_rows] or NULL; one and above: no limit, not above
+ *                     zero (or NaN): the first token alone.
+ *   min_p             fp32 [num_rows] or NULL; zero and below: no limit, above
+ *                     one (or NaN): the first token alone.
+ *   uniforms          fp32 [num_rows] in [0, 1).  May be NULL without tokens.
+ *   tokens            int32 [num_rows] out, or NULL.  -1 where a row has no token
+ *                     that is not masked out.
+ *   rows, rows_stride, rows_kind
+ *                     [num_rows, vocab] out in the logits' dtype, row stride
+ *                     rows_stride (>= vocab); the logits themselves (in place) or
+ *                     no memory that the call reads.  SPEC_SAMPLE_PROBS: the
+ *                     tokens' probabilities, zero for those that do not stay;
+ *                     SPEC_SAMPLE_LOGITS: l / T (one token alone: 0), the type's
+ *                     lowest value for those that do not stay; SPEC_SAMPLE_NONE:
+ *                     not written (rows may be NULL).  A row without tokens has
+ *                     zero probabilities, or all logits at the lowest value.
+ * Weights are taken and summed in 64 bits (off by 1e-10 of their value at most), so
+ * that tokens and the sets that stay are those of the definition unless a sum is
+ * that near to its border.  Results are deterministic.
+ */
+typedef struct spec_sample_args {
+  int32_t num_rows;
+  int32_t vocab;
+  spec_dtype_t dtype;
+  int32_t rows_kind;
+  const void* logits;
+  int64_t logits_stride;
+  const float* temperature;
+  const int32_t* top_k;
+  const float* top_p;
+  const float* min_p;
+  const float* uniforms;
+  int32_t* tokens;
+  void* rows;
+  int64_t rows_stride;
+} spec_sample_args_t;
+
+/* Device workspace of a call (256-byte aligned; may be zero bytes). */
+SPEC_API spec_status_t spec_sample_workspace_bytes(const spec_sample_args_t* args, size_t* device_bytes);
+
+SPEC_API spec_status_t spec_sample(const spec_sample_args_t* args, void* workspace, size_t workspace_bytes,
+                                   void* stream);
+
+#ifdef __cplusplus
+}
+#endif
+#endif /* SPECSAMPLE_H */

@@ -23,6 +23,9 @@ What it computes (each function cites the passage it follows):
   positions' final hidden states (the forward of Sec. 2.2 whose output is
   the target distributions of Eq. (1)).
 
+* ``sample.sample`` -- a token by temperature, top-k, top-p and min-p, and the
+  distribution it was drawn from: the draft distributions of Eq. (1).
+
 * ``scheduler.simulate`` -- the LAPS-SD request scheduler of Algorithm 1
   (Sec. 4: priority queues with exponential thresholds, demotion by attained
   service, the acceptance-rate stability test, the Eq. (6) estimate, and
@@ -36,5 +39,6 @@ so the oracle is that definition written out, not an approximation.
 """
 from .attention import verify_attention, ancestors_or_self, widen  # noqa: F401
 from .lm_head import lm_head_logits  # noqa: F401
+from .sample import sample  # noqa: F401
 from .accept import (accept_chain, accept_tree, accept_tree_sequential, verify_accept, softmax64,  # noqa: F401
                      inverse_cdf, NEAR_TIE, NEAR_TIE_MASS)

@@ -17,6 +17,7 @@ SPEC_OK, SPEC_ERR_INVALID_ARG, SPEC_ERR_UNSUPPORTED, SPEC_ERR_WORKSPACE, SPEC_ER
     SPEC_ERR_NO_PAGES = range(6)
 SPEC_F32, SPEC_BF16 = 0, 1
 SPEC_TREE_INDEPENDENT, SPEC_TREE_SEQUENTIAL = 0, 1
+SPEC_SAMPLE_NONE, SPEC_SAMPLE_PROBS, SPEC_SAMPLE_LOGITS = range(3)
 SPEC_MAX_DRAFT = 16
 SPEC_MAX_TREE_NODES = 32
 SPEC_NOALLOC_SCRATCH_BYTES = 32 << 20
@@ -31,6 +32,7 @@ EXPORTS = ("spec_workspace_bytes", "spec_verify_attn", "spec_accept", "spec_veri
            "spec_cache_copy_pages", "spec_pages_create", "spec_pages_destroy", "spec_pages_open",
            "spec_pages_resize", "spec_pages_fork", "spec_pages_close", "spec_pages_table", "spec_pages_compact",
            "spec_pages_free_count",
+           "spec_sample_workspace_bytes", "spec_sample",
            "spec_sched_create", "spec_sched_destroy", "spec_sched_submit", "spec_sched_next",
            "spec_sched_report", "spec_sched_query", "spec_sched_simulate")
 
@@ -178,6 +180,23 @@ class SpecPageCopy(C.Structure):
     _fields_ = [("src", C.c_int32), ("dst", C.c_int32), ("tokens", C.c_int32)]
 
 
+class SpecSampleArgs(C.Structure):
+    _fields_ = [("num_rows", C.c_int32),
+                ("vocab", C.c_int32),
+                ("dtype", C.c_int),
+                ("rows_kind", C.c_int32),
+                ("logits", C.c_void_p),
+                ("logits_stride", C.c_int64),
+                ("temperature", C.c_void_p),
+                ("top_k", C.c_void_p),
+                ("top_p", C.c_void_p),
+                ("min_p", C.c_void_p),
+                ("uniforms", C.c_void_p),
+                ("tokens", C.c_void_p),
+                ("rows", C.c_void_p),
+                ("rows_stride", C.c_int64)]
+
+
 class SpecSchedParams(C.Structure):
     _fields_ = [("K", C.c_int32),
                 ("M", C.c_int32),
@@ -316,6 +335,10 @@ def load(path: str = LIB_PATH) -> C.CDLL:
     lib.spec_pages_compact.restype = C.c_int
     lib.spec_pages_free_count.argtypes = [C.c_void_p]
     lib.spec_pages_free_count.restype = C.c_int32
+    lib.spec_sample_workspace_bytes.argtypes = [P(SpecSampleArgs), P(C.c_size_t)]
+    lib.spec_sample_workspace_bytes.restype = C.c_int
+    lib.spec_sample.argtypes = [P(SpecSampleArgs), C.c_void_p, C.c_size_t, C.c_void_p]
+    lib.spec_sample.restype = C.c_int
     lib.spec_sched_create.argtypes = [C.c_int32, P(SpecSchedParams), C.c_int32, P(C.c_void_p)]
     lib.spec_sched_create.restype = C.c_int
     lib.spec_sched_destroy.argtypes = [C.c_void_p]
@@ -463,6 +486,17 @@ def spec_cache_commit(req, cache, accepted_node: int, stream: int) -> int:
 
 def spec_cache_copy_pages(cache, copies: int, n: int, stream: int) -> int:
     return load().spec_cache_copy_pages(_ref(cache), copies, n, stream)
+
+
+def spec_sample_workspace_bytes(args: SpecSampleArgs):
+    """Returns (status, device_bytes)."""
+    dev = C.c_size_t(0)
+    st = load().spec_sample_workspace_bytes(_ref(args), C.byref(dev))
+    return st, dev.value
+
+
+def spec_sample(args, ws: int, ws_bytes: int, stream: int) -> int:
+    return load().spec_sample(_ref(args), ws, ws_bytes, stream)
 
 
 def int32(x) -> int:

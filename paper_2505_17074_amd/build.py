@@ -9,7 +9,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libspecverify.so")
 SOURCES = ["attention.hip", "accept.hip", "probe.hip", "noalloc.hip", "lmhead.hip", "chunk.hip", "cache.hip",
-           "specverify.cpp", "cache.cpp", "pages.cpp", "scheduler.cpp"]
+           "sample.hip", "specverify.cpp", "cache.cpp", "sample.cpp", "pages.cpp", "scheduler.cpp"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 
 FLAGS = [
