@@ -84,7 +84,8 @@ typedef struct spec_sample_args {
   int64_t rows_stride;
 } spec_sample_args_t;
 
-/* Device workspace of a call (256-byte aligned; may be zero bytes). */
+/* Device workspace of a call (256-byte aligned; it needs no initialisation and may hold
+ * anything between calls). */
 SPEC_API spec_status_t spec_sample_workspace_bytes(const spec_sample_args_t* args, size_t* device_bytes);
 
 SPEC_API spec_status_t spec_sample(const spec_sample_args_t* args, void* workspace, size_t workspace_bytes,

@@ -4,9 +4,13 @@
 
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
+
 #include "sv_sample.h"
 
 namespace {
+
+constexpr size_t kAlign = 256;
 
 spec_status_t check_sample(const spec_sample_args_t* a) {
   if (!a || a->num_rows < 1 || a->vocab < 1) return SPEC_ERR_INVALID_ARG;
@@ -33,6 +37,34 @@ spec_status_t check_sample(const spec_sample_args_t* a) {
   return SPEC_OK;
 }
 
+// How a row is cut: the fewest runs of ids of 64 units that a list of runs
+// holds, and as many slices as give the chip's compute units a work-group each,
+// none of less than 1024 units.
+struct SamplePlan {
+  int32_t slices, slice_units, slab_units, fix;
+  int64_t row_bytes;
+  size_t bytes;
+};
+SamplePlan plan_sample(const spec_sample_args_t* a) {
+  SamplePlan P;
+  const int64_t vec = a->dtype == SPEC_F32 ? 4 : 8;
+  const int64_t units = a->vocab / vec + 2;                 // wherever the row begins
+  const int64_t rounds = (units + 64 * sv::kSampleSlabs - 1) / (64 * sv::kSampleSlabs);
+  P.slab_units = (int32_t)(64 * rounds);
+  const int64_t slabs = (units + P.slab_units - 1) / P.slab_units;
+  int64_t slices = std::min<int64_t>(sv::kSampleSlices, 256 / a->num_rows);
+  slices = std::max<int64_t>(1, std::min(slices, units / 1024));
+  const int64_t per = (slabs + slices - 1) / slices;
+  P.slices = (int32_t)((slabs + per - 1) / per);
+  P.slice_units = (int32_t)(per * P.slab_units);
+  // 44 bits behind the point for slices of up to 2^18 tokens
+  P.fix = 44;
+  while (((int64_t)P.slice_units * vec) >> (62 - P.fix)) --P.fix;
+  P.row_bytes = sv::sample_row_bytes(P.slices);
+  P.bytes = (size_t)(P.row_bytes * a->num_rows + kAlign - 1) / kAlign * kAlign;
+  return P;
+}
+
 }  // namespace
 
 extern "C" {
@@ -40,15 +72,15 @@ extern "C" {
 spec_status_t spec_sample_workspace_bytes(const spec_sample_args_t* args, size_t* device_bytes) {
   if (!device_bytes) return SPEC_ERR_INVALID_ARG;
   const spec_status_t st = check_sample(args);
-  if (st == SPEC_OK) *device_bytes = 0;
+  if (st == SPEC_OK) *device_bytes = plan_sample(args).bytes;
   return st;
 }
 
 spec_status_t spec_sample(const spec_sample_args_t* args, void* workspace, size_t workspace_bytes, void* stream) {
   const spec_status_t st = check_sample(args);
   if (st != SPEC_OK) return st;
-  (void)workspace;
-  (void)workspace_bytes;
+  const SamplePlan P = plan_sample(args);
+  if (!workspace || reinterpret_cast<uintptr_t>(workspace) % kAlign || workspace_bytes < P.bytes) return SPEC_ERR_WORKSPACE;
   sv::SampleParams p{};
   p.logits = args->logits;
   p.stride = args->logits_stride;
@@ -62,6 +94,12 @@ spec_status_t spec_sample(const spec_sample_args_t* args, void* workspace, size_
   p.rows_stride = args->rows_stride;
   p.V = args->vocab;
   p.kind = args->rows_kind;
+  p.work = static_cast<char*>(workspace);
+  p.row_bytes = P.row_bytes;
+  p.slices = P.slices;
+  p.slice_units = P.slice_units;
+  p.slab_units = P.slab_units;
+  p.fix = P.fix;
   return sv::launch_sample(p, args->num_rows, args->dtype == SPEC_F32, static_cast<hipStream_t>(stream)) == hipSuccess
              ? SPEC_OK
              : SPEC_ERR_HIP;

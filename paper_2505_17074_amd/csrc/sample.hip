@@ -18,8 +18,11 @@ namespace {
 
 constexpr int kThreads = 1024, kWaves = kThreads / 64;
 constexpr int kBins = 2048;            // ranges of a histogram
-constexpr int kList = 1024;            // tokens of a list: one a thread
-constexpr int kSlabs = 256;            // runs of ids whose weights are summed apart
+constexpr int kRank = 1024;            // tokens ranked by counting: one a thread
+constexpr int kList = kSampleList;     // tokens of a sorted list
+constexpr int kSlabs = kSampleSlabs;   // runs of ids whose weights are summed apart
+constexpr int kAhead = 8;              // units that a thread loads at once
+static_assert(kBins == kSampleBins, "a slice's histogram in the workspace");
 
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
@@ -74,6 +77,38 @@ struct Row {
     const uint32_t m = b & 0x7fffffffu;
     return __uint_as_float(m > 0x7f800000u ? 0xff800000u : m == 0 ? 0 : b);
   }
+  // Unit u as it is; elements outside the row are minus infinity.
+  __device__ __forceinline__ u32x4 raw(int u) const {
+    if (whole(u)) return *reinterpret_cast<const u32x4*>(base + (int64_t)u * 16);
+    u32x4 r;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      uint32_t b = F32 ? 0xff800000u : 0xff80ff80u;
+#pragma unroll
+      for (int h = 0; h < VEC / 4; ++h) {
+        const int i = w * (VEC / 4) + h, id = first_id(u) + i;
+        if (u < units && id >= 0 && id < V) {
+          const char* at = base + ((int64_t)u * VEC + i) * EB;
+          if constexpr (F32) b = *reinterpret_cast<const uint32_t*>(at);
+          else b = (b & ~(0xffffu << 16 * h)) | (uint32_t)*reinterpret_cast<const uint16_t*>(at) << 16 * h;
+        }
+      }
+      r[w] = b;
+    }
+    return r;
+  }
+  // Its values; a NaN among them fails every comparison below, as minus infinity does.
+  __device__ __forceinline__ static void values(u32x4 r, float (&x)[VEC]) {
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      if constexpr (F32) {
+        x[w] = __uint_as_float(r[w]);
+      } else {
+        x[2 * w] = __uint_as_float(r[w] << 16);
+        x[2 * w + 1] = __uint_as_float(r[w] & 0xffff0000u);
+      }
+    }
+  }
   // Unit u's values; elements outside the row are minus infinity.
   __device__ __forceinline__ void load(int u, float (&x)[VEC]) const {
     if (whole(u)) {
@@ -106,12 +141,18 @@ struct Shared {
   union {
     uint32_t count[kBins];
     unsigned long long mass[kBins];
+    unsigned long long by_id[kList];
+    unsigned long long add[kSlabs];
   };
-  struct {
-    float x[kList];
-    int id[kList];
-    double w[kList];
-  } list;
+  union {
+    struct {
+      float x[kRank];
+      int id[kRank];
+      double w[kRank];
+    } list;
+    unsigned long long keys[kList];
+  };
+  double w[kList];
   int n;                               // of the list
   unsigned long long red[kWaves];
   unsigned long long out[2];
@@ -238,7 +279,7 @@ struct Sampler {
       lo = block_reduce(lo, [](uint32_t a, uint32_t b) { return min(a, b); });
       hi = block_reduce(hi, [](uint32_t a, uint32_t b) { return max(a, b); });
       n = block_reduce(n, [](int a, int b) { return a + b; });
-      if (n <= kList || lo == hi) break;
+      if (n <= kRank || lo == hi) break;
       // again, over keys lo .. hi
       const int shift = max(0, 21 - __builtin_clz((hi - lo) | 1));
       const uint32_t first = lo, last = hi;
@@ -266,7 +307,7 @@ struct Sampler {
         }
       });
     }
-    if (n > kList) return tie<MASS>(lo, mark, sum, in);
+    if (n > kRank) return tie<MASS>(lo, mark, sum, in);
     // the tokens as a list, and for each what comes before it in the order
     if (threadIdx.x == 0) sh.n = 0;
     __syncthreads();
@@ -354,41 +395,510 @@ struct Sampler {
   }
 };
 
-// One work-group a row.
+// ---------------------------------------------------------------------------
+// The same in slices, so that a few long rows fill the chip.  A row is cut into
+// `slices` runs of units, one work-group each:
+//   sample_scan     a slice's largest value and a histogram below it, of counts
+//                   (top-k) or weights (top-p without it), over ranges of values
+//                   that all slices have in common;
+//   sample_collect  every slice's work-group adds the row's histograms and finds
+//                   the range where the mark is reached; it lists its tokens of
+//                   that range (and, for a small top-k, of all ranges before) and
+//                   sums the weights of those before it, run of ids by run of ids;
+//   sample_token    one work-group a row sorts the list, cuts it, and finds the
+//                   token;
+//   sample_rows     writes the distribution.
+// With one slice the four are one kernel.  A row that this does not suit (its
+// mark past the 2048 ranges, more tokens in one range than a list holds, a
+// top-p behind a large top-k) takes the way above in sample_token.
+
+enum Mode { kAll = 0, kFirst = 1, kEdge = 2, kHard = 3, kNone = 4 };
+
+constexpr double kListUnit = 281474976710656.0;      // 2^48: a list's weights in fixed point
+
+// What a row asks for.
+struct Rule {
+  float T, top_p, min_p;
+  int k;
+  bool one, by_count, by_mass;         // a cut by top-k, by top-p alone
+  float scale;                         // ranges a unit of value
+  double c;                            // log2(e) / T
+
+  __device__ Rule(const SampleParams& p, int r) {
+    T = p.temperature ? p.temperature[r] : 1.f;
+    k = p.top_k ? p.top_k[r] : 0;
+    top_p = p.top_p ? p.top_p[r] : 1.f;
+    min_p = p.min_p ? p.min_p[r] : 0.f;
+    one = !(T > 0.f) || !(top_p > 0.f) || !(min_p <= 1.f);
+    if (k < 1 || k > p.V) k = p.V;
+    if (one) k = 1, T = 1.f, top_p = 1.f, min_p = 0.f;
+    c = 1.4426950408889634074 / (double)T;
+    by_count = k < p.V;
+    by_mass = !by_count && top_p < 1.f;
+    // counts: 64 units of value in all, logits' own scale; weights: 32 T, past
+    // which e^-32 of the largest weight is left a token
+    scale = by_count ? (float)kBins / 64.f : (float)kBins / (32.f * T);
+  }
+  // The range of a value, counted upwards (whole numbers in fp32: exact below 2^24).
+  __device__ __forceinline__ float range(float x) const { return floorf(x * scale); }
+};
+
+// What sample_collect leaves of a row, the same from all its slices.
+struct RowState {
+  int mode;
+  float range;                         // the one where the mark is reached
+  double before, mark;                 // sums ahead of it (counts or weights), the mark
+};
+
+struct RowView {
+  SampleRow s;
+  __device__ RowView(const SampleParams& p, int r) {
+    char* at = p.work + (int64_t)r * p.row_bytes;
+    s.top = reinterpret_cast<float*>(at);
+    s.n = reinterpret_cast<int32_t*>(at + 64);
+    s.sum = reinterpret_cast<double*>(at + 128);
+    s.state = at + 192;
+    s.done = at + 256;
+    s.slab = reinterpret_cast<double*>(at + kSampleHead);
+    s.list = reinterpret_cast<unsigned long long*>(at + kSampleHead + sizeof(double) * kSlabs);
+    s.hist = s.list + (int64_t)p.slices * kList;
+  }
+};
+static_assert(sizeof(RowState) <= 64, "a row's state");
+
+// What sample_token leaves for sample_rows.
+struct RowDone {
+  Cut cut;
+  double total;
+  float top;
+  int kept;                            // none: all masked out
+};
+static_assert(sizeof(RowDone) <= 64, "a row's outcome");
+
 template <bool F32>
-__global__ __launch_bounds__(kThreads) void sample_row(SampleParams p) {
-  __shared__ Shared sh;
-  const int r = blockIdx.x, t = threadIdx.x;
-  const Row<F32> row(static_cast<const char*>(p.logits) + r * p.stride * Row<F32>::EB, p.V);
-  constexpr int VEC = Row<F32>::VEC;
-  Sampler<F32> S(row, sh);
+struct Slices {
+  using R = Row<F32>;
+  static constexpr int VEC = R::VEC;
+  const SampleParams& p;
+  const R& row;
+  Shared& sh;
+  const Rule& rule;
+  SampleRow ws;
+  float top;
 
-  float top = -INFINITY;
-  S.each([&](float x, int) { top = fmaxf(top, x); });
-  top = S.block_reduce(top, [](float a, float b) { return fmaxf(a, b); });
-  S.top = top;
+  __device__ __forceinline__ int begin(int slice) const { return slice * p.slice_units; }
+  __device__ __forceinline__ int end(int slice) const { return min((slice + 1) * p.slice_units, row.units); }
+  __device__ __forceinline__ double weight(float x) const { return x == top ? 1.0 : exp2_64(((double)x - (double)top) * rule.c); }
+  // w in units of 1 / unit: the integer in the low bits of a double between 2^52 and 2^53
+  __device__ __forceinline__ static unsigned long long fixed(double w, double unit) {
+    return __builtin_bit_cast(unsigned long long, __builtin_fma(w, unit, 4503599627370496.0)) & 0xfffffffffffffull;
+  }
 
-  float T = p.temperature ? p.temperature[r] : 1.f;
-  int k = p.top_k ? p.top_k[r] : 0;
-  float tp = p.top_p ? p.top_p[r] : 1.f;
-  float mp = p.min_p ? p.min_p[r] : 0.f;
-  const bool one = !(T > 0.f) || !(tp > 0.f) || !(mp <= 1.f);
-  if (k < 1 || k > p.V) k = p.V;
-  if (one) k = 1;
-  if (!(T > 0.f) || one) T = 1.f;
-  if (one) tp = 1.f, mp = 0.f;
-  S.c = 1.4426950408889634074 / (double)T;
-  S.bins = (float)kBins / (32.f * T);
-  S.fix = 62 - (32 - __builtin_clz(p.V));
+  template <typename T, typename F>
+  __device__ __forceinline__ T reduce(T x, F&& f) const {
+#pragma unroll
+    for (int i = 32; i > 0; i >>= 1) x = f(x, __shfl_xor(x, i));
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0) reinterpret_cast<T*>(sh.red)[threadIdx.x / 64] = x;
+    __syncthreads();
+    x = reinterpret_cast<T*>(sh.red)[0];
+#pragma unroll
+    for (int i = 1; i < kWaves; ++i) x = f(x, reinterpret_cast<T*>(sh.red)[i]);
+    return x;
+  }
+  // Sums of x over the threads up to and including this one.
+  __device__ __forceinline__ double scan(double x) const {
+#pragma unroll
+    for (int i = 1; i < 64; i <<= 1) {
+      const double y = __shfl_up(x, i);
+      if ((threadIdx.x & 63) >= i) x += y;
+    }
+    __syncthreads();
+    if ((threadIdx.x & 63) == 63) reinterpret_cast<double*>(sh.red)[threadIdx.x / 64] = x;
+    __syncthreads();
+    double base = 0.0;
+    for (int i = 0; i < (int)threadIdx.x / 64; ++i) base += reinterpret_cast<double*>(sh.red)[i];
+    return base + x;
+  }
 
-  Cut cut = {-INFINITY, 0x7fffffff};
-  if (top > -INFINITY) {
+  __device__ void scan_slice(int slice) {
+    const int t = threadIdx.x, u0 = begin(slice), u1 = end(slice);
+    u32x4 r[kAhead];
+    float m = -INFINITY;
+    auto load = [&](int at) {
+#pragma unroll
+      for (int j = 0; j < kAhead; ++j) {
+        const int u = at + t + j * kThreads;
+        r[j] = u < u1 ? row.raw(u) : u32x4{0xffffffffu, 0xffffffffu, 0xffffffffu, 0xffffffffu};     // NaN
+      }
+    };
+    load(u0);
+    for (int at = u0;;) {
+#pragma unroll
+      for (int j = 0; j < kAhead; ++j) {
+        float x[VEC];
+        R::values(r[j], x);
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) m = fmaxf(m, x[i]);
+      }
+      at += kAhead * kThreads;
+      if (at >= u1) break;
+      load(at);
+    }
+    top = reduce(m, [](float a, float b) { return fmaxf(a, b); });
+    if (t == 0) ws.top[slice] = top;
+    if (!rule.by_count && !rule.by_mass) return;
+    for (int i = t; i < kBins; i += kThreads) sh.mass[i] = 0;
+    __syncthreads();
+    const float first = rule.range(top);
+    const double unit = __builtin_amdgcn_ldexp(1.0, p.fix);
+    unsigned long long all = 0;
+    if (top > -INFINITY) {
+      const bool one_batch = u0 + kAhead * kThreads >= u1;
+      for (int at = u0; at < u1; at += kAhead * kThreads) {
+        if (!one_batch) load(at);
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j) {
+          if (at + j * kThreads >= u1) break;
+          float x[VEC];
+          R::values(r[j], x);
+#pragma unroll
+          for (int i = 0; i < VEC; ++i) {
+            if (!(x[i] > -INFINITY)) continue;
+            const int b = (int)fminf(first - rule.range(x[i]), (float)(kBins - 1));
+            if (rule.by_count) {
+              atomicAdd(&sh.count[b], 1u);
+              ++all;
+            } else {
+              const unsigned long long w = fixed(weight(x[i]), unit);
+              atomicAdd(&sh.mass[b], w);
+              all += w;
+            }
+          }
+        }
+      }
+    }
+    all = reduce(all, [](unsigned long long a, unsigned long long b) { return a + b; });
+    if (t == 0) ws.sum[slice] = rule.by_count ? (double)all : (double)all / unit;
+    unsigned long long* to = ws.hist + (int64_t)slice * kBins;
+    if (rule.by_count) {
+      for (int i = t; i < kBins; i += kThreads) reinterpret_cast<uint32_t*>(to)[i] = sh.count[i];
+    } else {
+      for (int i = t; i < kBins; i += kThreads) to[i] = sh.mass[i];
+    }
+  }
+
+  // The row's largest value, and where its mark is reached.
+  __device__ RowState state() {
+    top = -INFINITY;
+    for (int s = 0; s < p.slices; ++s) top = fmaxf(top, ws.top[s]);
+    RowState st = {kAll, 0.f, 0.0, 0.0};
+    if (!(top > -INFINITY)) st.mode = kNone;
+    if (st.mode == kNone || (!rule.by_count && !rule.by_mass)) return st;
+    const float first = rule.range(top);
+    if (!(fabsf(first) < 8388608.f)) {                     // ranges are not whole numbers apart (or the largest is infinite)
+      st.mode = kHard;
+      return st;
+    }
+    // ranges 2 t and 2 t + 1 of the row: the sums of its slices', each further
+    // down by what its own largest value is
+    const double unit = __builtin_amdgcn_ldexp(1.0, -p.fix);
+    double a = 0.0, b = 0.0, all = 0.0;
+    for (int s = 0; s < p.slices; ++s) {
+      const float ts = ws.top[s];
+      if (!(ts > -INFINITY)) continue;
+      const double f = rule.by_count ? 1.0 : weight(ts) * unit;
+      all += ws.sum[s] * (rule.by_count ? 1.0 : weight(ts));
+      const int off = (int)fminf(first - rule.range(ts), (float)kBins);
+      const unsigned long long* h = ws.hist + (int64_t)s * kBins;
+      const int j = 2 * (int)threadIdx.x - off;
+      if (rule.by_count) {
+        const uint32_t* hc = reinterpret_cast<const uint32_t*>(h);
+        if (j >= 0 && j < kBins - 1) a += (double)hc[j];
+        if (j + 1 >= 0 && j + 1 < kBins - 1) b += (double)hc[j + 1];
+      } else {
+        if (j >= 0 && j < kBins - 1) a += (double)h[j] * f;
+        if (j + 1 >= 0 && j + 1 < kBins - 1) b += (double)h[j + 1] * f;
+      }
+    }
+    if (2 * threadIdx.x + 1 >= kBins - 1) b = 0.0;         // the last range has what lies further down
+    if (rule.by_count && (double)rule.k >= all) {
+      st.mode = rule.top_p < 1.f ? kHard : kAll;           // nothing is cut
+      return st;
+    }
+    st.mark = rule.by_count ? (double)rule.k : (double)rule.top_p * all;
+    const double s2 = scan(a + b), s1 = s2 - b, s0 = s1 - a;
+    if (threadIdx.x == 0) sh.out[0] = kBins;
+    __syncthreads();
+    // the first range that reaches the mark: the sums do not fall, but for rounding
+    if (s2 >= st.mark) atomicMin(&sh.out[0], (unsigned long long)(2 * threadIdx.x + (s1 >= st.mark ? 0 : 1)));
+    __syncthreads();
+    const int bin = (int)sh.out[0];
+    if (bin < kBins && (int)threadIdx.x == bin / 2) reinterpret_cast<double*>(sh.red)[0] = bin & 1 ? s1 : s0;
+    __syncthreads();
+    st.before = reinterpret_cast<double*>(sh.red)[0];
+    __syncthreads();
+    if (bin >= kBins - 1) st.mode = kHard;
+    else if (rule.by_count && rule.k <= kSampleFirst) st.mode = kFirst;
+    else st.mode = rule.by_count && rule.top_p < 1.f ? kHard : kEdge;
+    st.range = first - (float)bin;
+    return st;
+  }
+
+  __device__ void collect_slice(int slice, const RowState& st) {
+    const int t = threadIdx.x, lane = t & 63;
+    if (t == 0) sh.n = 0;
+    __syncthreads();
+    if (slice == 0 && t == 0) *reinterpret_cast<RowState*>(ws.state) = st;
+    if (st.mode == kHard || st.mode == kNone) return;
+    unsigned long long* list = ws.list + (int64_t)slice * kList;
+    const double least = rule.min_p;
+    // a slice's units are whole runs of ids
+    const int per = p.slab_units, u1 = end(slice);
+    for (int u0 = begin(slice) + t / 64 * per; u0 < u1; u0 += kWaves * per) {
+      double sum = 0.0;
+      for (int at = u0; at < min(u0 + per, u1); at += 64) {
+        const int u = at + lane;
+        if (u >= u1) continue;
+        float x[VEC];
+        R::values(row.raw(u), x);
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) {
+          if (!(x[i] > -INFINITY)) continue;
+          bool ahead = st.mode == kAll, listed = false;
+          if (st.mode != kAll) {
+            const float g = rule.range(x[i]);
+            listed = st.mode == kFirst ? g >= st.range : g == st.range;
+            ahead = st.mode == kEdge && g > st.range;
+          }
+          if (ahead) {
+            const double w = weight(x[i]);
+            if (w >= least) sum += w;
+          }
+          if (listed) {
+            const int n = atomicAdd(&sh.n, 1);
+            if (n < kList) list[n] = (unsigned long long)key_of(R::clean(__float_as_uint(x[i]))) << 32 | (uint32_t)(row.first_id(u) + i);
+          }
+        }
+      }
+      if (st.mode != kFirst) {
+        sum = wave_sum(sum);
+        if (lane == 0) ws.slab[u0 / per] = sum;
+      }
+    }
+    __syncthreads();
+    if (t == 0) ws.n[slice] = sh.n;
+  }
+
+  // sh.keys[0 .. n) ascending (n <= kList); entries up to the next power of two are written.
+  __device__ void sort(unsigned long long* keys, int n) const {
+    int N = 64;
+    while (N < n) N *= 2;
+    for (int i = n + threadIdx.x; i < N; i += kThreads) keys[i] = ~0ull;
+    __syncthreads();
+    for (int k = 2; k <= N; k *= 2)
+      for (int j = k / 2; j > 0; j /= 2) {
+        for (int i = threadIdx.x; i < N / 2; i += kThreads) {
+          const int a = (i & ~(j - 1)) * 2 + (i & (j - 1)), b = a + j;
+          const unsigned long long x = keys[a], y = keys[b];
+          if ((x > y) == ((a & k) == 0)) {
+            keys[a] = y;
+            keys[b] = x;
+          }
+        }
+        __syncthreads();
+      }
+  }
+  __device__ __forceinline__ static float value_of(unsigned long long key) {
+    const uint32_t k = (uint32_t)(key >> 32);
+    return __uint_as_float((int32_t)k < 0 ? k : ~k & 0x7fffffffu);
+  }
+  // The weights of two neighbours of the list, and their sums from the list's start.
+  struct Two {
+    double w0, w1, s0, s1;
+  };
+  __device__ __forceinline__ Two weights(int n) const {
+    const int i = 2 * threadIdx.x;
+    Two y;
+    y.w0 = i < n ? weight(value_of(sh.keys[i])) : 0.0;
+    y.w1 = i + 1 < n ? weight(value_of(sh.keys[i + 1])) : 0.0;
+    y.s1 = scan(y.w0 + y.w1);
+    y.s0 = y.s1 - y.w1;
+    return y;
+  }
+  // The number of list entries that `f(entry, weight, sum)` holds for (a run from the front).
+  template <typename F>
+  __device__ __forceinline__ int count(const Two& y, int n, F&& f) const {
+    const int i = 2 * threadIdx.x;
+    const int c = (i < n && f(i, y.w0, y.s0)) + (i + 1 < n && f(i + 1, y.w1, y.s1));
+    return reduce(c, [](int a, int b) { return a + b; });
+  }
+
+  // The token and what stays.  False: the row takes the other way.
+  __device__ bool finish(int r, const RowState& st, RowDone& done, int& token) {
+    const int t = threadIdx.x;
+    top = -INFINITY;
+    for (int s = 0; s < p.slices; ++s) top = fmaxf(top, ws.top[s]);
+    done = {{-INFINITY, 0x7fffffff}, 1.0, top, 1};
+    token = -1;
+    if (st.mode == kNone) {
+      done.kept = 0;
+      return true;
+    }
+    if (st.mode == kHard) return false;
+    int n = 0;
+    if (st.mode != kAll) {
+      for (int s = 0; s < p.slices; ++s) {
+        const int m = ws.n[s];
+        if (n + m > kList) return false;                   // the same for all threads
+        for (int i = t; i < m; i += kThreads) sh.keys[n + i] = ws.list[(int64_t)s * kList + i];
+        n += m;
+      }
+      sort(sh.keys, n);
+    }
+    const double u = p.tokens ? (double)p.uniforms[r] : 0.0, least = rule.min_p;
+    if (st.mode == kFirst) {
+      n = min(n, rule.k);
+      Two y = weights(n);
+      int stay = n;
+      if (rule.top_p < 1.f) {
+        if (2 * t == (n - 1) / 2 * 2) reinterpret_cast<double*>(sh.out)[0] = n & 1 ? y.s0 : y.s1;
+        __syncthreads();
+        const double mark = (double)rule.top_p * reinterpret_cast<double*>(sh.out)[0];
+        stay = min(stay, 1 + count(y, n, [&](int, double, double s) { return s < mark; }));
+      }
+      if (least > 0.0) stay = min(stay, max(1, count(y, n, [&](int, double w, double) { return w >= least; })));
+      done.cut = {value_of(sh.keys[stay - 1]), (int)(uint32_t)sh.keys[stay - 1]};
+      // ids ascending: (id, place in the list)
+      for (int i = t; i < stay; i += kThreads) {
+        sh.by_id[i] = (sh.keys[i] << 32) | (uint32_t)i;
+        sh.w[i] = weight(value_of(sh.keys[i]));
+      }
+      __syncthreads();
+      sort(sh.by_id, stay);
+      const int i = 2 * t;
+      const double w0 = i < stay ? sh.w[(uint32_t)sh.by_id[i]] : 0.0, w1 = i + 1 < stay ? sh.w[(uint32_t)sh.by_id[i + 1]] : 0.0;
+      const double s1 = scan(w0 + w1), s0 = s1 - w1;
+      if (t == (stay - 1) / 2) reinterpret_cast<double*>(sh.out)[0] = s1;
+      __syncthreads();
+      done.total = reinterpret_cast<double*>(sh.out)[0];
+      __syncthreads();
+      // the first whose sum exceeds the mark (none: the last that has weight)
+      const double mark = u * done.total;
+      int best = 0x7fffffff, last = 0;
+      if (w1 > 0.0) last = i + 1;
+      else if (w0 > 0.0) last = i;
+      if (w1 > 0.0 && s1 > mark) best = i + 1;
+      if (w0 > 0.0 && s0 > mark) best = i;
+      best = reduce(best, [](int a, int b) { return min(a, b); });
+      last = reduce(last, [](int a, int b) { return max(a, b); });
+      token = (int)(sh.by_id[min(best, last)] >> 32);
+      return true;
+    }
+    if (st.mode == kEdge) {
+      if (n == 0) return false;
+      const Two y = weights(n);
+      // how many of the list stay: the first that reaches what is left of the mark is the last
+      const double left = st.mark - st.before;
+      const int stay = rule.by_count ? min(max((int)left, 1), n)
+                                     : min(1 + count(y, n, [&](int, double, double s) { return s < left; }), n);
+      done.cut = {value_of(sh.keys[stay - 1]), (int)(uint32_t)sh.keys[stay - 1]};
+      for (int i = t; i < kSlabs; i += kThreads) sh.add[i] = 0;
+      __syncthreads();
+      // to the sums of their runs, in units of 2^-48 so that their order does not matter
+      for (int k = 0; k < 2; ++k) {
+        const int i = 2 * t + k;
+        const double w = k ? y.w1 : y.w0;
+        if (i < stay && w >= least)
+          atomicAdd(&sh.add[((int)(uint32_t)sh.keys[i] + row.head) / VEC / p.slab_units], fixed(w, kListUnit));
+      }
+      __syncthreads();
+    }
+    by_runs(st.mode == kEdge, u, done, token);
+    return true;
+  }
+
+  // The total, and the token, of what stays by the sums of its runs of ids (`list`: and
+  // the listed ones').
+  __device__ void by_runs(bool list, double u, RowDone& done, int& token) {
+    static_assert(kSlabs == kThreads, "a run a thread");
+    const int t = threadIdx.x, slabs = (row.units + p.slab_units - 1) / p.slab_units;
+    double mine = t < slabs ? ws.slab[t] : 0.0;
+    if (list && t < slabs) mine += (double)sh.add[t] * (1.0 / kListUnit);
+    const double s1 = scan(mine);
+    if (t == kThreads - 1) reinterpret_cast<double*>(sh.out)[0] = s1;
+    __syncthreads();
+    done.total = reinterpret_cast<double*>(sh.out)[0];
+    if (!p.tokens) return;
+    const double mark = u * done.total;
+    int best = reduce(mine > 0.0 && s1 > mark ? t : 0x7fffffff, [](int a, int b) { return min(a, b); });
+    best = min(best, reduce(mine > 0.0 ? t : 0, [](int a, int b) { return max(a, b); }));
+    if (t == best) reinterpret_cast<double*>(sh.out)[0] = s1 - mine;
+    __syncthreads();
+    const double before = reinterpret_cast<double*>(sh.out)[0];
+    if (t < 64)
+      token = in_run(best * p.slab_units, min((best + 1) * p.slab_units, row.units), before, mark, done.cut, rule.min_p);
+  }
+
+  // The first token of units [u0, u1) where the sum of what stays, from `run` on, exceeds
+  // `mark`, or the last that has weight; by one wave.
+  __device__ int in_run(int u0, int u1, double run, double mark, const Cut& cut, double least) const {
+    const int lane = threadIdx.x;
+    int best = 0x7fffffff, behind = -1;
+    for (; u0 < u1 && best == 0x7fffffff; u0 += 64) {
+      const int u = u0 + lane;
+      float x[VEC];
+      double y[VEC], mine = 0.0;
+      if (u < u1) row.load(u, x);
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) {
+        y[i] = 0.0;
+        if (u < u1 && x[i] > -INFINITY && cut.keeps(x[i], row.first_id(u) + i)) {
+          y[i] = weight(x[i]);
+          if (!(y[i] >= least)) y[i] = 0.0;
+        }
+        mine += y[i];
+      }
+      double sum = mine;
+#pragma unroll
+      for (int i = 1; i < 64; i <<= 1) {
+        const double z = __shfl_up(sum, i);
+        if (lane >= i) sum += z;
+      }
+      double at = run + sum - mine;
+      int found = 0x7fffffff;
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) {
+        at += y[i];
+        if (y[i] > 0.0) behind = row.first_id(u) + i;
+        if (y[i] > 0.0 && at > mark && found == 0x7fffffff) found = row.first_id(u) + i;
+      }
+#pragma unroll
+      for (int i = 32; i > 0; i >>= 1) found = min(found, __shfl_xor(found, i));
+      best = found;
+      run += __shfl(sum, 63);
+    }
+#pragma unroll
+    for (int i = 32; i > 0; i >>= 1) behind = max(behind, __shfl_xor(behind, i));
+    return best == 0x7fffffff ? behind : best;
+  }
+
+  // The row by the histograms of the whole of it (the first half of this file).
+  __device__ void hard(int r, RowDone& done, int& token) {
+    const int t = threadIdx.x;
+    __syncthreads();
+    Sampler<F32> S(row, sh);
+    S.top = top;
+    S.c = rule.c;
+    S.bins = (float)kBins / (32.f * rule.T);
+    S.fix = 62 - (32 - __builtin_clz(p.V));
+    Cut cut = {-INFINITY, 0x7fffffff};
     auto clear = [&] {
       __syncthreads();
       for (int i = t; i < kBins; i += kThreads) sh.mass[i] = 0;
       __syncthreads();
     };
-    if (k < p.V) {
+    if (rule.k < p.V) {
       clear();
       int n = 0;
       S.each([&](float x, int) {
@@ -396,9 +906,9 @@ __global__ __launch_bounds__(kThreads) void sample_row(SampleParams p) {
         ++n;
       });
       n = S.block_reduce(n, [](int a, int b) { return a + b; });
-      if (k < n) cut = S.template last_of<false>((unsigned long long)k, cut);
+      if (rule.k < n) cut = S.template last_of<false>((unsigned long long)rule.k, cut);
     }
-    if (tp < 1.f) {
+    if (rule.top_p < 1.f) {
       clear();
       unsigned long long all = 0;
       S.each([&](float x, int id) {
@@ -408,138 +918,127 @@ __global__ __launch_bounds__(kThreads) void sample_row(SampleParams p) {
         all += w;
       });
       all = S.block_reduce(all, [](unsigned long long a, unsigned long long b) { return a + b; });
-      const unsigned long long mark = (unsigned long long)ceil((double)tp * (double)all);
+      const unsigned long long mark = (unsigned long long)ceil((double)rule.top_p * (double)all);
       cut = S.template last_of<true>(min(max(mark, 1ull), all), cut);
     }
-  }
-  const double least = mp;
-  auto kept = [&](float x, int id) { return x > -INFINITY && cut.keeps(x, id); };
-
-  // sums of the weights over runs of ids, in the ids' order
-  double total = 0.0;
-  const int per = (row.units + kSlabs - 1) / kSlabs;       // units of a run
-  const int w = t / 64, lane = t & 63;
-  for (int s = w; s < kSlabs; s += kWaves) {
-    double sum = 0.0;
-    for (int u0 = s * per; u0 < min((s + 1) * per, row.units); u0 += 64) {
-      const int u = u0 + lane;
-      if (u < (s + 1) * per) {
+    // sums of the weights over runs of ids, in the ids' order
+    const double least = rule.min_p;
+    const int lane = t & 63, per = p.slab_units, slabs = (row.units + per - 1) / per;
+    for (int s = t / 64; s < slabs; s += kWaves) {
+      double sum = 0.0;
+      for (int u = s * per + lane; u < min((s + 1) * per, row.units); u += 64) {
         float x[VEC];
         row.load(u, x);
 #pragma unroll
-        for (int i = 0; i < VEC; ++i) {
-          if (kept(x[i], row.first_id(u) + i)) {
-            const double y = S.weight(x[i]);
+        for (int i = 0; i < VEC; ++i)
+          if (x[i] > -INFINITY && cut.keeps(x[i], row.first_id(u) + i)) {
+            const double y = weight(x[i]);
             if (y >= least) sum += y;
           }
-        }
       }
+      sum = wave_sum(sum);
+      if (lane == 0) ws.slab[s] = sum;
     }
-    sum = wave_sum(sum);
-    if (lane == 0) sh.slab[s] = sum;
-  }
-  __syncthreads();
-  for (int s = 0; s < kSlabs; ++s) total += sh.slab[s];
-
-  if (p.tokens && w == 0) {
-    int token = -1;
-    if (top > -INFINITY) {
-      const double mark = (double)p.uniforms[r] * total;
-      double run = 0.0;
-      int s = 0, last = 0;
-      for (; s < kSlabs; ++s) {
-        if (sh.slab[s] > 0.0) last = s;
-        if (run + sh.slab[s] > mark) break;
-        run += sh.slab[s];
-      }
-      if (s == kSlabs) {                                   // a uniform of one: the last token that has weight
-        s = last;
-        run = 0.0;
-        for (int i = 0; i < s; ++i) run += sh.slab[i];
-      }
-      int best = 0x7fffffff, behind = -1;
-      for (int u0 = s * per; u0 < min((s + 1) * per, row.units) && best == 0x7fffffff; u0 += 64) {
-        const int u = u0 + lane;
-        float x[VEC];
-        double y[VEC], mine = 0.0;
-        if (u < (s + 1) * per) row.load(u, x);
-#pragma unroll
-        for (int i = 0; i < VEC; ++i) {
-          y[i] = 0.0;
-          if (u < (s + 1) * per && kept(x[i], row.first_id(u) + i)) {
-            y[i] = S.weight(x[i]);
-            if (!(y[i] >= least)) y[i] = 0.0;
-          }
-          mine += y[i];
-        }
-        double sum = mine;
-#pragma unroll
-        for (int i = 1; i < 64; i <<= 1) {
-          const double z = __shfl_up(sum, i);
-          if (lane >= i) sum += z;
-        }
-        double at = run + sum - mine;
-        int found = 0x7fffffff;
-#pragma unroll
-        for (int i = 0; i < VEC; ++i) {
-          at += y[i];
-          if (y[i] > 0.0) behind = row.first_id(u) + i;
-          if (y[i] > 0.0 && at > mark && found == 0x7fffffff) found = row.first_id(u) + i;
-        }
-#pragma unroll
-        for (int i = 32; i > 0; i >>= 1) found = min(found, __shfl_xor(found, i));
-        best = found;
-        run += __shfl(sum, 63);
-      }
-#pragma unroll
-      for (int i = 32; i > 0; i >>= 1) behind = max(behind, __shfl_xor(behind, i));
-      token = best == 0x7fffffff ? behind : best;
-    }
-    if (lane == 0) p.tokens[r] = token;
+    __syncthreads();
+    done.cut = cut;
+    by_runs(false, p.tokens ? (double)p.uniforms[r] : 0.0, done, token);
   }
 
-  if (p.kind == 0) return;
-  __syncthreads();                                         // the rows may be the logits
-  char* out = static_cast<char*>(p.rows) + r * p.rows_stride * Row<F32>::EB;
-  const float lowest = F32 ? -3.4028234663852886e38f : -3.3895313892515355e38f;
-  const bool lines = (reinterpret_cast<uintptr_t>(out) - (uintptr_t)(row.head * Row<F32>::EB)) % 16 == 0;
-  S.each_unit([&](int u, const float (&x)[VEC]) {
-    float y[VEC];
-#pragma unroll
-    for (int i = 0; i < VEC; ++i) {
-      y[i] = p.kind == 1 ? 0.f : lowest;
-      if (kept(x[i], row.first_id(u) + i)) {
-        const double q = S.weight(x[i]);
-        if (q >= least) y[i] = p.kind == 1 ? (float)(q / total) : one ? 0.f : (float)((double)x[i] / (double)T);
-      }
-    }
-    uint32_t raw[VEC];
-#pragma unroll
-    for (int i = 0; i < VEC; ++i) raw[i] = F32 ? __float_as_uint(y[i]) : (uint32_t)__builtin_bit_cast(uint16_t, (__bf16)y[i]);
-    char* at = out + (int64_t)row.first_id(u) * Row<F32>::EB;
-    if (lines && row.whole(u)) {
-      u32x4 z;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) z[i] = F32 ? raw[i] : raw[(2 * i) % VEC] | raw[(2 * i + 1) % VEC] << 16;
-      *reinterpret_cast<u32x4*>(at) = z;
-    } else {
+  __device__ void write_rows(int r, int slice, const RowDone& done) {
+    top = done.top;
+    char* out = static_cast<char*>(p.rows) + r * p.rows_stride * R::EB;
+    const bool probs = p.kind == 1;
+    const float none = probs ? 0.f : F32 ? -3.4028234663852886e38f : -3.3895313892515355e38f;
+    const bool lines = (reinterpret_cast<uintptr_t>(out) - (uintptr_t)(row.head * R::EB)) % 16 == 0;
+    const double least = rule.min_p, share = 1.0 / done.total;
+    for (int u = begin(slice) + threadIdx.x; u < end(slice); u += kThreads) {
+      float x[VEC], y[VEC];
+      row.load(u, x);
+      uint32_t raw[VEC];
 #pragma unroll
       for (int i = 0; i < VEC; ++i) {
-        const int id = row.first_id(u) + i;
-        if (id < 0 || id >= p.V) continue;
-        if constexpr (F32) reinterpret_cast<uint32_t*>(at)[i] = raw[i];
-        else reinterpret_cast<uint16_t*>(at)[i] = (uint16_t)raw[i];
+        y[i] = none;
+        if (done.kept && x[i] > -INFINITY && done.cut.keeps(x[i], row.first_id(u) + i)) {
+          const double q = weight(x[i]);
+          if (q >= least) y[i] = probs ? (float)(q * share) : rule.one ? 0.f : (float)((double)x[i] / (double)rule.T);
+        }
+        raw[i] = F32 ? __float_as_uint(y[i]) : (uint32_t)__builtin_bit_cast(uint16_t, (__bf16)y[i]);
+      }
+      char* at = out + (int64_t)row.first_id(u) * R::EB;
+      if (lines && row.whole(u)) {
+        u32x4 z;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) z[i] = F32 ? raw[i] : raw[(2 * i) % VEC] | raw[(2 * i + 1) % VEC] << 16;
+        *reinterpret_cast<u32x4*>(at) = z;
+      } else {
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) {
+          const int id = row.first_id(u) + i;
+          if (id < 0 || id >= p.V) continue;
+          if constexpr (F32) reinterpret_cast<uint32_t*>(at)[i] = raw[i];
+          else reinterpret_cast<uint16_t*>(at)[i] = (uint16_t)raw[i];
+        }
       }
     }
-  });
+  }
+};
+
+// STEP: 0 scan, 1 collect, 2 token, 3 rows; 4: all of them for one slice a row.
+template <bool F32, int STEP>
+__global__ __launch_bounds__(kThreads) void sample_step(SampleParams p) {
+  __shared__ Shared sh;
+  const int r = STEP == 2 || STEP == 4 ? blockIdx.x : blockIdx.x / p.slices;
+  const int slice = STEP == 2 || STEP == 4 ? 0 : blockIdx.x - r * p.slices;
+  const Row<F32> row(static_cast<const char*>(p.logits) + r * p.stride * Row<F32>::EB, p.V);
+  const Rule rule(p, r);
+  const RowView view(p, r);
+  Slices<F32> S{p, row, sh, rule, view.s, 0.f};
+  RowState st;
+  RowDone done;
+  if constexpr (STEP == 0 || STEP == 4) S.scan_slice(slice);
+  if constexpr (STEP == 4) __syncthreads();
+  if constexpr (STEP == 1 || STEP == 4) {
+    st = S.state();
+    S.collect_slice(slice, st);
+  }
+  if constexpr (STEP == 2) st = *reinterpret_cast<const RowState*>(view.s.state);
+  if constexpr (STEP == 4) __syncthreads();
+  if constexpr (STEP == 2 || STEP == 4) {
+    int token;
+    if (!S.finish(r, st, done, token)) S.hard(r, done, token);
+    if (threadIdx.x == 0) {
+      if (p.tokens) p.tokens[r] = token;
+      if (STEP == 2 && p.kind) *reinterpret_cast<RowDone*>(view.s.done) = done;
+    }
+  }
+  if constexpr (STEP == 3) done = *reinterpret_cast<const RowDone*>(view.s.done);
+  if constexpr (STEP == 4) __syncthreads();                // the rows may be the logits
+  if constexpr (STEP == 3 || STEP == 4) {
+    if (p.kind) S.write_rows(r, slice, done);
+  }
+}
+
+template <bool F32>
+hipError_t steps(const SampleParams& p, int rows, hipStream_t s) {
+  if (p.slices == 1) {
+    sample_step<F32, 4><<<dim3(rows), dim3(kThreads), 0, s>>>(p);
+    return hipGetLastError();
+  }
+  sample_step<F32, 0><<<dim3(rows * p.slices), dim3(kThreads), 0, s>>>(p);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  sample_step<F32, 1><<<dim3(rows * p.slices), dim3(kThreads), 0, s>>>(p);
+  if ((e = hipGetLastError()) != hipSuccess) return e;
+  sample_step<F32, 2><<<dim3(rows), dim3(kThreads), 0, s>>>(p);
+  if ((e = hipGetLastError()) != hipSuccess || p.kind == 0) return e;
+  sample_step<F32, 3><<<dim3(rows * p.slices), dim3(kThreads), 0, s>>>(p);
+  return hipGetLastError();
 }
 
 }  // namespace
 
 hipError_t launch_sample(const SampleParams& p, int num_rows, bool f32, hipStream_t s) {
-  if (f32) sample_row<true><<<dim3(num_rows), dim3(kThreads), 0, s>>>(p);
-  else sample_row<false><<<dim3(num_rows), dim3(kThreads), 0, s>>>(p);
-  return hipGetLastError();
+  return f32 ? steps<true>(p, num_rows, s) : steps<false>(p, num_rows, s);
 }
 
 }  // namespace sv

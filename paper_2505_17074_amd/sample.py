@@ -17,7 +17,11 @@ _HERE = contextlib.nullcontext()
 
 
 class Sampler:
-    """Runs spec_sample on one device.  An object is used by one thread at a time.
+    """Runs spec_sample on one device.  Owns a device workspace, which grows with
+    the batches.  Calls are serialised: one on another stream than the last waits
+    for it.  A graph is captured from B.spec_sample with a workspace of its own: a
+    replay would write this one beside later calls, so a call on a capturing stream
+    is refused.  An object is used by one thread at a time.
 
     A call runs on `stream`, or the current one, after what is on it already; its
     tensors are its caller's to order and to keep, as for any work on a stream
@@ -30,6 +34,25 @@ class Sampler:
         self._lib = B.load()
         self._args = B.SpecSampleArgs()
         self._ref = C.byref(self._args)
+        self._ws = self._ws_ptr = self._last = None
+        self._ws_bytes = 0
+
+    def _workspace(self, stream: torch.cuda.Stream) -> None:
+        """A workspace for the call, ordered after the last call's use of it."""
+        last = self._last
+        if last is not None and last != stream:
+            stream.wait_event(last.record_event())
+        self._last = stream
+        st, need = B.spec_sample_workspace_bytes(self._args)
+        B.check(st, "spec_sample_workspace_bytes")
+        if need > self._ws_bytes:
+            # the last one goes back to torch's allocator, which knows the streams it was used on
+            self._ws_bytes = need + need // 4
+            self._ws = torch.empty(self._ws_bytes + 256, dtype=torch.uint8, device=self.device)
+            self._ws_ptr = (self._ws.data_ptr() + 255) // 256 * 256
+            last = None
+        if last != stream:
+            self._ws.record_stream(stream)
 
     def _per_row(self, t: Optional[torch.Tensor], name: str, dtype: torch.dtype, rows: int) -> Optional[int]:
         if t is None:
@@ -80,5 +103,9 @@ class Sampler:
             raise ValueError("the logits are not in device memory")
         here = _HERE if torch.cuda.current_device() == self.device.index else torch.cuda.device(self.device)
         with here:
-            h = (stream or torch.cuda.current_stream(self.device)).cuda_stream
-            B.check(self._lib.spec_sample(self._ref, None, 0, h), "spec_sample")
+            stream = stream or torch.cuda.current_stream(self.device)
+            h = stream.cuda_stream
+            if B.stream_capturing(h):
+                raise RuntimeError("a graph's calls need a workspace of their own: capture B.spec_sample")
+            self._workspace(stream)
+            B.check(self._lib.spec_sample(self._ref, self._ws_ptr, self._ws_bytes, h), "spec_sample")

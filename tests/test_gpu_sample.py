@@ -223,28 +223,57 @@ def test_frequencies(gpu_lib):
     assert (got - torch.tensor([0.5, 0, 0.2, 0.15, 0.1]).double() / 0.95).abs().max() <= 1.0 / n
 
 
-def test_replayed_and_on_other_streams(gpu_lib):
-    print("[case] sample replay", flush=True)
-    kw = _filters("all")
-    x, u = _logits(5, 32000, F32, seed=11)
+@pytest.mark.parametrize("n,V", [(5, 32000), (1, 128256), (300, 1000)])
+def test_replayed_and_on_other_streams(gpu_lib, n, V):
+    print(f"[case] sample replay {n} {V}", flush=True)
+    kw = {k: v.repeat(n // 5 + 1)[1:n + 1].contiguous() for k, v in _filters("all").items()}
+    x, u = _logits(n, V, F32, seed=11)
     s = Sampler()
-    tokens, out = torch.empty(5, dtype=torch.int32, device="cuda"), torch.empty_like(x)
+    tokens, out = torch.empty(n, dtype=torch.int32, device="cuda"), torch.empty_like(x)
+    a = B.SpecSampleArgs()
+    a.num_rows, a.vocab, a.dtype, a.rows_kind = n, V, B.SPEC_F32, B.SPEC_SAMPLE_PROBS
+    a.logits, a.uniforms, a.tokens, a.rows = (t.data_ptr() for t in (x, u, tokens, out))
+    a.logits_stride = a.rows_stride = V
+    a.temperature, a.top_k, a.top_p, a.min_p = (kw[k].data_ptr() for k in ("temperature", "top_k", "top_p", "min_p"))
+    st, need = B.spec_sample_workspace_bytes(a)
+    assert st == B.SPEC_OK
+    ws = torch.full((need + 256,), 255, dtype=torch.uint8, device="cuda")           # it may hold anything
     stream, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
     torch.cuda.synchronize()
     with torch.cuda.graph(graph, stream=stream):
-        s.run(x, u, tokens, probs=out, stream=stream, **kw)
+        B.check(B.spec_sample(a, (ws.data_ptr() + 255) // 256 * 256, need, stream.cuda_stream), "spec_sample")
+        with pytest.raises(RuntimeError):
+            s.run(x, u, tokens, probs=out, stream=stream, **kw)
     for i in range(4):
-        y, v = _logits(5, 32000, F32, seed=20 + i)
+        y, v = _logits(n, V, F32, seed=20 + i)
         x.copy_(y)
         u.copy_(v)
         tokens.fill_(-3)
-        graph.replay()
         torch.cuda.synchronize()
+        graph.replay()
         again, rows = torch.empty_like(tokens), torch.empty_like(out)
+        torch.cuda.synchronize()
         s.run(x, u, again, probs=rows, stream=torch.cuda.Stream() if i % 2 else None, **kw)
         torch.cuda.synchronize()
         assert torch.equal(again, tokens) and torch.equal(rows, out)
         _check(x, u, tokens, *(kw[k] for k in ("temperature", "top_k", "top_p", "min_p")), probs=out)
+
+
+def test_growing_batches(gpu_lib):
+    """One object: batches that need more workspace, on streams in turn."""
+    print("[case] sample growing", flush=True)
+    s, streams = Sampler(), [torch.cuda.Stream() for _ in range(3)]
+    jobs = []
+    for i, (n, V) in enumerate([(1, 100), (3, 5000), (2, 128256), (64, 32000), (1, 100), (200, 9000)]):
+        x, u = _logits(n, V, BF16 if i % 2 else F32, seed=i)
+        p, tokens = torch.full((n,), 0.8, device="cuda"), torch.empty(n, dtype=torch.int32, device="cuda")
+        jobs.append((x, u, p, tokens))
+    torch.cuda.synchronize()
+    for i, (x, u, p, tokens) in enumerate(jobs):
+        s.run(x, u, tokens, top_p=p, stream=streams[i % 3])
+    torch.cuda.synchronize()
+    for x, u, p, tokens in jobs:
+        _check(x, u, tokens, p=p)
 
 
 def test_many_rows(gpu_lib):
