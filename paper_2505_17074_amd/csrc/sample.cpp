@@ -54,6 +54,7 @@ SamplePlan plan_sample(const spec_sample_args_t* a) {
   const int64_t slabs = (units + P.slab_units - 1) / P.slab_units;
   int64_t slices = std::min<int64_t>(sv::kSampleSlices, 256 / a->num_rows);
   slices = std::max<int64_t>(1, std::min(slices, units / 1024));
+  if (units <= sv::kSampleWhole) slices = 1;
   const int64_t per = (slabs + slices - 1) / slices;
   P.slices = (int32_t)((slabs + per - 1) / per);
   P.slice_units = (int32_t)(per * P.slab_units);
@@ -61,7 +62,7 @@ SamplePlan plan_sample(const spec_sample_args_t* a) {
   P.fix = 44;
   while (((int64_t)P.slice_units * vec) >> (62 - P.fix)) --P.fix;
   P.row_bytes = sv::sample_row_bytes(P.slices);
-  P.bytes = (size_t)(P.row_bytes * a->num_rows + kAlign - 1) / kAlign * kAlign;
+  P.bytes = std::max(kAlign, (size_t)(P.row_bytes * a->num_rows + kAlign - 1) / kAlign * kAlign);
   return P;
 }
 

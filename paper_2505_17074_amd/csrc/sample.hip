@@ -18,9 +18,10 @@ namespace {
 
 constexpr int kThreads = 1024, kWaves = kThreads / 64;
 constexpr int kBins = 2048;            // ranges of a histogram
-constexpr int kRank = 1024;            // tokens ranked by counting: one a thread
+constexpr int kRank = 768;             // tokens ranked by counting: one a thread
 constexpr int kList = kSampleList;     // tokens of a sorted list
 constexpr int kSlabs = kSampleSlabs;   // runs of ids whose weights are summed apart
+constexpr int kGroups = kBins / 32;
 constexpr int kAhead = 8;              // units that a thread loads at once
 static_assert(kBins == kSampleBins, "a slice's histogram in the workspace");
 
@@ -51,12 +52,56 @@ __device__ __forceinline__ uint32_t key_of(float x) {
   return (int32_t)b < 0 ? b : ~b & 0x7fffffffu;
 }
 
-template <typename T>
-__device__ __forceinline__ T wave_sum(T x) {
-#pragma unroll
-  for (int i = 32; i > 0; i >>= 1) x += __shfl_xor(x, i);
+// x of another lane by a data-parallel move (CTRL, in the rows of ROWS), `none`
+// where there is no such lane.
+template <int CTRL, int ROWS, typename T>
+__device__ __forceinline__ T moved(T x, T none) {
+  if constexpr (sizeof(T) == 4) {
+    return __builtin_bit_cast(
+        T, __builtin_amdgcn_update_dpp(__builtin_bit_cast(int, none), __builtin_bit_cast(int, x), CTRL, ROWS, 0xf, false));
+  } else {
+    const uint64_t a = __builtin_bit_cast(uint64_t, x), n = __builtin_bit_cast(uint64_t, none);
+    const uint32_t lo = (uint32_t)__builtin_amdgcn_update_dpp((int)(uint32_t)n, (int)(uint32_t)a, CTRL, ROWS, 0xf, false);
+    const uint32_t hi = (uint32_t)__builtin_amdgcn_update_dpp((int)(uint32_t)(n >> 32), (int)(uint32_t)(a >> 32), CTRL, ROWS, 0xf, false);
+    return __builtin_bit_cast(T, (uint64_t)hi << 32 | lo);
+  }
+}
+// f over the wave's lanes up to and including this one: within rows of 16 lanes by
+// shifts, then the rows before by broadcasts of their last lanes.
+template <typename T, typename F>
+__device__ __forceinline__ T wave_scan(T x, T none, F&& f) {
+  x = f(x, moved<0x111, 0xf>(x, none));
+  x = f(x, moved<0x112, 0xf>(x, none));
+  x = f(x, moved<0x114, 0xf>(x, none));
+  x = f(x, moved<0x118, 0xf>(x, none));
+  x = f(x, moved<0x142, 0xa>(x, none));
+  x = f(x, moved<0x143, 0xc>(x, none));
   return x;
 }
+template <typename T>
+__device__ __forceinline__ T last_lane(T x) {
+  if constexpr (sizeof(T) == 4) {
+    return __builtin_bit_cast(T, __builtin_amdgcn_readlane(__builtin_bit_cast(int, x), 63));
+  } else {
+    const uint64_t a = __builtin_bit_cast(uint64_t, x);
+    return __builtin_bit_cast(T, (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(a >> 32), 63) << 32 |
+                                     (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)a, 63));
+  }
+}
+struct Plus {
+  template <typename T>
+  __device__ __forceinline__ T operator()(T a, T b) const { return a + b; }
+};
+struct Least {
+  template <typename T>
+  __device__ __forceinline__ T operator()(T a, T b) const { return a < b ? a : b; }
+};
+struct Most {
+  template <typename T>
+  __device__ __forceinline__ T operator()(T a, T b) const { return a > b ? a : b; }
+};
+template <typename T>
+__device__ __forceinline__ T wave_sum(T x) { return last_lane(wave_scan(x, T(0), Plus{})); }
 
 // One row's elements, in 16-byte units on the memory's own 16-byte borders.
 template <bool F32>
@@ -65,7 +110,7 @@ struct Row {
   const char* base;          // of unit 0 (the row's first element is its `head`-th)
   int head, V, units;
 
-  __device__ Row(const void* p, int V_) : V(V_) {
+  __device__ __forceinline__ Row(const void* p, int V_) : V(V_) {
     head = (int)(reinterpret_cast<uintptr_t>(p) % 16) / EB;
     base = static_cast<const char*>(p) - head * EB;
     units = (V + head + VEC - 1) / VEC;
@@ -137,27 +182,48 @@ struct Row {
   }
 };
 
+// bf16 values of magnitude 2^-9 to 2^5 by their bits: two signs of 14 powers of
+// two of 128 values each.  A row's weights are those of so few values that they
+// are counted, or looked up, in place of an exponential each.
+constexpr int kOneSign = 14 * 128, kValues = 2 * kOneSign, kLeastValue = 118 << 7;
+__device__ __forceinline__ uint32_t value_place(uint32_t h) {       // >= kValues: another value
+  const uint32_t m = (h & 0x7fffu) - kLeastValue;
+  return m < kOneSign ? m + (h >> 15) * kOneSign : (uint32_t)kValues;
+}
+__device__ __forceinline__ float value_at(int i) {
+  const int sign = i >= kOneSign;
+  return __uint_as_float((uint32_t)(i - sign * kOneSign + kLeastValue) << 16 | (uint32_t)sign << 31);
+}
+
 struct Shared {
   union {
-    uint32_t count[kBins];
-    unsigned long long mass[kBins];
-    unsigned long long by_id[kList];
-    unsigned long long add[kSlabs];
-  };
-  union {
     struct {
-      float x[kRank];
-      int id[kRank];
-      double w[kRank];
-    } list;
-    unsigned long long keys[kList];
+      union {
+        uint32_t count[kBins];
+        unsigned long long mass[kBins];
+        unsigned long long by_id[kList];
+        unsigned long long add[kSlabs];
+      };
+      union {
+        struct {
+          float x[kRank];
+          int id[kRank];
+          double w[kRank];
+        } list;
+        uint32_t values[kValues];      // how often a bf16 value comes
+      };
+    };
+    double weights[kValues + 1];       // a bf16 value's weight, and none
   };
-  double w[kList];
+  unsigned long long keys[kList];      // a list: order and id
+  unsigned long long runs[kThreads];   // of 64 keys in order
+  double slab[kSlabs];                 // weights that stay, by runs of ids
+  unsigned long long group[kGroups];   // sums of 32 ranges
   int n;                               // of the list
   unsigned long long red[kWaves];
   unsigned long long out[2];
-  double slab[kSlabs];
 };
+static_assert(sizeof(Shared) <= 65536, "a work-group's LDS");
 
 // What stays of a row.
 struct Cut {
@@ -165,6 +231,33 @@ struct Cut {
   int id;
   __device__ __forceinline__ bool keeps(float y, int i) const { return y > x || (y == x && i <= id); }
 };
+
+// f over the work-group, the same for all threads.
+template <typename T, typename F>
+__device__ __forceinline__ T block_reduce(Shared& sh, T x, T none, F&& f) {
+  x = last_lane(wave_scan(x, none, f));
+  T* at = reinterpret_cast<T*>(sh.red);
+  __syncthreads();
+  if ((threadIdx.x & 63) == 0) at[threadIdx.x / 64] = x;
+  __syncthreads();
+  x = at[0];
+#pragma unroll
+  for (int i = 1; i < kWaves; ++i) x = f(x, at[i]);
+  return x;
+}
+// The sum over the threads up to and including this one.
+template <typename T>
+__device__ __forceinline__ T block_scan(Shared& sh, T x) {
+  x = wave_scan(x, T(0), Plus{});
+  T* at = reinterpret_cast<T*>(sh.red);
+  __syncthreads();
+  if ((threadIdx.x & 63) == 63) at[threadIdx.x / 64] = x;
+  __syncthreads();
+  T base = 0;
+#pragma unroll
+  for (int i = 0; i < kWaves; ++i) base += i < (int)threadIdx.x / 64 ? at[i] : T(0);
+  return base + x;
+}
 
 template <bool F32>
 struct Sampler {
@@ -177,7 +270,7 @@ struct Sampler {
   float bins;                          // kBins ranges to 32 T
   int fix;                             // fixed point: weights in units of 2^-fix
 
-  __device__ Sampler(const R& r, Shared& s) : row(r), sh(s) {}
+  __device__ __forceinline__ Sampler(const R& r, Shared& s) : row(r), sh(s) {}
 
   template <typename F>
   __device__ __forceinline__ void each_unit(F&& f) const {
@@ -201,19 +294,6 @@ struct Sampler {
     return (unsigned long long)__builtin_amdgcn_ldexp(weight(x), fix);
   }
 
-  template <typename T, typename F>
-  __device__ __forceinline__ T block_reduce(T x, F&& f) const {
-#pragma unroll
-    for (int i = 32; i > 0; i >>= 1) x = f(x, __shfl_xor(x, i));
-    __syncthreads();
-    if ((threadIdx.x & 63) == 0) reinterpret_cast<T*>(sh.red)[threadIdx.x / 64] = x;
-    __syncthreads();
-    x = reinterpret_cast<T*>(sh.red)[0];
-#pragma unroll
-    for (int i = 1; i < kWaves; ++i) x = f(x, reinterpret_cast<T*>(sh.red)[i]);
-    return x;
-  }
-
   // The range of the histogram where the running sum reaches `mark` (at least one,
   // at most the whole sum), and the sum before it.
   template <typename T>
@@ -222,19 +302,8 @@ struct Sampler {
     __syncthreads();
     const int t = threadIdx.x;
     const T a = hist[2 * t], b = hist[2 * t + 1];
-    unsigned long long x = (unsigned long long)a + b;
-    const unsigned long long own = x;
-#pragma unroll
-    for (int i = 1; i < 64; i <<= 1) {
-      const unsigned long long y = __shfl_up(x, i);
-      if ((t & 63) >= i) x += y;
-    }
-    if ((t & 63) == 63) sh.red[t / 64] = x;
     if (t == 0) sh.out[0] = 0;
-    __syncthreads();
-    unsigned long long base = 0;
-    for (int i = 0; i < t / 64; ++i) base += sh.red[i];
-    const unsigned long long s0 = base + x - own, s1 = s0 + a, s2 = s1 + b;
+    const unsigned long long s2 = block_scan(sh, (unsigned long long)a + b), s1 = s2 - b, s0 = s1 - a;
     // the only range that begins below the mark and does not end below it
     if (s0 < mark && s1 >= mark) {
       sh.out[0] = 2 * t + 1;
@@ -259,7 +328,7 @@ struct Sampler {
   // else of counts) first reaches `mark`, among the tokens that `in` keeps.  The
   // caller has filled the histogram of range_of over them.
   template <bool MASS>
-  __device__ Cut last_of(unsigned long long mark, const Cut& in) {
+  __device__ __forceinline__ Cut last_of(unsigned long long mark, const Cut& in) {
     using T = std::conditional_t<MASS, unsigned long long, uint32_t>;
     T* hist = reinterpret_cast<T*>(&sh.mass[0]);
     unsigned long long sum, before;
@@ -276,9 +345,9 @@ struct Sampler {
       }
     });
     for (;;) {
-      lo = block_reduce(lo, [](uint32_t a, uint32_t b) { return min(a, b); });
-      hi = block_reduce(hi, [](uint32_t a, uint32_t b) { return max(a, b); });
-      n = block_reduce(n, [](int a, int b) { return a + b; });
+      lo = block_reduce(sh, lo, 0xffffffffu, Least{});
+      hi = block_reduce(sh, hi, 0u, Most{});
+      n = block_reduce(sh, n, 0, Plus{});
       if (n <= kRank || lo == hi) break;
       // again, over keys lo .. hi
       const int shift = max(0, 21 - __builtin_clz((hi - lo) | 1));
@@ -352,7 +421,7 @@ struct Sampler {
 
   // The same among many tokens of one value: so many of them, the lower ids first.
   template <bool MASS>
-  __device__ Cut tie(uint32_t key, unsigned long long mark, unsigned long long sum, const Cut& in) {
+  __device__ __forceinline__ Cut tie(uint32_t key, unsigned long long mark, unsigned long long sum, const Cut& in) {
     const float x = __uint_as_float((int32_t)key < 0 ? key : ~key & 0x7fffffffu);
     const unsigned long long w = MASS ? fixed(x) : 1;
     // the smallest m with sum + m w >= mark
@@ -368,25 +437,12 @@ struct Sampler {
       int mine = 0;
 #pragma unroll
       for (int i = 0; i < VEC; ++i) mine += y[i] == x && in.keeps(y[i], row.first_id(u) + i);
-      int s = mine;
-#pragma unroll
-      for (int i = 1; i < 64; i <<= 1) {
-        const int z = __shfl_up(s, i);
-        if ((threadIdx.x & 63) >= i) s += z;
-      }
-      if ((threadIdx.x & 63) == 63) sh.red[threadIdx.x / 64] = s;
-      __syncthreads();
-      int base = 0, all = 0;
-      for (int i = 0; i < kWaves; ++i) {
-        base += i < (int)threadIdx.x / 64 ? (int)sh.red[i] : 0;
-        all += (int)sh.red[i];
-      }
-      long long at = so_far + base + s - mine;
+      const int upto = block_scan(sh, mine);
+      long long at = so_far + upto - mine;
 #pragma unroll
       for (int i = 0; i < VEC; ++i)
         if (y[i] == x && in.keeps(y[i], row.first_id(u) + i) && ++at == m) sh.out[0] = row.first_id(u) + i;
-      so_far += all;
-      __syncthreads();
+      so_far += block_reduce(sh, mine, 0, Plus{});
       if (so_far >= m) break;
     }
     const Cut cut = {x, (int)sh.out[0]};
@@ -414,6 +470,8 @@ struct Sampler {
 
 enum Mode { kAll = 0, kFirst = 1, kEdge = 2, kHard = 3, kNone = 4 };
 
+constexpr int kFew = 512;
+constexpr int kWindow = kBins - 32;    // ranges of a histogram below its largest value's (below)
 constexpr double kListUnit = 281474976710656.0;      // 2^48: a list's weights in fixed point
 
 // What a row asks for.
@@ -421,20 +479,27 @@ struct Rule {
   float T, top_p, min_p;
   int k;
   bool one, by_count, by_mass;         // a cut by top-k, by top-p alone
+  bool few;                            // a top-k for which the threads' largest values tell the range
   float scale;                         // ranges a unit of value
   double c;                            // log2(e) / T
 
-  __device__ Rule(const SampleParams& p, int r) {
-    T = p.temperature ? p.temperature[r] : 1.f;
-    k = p.top_k ? p.top_k[r] : 0;
-    top_p = p.top_p ? p.top_p[r] : 1.f;
-    min_p = p.min_p ? p.min_p[r] : 0.f;
+  __device__ __forceinline__ Rule(const SampleParams& p, int r) {
+    // loads from some place in any case, so that none waits for another
+    const float* any = reinterpret_cast<const float*>(p.work);
+    const float t0 = *(p.temperature ? p.temperature + r : any), p0 = *(p.top_p ? p.top_p + r : any);
+    const float m0 = *(p.min_p ? p.min_p + r : any);
+    const int k0 = *(p.top_k ? p.top_k + r : reinterpret_cast<const int*>(any));
+    T = p.temperature ? t0 : 1.f;
+    k = p.top_k ? k0 : 0;
+    top_p = p.top_p ? p0 : 1.f;
+    min_p = p.min_p ? m0 : 0.f;
     one = !(T > 0.f) || !(top_p > 0.f) || !(min_p <= 1.f);
     if (k < 1 || k > p.V) k = p.V;
     if (one) k = 1, T = 1.f, top_p = 1.f, min_p = 0.f;
     c = 1.4426950408889634074 / (double)T;
     by_count = k < p.V;
     by_mass = !by_count && top_p < 1.f;
+    few = by_count && k <= kFew;
     // counts: 64 units of value in all, logits' own scale; weights: 32 T, past
     // which e^-32 of the largest weight is left a token
     scale = by_count ? (float)kBins / 64.f : (float)kBins / (32.f * T);
@@ -452,7 +517,7 @@ struct RowState {
 
 struct RowView {
   SampleRow s;
-  __device__ RowView(const SampleParams& p, int r) {
+  __device__ __forceinline__ RowView(const SampleParams& p, int r) {
     char* at = p.work + (int64_t)r * p.row_bytes;
     s.top = reinterpret_cast<float*>(at);
     s.n = reinterpret_cast<int32_t*>(at + 64);
@@ -462,6 +527,7 @@ struct RowView {
     s.slab = reinterpret_cast<double*>(at + kSampleHead);
     s.list = reinterpret_cast<unsigned long long*>(at + kSampleHead + sizeof(double) * kSlabs);
     s.hist = s.list + (int64_t)p.slices * kList;
+    s.group = s.hist + (int64_t)p.slices * kBins;
   }
 };
 static_assert(sizeof(RowState) <= 64, "a row's state");
@@ -475,7 +541,8 @@ struct RowDone {
 };
 static_assert(sizeof(RowDone) <= 64, "a row's outcome");
 
-template <bool F32>
+// ONE: a row is one slice, and what the steps leave for each other stays in LDS.
+template <bool F32, bool ONE>
 struct Slices {
   using R = Row<F32>;
   static constexpr int VEC = R::VEC;
@@ -485,6 +552,7 @@ struct Slices {
   const Rule& rule;
   SampleRow ws;
   float top;
+  double sum_all;                      // ONE: the histogram's
 
   __device__ __forceinline__ int begin(int slice) const { return slice * p.slice_units; }
   __device__ __forceinline__ int end(int slice) const { return min((slice + 1) * p.slice_units, row.units); }
@@ -494,34 +562,7 @@ struct Slices {
     return __builtin_bit_cast(unsigned long long, __builtin_fma(w, unit, 4503599627370496.0)) & 0xfffffffffffffull;
   }
 
-  template <typename T, typename F>
-  __device__ __forceinline__ T reduce(T x, F&& f) const {
-#pragma unroll
-    for (int i = 32; i > 0; i >>= 1) x = f(x, __shfl_xor(x, i));
-    __syncthreads();
-    if ((threadIdx.x & 63) == 0) reinterpret_cast<T*>(sh.red)[threadIdx.x / 64] = x;
-    __syncthreads();
-    x = reinterpret_cast<T*>(sh.red)[0];
-#pragma unroll
-    for (int i = 1; i < kWaves; ++i) x = f(x, reinterpret_cast<T*>(sh.red)[i]);
-    return x;
-  }
-  // Sums of x over the threads up to and including this one.
-  __device__ __forceinline__ double scan(double x) const {
-#pragma unroll
-    for (int i = 1; i < 64; i <<= 1) {
-      const double y = __shfl_up(x, i);
-      if ((threadIdx.x & 63) >= i) x += y;
-    }
-    __syncthreads();
-    if ((threadIdx.x & 63) == 63) reinterpret_cast<double*>(sh.red)[threadIdx.x / 64] = x;
-    __syncthreads();
-    double base = 0.0;
-    for (int i = 0; i < (int)threadIdx.x / 64; ++i) base += reinterpret_cast<double*>(sh.red)[i];
-    return base + x;
-  }
-
-  __device__ void scan_slice(int slice) {
+  __device__ __forceinline__ void scan_slice(int slice) {
     const int t = threadIdx.x, u0 = begin(slice), u1 = end(slice);
     u32x4 r[kAhead];
     float m = -INFINITY;
@@ -545,41 +586,110 @@ struct Slices {
       if (at >= u1) break;
       load(at);
     }
-    top = reduce(m, [](float a, float b) { return fmaxf(a, b); });
-    if (t == 0) ws.top[slice] = top;
+    top = block_reduce(sh, m, -INFINITY, Most{});
+    if (!ONE && t == 0) ws.top[slice] = top;
     if (!rule.by_count && !rule.by_mass) return;
     for (int i = t; i < kBins; i += kThreads) sh.mass[i] = 0;
     __syncthreads();
-    const float first = rule.range(top);
+    // Range g is at place g mod 2048, so that the slices' places agree; the window
+    // ends 32 ranges short of the whole, so that a group of 32 ranges aligned to 32
+    // never holds some from both of its ends.
+    const float first = rule.range(top), lowest = first - (float)(kWindow - 1);
     const double unit = __builtin_amdgcn_ldexp(1.0, p.fix);
     unsigned long long all = 0;
-    if (top > -INFINITY) {
-      const bool one_batch = u0 + kAhead * kThreads >= u1;
+    auto put = [&](float x, uint32_t n) {
+      const float g = rule.range(x);
+      const unsigned long long w = fixed(weight(x), unit) * n;
+      if (g >= lowest) atomicAdd(&sh.mass[(int)g & (kBins - 1)], w);
+      all += w;
+    };
+    auto tell = [&](float x) {
+      if (!(x > -INFINITY)) return;
+      const float g = rule.range(x);
+      if (g >= lowest) atomicAdd(&sh.count[(int)g & (kBins - 1)], 1u);
+      ++all;
+    };
+    // f(the slice's units, as they are, and which they are); one batch is still in r
+    const bool one_batch = u0 + kAhead * kThreads >= u1;
+    auto units = [&](auto&& f) {
       for (int at = u0; at < u1; at += kAhead * kThreads) {
         if (!one_batch) load(at);
 #pragma unroll
         for (int j = 0; j < kAhead; ++j) {
           if (at + j * kThreads >= u1) break;
-          float x[VEC];
-          R::values(r[j], x);
-#pragma unroll
-          for (int i = 0; i < VEC; ++i) {
-            if (!(x[i] > -INFINITY)) continue;
-            const int b = (int)fminf(first - rule.range(x[i]), (float)(kBins - 1));
-            if (rule.by_count) {
-              atomicAdd(&sh.count[b], 1u);
-              ++all;
-            } else {
-              const unsigned long long w = fixed(weight(x[i]), unit);
-              atomicAdd(&sh.mass[b], w);
-              all += w;
-            }
-          }
+          f(r[j], at + t + j * kThreads);
         }
       }
+    };
+    // A few of them: k threads' largest values are as many tokens, so the k-th
+    // largest of those is no larger than the k-th token, and few tokens lie between.
+    if (rule.few) {
+      tell(m);
+    } else if (top > -INFINITY && rule.by_count) {
+      units([&](u32x4 y, int) {
+        float x[VEC];
+        R::values(y, x);
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) tell(x[i]);
+      });
+    } else if (top > -INFINITY) {
+      if constexpr (F32) {
+        units([&](u32x4 y, int) {
+          float x[VEC];
+          R::values(y, x);
+#pragma unroll
+          for (int i = 0; i < VEC; ++i)
+            if (x[i] > -INFINITY) put(x[i], 1);
+        });
+      } else {
+        for (int i = t; i < kValues; i += kThreads) sh.values[i] = 0;
+        __syncthreads();
+        uint64_t others = 0;                               // units that hold other values, by the thread's count of them
+        int nth = 0;
+        units([&](u32x4 y, int) {
+          bool other = false;
+#pragma unroll
+          for (int i = 0; i < VEC; ++i) {
+            const uint32_t v = value_place(i & 1 ? y[i / 2] >> 16 : y[i / 2] & 0xffffu);
+            if (v < kValues) atomicAdd(&sh.values[v], 1u);
+            else other = true;
+          }
+          others |= (uint64_t)other << min(nth, 63);       // the 64th and all after it: looked at again
+          ++nth;
+        });
+        while (others) {
+          const int k = __builtin_ctzll(others);
+          others &= others - 1;
+          for (int u = u0 + t + k * kThreads; u < u1; u += kThreads) {
+            float x[VEC];
+            R::values(row.raw(u), x);
+#pragma unroll
+            for (int i = 0; i < VEC; ++i)
+              if (x[i] > -INFINITY && value_place(__float_as_uint(x[i]) >> 16) >= kValues) put(x[i], 1);
+            if (k < 63) break;
+          }
+        }
+        __syncthreads();
+        for (int i = t; i < kValues; i += kThreads)
+          if (const uint32_t n = sh.values[i]) put(value_at(i), n);
+      }
     }
-    all = reduce(all, [](unsigned long long a, unsigned long long b) { return a + b; });
-    if (t == 0) ws.sum[slice] = rule.by_count ? (double)all : (double)all / unit;
+    all = block_reduce(sh, all, 0ull, Plus{});
+    const double sum = rule.by_count ? (double)all : (double)all / unit;
+    // groups of 32 ranges: 16 threads' pairs
+    unsigned long long group = rule.by_count ? (unsigned long long)sh.count[2 * t] + sh.count[2 * t + 1]
+                                             : sh.mass[2 * t] + sh.mass[2 * t + 1];
+    group += moved<0x111, 0xf>(group, 0ull);
+    group += moved<0x112, 0xf>(group, 0ull);
+    group += moved<0x114, 0xf>(group, 0ull);
+    group += moved<0x118, 0xf>(group, 0ull);
+    if constexpr (ONE) {
+      sum_all = sum;
+      if (t % 16 == 15) sh.group[t / 16] = group;
+      return;                                              // the histogram is where state() reads it
+    }
+    if (t == 0) ws.sum[slice] = sum;
+    if (t % 16 == 15) ws.group[slice * kGroups + t / 16] = group;
     unsigned long long* to = ws.hist + (int64_t)slice * kBins;
     if (rule.by_count) {
       for (int i = t; i < kBins; i += kThreads) reinterpret_cast<uint32_t*>(to)[i] = sh.count[i];
@@ -588,110 +698,238 @@ struct Slices {
     }
   }
 
-  // The row's largest value, and where its mark is reached.
-  __device__ RowState state() {
+  __device__ __forceinline__ void load_tops(float (&tops)[kSampleSlices]) {
+    if constexpr (ONE) return;                             // as scan_slice left it
     top = -INFINITY;
-    for (int s = 0; s < p.slices; ++s) top = fmaxf(top, ws.top[s]);
+#pragma unroll
+    for (int s = 0; s < kSampleSlices; ++s) tops[s] = ws.top[min(s, p.slices - 1)];
+#pragma unroll
+    for (int s = 0; s < kSampleSlices; ++s) tops[s] = s < p.slices ? tops[s] : -INFINITY;
+#pragma unroll
+    for (int s = 0; s < kSampleSlices; ++s) top = fmaxf(top, tops[s]);
+  }
+  template <typename T>
+  __device__ __forceinline__ static T of_lane(T x, int lane) {
+    const uint64_t a = __builtin_bit_cast(uint64_t, x);
+    return __builtin_bit_cast(T, (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(a >> 32), lane) << 32 |
+                                     (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)a, lane));
+  }
+
+  // The row's largest value, and where its mark is reached: first among the groups
+  // of 32 ranges, a wave adding each slice's, then among the group's ranges.  Every
+  // wave finds it for itself.
+  __device__ __forceinline__ RowState state() {
+    float tops[kSampleSlices];
+    load_tops(tops);
     RowState st = {kAll, 0.f, 0.0, 0.0};
     if (!(top > -INFINITY)) st.mode = kNone;
     if (st.mode == kNone || (!rule.by_count && !rule.by_mass)) return st;
+    st.mode = kHard;
     const float first = rule.range(top);
-    if (!(fabsf(first) < 8388608.f)) {                     // ranges are not whole numbers apart (or the largest is infinite)
-      st.mode = kHard;
-      return st;
+    // ranges that are not whole numbers apart, or all the same
+    if (!(fabsf(first) < 8388608.f) || !(rule.scale > 0.f) || !(rule.scale < INFINITY)) return st;
+    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), n = ONE ? 1 : p.slices;
+    const int start = (int)first & ~31;                    // of the first group
+    double* part = reinterpret_cast<double*>(sh.runs);     // [slices][64], sums, [slices][32]
+    float own = top;                                       // of the wave's slice
+    double f = 1.0;
+    if constexpr (!ONE) {
+#pragma unroll
+      for (int s = 0; s < kSampleSlices; ++s) own = s == w ? tops[s] : own;
     }
-    // ranges 2 t and 2 t + 1 of the row: the sums of its slices', each further
-    // down by what its own largest value is
-    const double unit = __builtin_amdgcn_ldexp(1.0, -p.fix);
-    double a = 0.0, b = 0.0, all = 0.0;
-    for (int s = 0; s < p.slices; ++s) {
-      const float ts = ws.top[s];
-      if (!(ts > -INFINITY)) continue;
-      const double f = rule.by_count ? 1.0 : weight(ts) * unit;
-      all += ws.sum[s] * (rule.by_count ? 1.0 : weight(ts));
-      const int off = (int)fminf(first - rule.range(ts), (float)kBins);
-      const unsigned long long* h = ws.hist + (int64_t)s * kBins;
-      const int j = 2 * (int)threadIdx.x - off;
-      if (rule.by_count) {
-        const uint32_t* hc = reinterpret_cast<const uint32_t*>(h);
-        if (j >= 0 && j < kBins - 1) a += (double)hc[j];
-        if (j + 1 >= 0 && j + 1 < kBins - 1) b += (double)hc[j + 1];
-      } else {
-        if (j >= 0 && j < kBins - 1) a += (double)h[j] * f;
-        if (j + 1 >= 0 && j + 1 < kBins - 1) b += (double)h[j + 1] * f;
+    const float own_first = rule.range(own);
+    const bool has = w < n && own > -INFINITY;
+    if (w < n) {
+      const int low = start - 32 * lane;
+      double y = 0.0;
+      if (has) {
+        if (rule.by_mass) f = weight(own) * __builtin_amdgcn_ldexp(1.0, -p.fix);
+        const unsigned long long* g = ONE ? sh.group : ws.group + w * kGroups;
+        const unsigned long long x = g[(low >> 5) & (kGroups - 1)];
+        y = own_first >= (float)low ? (double)x * f : 0.0;
       }
+      part[w * 64 + lane] = y;
+      if (lane == 0) part[512 + w] = !has ? 0.0 : (ONE ? sum_all : ws.sum[w]) * (rule.by_mass ? weight(own) : 1.0);
     }
-    if (2 * threadIdx.x + 1 >= kBins - 1) b = 0.0;         // the last range has what lies further down
+    __syncthreads();
+    double y = 0.0, all = 0.0;
+    for (int s = 0; s < n; ++s) {
+      y += part[s * 64 + lane];
+      all += part[512 + s];
+    }
     if (rule.by_count && (double)rule.k >= all) {
-      st.mode = rule.top_p < 1.f ? kHard : kAll;           // nothing is cut
+      if (rule.few) {                                      // fewer threads with tokens than k: all tokens are listed
+        st.mode = kFirst;
+        st.range = -INFINITY;
+      } else if (!(rule.top_p < 1.f)) {
+        st.mode = kAll;                                    // nothing is cut
+      }
       return st;
     }
     st.mark = rule.by_count ? (double)rule.k : (double)rule.top_p * all;
-    const double s2 = scan(a + b), s1 = s2 - b, s0 = s1 - a;
-    if (threadIdx.x == 0) sh.out[0] = kBins;
+    double upto = wave_scan(y, 0.0, Plus{});
+    uint64_t reached = __ballot(upto >= st.mark);
+    if (!reached) return st;
+    const int q = __builtin_ctzll(reached), low = start - 32 * q;
+    if ((float)low < first - (float)(kWindow - 1)) return st;        // the group is not whole in the window
+    st.before = of_lane(upto, q) - of_lane(y, q);
+    if (w < n && lane < 32) {
+      const int g = low + 31 - lane, at = g & (kBins - 1);
+      double z = 0.0;
+      if (has) {
+        unsigned long long x;
+        if constexpr (ONE) x = rule.by_count ? sh.count[at] : sh.mass[at];
+        else x = rule.by_count ? reinterpret_cast<const uint32_t*>(ws.hist + (int64_t)w * kBins)[at]
+                               : ws.hist[(int64_t)w * kBins + at];
+        z = own_first >= (float)g ? (double)x * f : 0.0;
+      }
+      part[576 + w * 32 + lane] = z;
+    }
     __syncthreads();
-    // the first range that reaches the mark: the sums do not fall, but for rounding
-    if (s2 >= st.mark) atomicMin(&sh.out[0], (unsigned long long)(2 * threadIdx.x + (s1 >= st.mark ? 0 : 1)));
-    __syncthreads();
-    const int bin = (int)sh.out[0];
-    if (bin < kBins && (int)threadIdx.x == bin / 2) reinterpret_cast<double*>(sh.red)[0] = bin & 1 ? s1 : s0;
-    __syncthreads();
-    st.before = reinterpret_cast<double*>(sh.red)[0];
-    __syncthreads();
-    if (bin >= kBins - 1) st.mode = kHard;
-    else if (rule.by_count && rule.k <= kSampleFirst) st.mode = kFirst;
-    else st.mode = rule.by_count && rule.top_p < 1.f ? kHard : kEdge;
-    st.range = first - (float)bin;
+    y = 0.0;
+    if (lane < 32)
+      for (int s = 0; s < n; ++s) y += part[576 + s * 32 + lane];
+    upto = st.before + wave_scan(y, 0.0, Plus{});
+    reached = __ballot(upto >= st.mark);
+    const int i = min(reached ? __builtin_ctzll(reached) : 31, 31);  // none, by the sums' rounding: the last
+    st.before = of_lane(upto, i) - of_lane(y, i);
+    st.range = (float)(low + 31 - i);
+    if (rule.by_count && rule.k <= kSampleFirst) st.mode = kFirst;
+    else if (!rule.by_count || !(rule.top_p < 1.f)) st.mode = kEdge;
     return st;
   }
 
-  __device__ void collect_slice(int slice, const RowState& st) {
+  __device__ __forceinline__ void collect_slice(int slice, const RowState& st) {
     const int t = threadIdx.x, lane = t & 63;
     if (t == 0) sh.n = 0;
     __syncthreads();
-    if (slice == 0 && t == 0) *reinterpret_cast<RowState*>(ws.state) = st;
+    if (!ONE && slice == 0 && t == 0) *reinterpret_cast<RowState*>(ws.state) = st;
     if (st.mode == kHard || st.mode == kNone) return;
-    unsigned long long* list = ws.list + (int64_t)slice * kList;
+    unsigned long long* list = ONE ? sh.keys : ws.list + (int64_t)slice * kList;
+    double* slab = ONE ? sh.slab : ws.slab;
     const double least = rule.min_p;
-    // a slice's units are whole runs of ids
-    const int per = p.slab_units, u1 = end(slice);
-    for (int u0 = begin(slice) + t / 64 * per; u0 < u1; u0 += kWaves * per) {
-      double sum = 0.0;
-      for (int at = u0; at < min(u0 + per, u1); at += 64) {
-        const int u = at + lane;
-        if (u >= u1) continue;
-        float x[VEC];
-        R::values(row.raw(u), x);
+    // A value's range from a product alone: floor(x scale) >= g where x scale >= g.
+    const float edge = st.range, past = st.range + 1.f;
+    auto ahead = [&](float x) { return st.mode == kAll || x * rule.scale >= past; };       // summed, not listed
+    const bool table = !F32 && st.mode != kFirst;
+    if (table) {
+      for (int i = t; i < kValues; i += kThreads) {
+        const double y = ahead(value_at(i)) ? weight(value_at(i)) : 0.0;
+        sh.weights[i] = y >= least ? y : 0.0;
+      }
+      if (t == 0) sh.weights[kValues] = 0.0;
+      __syncthreads();
+    }
+    // a slice's units are whole runs of ids, a wave takes every sixteenth; so many
+    // 64-unit parts of them at once
+    constexpr int kAtOnce = F32 ? kAhead : 4;
+    const int per = p.slab_units, parts = per / 64, u1 = end(slice), w = t / 64;
+    const int runs = (u1 - begin(slice) + per - 1) / per;
+    const int steps = w < runs ? ((runs - w + kWaves - 1) / kWaves) * parts : 0;      // parts of this wave
+    auto unit_of = [&](int k) { return begin(slice) + (w + k / parts * kWaves) * per + k % parts * 64 + lane; };
+    double sum = 0.0;
+    for (int k0 = 0; k0 < steps; k0 += kAtOnce) {
+      u32x4 r[kAtOnce];
 #pragma unroll
-        for (int i = 0; i < VEC; ++i) {
-          if (!(x[i] > -INFINITY)) continue;
-          bool ahead = st.mode == kAll, listed = false;
-          if (st.mode != kAll) {
-            const float g = rule.range(x[i]);
-            listed = st.mode == kFirst ? g >= st.range : g == st.range;
-            ahead = st.mode == kEdge && g > st.range;
+      for (int j = 0; j < kAtOnce; ++j) {
+        const int u = unit_of(k0 + j);
+        r[j] = k0 + j < steps && u < u1 ? row.raw(u) : u32x4{0xffffffffu, 0xffffffffu, 0xffffffffu, 0xffffffffu};
+      }
+#pragma unroll
+      for (int j = 0; j < kAtOnce; ++j) {
+        if (k0 + j >= steps) break;
+        float x[VEC];
+        R::values(r[j], x);
+        auto list_it = [&](int i) {
+          const int n = atomicAdd(&sh.n, 1);
+          if (n < kList)
+            list[n] = (unsigned long long)key_of(R::clean(__float_as_uint(x[i]))) << 32 |
+                      (uint32_t)(row.first_id(unit_of(k0 + j)) + i);
+        };
+        float most = x[0];
+#pragma unroll
+        for (int i = 1; i < VEC; ++i) most = fmaxf(most, x[i]);
+        if (st.mode == kFirst) {
+          if (most * rule.scale >= edge && most > -INFINITY) {
+#pragma unroll
+            for (int i = 0; i < VEC; ++i)
+              if (x[i] * rule.scale >= edge && x[i] > -INFINITY) list_it(i);
           }
-          if (ahead) {
-            const double w = weight(x[i]);
-            if (w >= least) sum += w;
+        } else if (st.mode == kAll || most * rule.scale >= edge) {
+          bool some = false;                               // of the list, or another value than the table's
+#pragma unroll
+          for (int i = 0; i < VEC; ++i) {
+            const float g = x[i] * rule.scale;
+            some |= st.mode == kEdge && g >= edge && g < past;
+            if constexpr (F32) {
+              if (x[i] > -INFINITY && ahead(x[i])) {
+                const double y = weight(x[i]);
+                if (y >= least) sum += y;
+              }
+            } else {
+              const uint32_t v = value_place(i & 1 ? r[j][i / 2] >> 16 : r[j][i / 2] & 0xffffu);
+              sum += sh.weights[v];
+              some |= v == kValues;
+            }
           }
-          if (listed) {
-            const int n = atomicAdd(&sh.n, 1);
-            if (n < kList) list[n] = (unsigned long long)key_of(R::clean(__float_as_uint(x[i]))) << 32 | (uint32_t)(row.first_id(u) + i);
+          if (some) {
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) {
+              const float g = x[i] * rule.scale;
+              if (st.mode == kEdge && g >= edge && g < past) list_it(i);
+              if constexpr (!F32) {
+                if (value_place(__float_as_uint(x[i]) >> 16) == kValues && x[i] > -INFINITY && ahead(x[i])) {
+                  const double y = weight(x[i]);
+                  if (y >= least) sum += y;
+                }
+              }
+            }
           }
         }
-      }
-      if (st.mode != kFirst) {
-        sum = wave_sum(sum);
-        if (lane == 0) ws.slab[u0 / per] = sum;
+        if (st.mode != kFirst && (k0 + j) % parts == parts - 1) {
+          sum = wave_sum(sum);
+          if (lane == 0) slab[begin(slice) / per + w + (k0 + j) / parts * kWaves] = sum;
+          sum = 0.0;
+        }
       }
     }
     __syncthreads();
-    if (t == 0) ws.n[slice] = sh.n;
+    if (!ONE && t == 0) ws.n[slice] = sh.n;
   }
 
-  // sh.keys[0 .. n) ascending (n <= kList); entries up to the next power of two are written.
-  __device__ void sort(unsigned long long* keys, int n) const {
+  // keys[0 .. n) ascending (n <= kList; all different).  Up to 1024: a wave puts 64
+  // of them in order by counting for each how many are smaller, then each finds
+  // its place among the other runs of 64 by bisection (400 of them 2 us; by counting
+  // over all of them 6.5).  More by a bitonic sort (entries up to the next power of
+  // two are written).
+  __device__ __forceinline__ void sort(unsigned long long* keys, int n) const {
+    if (n <= kThreads) {
+      unsigned long long* runs = sh.runs;
+      const int t = threadIdx.x, lane = t & 63, r0 = t - lane;
+      unsigned long long mine = ~0ull;
+      int at = 0;
+      if (r0 < n) {
+        mine = t < n ? keys[t] : ~0ull;
+        const int m = min(64, n - r0);
+#pragma unroll 8
+        for (int j = 0; j < m; ++j) at += keys[r0 + j] < mine;
+        runs[r0 + (lane < m ? at : lane)] = mine;
+      }
+      __syncthreads();
+      if (t < n) {
+#pragma unroll 4
+        for (int r = 0; r < n; r += 64) {
+          if (r == r0) continue;
+          int k = 0;
+#pragma unroll
+          for (int step = 32; step > 0; step /= 2) k += runs[r + k + step - 1] < mine ? step : 0;
+          at += k + (runs[r + k] < mine);
+        }
+        keys[at] = mine;
+      }
+      __syncthreads();
+      return;
+    }
     int N = 64;
     while (N < n) N *= 2;
     for (int i = n + threadIdx.x; i < N; i += kThreads) keys[i] = ~0ull;
@@ -722,7 +960,7 @@ struct Slices {
     Two y;
     y.w0 = i < n ? weight(value_of(sh.keys[i])) : 0.0;
     y.w1 = i + 1 < n ? weight(value_of(sh.keys[i + 1])) : 0.0;
-    y.s1 = scan(y.w0 + y.w1);
+    y.s1 = block_scan(sh, y.w0 + y.w1);
     y.s0 = y.s1 - y.w1;
     return y;
   }
@@ -731,14 +969,14 @@ struct Slices {
   __device__ __forceinline__ int count(const Two& y, int n, F&& f) const {
     const int i = 2 * threadIdx.x;
     const int c = (i < n && f(i, y.w0, y.s0)) + (i + 1 < n && f(i + 1, y.w1, y.s1));
-    return reduce(c, [](int a, int b) { return a + b; });
+    return block_reduce(sh, c, 0, Plus{});
   }
 
   // The token and what stays.  False: the row takes the other way.
-  __device__ bool finish(int r, const RowState& st, RowDone& done, int& token) {
+  __device__ __forceinline__ bool finish(int r, const RowState& st, RowDone& done, int& token) {
     const int t = threadIdx.x;
-    top = -INFINITY;
-    for (int s = 0; s < p.slices; ++s) top = fmaxf(top, ws.top[s]);
+    float tops[kSampleSlices];
+    load_tops(tops);
     done = {{-INFINITY, 0x7fffffff}, 1.0, top, 1};
     token = -1;
     if (st.mode == kNone) {
@@ -748,11 +986,26 @@ struct Slices {
     if (st.mode == kHard) return false;
     int n = 0;
     if (st.mode != kAll) {
-      for (int s = 0; s < p.slices; ++s) {
-        const int m = ws.n[s];
-        if (n + m > kList) return false;                   // the same for all threads
-        for (int i = t; i < m; i += kThreads) sh.keys[n + i] = ws.list[(int64_t)s * kList + i];
-        n += m;
+      if constexpr (ONE) {
+        n = sh.n;
+        if (n > kList) return false;                       // the same for all threads
+      } else {
+        int m[kSampleSlices];
+#pragma unroll
+        for (int s = 0; s < kSampleSlices; ++s) m[s] = ws.n[min(s, p.slices - 1)];
+#pragma unroll
+        for (int s = 0; s < kSampleSlices; ++s) m[s] = s < p.slices ? min(m[s], kList + 1) : 0;
+#pragma unroll
+        for (int s = 0; s < kSampleSlices; ++s) n += m[s];
+        if (n > kList) return false;                         // the same for all threads
+        for (int i = t; i < n; i += kThreads) {
+          int s = 0, at = i;
+#pragma unroll
+          for (int y = 0; y < kSampleSlices - 1; ++y)
+            if (s == y && at >= m[y]) at -= m[y], ++s;
+          sh.keys[i] = ws.list[(int64_t)s * kList + at];
+        }
+        __syncthreads();
       }
       sort(sh.keys, n);
     }
@@ -770,15 +1023,13 @@ struct Slices {
       if (least > 0.0) stay = min(stay, max(1, count(y, n, [&](int, double w, double) { return w >= least; })));
       done.cut = {value_of(sh.keys[stay - 1]), (int)(uint32_t)sh.keys[stay - 1]};
       // ids ascending: (id, place in the list)
-      for (int i = t; i < stay; i += kThreads) {
-        sh.by_id[i] = (sh.keys[i] << 32) | (uint32_t)i;
-        sh.w[i] = weight(value_of(sh.keys[i]));
-      }
+      for (int i = t; i < stay; i += kThreads) sh.by_id[i] = (sh.keys[i] << 32) | (uint32_t)i;
       __syncthreads();
       sort(sh.by_id, stay);
       const int i = 2 * t;
-      const double w0 = i < stay ? sh.w[(uint32_t)sh.by_id[i]] : 0.0, w1 = i + 1 < stay ? sh.w[(uint32_t)sh.by_id[i + 1]] : 0.0;
-      const double s1 = scan(w0 + w1), s0 = s1 - w1;
+      const double w0 = i < stay ? weight(value_of(sh.keys[(uint32_t)sh.by_id[i]])) : 0.0;
+      const double w1 = i + 1 < stay ? weight(value_of(sh.keys[(uint32_t)sh.by_id[i + 1]])) : 0.0;
+      const double s1 = block_scan(sh, w0 + w1), s0 = s1 - w1;
       if (t == (stay - 1) / 2) reinterpret_cast<double*>(sh.out)[0] = s1;
       __syncthreads();
       done.total = reinterpret_cast<double*>(sh.out)[0];
@@ -790,8 +1041,8 @@ struct Slices {
       else if (w0 > 0.0) last = i;
       if (w1 > 0.0 && s1 > mark) best = i + 1;
       if (w0 > 0.0 && s0 > mark) best = i;
-      best = reduce(best, [](int a, int b) { return min(a, b); });
-      last = reduce(last, [](int a, int b) { return max(a, b); });
+      best = block_reduce(sh, best, 0x7fffffff, Least{});
+      last = block_reduce(sh, last, 0, Most{});
       token = (int)(sh.by_id[min(best, last)] >> 32);
       return true;
     }
@@ -814,25 +1065,25 @@ struct Slices {
       }
       __syncthreads();
     }
-    by_runs(st.mode == kEdge, u, done, token);
+    by_runs(ONE ? sh.slab : ws.slab, st.mode == kEdge, u, done, token);
     return true;
   }
 
   // The total, and the token, of what stays by the sums of its runs of ids (`list`: and
   // the listed ones').
-  __device__ void by_runs(bool list, double u, RowDone& done, int& token) {
+  __device__ __forceinline__ void by_runs(const double* slab, bool list, double u, RowDone& done, int& token) {
     static_assert(kSlabs == kThreads, "a run a thread");
     const int t = threadIdx.x, slabs = (row.units + p.slab_units - 1) / p.slab_units;
-    double mine = t < slabs ? ws.slab[t] : 0.0;
+    double mine = t < slabs ? slab[t] : 0.0;
     if (list && t < slabs) mine += (double)sh.add[t] * (1.0 / kListUnit);
-    const double s1 = scan(mine);
+    const double s1 = block_scan(sh, mine);
     if (t == kThreads - 1) reinterpret_cast<double*>(sh.out)[0] = s1;
     __syncthreads();
     done.total = reinterpret_cast<double*>(sh.out)[0];
     if (!p.tokens) return;
     const double mark = u * done.total;
-    int best = reduce(mine > 0.0 && s1 > mark ? t : 0x7fffffff, [](int a, int b) { return min(a, b); });
-    best = min(best, reduce(mine > 0.0 ? t : 0, [](int a, int b) { return max(a, b); }));
+    int best = block_reduce(sh, mine > 0.0 && s1 > mark ? t : 0x7fffffff, 0x7fffffff, Least{});
+    best = min(best, block_reduce(sh, mine > 0.0 ? t : 0, 0, Most{}));
     if (t == best) reinterpret_cast<double*>(sh.out)[0] = s1 - mine;
     __syncthreads();
     const double before = reinterpret_cast<double*>(sh.out)[0];
@@ -842,7 +1093,7 @@ struct Slices {
 
   // The first token of units [u0, u1) where the sum of what stays, from `run` on, exceeds
   // `mark`, or the last that has weight; by one wave.
-  __device__ int in_run(int u0, int u1, double run, double mark, const Cut& cut, double least) const {
+  __device__ __forceinline__ int in_run(int u0, int u1, double run, double mark, const Cut& cut, double least) const {
     const int lane = threadIdx.x;
     int best = 0x7fffffff, behind = -1;
     for (; u0 < u1 && best == 0x7fffffff; u0 += 64) {
@@ -859,12 +1110,7 @@ struct Slices {
         }
         mine += y[i];
       }
-      double sum = mine;
-#pragma unroll
-      for (int i = 1; i < 64; i <<= 1) {
-        const double z = __shfl_up(sum, i);
-        if (lane >= i) sum += z;
-      }
+      const double sum = wave_scan(mine, 0.0, Plus{});
       double at = run + sum - mine;
       int found = 0x7fffffff;
 #pragma unroll
@@ -873,18 +1119,15 @@ struct Slices {
         if (y[i] > 0.0) behind = row.first_id(u) + i;
         if (y[i] > 0.0 && at > mark && found == 0x7fffffff) found = row.first_id(u) + i;
       }
-#pragma unroll
-      for (int i = 32; i > 0; i >>= 1) found = min(found, __shfl_xor(found, i));
-      best = found;
-      run += __shfl(sum, 63);
+      best = last_lane(wave_scan(found, 0x7fffffff, Least{}));
+      run += last_lane(sum);
     }
-#pragma unroll
-    for (int i = 32; i > 0; i >>= 1) behind = max(behind, __shfl_xor(behind, i));
+    behind = last_lane(wave_scan(behind, -1, Most{}));
     return best == 0x7fffffff ? behind : best;
   }
 
   // The row by the histograms of the whole of it (the first half of this file).
-  __device__ void hard(int r, RowDone& done, int& token) {
+  __device__ __forceinline__ void hard(int r, RowDone& done, int& token) {
     const int t = threadIdx.x;
     __syncthreads();
     Sampler<F32> S(row, sh);
@@ -905,7 +1148,7 @@ struct Slices {
         atomicAdd(&sh.count[S.range_of(x)], 1u);
         ++n;
       });
-      n = S.block_reduce(n, [](int a, int b) { return a + b; });
+      n = block_reduce(sh, n, 0, Plus{});
       if (rule.k < n) cut = S.template last_of<false>((unsigned long long)rule.k, cut);
     }
     if (rule.top_p < 1.f) {
@@ -917,7 +1160,7 @@ struct Slices {
         atomicAdd(&sh.mass[S.range_of(x)], w);
         all += w;
       });
-      all = S.block_reduce(all, [](unsigned long long a, unsigned long long b) { return a + b; });
+      all = block_reduce(sh, all, 0ull, Plus{});
       const unsigned long long mark = (unsigned long long)ceil((double)rule.top_p * (double)all);
       cut = S.template last_of<true>(min(max(mark, 1ull), all), cut);
     }
@@ -937,23 +1180,23 @@ struct Slices {
           }
       }
       sum = wave_sum(sum);
-      if (lane == 0) ws.slab[s] = sum;
+      if (lane == 0) sh.slab[s] = sum;
     }
     __syncthreads();
     done.cut = cut;
-    by_runs(false, p.tokens ? (double)p.uniforms[r] : 0.0, done, token);
+    by_runs(sh.slab, false, p.tokens ? (double)p.uniforms[r] : 0.0, done, token);
   }
 
-  __device__ void write_rows(int r, int slice, const RowDone& done) {
+  __device__ __forceinline__ void write_rows(int r, int slice, const RowDone& done) {
     top = done.top;
     char* out = static_cast<char*>(p.rows) + r * p.rows_stride * R::EB;
     const bool probs = p.kind == 1;
     const float none = probs ? 0.f : F32 ? -3.4028234663852886e38f : -3.3895313892515355e38f;
     const bool lines = (reinterpret_cast<uintptr_t>(out) - (uintptr_t)(row.head * R::EB)) % 16 == 0;
     const double least = rule.min_p, share = 1.0 / done.total;
-    for (int u = begin(slice) + threadIdx.x; u < end(slice); u += kThreads) {
+    auto write = [&](int u, u32x4 in) {
       float x[VEC], y[VEC];
-      row.load(u, x);
+      R::values(in, x);
       uint32_t raw[VEC];
 #pragma unroll
       for (int i = 0; i < VEC; ++i) {
@@ -979,41 +1222,44 @@ struct Slices {
           else reinterpret_cast<uint16_t*>(at)[i] = (uint16_t)raw[i];
         }
       }
-    }
+    };
+    for (int u = begin(slice) + threadIdx.x; u < end(slice); u += kThreads) write(u, row.raw(u));
   }
 };
 
-// STEP: 0 scan, 1 collect, 2 token, 3 rows; 4: all of them for one slice a row.
+// STEP: 0 scan, 1 collect, 2 token, 3 rows; 4: all of them for one slice a row; 5:
+// 2 and 3, the former again in every slice (the rows are not the logits).
 template <bool F32, int STEP>
 __global__ __launch_bounds__(kThreads) void sample_step(SampleParams p) {
   __shared__ Shared sh;
-  const int r = STEP == 2 || STEP == 4 ? blockIdx.x : blockIdx.x / p.slices;
-  const int slice = STEP == 2 || STEP == 4 ? 0 : blockIdx.x - r * p.slices;
+  constexpr bool ONE = STEP == 4;
+  const int r = STEP == 2 || ONE ? blockIdx.x : blockIdx.x / p.slices;
+  const int slice = STEP == 2 || ONE ? 0 : blockIdx.x - r * p.slices;
   const Row<F32> row(static_cast<const char*>(p.logits) + r * p.stride * Row<F32>::EB, p.V);
   const Rule rule(p, r);
   const RowView view(p, r);
-  Slices<F32> S{p, row, sh, rule, view.s, 0.f};
+  Slices<F32, ONE> S{p, row, sh, rule, view.s, 0.f, 0.0};
   RowState st;
   RowDone done;
-  if constexpr (STEP == 0 || STEP == 4) S.scan_slice(slice);
-  if constexpr (STEP == 4) __syncthreads();
-  if constexpr (STEP == 1 || STEP == 4) {
+  if constexpr (STEP == 0 || ONE) S.scan_slice(slice);
+  if constexpr (ONE) __syncthreads();
+  if constexpr (STEP == 1 || ONE) {
     st = S.state();
     S.collect_slice(slice, st);
   }
-  if constexpr (STEP == 2) st = *reinterpret_cast<const RowState*>(view.s.state);
-  if constexpr (STEP == 4) __syncthreads();
-  if constexpr (STEP == 2 || STEP == 4) {
+  if constexpr (STEP == 2 || STEP == 5) st = *reinterpret_cast<const RowState*>(view.s.state);
+  if constexpr (ONE) __syncthreads();
+  if constexpr (STEP == 2 || STEP == 5 || ONE) {
     int token;
     if (!S.finish(r, st, done, token)) S.hard(r, done, token);
-    if (threadIdx.x == 0) {
+    if (threadIdx.x == 0 && slice == 0) {
       if (p.tokens) p.tokens[r] = token;
       if (STEP == 2 && p.kind) *reinterpret_cast<RowDone*>(view.s.done) = done;
     }
   }
   if constexpr (STEP == 3) done = *reinterpret_cast<const RowDone*>(view.s.done);
-  if constexpr (STEP == 4) __syncthreads();                // the rows may be the logits
-  if constexpr (STEP == 3 || STEP == 4) {
+  if constexpr (ONE) __syncthreads();                      // the rows may be the logits
+  if constexpr (STEP == 3 || STEP == 5 || ONE) {
     if (p.kind) S.write_rows(r, slice, done);
   }
 }
@@ -1029,6 +1275,10 @@ hipError_t steps(const SampleParams& p, int rows, hipStream_t s) {
   if (e != hipSuccess) return e;
   sample_step<F32, 1><<<dim3(rows * p.slices), dim3(kThreads), 0, s>>>(p);
   if ((e = hipGetLastError()) != hipSuccess) return e;
+  if (p.kind != 0 && p.rows != p.logits) {
+    sample_step<F32, 5><<<dim3(rows * p.slices), dim3(kThreads), 0, s>>>(p);
+    return hipGetLastError();
+  }
   sample_step<F32, 2><<<dim3(rows), dim3(kThreads), 0, s>>>(p);
   if ((e = hipGetLastError()) != hipSuccess || p.kind == 0) return e;
   sample_step<F32, 3><<<dim3(rows * p.slices), dim3(kThreads), 0, s>>>(p);

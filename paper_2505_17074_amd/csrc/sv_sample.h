@@ -10,6 +10,7 @@ constexpr int kSampleBins = 2048;      // ranges of a histogram
 constexpr int kSampleList = 2048;      // tokens of a list
 constexpr int kSampleSlabs = 1024;     // runs of ids of a row, at most
 constexpr int kSampleSlices = 8;       // slices of a row, at most
+constexpr int kSampleWhole = 8192;     // 16-byte units of a row that is not cut
 constexpr int kSampleFirst = 1024;     // a top-k whose tokens are listed whole
 constexpr int64_t kSampleHead = 512;   // bytes of a row's workspace before its arrays
 
@@ -23,9 +24,11 @@ struct SampleRow {
   double* slab;                        // [kSampleSlabs] weights that stay, by runs of ids
   unsigned long long* list;            // [slices][kSampleList] order and id
   unsigned long long* hist;            // [slices][kSampleBins]
+  unsigned long long* group;           // [slices][kSampleBins / 32]
 };
 inline int64_t sample_row_bytes(int slices) {
-  return kSampleHead + 8 * (kSampleSlabs + (int64_t)slices * (kSampleList + kSampleBins));
+  if (slices == 1) return 0;           // it all stays in LDS
+  return kSampleHead + 8 * (kSampleSlabs + (int64_t)slices * (kSampleList + kSampleBins + kSampleBins / 32));
 }
 
 struct SampleParams {

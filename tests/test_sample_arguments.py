@@ -64,7 +64,7 @@ def test_workspaces_of_long_rows():
     """A row's runs of ids, lists and histograms: bounded whatever its length."""
     for rows, vocab in ((1, 1), (1, 1 << 28), (1000, 50), (3, 128256), (256, 128256), (257, 1 << 20)):
         st, need = B.spec_sample_workspace_bytes(_args(num_rows=rows, vocab=vocab, logits_stride=1 << 30))
-        assert st == B.SPEC_OK and 0 < need <= rows * (512 + 8192 + 8 * 32768) + 256
+        assert st == B.SPEC_OK and 0 < need <= rows * (512 + 8192 + 8 * 33280) + 256
 
 
 def test_null_arguments():
