@@ -39,7 +39,10 @@ spec_status_t check_sample(const spec_sample_args_t* a) {
 
 // How a row is cut: the fewest runs of ids of 64 units that a list of runs
 // holds, and as many slices as give the chip's compute units a work-group each,
-// none of less than 1024 units.
+// none of less than 1024 units.  One launch in place of three or four is worth
+// more where a row is short, and where a few have a top-k, whose rows need no
+// sums of weights (fp32, one row of 32000: top-k 50 17 us whole and 22 in eight
+// slices; 64 rows, some with top-p alone, 50 whole and 39 in four).
 struct SamplePlan {
   int32_t slices, slice_units, slab_units, fix;
   int64_t row_bytes;
@@ -54,7 +57,7 @@ SamplePlan plan_sample(const spec_sample_args_t* a) {
   const int64_t slabs = (units + P.slab_units - 1) / P.slab_units;
   int64_t slices = std::min<int64_t>(sv::kSampleSlices, 256 / a->num_rows);
   slices = std::max<int64_t>(1, std::min(slices, units / 1024));
-  if (units <= sv::kSampleWhole) slices = 1;
+  if (units <= sv::kSampleShort || (units <= sv::kSampleWhole && a->top_k && a->num_rows <= sv::kSampleAlone)) slices = 1;
   const int64_t per = (slabs + slices - 1) / slices;
   P.slices = (int32_t)((slabs + per - 1) / per);
   P.slice_units = (int32_t)(per * P.slab_units);

@@ -10,7 +10,9 @@ constexpr int kSampleBins = 2048;      // ranges of a histogram
 constexpr int kSampleList = 2048;      // tokens of a list
 constexpr int kSampleSlabs = 1024;     // runs of ids of a row, at most
 constexpr int kSampleSlices = 8;       // slices of a row, at most
-constexpr int kSampleWhole = 8192;     // 16-byte units of a row that is not cut
+constexpr int kSampleShort = 2048;     // 16-byte units of a row that is not cut
+constexpr int kSampleWhole = 8192;     // and of one with a top-k in a batch of up to
+constexpr int kSampleAlone = 4;        // rows
 constexpr int kSampleFirst = 1024;     // a top-k whose tokens are listed whole
 constexpr int64_t kSampleHead = 512;   // bytes of a row's workspace before its arrays
 
