@@ -240,34 +240,42 @@ class PagedCache:
         and i + len(freq), or, interleaved, 2 i and 2 i + 1.  freq is fp32;
         positions int32 [rows], without them a row's place in its request."""
         layers = self._new_rows(chunks, k_new, v_new, layer)
-        rows = chunks.rows
-        if freq.dtype != torch.float32 or freq.dim() != 1 or freq.device != self.device or _stride(freq, 0, 1) != 1:
-            raise ValueError("freq is fp32 [rotary dim / 2] on the pools' device")
-        if positions is not None and (positions.dtype != torch.int32 or positions.dim() != 1 or
-                                      positions.device != self.device or positions.shape[0] < rows or
-                                      _stride(positions, 0, 1) != 1):
-            raise ValueError("positions are int32 [rows] on the pools' device")
+        rows, dtype, device = chunks.rows, self.dtype, self.device
         r = self._rotation
-        r.rotary_dim, r.interleaved = 2 * freq.shape[0], 1 if interleaved else 0
-        r.freq = freq.data_ptr()
-        r.positions = None if positions is None else positions.data_ptr()
-        r.num_q_heads = 0
+        shape = freq.shape
+        if freq.dtype != torch.float32 or len(shape) != 1 or freq.device != device or \
+                (shape[0] > 1 and freq.stride(0) != 1):
+            raise ValueError("freq is fp32 [rotary dim / 2] on the pools' device")
+        r.rotary_dim, r.interleaved, r.freq = 2 * shape[0], 1 if interleaved else 0, freq.data_ptr()
+        if positions is None:
+            r.positions = None
+        else:
+            shape = positions.shape
+            if positions.dtype != torch.int32 or len(shape) != 1 or positions.device != device or shape[0] < rows or \
+                    (shape[0] > 1 and positions.stride(0) != 1):
+                raise ValueError("positions are int32 [rows] on the pools' device")
+            r.positions = positions.data_ptr()
         if (q is None) != (q_out is None):
             raise ValueError("q and q_out go together")
-        if q is not None:
+        if q is None:
+            r.num_q_heads = 0
+        else:
+            shape, to, st, so = q.shape, q_out.shape, q.stride(), q_out.stride()
+            if len(shape) != 3 or len(to) != 3:
+                raise ValueError("q and q_out are [rows, Hq, d]")
+            n, heads, d = shape
+            m = to[0]
+            if n < rows or m < rows or to[1] != heads or heads < 1 or d != self._head[1] or to[2] != d or \
+                    ((st[2] != 1 or so[2] != 1) and d > 1):
+                raise ValueError("q and q_out are [rows, Hq, d], a row for every new token")
+            if q.dtype != dtype or q_out.dtype != dtype or q.device != device or q_out.device != device:
+                raise ValueError("q and q_out have the pools' type and device")
             if layers != 1:
                 raise ValueError("queries belong to one layer")
-            for t in (q, q_out):
-                if t.dim() != 3 or t.shape[0] < rows or t.shape[1] != q.shape[1] or t.shape[1] < 1 or \
-                        t.shape[2] != self._head[1] or (t.stride(2) != 1 and t.shape[2] > 1):
-                    raise ValueError("q and q_out are [rows, Hq, d], a row for every new token")
-                if t.dtype != self.dtype or t.device != self.device:
-                    raise ValueError("q and q_out have the pools' type and device")
-            r.num_q_heads = q.shape[1]
-            wide = q.shape[1] * q.shape[2]
-            r.q, r.q_out = q.data_ptr(), q_out.data_ptr()
-            r.q_stride_tok, r.q_stride_head = _stride(q, 0, wide), _stride(q, 1, q.shape[2])
-            r.out_stride_tok, r.out_stride_head = _stride(q_out, 0, wide), _stride(q_out, 1, q.shape[2])
+            r.num_q_heads, r.q, r.q_out = heads, q.data_ptr(), q_out.data_ptr()
+            # of a dimension with one entry any stride will do
+            r.q_stride_tok, r.out_stride_tok = st[0] if n > 1 else heads * d, so[0] if m > 1 else heads * d
+            r.q_stride_head, r.out_stride_head = (st[1], so[1]) if heads > 1 else (d, d)
         with self._enter():
             B.check(self._lib.spec_cache_append_rotated(chunks, self._ref, self._append_ref, self._rotation_ref,
                                                         self._stream(stream)), "spec_cache_append_rotated")

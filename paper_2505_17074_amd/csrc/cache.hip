@@ -119,7 +119,7 @@ struct Turned {                        // a 16-byte unit's elements in fp32
 //   (x, y) -> (x cos - y sin, y cos + x sin),
 // in fp32, each result rounded once.  Pairs are elements i and i + pairs, or 2 i
 // and 2 i + 1 (INTER).
-// blockIdx: (block of 4 rows, segment, layer).  The block's angles are computed
+// blockIdx: (block of two or four rows, segment, layer).  The block's angles are computed
 // once, into LDS, beside the first loads; a thread keeps its columns of a head
 // (two units, INTER or without a partner one) and goes from head to head and
 // row to row, the queries' heads first, then K's and V's.
@@ -128,8 +128,8 @@ __global__ __launch_bounds__(256) void cache_append_rotated(RotateParams<N> p) {
   constexpr int VEC = Turned<F32>::VEC, AHEAD = 4;
   __shared__ float cs[kTurnRows][2][kMaxTurned];
   const AppendSegment sg = p.seg[N > 1 ? blockIdx.y : 0];
-  const int b0 = (sg.pos & ~(kTurnRows - 1)) + kTurnRows * (int)blockIdx.x;
-  const int lo = max(b0, sg.pos), n = min(b0 + kTurnRows, sg.pos + sg.n) - lo;
+  const int b0 = (sg.pos & ~(p.rows - 1)) + p.rows * (int)blockIdx.x;
+  const int lo = max(b0, sg.pos), n = min(b0 + p.rows, sg.pos + sg.n) - lo;
   if (n <= 0) return;
   const int pg = p.bt[(int64_t)sg.req * p.bt_stride + lo / p.c.page_tokens];
   const bool kept = pg >= 0 && pg < p.c.num_pages;
@@ -335,7 +335,7 @@ static AppendParams<M> small(const AppendParams<N>& p) {
 template <int M, int N>
 static RotateParams<M> small(const RotateParams<N>& p) {
   RotateParams<M> q{p.c,      p.k_new,  p.v_new, p.q,    p.q_out, p.bt,        p.freq,    p.positions, p.new_sl, p.new_st,
-                    p.q_st,   p.out_st, p.new_sh, p.q_sh, p.out_sh, p.bt_stride, p.q_heads, p.pairs,     {}};
+                    p.q_st,   p.out_st, p.new_sh, p.q_sh, p.out_sh, p.bt_stride, p.q_heads, p.pairs,     p.rows,  {}};
   for (int i = 0; i < M; ++i) q.seg[i] = p.seg[i];
   return q;
 }

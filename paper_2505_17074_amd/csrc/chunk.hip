@@ -105,12 +105,13 @@ struct Fetch {
   int64_t page_bytes;
   int32_t page_tokens, num_pages, row_bytes;
   int32_t ke;
-  int32_t first, skip;       // SOME: key t >= first is the request's row t + skip
+  int32_t first, skip;       // key t >= first is the request's row t + skip
 };
 // The request's row that is key t of the item.
-template <bool SOME>
+template <Keys KEYS>
 __device__ __forceinline__ int row_of(const Fetch& f, int t) {
-  if constexpr (SOME) return t < f.first ? t : t + f.skip;
+  if constexpr (KEYS == kWindowed) return t < f.first ? t : t + f.skip;
+  if constexpr (KEYS == kBehind) return t + f.skip;
   return t;
 }
 
@@ -125,9 +126,9 @@ struct Window {
   int b;
   int pg, place;
 };
-template <bool SOME>
+template <Keys KEYS>
 __device__ __forceinline__ void look(Window& x, const Fetch& f, int kb, int b, int lane) {
-  const int t = row_of<SOME>(f, min(kb + 32 * (b + lane), (f.ke - 1) & ~31));
+  const int t = row_of<KEYS>(f, min(kb + 32 * (b + lane), (f.ke - 1) & ~31));
   const int i = t / f.page_tokens;
   x.b = b;
   x.place = t - i * f.page_tokens;
@@ -135,9 +136,9 @@ __device__ __forceinline__ void look(Window& x, const Fetch& f, int kb, int b, i
 }
 
 // Byte offset of key t's row in the pools.
-template <bool SOME>
+template <Keys KEYS>
 __device__ __forceinline__ int64_t place_of(const Fetch& f, int t) {
-  const int r = row_of<SOME>(f, min(t, f.ke - 1));
+  const int r = row_of<KEYS>(f, min(t, f.ke - 1));
   const int i = __builtin_amdgcn_readfirstlane(r / f.page_tokens);
   const int pg = ((const const_int32*)f.pages)[i];
   return __builtin_amdgcn_readfirstlane(min(max(pg, 0), f.num_pages - 1)) * f.page_bytes +
@@ -152,10 +153,10 @@ struct Rows {
   f32x16 o[D / 32];          // o[eb][i]: column 32 eb + 8 (i / 4) + 4 (l / 32) + i % 4
   float m, l;                // reference (log2 units) and this half's sum
   int32_t last;              // the row's last visible key
-  int32_t low, sinks;        // SOME: it sees keys from low on, and those below sinks
-  template <bool SOME>
+  int32_t low, sinks;        // kWindowed: it sees keys from low on, and those below sinks
+  template <Keys KEYS>
   __device__ __forceinline__ bool sees(int t) const {
-    return t <= last && (!SOME || t >= low || t < sinks);
+    return t <= last && (KEYS != kWindowed || t >= low || t < sinks);
   }
   __device__ __forceinline__ void clear() {
     m = -INFINITY;
@@ -185,7 +186,7 @@ struct Piece {
 };
 // A row tile's work-groups are next to each other, those of a piece (HEADS: the
 // XCDs read different heads) or of a head (a head's keys stream past in order).
-template <bool HEADS, bool SOME>
+template <bool HEADS, Keys KEYS>
 __device__ __forceinline__ Piece piece_of(const ChunkParams& p, int b) {
   if (b >= p.turn0 && b < p.turn1) b = p.turn0 + p.turn1 - 1 - b;
   const int i = b / p.Hkv;
@@ -195,11 +196,11 @@ __device__ __forceinline__ Piece piece_of(const ChunkParams& p, int b) {
   const int s = HEADS ? x.piece : g - h * x.pieces;
   const int kb = s * x.len;
   return {x.req, h, x.r0, x.rows, kb, min(x.keys, kb + x.len), x.ctx, x.q0,
-          (SOME ? x.part >= 0 : x.pieces > 1) ? x.part + ((int64_t)h * x.pieces + s) * x.rows : -1, x.skip};
+          (KEYS != kEvery ? x.part >= 0 : x.pieces > 1) ? x.part + ((int64_t)h * x.pieces + s) * x.rows : -1, x.skip};
 }
 
 // Rows wr0 .. wr0 + 31 of the item (past its last: that one again).
-template <bool SOME, int D>
+template <Keys KEYS, int D>
 __device__ __forceinline__ void load_rows(Rows<D>& S, const ChunkParams& p, const Piece& it, int wr0, int l32,
                                           int half) {
   const int r = it.r0 + min(wr0 + l32, it.rows - 1);
@@ -210,7 +211,7 @@ __device__ __forceinline__ void load_rows(Rows<D>& S, const ChunkParams& p, cons
 #pragma unroll
   for (int ks = 0; ks < D / 16; ++ks) S.q[ks] = *reinterpret_cast<const bf16x8*>(src + ks * 32);
   S.last = min(it.ctx + j, it.ke - 1);
-  if constexpr (SOME) {
+  if constexpr (KEYS == kWindowed) {
     S.low = it.ctx + j - p.window + 1;
     S.sinks = p.sinks;
   }
@@ -277,10 +278,10 @@ __device__ __forceinline__ void join_rows(Rows<D>& S, float m1, float l1, const 
 // The wave's rows over keys [t, last] one at a time, by the rows' own
 // visibility: a value of a key that a row does not see never meets the row, not
 // even as a product with zero.
-template <bool SOME, int D>
+template <Keys KEYS, int D>
 __device__ __forceinline__ void one_by_one(const Fetch& f, Rows<D>& S, int t, int last, float c, int half) {
   for (; t <= last; ++t) {
-    const int64_t at = place_of<SOME>(f, t);
+    const int64_t at = place_of<KEYS>(f, t);
     const bf16x8* k = reinterpret_cast<const bf16x8*>(f.k + at) + half;
     const bf16x4* v = reinterpret_cast<const bf16x4*>(f.v + at) + half;
     float s = 0.f;
@@ -291,7 +292,7 @@ __device__ __forceinline__ void one_by_one(const Fetch& f, Rows<D>& S, int t, in
       for (int i = 0; i < 8; ++i) s = fmaf((float)S.q[ks][i], (float)y[i], s);
     }
     s = (s + __shfl_xor(s, 32)) * c;
-    const bool sees = S.template sees<SOME>(t);
+    const bool sees = S.template sees<KEYS>(t);
     const float m = sees ? fmaxf(S.m, s) : S.m, ref = m == -INFINITY ? 0.f : m;
     const float alpha = __builtin_amdgcn_exp2f(S.m - ref), w = sees ? __builtin_amdgcn_exp2f(s - ref) : 0.f;
     S.m = m;
@@ -344,9 +345,9 @@ __device__ __forceinline__ void one_by_one(const Fetch& f, Rows<D>& S, int t, in
 // row's norm in place of 0.0021-0.0024, and it takes one: who needs the better
 // product there asks for an fp32 output.
 // ---------------------------------------------------------------------------
-// SOME: items that leave keys out (sv_chunk.h).  What a row does not see at the
+// KEYS: which keys an item leaves out (sv_chunk.h).  What a row does not see at a
 // window's start is masked as behind its own token; whole tiles lie between.
-template <int D, int NW, int TK, int PARTS, bool SOME>
+template <int D, int NW, int TK, int PARTS, Keys KEYS>
 struct Chunk {
   using TL = Tile<D, TK>;
   using DL = Deal<D, TK, NW>;
@@ -442,13 +443,13 @@ struct Chunk {
   template <int N>
   static __device__ __forceinline__ void mask(ScoresOf<N>& x, const Rows<D>& S, int t0, int half) {
     const int lim = S.last - t0 - 8 * half;
-    const int low = SOME ? S.low - t0 - 8 * half : 0, sinks = SOME ? S.sinks - t0 - 8 * half : 0;
+    const int low = KEYS == kWindowed ? S.low - t0 - 8 * half : 0, sinks = KEYS == kWindowed ? S.sinks - t0 - 8 * half : 0;
 #pragma unroll
     for (int kb = 0; kb < N; ++kb)
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
         const int k = 32 * kb + 16 * (i >> 3) + (i & 7);
-        x.s[kb][i] = k <= lim && (!SOME || k >= low || k < sinks) ? x.s[kb][i] : -INFINITY;
+        x.s[kb][i] = k <= lim && (KEYS != kWindowed || k >= low || k < sinks) ? x.s[kb][i] : -INFINITY;
       }
   }
 
@@ -600,18 +601,18 @@ struct Chunk {
   static __device__ __forceinline__ void again(const Fetch& f, Rows<D>& S, int kb, int last, float c, int l32, int half) {
 #if defined(__HIP_DEVICE_COMPILE__)
     const int all = __builtin_amdgcn_readfirstlane(S.last);
-    const int low = SOME ? __builtin_amdgcn_readlane(S.low, 31) : 0;       // from here on all of them see a key
+    const int low = KEYS == kWindowed ? __builtin_amdgcn_readlane(S.low, 31) : 0;       // from here on all of them see a key
     asm volatile("" : "+v"(l32), "+v"(half));          // none of the addresses below is held in the loops above
     S.clear();
     int t = kb;
-    for (; SOME ? t <= last : t + 31 <= all; t += 32) {
-      if constexpr (SOME) {
+    for (; KEYS == kWindowed ? t <= last : t + 31 <= all; t += 32) {
+      if constexpr (KEYS == kWindowed) {
         if (t + 31 > all || (t < low && t + 31 >= S.sinks)) {
-          one_by_one<SOME, D>(f, S, t, min(t + 31, last), c, half);
+          one_by_one<KEYS, D>(f, S, t, min(t + 31, last), c, half);
           continue;
         }
       }
-      const int64_t at = place_of<SOME>(f, t);
+      const int64_t at = place_of<KEYS>(f, t);
       const char* k = f.k + at + (int64_t)key_of(l32) * f.row_bytes + half * 16;
       const char* v = f.v + at + (int64_t)(8 * half) * f.row_bytes + l32 * 2;
       ScoresOf<1> x;
@@ -639,7 +640,7 @@ struct Chunk {
         }
       }
     }
-    if constexpr (!SOME) one_by_one<SOME, D>(f, S, t, last, c, half);
+    if constexpr (KEYS != kWindowed) one_by_one<KEYS, D>(f, S, t, last, c, half);
 #endif
   }
   // Step t of a wave that has 32 keys of every second tile, `cur` moved to them
@@ -673,7 +674,7 @@ struct Chunk {
     const int l32 = lane & 31, half = lane >> 5;
     lds_char* ring = (lds_char*)lds;
     int2 before = make_int2(0, 0);
-    load_rows<SOME>(S, p, it, 0, l32, half);
+    load_rows<KEYS>(S, p, it, 0, l32, half);
 #pragma unroll
     for (int j = 0; j < NS; ++j) issue<2>(ring + j * TL::STAGE, f, j, it.kb, win, before, w, A);
     S.clear();
@@ -685,7 +686,7 @@ struct Chunk {
     for (int t = 0; t < ntiles; ++t) {
       wait_vm<0>();
       tile_barrier();
-      if (block_of(t + NS, w) >= win.b + 64) look<SOME>(win, f, it.kb, block_of(t + NS, w), lane);
+      if (block_of(t + NS, w) >= win.b + 64) look<KEYS>(win, f, it.kb, block_of(t + NS, w), lane);
       shared_step(ring + (t % NS) * TL::STAGE, ring + ((t + 1) % NS) * TL::STAGE + hb * TL::HALF, t + NS <= ntiles, f,
                   t + NS, it.kb, win, before, w, A, S, x, (t & 1) == par, it.kb + TK * t + 32 * hb, p.scale_log2, lane);
     }
@@ -723,10 +724,10 @@ struct Chunk {
 };
 
 // (d = 64: three waves a SIMD.)
-template <int D, int NW, int TK, int NS, int PARTS, bool F32, bool SOME>
+template <int D, int NW, int TK, int NS, int PARTS, bool F32, Keys KEYS>
 __global__ __launch_bounds__(64 * NW, D == 64 ? 3 : 2) void chunk_attn(ChunkParams p) {
 #if defined(__HIP_DEVICE_COMPILE__)   // the host pass needs the signature only
-  using C = Chunk<D, NW, TK, PARTS, SOME>;
+  using C = Chunk<D, NW, TK, PARTS, KEYS>;
   using TL = Tile<D, TK>;
   using DL = Deal<D, TK, NW>;
   __shared__ __attribute__((aligned(1024))) char lds[NS * TL::STAGE];
@@ -734,7 +735,7 @@ __global__ __launch_bounds__(64 * NW, D == 64 ? 3 : 2) void chunk_attn(ChunkPara
   const int lane = threadIdx.x & 63;
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int l32 = lane & 31, half = lane >> 5;
-  const Piece it = piece_of<NW != 1, SOME>(p, blockIdx.x);
+  const Piece it = piece_of<NW != 1, KEYS>(p, blockIdx.x);
   const int ntiles = (it.ke - it.kb + TK - 1) / TK;
 
   Fetch f;
@@ -746,7 +747,7 @@ __global__ __launch_bounds__(64 * NW, D == 64 ? 3 : 2) void chunk_attn(ChunkPara
   f.page_bytes = (int64_t)p.page_tokens * f.row_bytes;
   f.num_pages = p.num_pages;
   f.ke = it.ke;
-  if constexpr (SOME) {
+  if constexpr (KEYS != kEvery) {
     f.first = (p.sinks + 31) & ~31;
     f.skip = it.skip;
   }
@@ -759,7 +760,7 @@ __global__ __launch_bounds__(64 * NW, D == 64 ? 3 : 2) void chunk_attn(ChunkPara
     A.offv = (uint32_t)(lane / TL::CH * f.row_bytes + ((ch ^ swv<D>(row)) * 16));   // the same for every x
   }
   Window win;
-  look<SOME>(win, f, it.kb, 0, lane);
+  look<KEYS>(win, f, it.kb, 0, lane);
   int2 before = make_int2(0, 0);                         // a second unit's: what the first had last
 
   lds_char* ring = (lds_char*)lds;
@@ -773,7 +774,7 @@ __global__ __launch_bounds__(64 * NW, D == 64 ? 3 : 2) void chunk_attn(ChunkPara
   Rows<D> S;
   bool bad;
   if (!shared) {
-    load_rows<SOME>(S, p, it, wr0, l32, half);
+    load_rows<KEYS>(S, p, it, wr0, l32, half);
 #pragma unroll
     for (int j = 0; j < NS; ++j) C::issue(ring + j * TL::STAGE, f, j, it.kb, win, before, w, A);
     S.clear();
@@ -789,7 +790,7 @@ __global__ __launch_bounds__(64 * NW, D == 64 ? 3 : 2) void chunk_attn(ChunkPara
     // Step t: stage t + 1 has landed here and everywhere, and every wave has read
     // what it needs of stage t, where stage t + NS goes.
     int t = 0;
-    if constexpr (SOME) {
+    if constexpr (KEYS == kWindowed) {
       // the tiles that begin before the last row's window, and one more where the
       // ring's stages ask for it
       const int low = it.ctx + (it.r0 + it.rows - 1) / p.G - p.window + 1;
@@ -800,7 +801,7 @@ __global__ __launch_bounds__(64 * NW, D == 64 ? 3 : 2) void chunk_attn(ChunkPara
       for (; t < edge; ++t) {
         wait_vm<0>();
         tile_barrier();
-        if (C::block_of(t + NS, w) >= win.b + 64) look<SOME>(win, f, it.kb, C::block_of(t + NS, w), lane);
+        if (C::block_of(t + NS, w) >= win.b + 64) look<KEYS>(win, f, it.kb, C::block_of(t + NS, w), lane);
         const int t0 = it.kb + TK * t, t1 = t0 + TK;
         C::edge_step(ring + (t % NS) * TL::STAGE, ring + ((t + 1) % NS) * TL::STAGE, t + NS <= ntiles, f, t + NS, it.kb,
                      win, before, w, A, S, x, top, t0, t0 <= wave_sees && (t1 > wave_low || t0 < p.sinks),
@@ -810,7 +811,7 @@ __global__ __launch_bounds__(64 * NW, D == 64 ? 3 : 2) void chunk_attn(ChunkPara
     }
     if (wave_sees >= it.kb) {
       while (t + NS <= nfull) {
-        if (C::block_of(t + 2 * NS - 1, w) >= win.b + 64) look<SOME>(win, f, it.kb, C::block_of(t + NS, w), lane);
+        if (C::block_of(t + 2 * NS - 1, w) >= win.b + 64) look<KEYS>(win, f, it.kb, C::block_of(t + NS, w), lane);
         static_for<0, NS>([&](auto st) {
           constexpr int ST = decltype(st)::value;
           wait_vm<(NS - 2) * DL::PER>();
@@ -824,7 +825,7 @@ __global__ __launch_bounds__(64 * NW, D == 64 ? 3 : 2) void chunk_attn(ChunkPara
     for (; t < ntiles; ++t) {
       wait_vm<0>();
       tile_barrier();
-      if (C::block_of(t + NS, w) >= win.b + 64) look<SOME>(win, f, it.kb, C::block_of(t + NS, w), lane);
+      if (C::block_of(t + NS, w) >= win.b + 64) look<KEYS>(win, f, it.kb, C::block_of(t + NS, w), lane);
       const int t0 = it.kb + TK * t;
       C::edge_step(ring + (t % NS) * TL::STAGE, ring + ((t + 1) % NS) * TL::STAGE, t + NS <= ntiles, f, t + NS, it.kb,
                    win, before, w, A, S, x, top, t0, t0 <= wave_sees, t + 1 < ntiles && t0 + TK <= wave_sees,
@@ -926,14 +927,26 @@ __global__ __launch_bounds__(256) void chunk_meet(MeetParams p) {
       __builtin_bit_cast(u32x2, __builtin_convertvector(y, bf16x4));
 }
 
-template <int D, bool F32, bool SOME>
+template <int D, bool F32, Keys KEYS>
 static hipError_t launch_d(const ChunkParams& p, const JoinParams& j, const MeetParams& m, const ChunkLaunch& l,
                            hipStream_t s) {
-  if (l.tall) chunk_attn<D, 4, 64, 2, F32 ? 3 : 1, F32, SOME><<<dim3(l.n_items * p.Hkv), dim3(256), 0, s>>>(p);
-  else chunk_attn<D, 1, 32, 2, F32 ? 3 : 2, F32, SOME><<<dim3(l.n_items * p.Hkv), dim3(64), 0, s>>>(p);
-  constexpr int NG = 1024 / D;
-  hipError_t e = hipGetLastError();
-  if (e == hipSuccess && SOME && l.n_meets > 0) {
+  // a prefix's tall tiles beside low ones of the requests' own: P as in these
+  constexpr int TALL = F32 ? 3 : 1, BESIDE = F32 ? 3 : KEYS == kBehind ? 2 : 1, NG = 1024 / D;
+  hipError_t e = hipSuccess;
+  if (l.n_tall > 0) {
+    const dim3 g(l.n_tall * p.Hkv);
+    if (l.two_parts) chunk_attn<D, 4, 64, 2, BESIDE, F32, KEYS><<<g, dim3(256), 0, s>>>(p);
+    else chunk_attn<D, 4, 64, 2, TALL, F32, KEYS><<<g, dim3(256), 0, s>>>(p);
+    e = hipGetLastError();
+  }
+  if (e == hipSuccess && l.n_low > 0) {
+    ChunkParams low = p;
+    low.items += l.n_tall;
+    low.turn0 = low.turn1 = 0;
+    chunk_attn<D, 1, 32, 2, F32 ? 3 : 2, F32, KEYS><<<dim3(l.n_low * p.Hkv), dim3(64), 0, s>>>(low);
+    e = hipGetLastError();
+  }
+  if (e == hipSuccess && KEYS == kBehind && l.n_meets > 0) {
     chunk_meet<D, F32><<<dim3(l.n_meets * p.Hkv, (l.meet_rows + NG - 1) / NG), dim3(256), 0, s>>>(m);
     e = hipGetLastError();
   }
@@ -947,12 +960,16 @@ static hipError_t launch_d(const ChunkParams& p, const JoinParams& j, const Meet
 
 hipError_t launch_chunk(const ChunkParams& p, const JoinParams& j, const MeetParams& m, const ChunkLaunch& l,
                         hipStream_t s) {
-  auto some = [&](auto d, auto f32) {
+  auto keys = [&](auto d, auto f32) {
     constexpr int D = decltype(d)::value;
     constexpr bool F32 = decltype(f32)::value;
-    return l.some ? launch_d<D, F32, true>(p, j, m, l, s) : launch_d<D, F32, false>(p, j, m, l, s);
+    switch (l.keys) {
+      case kBehind: return launch_d<D, F32, kBehind>(p, j, m, l, s);
+      case kWindowed: return launch_d<D, F32, kWindowed>(p, j, m, l, s);
+      default: return launch_d<D, F32, kEvery>(p, j, m, l, s);
+    }
   };
-  auto out = [&](auto d) { return l.out_f32 ? some(d, std::true_type{}) : some(d, std::false_type{}); };
+  auto out = [&](auto d) { return l.out_f32 ? keys(d, std::true_type{}) : keys(d, std::false_type{}); };
   return l.D == 128 ? out(std::integral_constant<int, 128>{}) : out(std::integral_constant<int, 64>{});
 }
 

@@ -21,18 +21,19 @@ struct ChunkItem {
   int32_t ctx;
   int64_t part;     // the tile's first partial row (pieces > 1): head h's piece s from (h pieces + s) rows on
   int32_t q0;       // the request's first row of q and out
-  int32_t skip;     // SOME: keys left out behind the first ones (below), a multiple of 32
+  int32_t skip;     // keys left out behind the first ones (below), a multiple of 32
 };
 static_assert(sizeof(ChunkItem) == 48, "ChunkItem is read as 16-byte units");
 
-// Items that leave out a run of keys (SOME: windows behind their sinks, requests
-// behind a shared prefix).  Their keys are counted without it: key t of an item is
-// the request's row t where t < first, else t + skip, `first` the sinks rounded up
-// to 32 (ChunkParams::sinks), and `keys` and `ctx` are in these counts (ctx may be
-// negative).  New token j sees the keys t <= ctx + j with t > ctx + j - window
-// or t < sinks.  The run begins and ends on a 32-row border of the request, so
-// that a 32-key block is of one page.  `part` is negative where the item writes
-// out itself.
+// Items that leave out a run of keys: requests behind a shared prefix (kBehind),
+// windows behind their sinks (kWindowed).  Their keys are counted without it: key t
+// of an item is the request's row t where t < first, else t + skip, `first` the
+// sinks rounded up to 32 (ChunkParams::sinks), and `keys` and `ctx` are in these
+// counts (ctx may be negative).  New token j sees the keys t <= ctx + j, of a
+// window those with t > ctx + j - window or t < sinks.  The run begins and ends on a
+// 32-row border of the request, so that a 32-key block is of one page.  `part` is
+// negative where the item writes out itself.
+enum Keys { kEvery, kBehind, kWindowed };
 
 // One query-row tile whose key range was cut: a head's pieces' partial rows
 // follow each other, `rows` apart, the heads `pieces * rows` apart.
@@ -66,7 +67,7 @@ struct ChunkParams {
   int32_t Hkv, G;
   int32_t turn0, turn1; // work-groups [turn0, turn1) take their places from the end
   float scale_log2;
-  int32_t window, sinks;               // SOME
+  int32_t window, sinks;               // kWindowed (sinks: 0 otherwise)
 };
 
 // Rows whose keys two tiles had, the prefix's and the request's own (a join of
@@ -98,13 +99,15 @@ static_assert(sizeof(ChunkParams) <= kSmallArgs && sizeof(JoinParams) <= kSmallA
 
 // What the launches go by.
 struct ChunkLaunch {
-  int32_t n_items, n_joins;            // of one KV head
+  int32_t n_tall, n_low;               // items of one KV head: up to kChunkTallRows rows on four
+                                       // waves, then up to kChunkLowRows on one
+  int32_t n_joins;
   int32_t D;
   bool out_f32;
-  bool tall;            // items of up to kChunkTallRows rows on four waves, else kChunkLowRows on one
+  bool two_parts;       // a bf16 output: P in two bf16 parts in tall tiles too
   int32_t join_rows;    // rows of the tallest joined tile
   int32_t join_pieces;  // pieces of the longest
-  bool some;            // items that leave keys out
+  Keys keys;            // what the items leave out
   int32_t n_meets, meet_rows;
 };
 
@@ -143,7 +146,10 @@ struct AppendSegment {
   int32_t req, pos, row, n;
 };
 constexpr int kMoveRows = 16;          // rows of one work-group (divides a page)
-constexpr int kTurnRows = 4;           // of one that rotates them
+constexpr int kTurnRows = 4;           // of one that rotates them, at most (two in small batches)
+// Where four rows a work-group begin to pay: 960 rows of 24 KB 7.6 us with two
+// and 10.8 with four, 13300 of them 60.6 and 58.7.
+constexpr int64_t kManyTurned = 4096;
 constexpr int kMaxTurned = 256;        // pairs of a head that it rotates
 constexpr int kMoveSegments = 240;
 
@@ -174,6 +180,7 @@ struct RotateParams {
   int32_t new_sh, q_sh, out_sh;             // 16-byte units
   int32_t bt_stride;
   int32_t q_heads, pairs;
+  int32_t rows;                        // of a work-group: 2 or 4
   AppendSegment seg[N];
 };
 
