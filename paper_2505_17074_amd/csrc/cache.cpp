@@ -648,7 +648,8 @@ spec_status_t spec_cache_append_rotated(const spec_chunks_t* chunks, const spec_
   if (((int64_t)rot->num_q_heads + 2 * (int64_t)cache->num_kv_heads) * cache->head_dim >= 1 << 26) return SPEC_ERR_UNSUPPORTED;
   sv::RotateParams<sv::kMoveSegments> p{};
   p.c = pools(cache, args->layer, false);
-  const sv::MoveLaunch l = move_launch(p.c, args->num_layers, nq);
+  const int64_t wide = ((int64_t)rot->num_q_heads + 2 * (int64_t)cache->num_kv_heads * args->num_layers) * cache->head_dim * eb;
+  const sv::MoveLaunch l = {args->num_layers, nq * wide >= sv::kTurnStream};
   p.k_new = static_cast<const char*>(args->k_new);
   p.v_new = static_cast<const char*>(args->v_new);
   p.new_sl = args->num_layers > 1 ? args->new_stride_layer * eb : 0;
