@@ -182,17 +182,20 @@ struct Row {
   }
 };
 
-// bf16 values of magnitude 2^-9 to 2^5 by their bits: two signs of 14 powers of
-// two of 128 values each.  A row's weights are those of so few values that they
-// are counted, or looked up, in place of an exponential each.
-constexpr int kOneSign = 14 * 128, kValues = 2 * kOneSign, kLeastValue = 118 << 7;
-__device__ __forceinline__ uint32_t value_place(uint32_t h) {       // >= kValues: another value
-  const uint32_t m = (h & 0x7fffu) - kLeastValue;
-  return m < kOneSign ? m + (h >> 15) * kOneSign : (uint32_t)kValues;
+// bf16 values of magnitude 2^-13 to 2^5 by their bits: two signs of 18 powers of
+// two of 128 values each, and a place a sign for all others.  A row's weights are
+// those of so few values that they are counted, or looked up, in place of an
+// exponential each.
+constexpr int kOneSign = 18 * 128, kValues = 2 * (kOneSign + 1), kLeastValue = 114 << 7;
+__device__ __forceinline__ uint32_t value_place(uint32_t m, uint32_t sign) {       // m: value_bits()
+  return min(m, (uint32_t)kOneSign) + sign * (kOneSign + 1);
 }
+__device__ __forceinline__ uint32_t value_bits(uint32_t h) { return (h & 0x7fffu) - kLeastValue; }
+// The value at a place; that of the others' place is none of the table's.
+__device__ __forceinline__ bool value_other(int i) { return i % (kOneSign + 1) == kOneSign; }
 __device__ __forceinline__ float value_at(int i) {
-  const int sign = i >= kOneSign;
-  return __uint_as_float((uint32_t)(i - sign * kOneSign + kLeastValue) << 16 | (uint32_t)sign << 31);
+  const int sign = i > kOneSign;
+  return __uint_as_float((uint32_t)(i - sign * (kOneSign + 1) + kLeastValue) << 16 | (uint32_t)sign << 31);
 }
 
 struct Shared {
@@ -211,12 +214,12 @@ struct Shared {
           double w[kRank];
         } list;
         uint32_t values[kValues];      // how often a bf16 value comes
+        unsigned long long runs[kThreads];       // of 64 keys in order
       };
     };
-    double weights[kValues + 1];       // a bf16 value's weight, and none
+    double weights[kValues];           // a bf16 value's weight
   };
   unsigned long long keys[kList];      // a list: order and id
-  unsigned long long runs[kThreads];   // of 64 keys in order
   double slab[kSlabs];                 // weights that stay, by runs of ids
   unsigned long long group[kGroups];   // sums of 32 ranges
   int n;                               // of the list
@@ -647,13 +650,14 @@ struct Slices {
         uint64_t others = 0;                               // units that hold other values, by the thread's count of them
         int nth = 0;
         units([&](u32x4 y, int) {
-          bool other = false;
+          uint32_t most = 0;
 #pragma unroll
           for (int i = 0; i < VEC; ++i) {
-            const uint32_t v = value_place(i & 1 ? y[i / 2] >> 16 : y[i / 2] & 0xffffu);
-            if (v < kValues) atomicAdd(&sh.values[v], 1u);
-            else other = true;
+            const uint32_t m = value_bits(i & 1 ? y[i / 2] >> 16 : y[i / 2]);
+            atomicAdd(&sh.values[value_place(m, i & 1 ? y[i / 2] >> 31 : y[i / 2] >> 15 & 1)], 1u);
+            most = max(most, m);
           }
+          const bool other = most >= kOneSign;
           others |= (uint64_t)other << min(nth, 63);       // the 64th and all after it: looked at again
           ++nth;
         });
@@ -665,13 +669,13 @@ struct Slices {
             R::values(row.raw(u), x);
 #pragma unroll
             for (int i = 0; i < VEC; ++i)
-              if (x[i] > -INFINITY && value_place(__float_as_uint(x[i]) >> 16) >= kValues) put(x[i], 1);
+              if (x[i] > -INFINITY && value_bits(__float_as_uint(x[i]) >> 16) >= kOneSign) put(x[i], 1);
             if (k < 63) break;
           }
         }
         __syncthreads();
         for (int i = t; i < kValues; i += kThreads)
-          if (const uint32_t n = sh.values[i]) put(value_at(i), n);
+          if (const uint32_t n = value_other(i) ? 0 : sh.values[i]) put(value_at(i), n);
       }
     }
     all = block_reduce(sh, all, 0ull, Plus{});
@@ -810,14 +814,17 @@ struct Slices {
     const double least = rule.min_p;
     // A value's range from a product alone: floor(x scale) >= g where x scale >= g.
     const float edge = st.range, past = st.range + 1.f;
+    auto in_edge = [&](float x) { return st.mode == kEdge && x * rule.scale >= edge && x * rule.scale < past; };
     auto ahead = [&](float x) { return st.mode == kAll || x * rule.scale >= past; };       // summed, not listed
     const bool table = !F32 && st.mode != kFirst;
     if (table) {
+      // NaN where a value needs a closer look: listed, or none of the table's
       for (int i = t; i < kValues; i += kThreads) {
-        const double y = ahead(value_at(i)) ? weight(value_at(i)) : 0.0;
-        sh.weights[i] = y >= least ? y : 0.0;
+        const float v = value_at(i);
+        double y = ahead(v) ? weight(v) : 0.0;
+        y = y >= least ? y : 0.0;
+        sh.weights[i] = value_other(i) || in_edge(v) ? NAN : y;
       }
-      if (t == 0) sh.weights[kValues] = 0.0;
       __syncthreads();
     }
     // a slice's units are whole runs of ids, a wave takes every sixteenth; so many
@@ -856,32 +863,32 @@ struct Slices {
               if (x[i] * rule.scale >= edge && x[i] > -INFINITY) list_it(i);
           }
         } else if (st.mode == kAll || most * rule.scale >= edge) {
-          bool some = false;                               // of the list, or another value than the table's
-#pragma unroll
-          for (int i = 0; i < VEC; ++i) {
-            const float g = x[i] * rule.scale;
-            some |= st.mode == kEdge && g >= edge && g < past;
-            if constexpr (F32) {
-              if (x[i] > -INFINITY && ahead(x[i])) {
-                const double y = weight(x[i]);
-                if (y >= least) sum += y;
-              }
-            } else {
-              const uint32_t v = value_place(i & 1 ? r[j][i / 2] >> 16 : r[j][i / 2] & 0xffffu);
-              sum += sh.weights[v];
-              some |= v == kValues;
+          auto take = [&](int i) {
+            if (in_edge(x[i])) {
+              list_it(i);
+            } else if (x[i] > -INFINITY && ahead(x[i])) {
+              const double y = weight(x[i]);
+              if (y >= least) sum += y;
             }
-          }
-          if (some) {
+          };
+          if constexpr (F32) {
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) take(i);
+          } else {
+            double y[VEC], all = sum;
 #pragma unroll
             for (int i = 0; i < VEC; ++i) {
-              const float g = x[i] * rule.scale;
-              if (st.mode == kEdge && g >= edge && g < past) list_it(i);
-              if constexpr (!F32) {
-                if (value_place(__float_as_uint(x[i]) >> 16) == kValues && x[i] > -INFINITY && ahead(x[i])) {
-                  const double y = weight(x[i]);
-                  if (y >= least) sum += y;
-                }
+              const uint32_t h = r[j][i / 2];
+              y[i] = sh.weights[value_place(value_bits(i & 1 ? h >> 16 : h), i & 1 ? h >> 31 : h >> 15 & 1)];
+              all += y[i];
+            }
+            if (all == all) {
+              sum = all;
+            } else {
+#pragma unroll
+              for (int i = 0; i < VEC; ++i) {
+                if (y[i] == y[i]) sum += y[i];
+                else take(i);
               }
             }
           }
@@ -917,7 +924,7 @@ struct Slices {
       }
       __syncthreads();
       if (t < n) {
-#pragma unroll 4
+#pragma unroll 8
         for (int r = 0; r < n; r += 64) {
           if (r == r0) continue;
           int k = 0;
