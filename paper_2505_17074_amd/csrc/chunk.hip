@@ -135,14 +135,12 @@ __device__ __forceinline__ void look(Window& x, const Fetch& f, int kb, int b, i
   x.pg = min(max(f.pages[i], 0), f.num_pages - 1);
 }
 
-// Byte offset of key t's row in the pools.
+// The page of the item's key t.
 template <Keys KEYS>
-__device__ __forceinline__ int64_t place_of(const Fetch& f, int t) {
-  const int r = row_of<KEYS>(f, min(t, f.ke - 1));
-  const int i = __builtin_amdgcn_readfirstlane(r / f.page_tokens);
+__device__ __forceinline__ int page_of(const Fetch& f, int t) {
+  const int i = __builtin_amdgcn_readfirstlane(row_of<KEYS>(f, min(t, f.ke - 1)) / f.page_tokens);
   const int pg = ((const const_int32*)f.pages)[i];
-  return __builtin_amdgcn_readfirstlane(min(max(pg, 0), f.num_pages - 1)) * f.page_bytes +
-         (int64_t)(r % f.page_tokens) * f.row_bytes;
+  return __builtin_amdgcn_readfirstlane(min(max(pg, 0), f.num_pages - 1));
 }
 
 // The query rows of one wave: 32 rows, lane l holding row l % 32 (both halves
@@ -281,7 +279,7 @@ __device__ __forceinline__ void join_rows(Rows<D>& S, float m1, float l1, const 
 template <Keys KEYS, int D>
 __device__ __forceinline__ void one_by_one(const Fetch& f, Rows<D>& S, int t, int last, float c, int half) {
   for (; t <= last; ++t) {
-    const int64_t at = place_of<KEYS>(f, t);
+    const int64_t at = page_of<KEYS>(f, t) * f.page_bytes + (int64_t)(row_of<KEYS>(f, t) % f.page_tokens) * f.row_bytes;
     const bf16x8* k = reinterpret_cast<const bf16x8*>(f.k + at) + half;
     const bf16x4* v = reinterpret_cast<const bf16x4*>(f.v + at) + half;
     float s = 0.f;
@@ -612,7 +610,7 @@ struct Chunk {
           continue;
         }
       }
-      const int64_t at = place_of<KEYS>(f, t);
+      const int64_t at = page_of<KEYS>(f, t) * f.page_bytes + (int64_t)(row_of<KEYS>(f, t) % f.page_tokens) * f.row_bytes;
       const char* k = f.k + at + (int64_t)key_of(l32) * f.row_bytes + half * 16;
       const char* v = f.v + at + (int64_t)(8 * half) * f.row_bytes + l32 * 2;
       ScoresOf<1> x;
@@ -723,9 +721,11 @@ struct Chunk {
   }
 };
 
-// (d = 64: three waves a SIMD.)
+// (d = 64: three waves a SIMD; with a window and three parts of P two, whose
+// registers hold both ends' masks: 16 requests of 1-400 tokens, windows of 500, 31
+// us for 34.)
 template <int D, int NW, int TK, int NS, int PARTS, bool F32, Keys KEYS>
-__global__ __launch_bounds__(64 * NW, D == 64 ? 3 : 2) void chunk_attn(ChunkParams p) {
+__global__ __launch_bounds__(64 * NW, D == 64 && !(KEYS == kWindowed && PARTS == 3 && NW == 4) ? 3 : 2) void chunk_attn(ChunkParams p) {
 #if defined(__HIP_DEVICE_COMPILE__)   // the host pass needs the signature only
   using C = Chunk<D, NW, TK, PARTS, KEYS>;
   using TL = Tile<D, TK>;
