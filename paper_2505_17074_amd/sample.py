@@ -11,6 +11,7 @@ from typing import Optional
 import torch
 
 from . import binding as B
+from .cache import _current_raw_stream
 
 _DTYPE = {torch.bfloat16: B.SPEC_BF16, torch.float32: B.SPEC_F32}
 _HERE = contextlib.nullcontext()
@@ -34,30 +35,33 @@ class Sampler:
         self._lib = B.load()
         self._args = B.SpecSampleArgs()
         self._ref = C.byref(self._args)
-        self._ws = self._ws_ptr = self._last = None
+        self._ws = self._ws_ptr = None
         self._ws_bytes = 0
+        self._last = self._last_h = None       # the last call's stream
 
-    def _workspace(self, stream: torch.cuda.Stream) -> None:
-        """A workspace for the call, ordered after the last call's use of it."""
-        last = self._last
-        if last is not None and last != stream:
-            stream.wait_event(last.record_event())
-        self._last = stream
+    def _move(self, h: int, stream: torch.cuda.Stream) -> None:
+        """The next call runs on another stream than the last, whose use of the
+        workspace it waits for."""
+        if self._last is not None:
+            stream.wait_event(self._last.record_event())
+        if self._ws is not None:
+            self._ws.record_stream(stream)
+        self._last, self._last_h = stream, h
+
+    def _grow(self) -> None:
         st, need = B.spec_sample_workspace_bytes(self._args)
         B.check(st, "spec_sample_workspace_bytes")
-        if need > self._ws_bytes:
-            # the last one goes back to torch's allocator, which knows the streams it was used on
-            self._ws_bytes = need + need // 4
+        # the last one goes back to torch's allocator, which knows the streams it was used on
+        self._ws_bytes = need + need // 4
+        with torch.cuda.stream(self._last):    # a block that no other stream's pending work has
             self._ws = torch.empty(self._ws_bytes + 256, dtype=torch.uint8, device=self.device)
-            self._ws_ptr = (self._ws.data_ptr() + 255) // 256 * 256
-            last = None
-        if last != stream:
-            self._ws.record_stream(stream)
+        self._ws_ptr = (self._ws.data_ptr() + 255) // 256 * 256
 
     def _per_row(self, t: Optional[torch.Tensor], name: str, dtype: torch.dtype, rows: int) -> Optional[int]:
         if t is None:
             return None
-        if t.dtype != dtype or t.dim() != 1 or t.shape[0] != rows or t.device != self.device or \
+        shape = t.shape
+        if t.dtype != dtype or len(shape) != 1 or shape[0] != rows or t.device != self.device or \
                 (rows > 1 and t.stride(0) != 1):
             raise ValueError(f"{name} is {dtype} [rows] on the sampler's device")
         return t.data_ptr()
@@ -73,15 +77,15 @@ class Sampler:
         the temperature is 1).  probs: the distributions that the tokens were drawn
         from; kept_logits in its place: the logits of those distributions.  Both
         are [rows, vocab] of the logits' type and may be the logits themselves."""
-        kind = _DTYPE.get(logits.dtype)
-        if logits.dim() != 2 or kind is None or logits.device != self.device or logits.shape[0] < 1 or \
-                logits.shape[1] < 1 or (logits.shape[1] > 1 and logits.stride(1) != 1):
+        kind, shape = _DTYPE.get(logits.dtype), logits.shape
+        if len(shape) != 2 or kind is None or logits.device != self.device or shape[0] < 1 or shape[1] < 1 or \
+                (shape[1] > 1 and logits.stride(1) != 1):
             raise ValueError("logits are bf16 or fp32 [rows, vocab] on the sampler's device")
         if probs is not None and kept_logits is not None:
             raise ValueError("probs or kept_logits, not both")
         if tokens is not None and uniforms is None:
             raise ValueError("tokens need uniforms")
-        n, vocab = logits.shape
+        n, vocab = shape
         a = self._args
         a.num_rows, a.vocab, a.dtype = B.int32(n), B.int32(vocab), kind
         a.logits, a.logits_stride = logits.data_ptr(), logits.stride(0) if n > 1 else vocab
@@ -101,11 +105,15 @@ class Sampler:
             a.rows_kind = B.SPEC_SAMPLE_PROBS if probs is not None else B.SPEC_SAMPLE_LOGITS
         if self.device.type != "cuda":
             raise ValueError("the logits are not in device memory")
-        here = _HERE if torch.cuda.current_device() == self.device.index else torch.cuda.device(self.device)
-        with here:
-            stream = stream or torch.cuda.current_stream(self.device)
-            h = stream.cuda_stream
+        index = self.device.index
+        with _HERE if torch.cuda.current_device() == index else torch.cuda.device(self.device):
+            h = _current_raw_stream(index) if stream is None else stream.cuda_stream
             if B.stream_capturing(h):
                 raise RuntimeError("a graph's calls need a workspace of their own: capture B.spec_sample")
-            self._workspace(stream)
-            B.check(self._lib.spec_sample(self._ref, self._ws_ptr, self._ws_bytes, h), "spec_sample")
+            if h != self._last_h:
+                self._move(h, stream or torch.cuda.current_stream(index))
+            st = self._lib.spec_sample(self._ref, self._ws_ptr, self._ws_bytes, h)
+            if st == B.SPEC_ERR_WORKSPACE:
+                self._grow()
+                st = self._lib.spec_sample(self._ref, self._ws_ptr, self._ws_bytes, h)
+        B.check(st, "spec_sample")
