@@ -565,18 +565,32 @@ struct Slices {
     return __builtin_bit_cast(unsigned long long, __builtin_fma(w, unit, 4503599627370496.0)) & 0xfffffffffffffull;
   }
 
-  __device__ __forceinline__ void scan_slice(int slice) {
-    const int t = threadIdx.x, u0 = begin(slice), u1 = end(slice);
-    u32x4 r[kAhead];
-    float m = -INFINITY;
-    auto load = [&](int at) {
+  // The slice's units, kAhead of them a thread at once: f(unit as it is, which).
+  // `held`: r holds the first of them (all, where they fit).
+  __device__ __forceinline__ void load(int at, int u1, u32x4 (&r)[kAhead]) const {
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) {
+      const int u = at + (int)threadIdx.x + j * kThreads;
+      r[j] = u < u1 ? row.raw(u) : u32x4{0xffffffffu, 0xffffffffu, 0xffffffffu, 0xffffffffu};     // NaN
+    }
+  }
+  template <typename F>
+  __device__ __forceinline__ void units(int slice, u32x4 (&r)[kAhead], bool held, F&& f) const {
+    const int u0 = begin(slice), u1 = end(slice);
+    for (int at = u0; at < u1; at += kAhead * kThreads) {
+      if (!held || u0 + kAhead * kThreads < u1) load(at, u1, r);
 #pragma unroll
       for (int j = 0; j < kAhead; ++j) {
-        const int u = at + t + j * kThreads;
-        r[j] = u < u1 ? row.raw(u) : u32x4{0xffffffffu, 0xffffffffu, 0xffffffffu, 0xffffffffu};     // NaN
+        if (at + j * kThreads >= u1) break;
+        f(r[j], at + (int)threadIdx.x + j * kThreads);
       }
-    };
-    load(u0);
+    }
+  }
+
+  __device__ __forceinline__ void scan_slice(int slice, u32x4 (&r)[kAhead]) {
+    const int t = threadIdx.x, u0 = begin(slice), u1 = end(slice);
+    float m = -INFINITY;
+    load(u0, u1, r);
     for (int at = u0;;) {
 #pragma unroll
       for (int j = 0; j < kAhead; ++j) {
@@ -587,7 +601,7 @@ struct Slices {
       }
       at += kAhead * kThreads;
       if (at >= u1) break;
-      load(at);
+      load(at, u1, r);
     }
     top = block_reduce(sh, m, -INFINITY, Most{});
     if (!ONE && t == 0) ws.top[slice] = top;
@@ -612,24 +626,12 @@ struct Slices {
       if (g >= lowest) atomicAdd(&sh.count[(int)g & (kBins - 1)], 1u);
       ++all;
     };
-    // f(the slice's units, as they are, and which they are); one batch is still in r
-    const bool one_batch = u0 + kAhead * kThreads >= u1;
-    auto units = [&](auto&& f) {
-      for (int at = u0; at < u1; at += kAhead * kThreads) {
-        if (!one_batch) load(at);
-#pragma unroll
-        for (int j = 0; j < kAhead; ++j) {
-          if (at + j * kThreads >= u1) break;
-          f(r[j], at + t + j * kThreads);
-        }
-      }
-    };
     // A few of them: k threads' largest values are as many tokens, so the k-th
     // largest of those is no larger than the k-th token, and few tokens lie between.
     if (rule.few) {
       tell(m);
     } else if (top > -INFINITY && rule.by_count) {
-      units([&](u32x4 y, int) {
+      units(slice, r, true, [&](u32x4 y, int) {
         float x[VEC];
         R::values(y, x);
 #pragma unroll
@@ -637,7 +639,7 @@ struct Slices {
       });
     } else if (top > -INFINITY) {
       if constexpr (F32) {
-        units([&](u32x4 y, int) {
+        units(slice, r, true, [&](u32x4 y, int) {
           float x[VEC];
           R::values(y, x);
 #pragma unroll
@@ -649,7 +651,7 @@ struct Slices {
         __syncthreads();
         uint64_t others = 0;                               // units that hold other values, by the thread's count of them
         int nth = 0;
-        units([&](u32x4 y, int) {
+        units(slice, r, true, [&](u32x4 y, int) {
           uint32_t most = 0;
 #pragma unroll
           for (int i = 0; i < VEC; ++i) {
@@ -803,7 +805,7 @@ struct Slices {
     return st;
   }
 
-  __device__ __forceinline__ void collect_slice(int slice, const RowState& st) {
+  __device__ __forceinline__ void collect_slice(int slice, const RowState& st, u32x4 (&held)[kAhead]) {
     const int t = threadIdx.x, lane = t & 63;
     if (t == 0) sh.n = 0;
     __syncthreads();
@@ -814,10 +816,30 @@ struct Slices {
     const double least = rule.min_p;
     // A value's range from a product alone: floor(x scale) >= g where x scale >= g.
     const float edge = st.range, past = st.range + 1.f;
+    auto list_it = [&](float x, int id) {
+      const int n = atomicAdd(&sh.n, 1);
+      if (n < kList) list[n] = (unsigned long long)key_of(R::clean(__float_as_uint(x))) << 32 | (uint32_t)id;
+    };
+    if (st.mode == kFirst) {
+      units(slice, held, ONE, [&](u32x4 y, int u) {
+        float x[VEC];
+        R::values(y, x);
+        float most = x[0];
+#pragma unroll
+        for (int i = 1; i < VEC; ++i) most = fmaxf(most, x[i]);
+        if (most * rule.scale >= edge && most > -INFINITY) {
+#pragma unroll
+          for (int i = 0; i < VEC; ++i)
+            if (x[i] * rule.scale >= edge && x[i] > -INFINITY) list_it(x[i], row.first_id(u) + i);
+        }
+      });
+      __syncthreads();
+      if (!ONE && t == 0) ws.n[slice] = sh.n;
+      return;
+    }
     auto in_edge = [&](float x) { return st.mode == kEdge && x * rule.scale >= edge && x * rule.scale < past; };
     auto ahead = [&](float x) { return st.mode == kAll || x * rule.scale >= past; };       // summed, not listed
-    const bool table = !F32 && st.mode != kFirst;
-    if (table) {
+    if constexpr (!F32) {
       // NaN where a value needs a closer look: listed, or none of the table's
       for (int i = t; i < kValues; i += kThreads) {
         const float v = value_at(i);
@@ -847,25 +869,13 @@ struct Slices {
         if (k0 + j >= steps) break;
         float x[VEC];
         R::values(r[j], x);
-        auto list_it = [&](int i) {
-          const int n = atomicAdd(&sh.n, 1);
-          if (n < kList)
-            list[n] = (unsigned long long)key_of(R::clean(__float_as_uint(x[i]))) << 32 |
-                      (uint32_t)(row.first_id(unit_of(k0 + j)) + i);
-        };
         float most = x[0];
 #pragma unroll
         for (int i = 1; i < VEC; ++i) most = fmaxf(most, x[i]);
-        if (st.mode == kFirst) {
-          if (most * rule.scale >= edge && most > -INFINITY) {
-#pragma unroll
-            for (int i = 0; i < VEC; ++i)
-              if (x[i] * rule.scale >= edge && x[i] > -INFINITY) list_it(i);
-          }
-        } else if (st.mode == kAll || most * rule.scale >= edge) {
+        if (st.mode == kAll || most * rule.scale >= edge) {
           auto take = [&](int i) {
             if (in_edge(x[i])) {
-              list_it(i);
+              list_it(x[i], row.first_id(unit_of(k0 + j)) + i);
             } else if (x[i] > -INFINITY && ahead(x[i])) {
               const double y = weight(x[i]);
               if (y >= least) sum += y;
@@ -893,7 +903,7 @@ struct Slices {
             }
           }
         }
-        if (st.mode != kFirst && (k0 + j) % parts == parts - 1) {
+        if ((k0 + j) % parts == parts - 1) {
           sum = wave_sum(sum);
           if (lane == 0) slab[begin(slice) / per + w + (k0 + j) / parts * kWaves] = sum;
           sum = 0.0;
@@ -1248,11 +1258,12 @@ __global__ __launch_bounds__(kThreads) void sample_step(SampleParams p) {
   Slices<F32, ONE> S{p, row, sh, rule, view.s, 0.f, 0.0};
   RowState st;
   RowDone done;
-  if constexpr (STEP == 0 || ONE) S.scan_slice(slice);
+  u32x4 units[kAhead];
+  if constexpr (STEP == 0 || ONE) S.scan_slice(slice, units);
   if constexpr (ONE) __syncthreads();
   if constexpr (STEP == 1 || ONE) {
     st = S.state();
-    S.collect_slice(slice, st);
+    S.collect_slice(slice, st, units);
   }
   if constexpr (STEP == 2 || STEP == 5) st = *reinterpret_cast<const RowState*>(view.s.state);
   if constexpr (ONE) __syncthreads();
