@@ -22,7 +22,6 @@ constexpr int kRank = 768;             // tokens ranked by counting: one a threa
 constexpr int kList = kSampleList;     // tokens of a sorted list
 constexpr int kSlabs = kSampleSlabs;   // runs of ids whose weights are summed apart
 constexpr int kGroups = kBins / 32;
-constexpr int kAhead = 8;              // units that a thread loads at once
 static_assert(kBins == kSampleBins, "a slice's histogram in the workspace");
 
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
@@ -549,6 +548,7 @@ template <bool F32, bool ONE>
 struct Slices {
   using R = Row<F32>;
   static constexpr int VEC = R::VEC;
+  static constexpr int kAhead = ONE ? 8 : 2;       // units that a thread loads at once
   const SampleParams& p;
   const R& row;
   Shared& sh;
@@ -851,7 +851,7 @@ struct Slices {
     }
     // a slice's units are whole runs of ids, a wave takes every sixteenth; so many
     // 64-unit parts of them at once
-    constexpr int kAtOnce = F32 ? kAhead : 4;
+    constexpr int kAtOnce = ONE ? (F32 ? 8 : 4) : 2;
     const int per = p.slab_units, parts = per / 64, u1 = end(slice), w = t / 64;
     const int runs = (u1 - begin(slice) + per - 1) / per;
     const int steps = w < runs ? ((runs - w + kWaves - 1) / kWaves) * parts : 0;      // parts of this wave
@@ -1258,7 +1258,7 @@ __global__ __launch_bounds__(kThreads) void sample_step(SampleParams p) {
   Slices<F32, ONE> S{p, row, sh, rule, view.s, 0.f, 0.0};
   RowState st;
   RowDone done;
-  u32x4 units[kAhead];
+  u32x4 units[S.kAhead];
   if constexpr (STEP == 0 || ONE) S.scan_slice(slice, units);
   if constexpr (ONE) __syncthreads();
   if constexpr (STEP == 1 || ONE) {
