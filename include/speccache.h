@@ -181,8 +181,11 @@ SPEC_API spec_status_t spec_chunk_attn_window(const spec_chunks_t* chunks, const
  *               them; they are read through the block table's row of the group's
  *               first request, which need not have new tokens but has to have the
  *               prefix (its pages are as spec_pages_fork leaves them).
- * Groups of one request with new tokens, and prefixes of less than a few 64-row
- * tiles, are computed as without.
+ * Whole 64-row tiles of a prefix are shared, two at least, and only where that
+ * saves more than the joined outputs cost: groups whose requests fill row tiles
+ * of their own (128 query rows a KV head), and of one request with new tokens, are
+ * computed as without.  For SPEC_BF16 P has two parts or one by the requests' own
+ * rows, as without.
  */
 typedef struct spec_prefixes {
   int32_t num_groups;

@@ -63,9 +63,15 @@ typedef enum spec_sample_rows {
  *                     lowest value for those that do not stay; SPEC_SAMPLE_NONE:
  *                     not written (rows may be NULL).  A row without tokens has
  *                     zero probabilities, or all logits at the lowest value.
- * Weights are taken and summed in 64 bits (off by 1e-10 of their value at most), so
- * that tokens and the sets that stay are those of the definition unless a sum is
- * that near to its border.  Results are deterministic.
+ * Weights are taken in 64 bits, off by 1e-11 of their value at most, and summed in
+ * 64 bits, top-p's in fixed point: n weights to n^2 2^-61 of the largest (7e-9 for
+ * 128256 of them) at the worst.  Tokens and the sets that stay are those of the
+ * definition unless a sum is that near to its border.  Results are deterministic.
+ * A row costs two reads of its logits and of some of them a third; one whose top-p
+ * cut lies among more than 2048 tokens within T / 64 of each other's logits (logits
+ * that are nearly all the same), or behind a top-k of more than 512 that leaves more
+ * than 2048 near its own cut, is searched by one work-group alone: 0.2-0.45 ms for
+ * 32000-128256 tokens.
  */
 typedef struct spec_sample_args {
   int32_t num_rows;

@@ -18,6 +18,13 @@
 //   both: 8 chunks of 33-700 tokens and 16 single ones, 32 heads of their own
 //     (671 MB, 73 GFLOP): 151 us, 4.5 TB/s; MFMA busy 33 %, a fifth of it for the
 //     empty rows of partly filled tiles.
+//   windows: the keys in them.  64 single tokens, windows of 1024 (268 MB): 55 us, 4.9
+//     TB/s; 5000 tokens and 8 single ones, windows of 2000 (150 GFLOP seen): 173 us,
+//     0.87 PFLOP/s, MFMA busy 47 %, a tile in 16 of them masked at the window's start.
+//   shared prefixes: 64 single tokens behind 8000 rows, 10-400 of their own (89 MB, 8.6
+//     GFLOP): 34 us where each alone reads 204 us long: 30 us, MFMA busy 28 %, for
+//     the prefix's pieces of 12 key tiles beside 512 items of a few, and 6 for the
+//     joins.
 // An fp32 output has three products with V for one: 16 requests of 1-400 tokens
 // over 0-1500 rows, d = 64: 38 us, MFMA busy 31 %, 1.2 waves a SIMD on average:
 // the longest items' 28 key tiles (a unit's mean share is 25) outlast the rest.

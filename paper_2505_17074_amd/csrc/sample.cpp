@@ -61,8 +61,8 @@ SamplePlan plan_sample(const spec_sample_args_t* a) {
   const int64_t per = (slabs + slices - 1) / slices;
   P.slices = (int32_t)((slabs + per - 1) / per);
   P.slice_units = (int32_t)(per * P.slab_units);
-  // 44 bits behind the point for slices of up to 2^18 tokens
-  P.fix = 44;
+  // a slice of n tokens: weights rounded at 2^-fix, their sum below 2^62
+  P.fix = 50;
   while (((int64_t)P.slice_units * vec) >> (62 - P.fix)) --P.fix;
   P.row_bytes = sv::sample_row_bytes(P.slices);
   P.bytes = std::max(kAlign, (size_t)(P.row_bytes * a->num_rows + kAlign - 1) / kAlign * kAlign);
