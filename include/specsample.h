@@ -38,7 +38,8 @@ typedef enum spec_sample_rows {
  * cumulative weight, over ids ascending among what stays, exceeds u times the
  * total (spec_accept's convention).
  *
- *   num_rows, vocab   >= 1.
+ *   num_rows, vocab   >= 1; rows below 2^22, tokens up to 2^28
+ *                     (SPEC_ERR_UNSUPPORTED otherwise).
  *   dtype             of the logits: SPEC_F32 or SPEC_BF16.
  *   logits            [num_rows, vocab] (device), row stride logits_stride
  *                     elements (>= vocab), aligned to their elements.  Minus

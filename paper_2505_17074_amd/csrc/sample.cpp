@@ -34,6 +34,7 @@ spec_status_t check_sample(const spec_sample_args_t* a) {
   }
   // a row's ids and places are 32 bits, a sum of its weights 62
   if (a->vocab > 1 << 28) return SPEC_ERR_UNSUPPORTED;
+  if (a->num_rows >= 1 << 22) return SPEC_ERR_UNSUPPORTED;                 // a launch's work-items are 32 bits
   return SPEC_OK;
 }
 

@@ -37,6 +37,7 @@ constexpr int kGroups = kBins / 32;
 static_assert(kBins == kSampleBins, "a slice's histogram in the workspace");
 
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
 
 // 2^t for t <= 0 in 64 bits, off by 1e-11 of it: e^(f ln 2) by its series up to
 // the tenth power for |f| <= 1/2 (the next term is below 3e-13).
@@ -194,19 +195,38 @@ struct Row {
 };
 
 // bf16 values of magnitude 2^-13 to 2^5 by their bits: two signs of 18 powers of
-// two of 128 values each, and a place a sign for all others.  A row's weights are
-// those of so few values that they are counted, or looked up, in place of an
-// exponential each.
-constexpr int kOneSign = 18 * 128, kValues = 2 * (kOneSign + 1), kLeastValue = 114 << 7;
-__device__ __forceinline__ uint32_t value_place(uint32_t m, uint32_t sign) {       // m: value_bits()
-  return min(m, (uint32_t)kOneSign) + sign * (kOneSign + 1);
+// two of 128 values each, a place a sign for all others, one for the type's lowest
+// value and one for what is masked out (both as masks have them; one for each lane, so
+// that a row of them is not counted at one address).  A row's weights are those of
+// so few values that they are counted, or looked up, in place of an exponential each.
+constexpr int kOneSign = 18 * 128, kNegative = 2 * kOneSign + 1, kLowest = kNegative + 65, kMasked = kNegative + 130;
+constexpr int kValues = kMasked + 127;
+constexpr int kLeastValue = 114 << 7;
+__device__ __forceinline__ bool value_in_table(float x) {
+  const uint32_t h = __float_as_uint(x) >> 16;
+  return (h & 0x7fffu) - kLeastValue < (uint32_t)kOneSign || h == 0xff7fu;
 }
-__device__ __forceinline__ uint32_t value_bits(uint32_t h) { return (h & 0x7fffu) - kLeastValue; }
-// The value at a place; that of the others' place is none of the table's.
-__device__ __forceinline__ bool value_other(int i) { return i % (kOneSign + 1) == kOneSign; }
+// Two values' places times SIZE, below 2^16 each; `most` reaches kOneSign where one is
+// among a sign's others.
+template <int SIZE>
+__device__ __forceinline__ uint32_t value_places(uint32_t two, u16x2& most) {
+  static_assert(kValues * SIZE <= 65536, "16 bits");
+  const u16x2 h = __builtin_bit_cast(u16x2, two), one = {1, 1};
+  const u16x2 m = __builtin_elementwise_min((u16x2)((h & one * (uint16_t)0x7fff) - one * (uint16_t)kLeastValue), one * (uint16_t)kOneSign);
+  // 1 for the lowest, 2 for minus infinity and the NaNs behind it
+  const u16x2 low = __builtin_elementwise_min(__builtin_elementwise_sub_sat(h, one * (uint16_t)0xff7e), one * (uint16_t)2);
+  most = __builtin_elementwise_max(most, (u16x2)(m - low));
+  // from the negative others' place 65 .. 128 on, or twice that
+  const u16x2 on = low * (uint16_t)(65 + (threadIdx.x & 63)) + m;
+  return __builtin_bit_cast(uint32_t, (u16x2)(((h >> 15) * (uint16_t)(kOneSign + 1) + on) * (uint16_t)SIZE));
+}
+// The value at a place; those of the others' places and the masked ones' are none of
+// the table's.
+__device__ __forceinline__ bool value_other(int i) { return i == kOneSign || i == kNegative || i >= kMasked; }
 __device__ __forceinline__ float value_at(int i) {
   const int sign = i > kOneSign;
-  return __uint_as_float((uint32_t)(i - sign * (kOneSign + 1) + kLeastValue) << 16 | (uint32_t)sign << 31);
+  const uint32_t h = i >= kLowest ? 0xff7fu : (uint32_t)(i - sign * (kOneSign + 1) + kLeastValue) | (uint32_t)sign << 15;
+  return __uint_as_float(h << 16);
 }
 
 struct Shared {
@@ -234,7 +254,7 @@ struct Shared {
   double slab[kSlabs];                 // weights that stay, by runs of ids
   unsigned long long group[kGroups];   // sums of 32 ranges
   int n;                               // of the list
-  unsigned long long red[kWaves];
+  unsigned long long red[2][kWaves];   // taken in turn, so that one barrier an operation will do
   unsigned long long out[2];
 };
 static_assert(sizeof(Shared) <= 65536, "a work-group's LDS");
@@ -246,12 +266,13 @@ struct Cut {
   __device__ __forceinline__ bool keeps(float y, int i) const { return y > x || (y == x && i <= id); }
 };
 
-// f over the work-group, the same for all threads.
+// f over the work-group, the same for all threads.  `turn`: which of the places its
+// waves meet at, not the last operation's.
 template <typename T, typename F>
-__device__ __forceinline__ T block_reduce(Shared& sh, T x, T none, F&& f) {
+__device__ __forceinline__ T block_reduce(Shared& sh, int& turn, T x, T none, F&& f) {
   x = last_lane(wave_scan(x, none, f));
-  T* at = reinterpret_cast<T*>(sh.red);
-  __syncthreads();
+  T* at = reinterpret_cast<T*>(sh.red[turn]);
+  turn ^= 1;
   if ((threadIdx.x & 63) == 0) at[threadIdx.x / 64] = x;
   __syncthreads();
   x = at[0];
@@ -261,10 +282,10 @@ __device__ __forceinline__ T block_reduce(Shared& sh, T x, T none, F&& f) {
 }
 // The sum over the threads up to and including this one.
 template <typename T>
-__device__ __forceinline__ T block_scan(Shared& sh, T x) {
+__device__ __forceinline__ T block_scan(Shared& sh, int& turn, T x) {
   x = wave_scan(x, T(0), Plus{});
-  T* at = reinterpret_cast<T*>(sh.red);
-  __syncthreads();
+  T* at = reinterpret_cast<T*>(sh.red[turn]);
+  turn ^= 1;
   if ((threadIdx.x & 63) == 63) at[threadIdx.x / 64] = x;
   __syncthreads();
   T base = 0;
@@ -283,6 +304,7 @@ struct Sampler {
   double c;                            // log2(e) / T
   float bins;                          // kBins ranges to 32 T
   int fix;                             // fixed point: weights in units of 2^-fix
+  mutable int turn = 0;
 
   __device__ __forceinline__ Sampler(const R& r, Shared& s) : row(r), sh(s) {}
 
@@ -317,7 +339,7 @@ struct Sampler {
     const int t = threadIdx.x;
     const T a = hist[2 * t], b = hist[2 * t + 1];
     if (t == 0) sh.out[0] = 0;
-    const unsigned long long s2 = block_scan(sh, (unsigned long long)a + b), s1 = s2 - b, s0 = s1 - a;
+    const unsigned long long s2 = block_scan(sh, turn, (unsigned long long)a + b), s1 = s2 - b, s0 = s1 - a;
     // the only range that begins below the mark and does not end below it
     if (s0 < mark && s1 >= mark) {
       sh.out[0] = 2 * t + 1;
@@ -359,9 +381,9 @@ struct Sampler {
       }
     });
     for (;;) {
-      lo = block_reduce(sh, lo, 0xffffffffu, Least{});
-      hi = block_reduce(sh, hi, 0u, Most{});
-      n = block_reduce(sh, n, 0, Plus{});
+      lo = block_reduce(sh, turn, lo, 0xffffffffu, Least{});
+      hi = block_reduce(sh, turn, hi, 0u, Most{});
+      n = block_reduce(sh, turn, n, 0, Plus{});
       if (n <= kRank || lo == hi) break;
       // again, over keys lo .. hi
       const int shift = max(0, 21 - __builtin_clz((hi - lo) | 1));
@@ -451,12 +473,12 @@ struct Sampler {
       int mine = 0;
 #pragma unroll
       for (int i = 0; i < VEC; ++i) mine += y[i] == x && in.keeps(y[i], row.first_id(u) + i);
-      const int upto = block_scan(sh, mine);
+      const int upto = block_scan(sh, turn, mine);
       long long at = so_far + upto - mine;
 #pragma unroll
       for (int i = 0; i < VEC; ++i)
         if (y[i] == x && in.keeps(y[i], row.first_id(u) + i) && ++at == m) sh.out[0] = row.first_id(u) + i;
-      so_far += block_reduce(sh, mine, 0, Plus{});
+      so_far += block_reduce(sh, turn, mine, 0, Plus{});
       if (so_far >= m) break;
     }
     const Cut cut = {x, (int)sh.out[0]};
@@ -570,6 +592,7 @@ struct Slices {
   SampleRow ws;
   float top;
   double sum_all;                      // ONE: the histogram's
+  mutable int turn = 0;
 
   __device__ __forceinline__ int begin(int slice) const { return slice * p.slice_units; }
   __device__ __forceinline__ int end(int slice) const { return min((slice + 1) * p.slice_units, row.units); }
@@ -601,23 +624,78 @@ struct Slices {
     }
   }
 
+  // How often each of the table's values comes in the slice (sh.values), which of the
+  // thread's units hold others (the 64th and all after it by one bit), and the
+  // thread's share of the search for the largest value.
+  __device__ __forceinline__ float count_values(int slice, u32x4 (&r)[kAhead], uint64_t& others) const {
+    const int t = threadIdx.x;
+    for (int i = t; i < kValues; i += kThreads) sh.values[i] = 0;
+    __syncthreads();
+    int nth = 0;
+    float m = -INFINITY;
+    units(slice, r, false, [&](u32x4 y, int) {
+      u16x2 most = {0, 0};
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        const uint32_t at = value_places<4>(y[w], most);
+        atomicAdd(reinterpret_cast<uint32_t*>(reinterpret_cast<char*>(sh.values) + (at & 0xffffu)), 1u);
+        atomicAdd(reinterpret_cast<uint32_t*>(reinterpret_cast<char*>(sh.values) + (at >> 16)), 1u);
+      }
+      if (max(most.x, most.y) >= kOneSign) {
+        float x[VEC], z = -INFINITY;
+        R::values(y, x);
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) z = value_in_table(x[i]) ? z : fmaxf(z, x[i]);
+        m = fmaxf(m, z);
+        others |= (uint64_t)(z > -INFINITY) << min(nth, 63);
+      }
+      ++nth;
+    });
+    __syncthreads();
+    for (int i = t; i < kValues; i += kThreads)
+      if (!value_other(i) && sh.values[i]) m = fmaxf(m, value_at(i));
+    return m;
+  }
+  // f(value) of the values that are none of the table's.
+  template <typename F>
+  __device__ __forceinline__ void each_other(int slice, uint64_t others, F&& f) const {
+    const int u1 = end(slice);
+    while (others) {
+      const int k = __builtin_ctzll(others);
+      others &= others - 1;
+      for (int u = begin(slice) + threadIdx.x + k * kThreads; u < u1; u += kThreads) {
+        float x[VEC];
+        R::values(row.raw(u), x);
+#pragma unroll
+        for (int i = 0; i < VEC; ++i)
+          if (x[i] > -INFINITY && !value_in_table(x[i])) f(x[i]);
+        if (k < 63) break;
+      }
+    }
+  }
+
   __device__ __forceinline__ void scan_slice(int slice, u32x4 (&r)[kAhead]) {
     const int t = threadIdx.x, u0 = begin(slice), u1 = end(slice);
     float m = -INFINITY;
-    load(u0, u1, r);
-    for (int at = u0;;) {
+    uint64_t others = 0;                                   // units with values that are none of the table's
+    if (!F32 && rule.by_mass) {
+      m = count_values(slice, r, others);
+    } else {
+      load(u0, u1, r);
+      for (int at = u0;;) {
 #pragma unroll
-      for (int j = 0; j < kAhead; ++j) {
-        float x[VEC];
-        R::values(r[j], x);
+        for (int j = 0; j < kAhead; ++j) {
+          float x[VEC];
+          R::values(r[j], x);
 #pragma unroll
-        for (int i = 0; i < VEC; ++i) m = fmaxf(m, x[i]);
+          for (int i = 0; i < VEC; ++i) m = fmaxf(m, x[i]);
+        }
+        at += kAhead * kThreads;
+        if (at >= u1) break;
+        load(at, u1, r);
       }
-      at += kAhead * kThreads;
-      if (at >= u1) break;
-      load(at, u1, r);
     }
-    top = block_reduce(sh, m, -INFINITY, Most{});
+    top = block_reduce(sh, turn, m, -INFINITY, Most{});
     if (!ONE && t == 0) ws.top[slice] = top;
     if (!rule.by_count && !rule.by_mass) return;
     for (int i = t; i < kBins; i += kThreads) sh.mass[i] = 0;
@@ -661,40 +739,12 @@ struct Slices {
             if (x[i] > -INFINITY) put(x[i], 1);
         });
       } else {
-        for (int i = t; i < kValues; i += kThreads) sh.values[i] = 0;
-        __syncthreads();
-        uint64_t others = 0;                               // units that hold other values, by the thread's count of them
-        int nth = 0;
-        units(slice, r, true, [&](u32x4 y, int) {
-          uint32_t most = 0;
-#pragma unroll
-          for (int i = 0; i < VEC; ++i) {
-            const uint32_t m = value_bits(i & 1 ? y[i / 2] >> 16 : y[i / 2]);
-            atomicAdd(&sh.values[value_place(m, i & 1 ? y[i / 2] >> 31 : y[i / 2] >> 15 & 1)], 1u);
-            most = max(most, m);
-          }
-          const bool other = most >= kOneSign;
-          others |= (uint64_t)other << min(nth, 63);       // the 64th and all after it: looked at again
-          ++nth;
-        });
-        while (others) {
-          const int k = __builtin_ctzll(others);
-          others &= others - 1;
-          for (int u = u0 + t + k * kThreads; u < u1; u += kThreads) {
-            float x[VEC];
-            R::values(row.raw(u), x);
-#pragma unroll
-            for (int i = 0; i < VEC; ++i)
-              if (x[i] > -INFINITY && value_bits(__float_as_uint(x[i]) >> 16) >= kOneSign) put(x[i], 1);
-            if (k < 63) break;
-          }
-        }
-        __syncthreads();
+        each_other(slice, others, [&](float x) { put(x, 1); });
         for (int i = t; i < kValues; i += kThreads)
           if (const uint32_t n = value_other(i) ? 0 : sh.values[i]) put(value_at(i), n);
       }
     }
-    all = block_reduce(sh, all, 0ull, Plus{});
+    all = block_reduce(sh, turn, all, 0ull, Plus{});
     const double sum = rule.by_count ? (double)all : (double)all / unit;
     // groups of 32 ranges: 16 threads' pairs
     unsigned long long group = rule.by_count ? (unsigned long long)sh.count[2 * t] + sh.count[2 * t + 1]
@@ -739,6 +789,10 @@ struct Slices {
   // of 32 ranges, a wave adding each slice's, then among the group's ranges.  Every
   // wave finds it for itself.
   __device__ __forceinline__ RowState state() {
+    // asked for before the row's largest value says which of them are first
+    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), n = ONE ? 1 : p.slices;
+    const unsigned long long ahead = ONE || w >= n ? 0ull : ws.group[w * kGroups + lane];
+    const double sum = ONE || w >= n ? 0.0 : ws.sum[w];
     float tops[kSampleSlices];
     load_tops(tops);
     RowState st = {kAll, 0.f, 0.0, 0.0};
@@ -748,7 +802,6 @@ struct Slices {
     const float first = rule.range(top);
     // ranges that are not whole numbers apart, or all the same
     if (!(fabsf(first) < 8388608.f) || !(rule.scale > 0.f) || !(rule.scale < INFINITY)) return st;
-    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), n = ONE ? 1 : p.slices;
     const int start = (int)first & ~31;                    // of the first group
     double* part = reinterpret_cast<double*>(sh.runs);     // [slices][64], sums, [slices][32]
     float own = top;                                       // of the wave's slice
@@ -764,12 +817,14 @@ struct Slices {
       double y = 0.0;
       if (has) {
         if (rule.by_mass) f = weight(own) * __builtin_amdgcn_ldexp(1.0, -p.fix);
-        const unsigned long long* g = ONE ? sh.group : ws.group + w * kGroups;
-        const unsigned long long x = g[(low >> 5) & (kGroups - 1)];
+        const int at = (low >> 5) & (kGroups - 1);
+        unsigned long long x;
+        if constexpr (ONE) x = sh.group[at];
+        else x = __shfl(ahead, at);
         y = own_first >= (float)low ? (double)x * f : 0.0;
       }
       part[w * 64 + lane] = y;
-      if (lane == 0) part[512 + w] = !has ? 0.0 : (ONE ? sum_all : ws.sum[w]) * (rule.by_mass ? weight(own) : 1.0);
+      if (lane == 0) part[512 + w] = !has ? 0.0 : (ONE ? sum_all : sum) * (rule.by_mass ? weight(own) : 1.0);
     }
     __syncthreads();
     double y = 0.0, all = 0.0;
@@ -857,9 +912,9 @@ struct Slices {
       // NaN where a value needs a closer look: listed, or none of the table's
       for (int i = t; i < kValues; i += kThreads) {
         const float v = value_at(i);
-        double y = ahead(v) ? weight(v) : 0.0;
+        double y = ahead(v) && i < kMasked ? weight(v) : 0.0;
         y = y >= least ? y : 0.0;
-        sh.weights[i] = value_other(i) || in_edge(v) ? NAN : y;
+        sh.weights[i] = i < kMasked && (value_other(i) || in_edge(v)) ? NAN : y;
       }
       __syncthreads();
     }
@@ -881,39 +936,50 @@ struct Slices {
 #pragma unroll
       for (int j = 0; j < kAtOnce; ++j) {
         if (k0 + j >= steps) break;
-        float x[VEC];
-        R::values(r[j], x);
-        float most = x[0];
+        auto take = [&](float x, int i) {
+          if (in_edge(x)) {
+            list_it(x, row.first_id(unit_of(k0 + j)) + i);
+          } else if (x > -INFINITY && ahead(x)) {
+            const double y = weight(x);
+            if (y >= least) sum += y;
+          }
+        };
+        if constexpr (F32) {
+          float x[VEC];
+          R::values(r[j], x);
+          float most = x[0];
 #pragma unroll
-        for (int i = 1; i < VEC; ++i) most = fmaxf(most, x[i]);
-        if (st.mode == kAll || most * rule.scale >= edge) {
-          auto take = [&](int i) {
-            if (in_edge(x[i])) {
-              list_it(x[i], row.first_id(unit_of(k0 + j)) + i);
-            } else if (x[i] > -INFINITY && ahead(x[i])) {
-              const double y = weight(x[i]);
-              if (y >= least) sum += y;
-            }
-          };
-          if constexpr (F32) {
+          for (int i = 1; i < VEC; ++i) most = fmaxf(most, x[i]);
+          if (st.mode == kAll || most * rule.scale >= edge) {
 #pragma unroll
-            for (int i = 0; i < VEC; ++i) take(i);
+            for (int i = 0; i < VEC; ++i) take(x[i], i);
+          }
+        } else {
+          double y[VEC], all = sum;
+          u16x2 unused = {0, 0};
+#pragma unroll
+          for (int w = 0; w < 4; ++w) {
+            const uint32_t at = value_places<8>(r[j][w], unused);
+            y[2 * w] = *reinterpret_cast<const double*>(reinterpret_cast<const char*>(sh.weights) + (at & 0xffffu));
+            y[2 * w + 1] = *reinterpret_cast<const double*>(reinterpret_cast<const char*>(sh.weights) + (at >> 16));
+          }
+#pragma unroll
+          for (int i = 0; i < VEC; ++i) all += y[i];
+          if (all == all) {
+            sum = all;
           } else {
-            double y[VEC], all = sum;
+            uint32_t look = 0;
 #pragma unroll
             for (int i = 0; i < VEC; ++i) {
-              const uint32_t h = r[j][i / 2];
-              y[i] = sh.weights[value_place(value_bits(i & 1 ? h >> 16 : h), i & 1 ? h >> 31 : h >> 15 & 1)];
-              all += y[i];
+              const bool in = y[i] == y[i];
+              sum += in ? y[i] : 0.0;
+              look |= (uint32_t)!in << i;
             }
-            if (all == all) {
-              sum = all;
-            } else {
-#pragma unroll
-              for (int i = 0; i < VEC; ++i) {
-                if (y[i] == y[i]) sum += y[i];
-                else take(i);
-              }
+            while (look) {
+              const int i = __builtin_ctz(look);
+              look &= look - 1;
+              const uint32_t h = i < 4 ? (i < 2 ? r[j].x : r[j].y) : (i < 6 ? r[j].z : r[j].w);
+              take(__uint_as_float(i & 1 ? h & 0xffff0000u : h << 16), i);
             }
           }
         }
@@ -942,7 +1008,7 @@ struct Slices {
       if (r0 < n) {
         mine = t < n ? keys[t] : ~0ull;
         const int m = min(64, n - r0);
-#pragma unroll 8
+#pragma unroll 16
         for (int j = 0; j < m; ++j) at += keys[r0 + j] < mine;
         runs[r0 + (lane < m ? at : lane)] = mine;
       }
@@ -986,21 +1052,40 @@ struct Slices {
   struct Two {
     double w0, w1, s0, s1;
   };
+  // Up to 128 entries, two a lane, every wave has all of them and needs no barrier.
+  __device__ __forceinline__ static int entry_of(int n) { return 2 * (n <= 128 ? threadIdx.x & 63 : threadIdx.x); }
+  template <typename T>
+  __device__ __forceinline__ T scan(int n, T x) const {
+    return n <= 128 ? wave_scan(x, T(0), Plus{}) : block_scan(sh, turn, x);
+  }
+  template <typename T, typename F>
+  __device__ __forceinline__ T reduce(int n, T x, T none, F&& f) const {
+    return n <= 128 ? last_lane(wave_scan(x, none, f)) : block_reduce(sh, turn, x, none, f);
+  }
+  // x of the thread whose first entry is 2 i.
+  __device__ __forceinline__ double of_pair(int n, double x, int i) const {
+    if (n <= 128) return of_lane(x, __builtin_amdgcn_readfirstlane(i));
+    if ((int)threadIdx.x == i) reinterpret_cast<double*>(sh.out)[0] = x;
+    __syncthreads();
+    x = reinterpret_cast<double*>(sh.out)[0];
+    __syncthreads();
+    return x;
+  }
   __device__ __forceinline__ Two weights(int n) const {
-    const int i = 2 * threadIdx.x;
+    const int i = entry_of(n);
     Two y;
     y.w0 = i < n ? weight(value_of(sh.keys[i])) : 0.0;
     y.w1 = i + 1 < n ? weight(value_of(sh.keys[i + 1])) : 0.0;
-    y.s1 = block_scan(sh, y.w0 + y.w1);
+    y.s1 = scan(n, y.w0 + y.w1);
     y.s0 = y.s1 - y.w1;
     return y;
   }
   // The number of list entries that `f(entry, weight, sum)` holds for (a run from the front).
   template <typename F>
   __device__ __forceinline__ int count(const Two& y, int n, F&& f) const {
-    const int i = 2 * threadIdx.x;
+    const int i = entry_of(n);
     const int c = (i < n && f(i, y.w0, y.s0)) + (i + 1 < n && f(i + 1, y.w1, y.s1));
-    return block_reduce(sh, c, 0, Plus{});
+    return reduce(n, c, 0, Plus{});
   }
 
   // The token and what stays.  False: the row takes the other way.
@@ -1046,9 +1131,7 @@ struct Slices {
       Two y = weights(n);
       int stay = n;
       if (rule.top_p < 1.f) {
-        if (2 * t == (n - 1) / 2 * 2) reinterpret_cast<double*>(sh.out)[0] = n & 1 ? y.s0 : y.s1;
-        __syncthreads();
-        const double mark = (double)rule.top_p * reinterpret_cast<double*>(sh.out)[0];
+        const double mark = (double)rule.top_p * of_pair(n, n & 1 ? y.s0 : y.s1, (n - 1) / 2);
         stay = min(stay, 1 + count(y, n, [&](int, double, double s) { return s < mark; }));
       }
       if (least > 0.0) stay = min(stay, max(1, count(y, n, [&](int, double w, double) { return w >= least; })));
@@ -1057,14 +1140,11 @@ struct Slices {
       for (int i = t; i < stay; i += kThreads) sh.by_id[i] = (sh.keys[i] << 32) | (uint32_t)i;
       __syncthreads();
       sort(sh.by_id, stay);
-      const int i = 2 * t;
+      const int i = entry_of(stay);
       const double w0 = i < stay ? weight(value_of(sh.keys[(uint32_t)sh.by_id[i]])) : 0.0;
       const double w1 = i + 1 < stay ? weight(value_of(sh.keys[(uint32_t)sh.by_id[i + 1]])) : 0.0;
-      const double s1 = block_scan(sh, w0 + w1), s0 = s1 - w1;
-      if (t == (stay - 1) / 2) reinterpret_cast<double*>(sh.out)[0] = s1;
-      __syncthreads();
-      done.total = reinterpret_cast<double*>(sh.out)[0];
-      __syncthreads();
+      const double s1 = scan(stay, w0 + w1), s0 = s1 - w1;
+      done.total = of_pair(stay, s1, (stay - 1) / 2);
       // the first whose sum exceeds the mark (none: the last that has weight)
       const double mark = u * done.total;
       int best = 0x7fffffff, last = 0;
@@ -1072,8 +1152,8 @@ struct Slices {
       else if (w0 > 0.0) last = i;
       if (w1 > 0.0 && s1 > mark) best = i + 1;
       if (w0 > 0.0 && s0 > mark) best = i;
-      best = block_reduce(sh, best, 0x7fffffff, Least{});
-      last = block_reduce(sh, last, 0, Most{});
+      best = reduce(stay, best, 0x7fffffff, Least{});
+      last = reduce(stay, last, 0, Most{});
       token = (int)(sh.by_id[min(best, last)] >> 32);
       return true;
     }
@@ -1107,14 +1187,14 @@ struct Slices {
     const int t = threadIdx.x, slabs = (row.units + p.slab_units - 1) / p.slab_units;
     double mine = t < slabs ? slab[t] : 0.0;
     if (list && t < slabs) mine += (double)sh.add[t] * (1.0 / kListUnit);
-    const double s1 = block_scan(sh, mine);
+    const double s1 = block_scan(sh, turn, mine);
     if (t == kThreads - 1) reinterpret_cast<double*>(sh.out)[0] = s1;
     __syncthreads();
     done.total = reinterpret_cast<double*>(sh.out)[0];
     if (!p.tokens) return;
     const double mark = u * done.total;
-    int best = block_reduce(sh, mine > 0.0 && s1 > mark ? t : 0x7fffffff, 0x7fffffff, Least{});
-    best = min(best, block_reduce(sh, mine > 0.0 ? t : 0, 0, Most{}));
+    int best = block_reduce(sh, turn, mine > 0.0 && s1 > mark ? t : 0x7fffffff, 0x7fffffff, Least{});
+    best = min(best, block_reduce(sh, turn, mine > 0.0 ? t : 0, 0, Most{}));
     if (t == best) reinterpret_cast<double*>(sh.out)[0] = s1 - mine;
     __syncthreads();
     const double before = reinterpret_cast<double*>(sh.out)[0];
@@ -1179,7 +1259,7 @@ struct Slices {
         atomicAdd(&sh.count[S.range_of(x)], 1u);
         ++n;
       });
-      n = block_reduce(sh, n, 0, Plus{});
+      n = block_reduce(sh, turn, n, 0, Plus{});
       if (rule.k < n) cut = S.template last_of<false>((unsigned long long)rule.k, cut);
     }
     if (rule.top_p < 1.f) {
@@ -1191,7 +1271,7 @@ struct Slices {
         atomicAdd(&sh.mass[S.range_of(x)], w);
         all += w;
       });
-      all = block_reduce(sh, all, 0ull, Plus{});
+      all = block_reduce(sh, turn, all, 0ull, Plus{});
       const unsigned long long mark = (unsigned long long)ceil((double)rule.top_p * (double)all);
       cut = S.template last_of<true>(min(max(mark, 1ull), all), cut);
     }

@@ -149,6 +149,22 @@ def test_masked_and_not_finite(gpu_lib, dtype):
     assert (out[:2] == low).all()
 
 
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("V", [3000, 40000])
+def test_zeros_of_both_signs(gpu_lib, V, dtype):
+    """They are equal, so the lower id comes first."""
+    print(f"[case] sample signed zeros {V} {dtype}", flush=True)
+    x = torch.full((6, V), -1.0)
+    x[:, 1::7] = 0.0
+    x[:, 4::7] = -0.0
+    x = x.to(dtype).cuda()
+    u = _f(0.0, 0.2, 0.4, 0.6, 0.8, 0.99)
+    for kw in (dict(top_k=_i(1, 2, 3, 50, 300, 512)), dict(top_p=_f(1e-4, 1e-3, 0.01, 0.1, 0.3, 0.45)),
+               dict(top_k=_i(*[2] * 6), temperature=_f(*[0.0] * 6)), dict(top_k=_i(600, 601, 700, 800, 513, 514))):
+        tokens, out = _run(x, u, "probs", **kw)
+        _check(x, u, tokens, *(kw.get(k) for k in ("temperature", "top_k", "top_p", "min_p")), probs=out)
+
+
 def test_extreme_parameters(gpu_lib):
     print("[case] sample extremes", flush=True)
     nan, inf = float("nan"), float("inf")

@@ -40,7 +40,7 @@ PROBS = dict(rows_kind=B.SPEC_SAMPLE_PROBS, rows=2 * FAKE)
     (dict(tokens=None), INV),                                                # nothing to do
     (dict(PROBS, rows=None), INV), (dict(PROBS, rows=FAKE + 2), INV), (dict(PROBS, rows_stride=999), INV),
     (dict(PROBS, rows=FAKE, rows_stride=1004), INV),                         # in place with another stride
-    (dict(vocab=(1 << 28) + 1, logits_stride=1 << 30), UNS),
+    (dict(vocab=(1 << 28) + 1, logits_stride=1 << 30), UNS), (dict(num_rows=1 << 22), UNS),
 ])
 def test_refused(kw, expect):
     assert B.spec_sample(_args(**kw), FAKE, 1 << 30, 0) == expect
@@ -49,7 +49,7 @@ def test_refused(kw, expect):
 
 @pytest.mark.parametrize("kw", [
     dict(), dict(num_rows=1, logits_stride=0), PROBS, dict(PROBS, tokens=None, uniforms=None), dict(PROBS, rows=FAKE),
-    dict(dtype=B.SPEC_BF16, logits=FAKE + 2),
+    dict(dtype=B.SPEC_BF16, logits=FAKE + 2), dict(num_rows=(1 << 22) - 1),
 ])
 def test_accepted(kw):
     assert B.spec_sample_workspace_bytes(_args(**kw))[0] == B.SPEC_OK
