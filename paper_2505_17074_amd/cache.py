@@ -143,7 +143,7 @@ class PagedCache:
             raise ValueError("rows are contiguous and pages follow each other")
         self.k, self.v, self.device, self.dtype = k, v, k.device, k.dtype
         self._index = k.device.index
-        self._head = k.shape[3:]
+        self._head = tuple(k.shape[3:])
         self._width = k.shape[3] * k.shape[4]
         self._lib = B.load()
         c = self.c = B.SpecCache()
@@ -205,21 +205,26 @@ class PagedCache:
     def _new_rows(self, chunks: B.SpecChunks, k_new: torch.Tensor, v_new: torch.Tensor, layer: int) -> int:
         """The append arguments; the number of layers."""
         shape, st = k_new.shape, k_new.stride()
-        if not _alike(k_new, v_new) or len(shape) not in (3, 4) or \
-                shape[-2:] != self._head or shape[-3] < chunks.rows or (st[-1] != 1 and shape[-1] > 1):
+        if len(shape) not in (3, 4) or (v_new.shape != shape or v_new.stride() != st) and not _alike(k_new, v_new):
             raise ValueError("k_new and v_new are [layers, rows, Hkv, d], a row for every new token")
-        if k_new.dtype != self.dtype or v_new.dtype != self.dtype or k_new.device != self.device or \
-                v_new.device != self.device:
+        if len(shape) == 4:
+            (layers, rows, heads, d), (by_layer, by_row, by_head, by_one) = shape, st
+        else:
+            (rows, heads, d), (by_row, by_head, by_one) = shape, st
+            layers, by_layer = 1, by_row
+        if (heads, d) != self._head or rows < chunks.rows or (by_one != 1 and d > 1):
+            raise ValueError("k_new and v_new are [layers, rows, Hkv, d], a row for every new token")
+        dtype, device = self.dtype, self.device
+        if k_new.dtype != dtype or v_new.dtype != dtype or k_new.device != device or v_new.device != device:
             raise ValueError("k_new and v_new have the pools' type and device")
         self._requests(chunks.num_requests)
         a = self._append
-        a.layer, a.num_layers = B.int32(layer), shape[0] if len(shape) == 4 else 1
+        a.layer, a.num_layers = B.int32(layer), layers
         a.k_new, a.v_new = k_new.data_ptr(), v_new.data_ptr()
-        width = self._width
-        a.new_stride_layer = st[0]
-        a.new_stride_tok = st[-3] if shape[-3] > 1 else width
-        a.new_stride_head = st[-2] if shape[-2] > 1 else shape[-1]
-        return a.num_layers
+        a.new_stride_layer = by_layer
+        a.new_stride_tok = by_row if rows > 1 else self._width
+        a.new_stride_head = by_head if heads > 1 else d
+        return layers
 
     def append(self, chunks: B.SpecChunks, k_new: torch.Tensor, v_new: torch.Tensor, layer: int = 0,
                stream: Optional[torch.cuda.Stream] = None) -> None:
@@ -229,6 +234,19 @@ class PagedCache:
         with self._enter():
             B.check(self._lib.spec_cache_append(chunks, self._ref, self._append_ref, self._stream(stream)),
                     "spec_cache_append")
+
+    def _queries(self, q: torch.Tensor, rows: int):
+        """Heads, address, and strides of a row and a head of queries."""
+        shape = q.shape
+        if len(shape) != 3:
+            raise ValueError("q and q_out are [rows, Hq, d]")
+        (n, heads, d), (by_row, by_head, by_one) = shape, q.stride()
+        if n < rows or heads < 1 or d != self._head[1] or (by_one != 1 and d > 1):
+            raise ValueError("q and q_out are [rows, Hq, d], a row for every new token")
+        if q.dtype != self.dtype or q.device != self.device:
+            raise ValueError("q and q_out have the pools' type and device")
+        # of a dimension with one entry any stride will do
+        return heads, q.data_ptr(), by_row if n > 1 else heads * d, by_head if heads > 1 else d
 
     def append_rotated(self, chunks: B.SpecChunks, k_new: torch.Tensor, v_new: torch.Tensor, freq: torch.Tensor,
                        q: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None,
@@ -240,7 +258,7 @@ class PagedCache:
         and i + len(freq), or, interleaved, 2 i and 2 i + 1.  freq is fp32;
         positions int32 [rows], without them a row's place in its request."""
         layers = self._new_rows(chunks, k_new, v_new, layer)
-        rows, dtype, device = chunks.rows, self.dtype, self.device
+        rows, device = chunks.rows, self.device
         r = self._rotation
         shape = freq.shape
         if freq.dtype != torch.float32 or len(shape) != 1 or freq.device != device or \
@@ -260,22 +278,16 @@ class PagedCache:
         if q is None:
             r.num_q_heads = 0
         else:
-            shape, to, st, so = q.shape, q_out.shape, q.stride(), q_out.stride()
-            if len(shape) != 3 or len(to) != 3:
-                raise ValueError("q and q_out are [rows, Hq, d]")
-            n, heads, d = shape
-            m = to[0]
-            if n < rows or m < rows or to[1] != heads or heads < 1 or d != self._head[1] or to[2] != d or \
-                    ((st[2] != 1 or so[2] != 1) and d > 1):
-                raise ValueError("q and q_out are [rows, Hq, d], a row for every new token")
-            if q.dtype != dtype or q_out.dtype != dtype or q.device != device or q_out.device != device:
-                raise ValueError("q and q_out have the pools' type and device")
+            heads, r.q, r.q_stride_tok, r.q_stride_head = self._queries(q, rows)
+            if q_out is q:
+                r.q_out, r.out_stride_tok, r.out_stride_head = r.q, r.q_stride_tok, r.q_stride_head
+            else:
+                out_heads, r.q_out, r.out_stride_tok, r.out_stride_head = self._queries(q_out, rows)
+                if out_heads != heads:
+                    raise ValueError("q and q_out are [rows, Hq, d], a row for every new token")
             if layers != 1:
                 raise ValueError("queries belong to one layer")
-            r.num_q_heads, r.q, r.q_out = heads, q.data_ptr(), q_out.data_ptr()
-            # of a dimension with one entry any stride will do
-            r.q_stride_tok, r.out_stride_tok = st[0] if n > 1 else heads * d, so[0] if m > 1 else heads * d
-            r.q_stride_head, r.out_stride_head = (st[1], so[1]) if heads > 1 else (d, d)
+            r.num_q_heads = heads
         with self._enter():
             B.check(self._lib.spec_cache_append_rotated(chunks, self._ref, self._append_ref, self._rotation_ref,
                                                         self._stream(stream)), "spec_cache_append_rotated")
