@@ -914,17 +914,24 @@ __global__ __launch_bounds__(256) void chunk_meet(MeetParams p) {
   const int rr = (int)blockIdx.y * NG + (int)threadIdx.x / LPR, x = threadIdx.x % LPR;
   if (rr >= mt.rows) return;
   Joined j = {f32x4{0.f, 0.f, 0.f, 0.f}, -INFINITY, 0.f};
+  // both tiles' pieces as one run, so many at once (the last again where there are fewer)
+  constexpr int kAtOnce = 8;
+  const int64_t first = mt.part[0] + (int64_t)kvh * mt.pieces[0] * mt.stride[0] + rr;
+  const int64_t own = mt.part[1] + (int64_t)kvh * mt.pieces[1] * mt.stride[1] + rr;
+  const int all = mt.pieces[0] + mt.pieces[1];
+  for (int s0 = 0; s0 < all; s0 += kAtOnce) {
+    float2 y[kAtOnce];
+    f32x4 o[kAtOnce];
 #pragma unroll
-  for (int side = 0; side < 2; ++side) {
-    const int64_t first = mt.part[side] + (int64_t)kvh * mt.pieces[side] * mt.stride[side] + rr;
-    const float2* ml = reinterpret_cast<const float2*>(p.part) - 1 - first;
-    const float* po = p.part + first * D + 4 * x;
-#pragma unroll 4
-    for (int s = 0; s < mt.pieces[side]; ++s) {
-      const int64_t at = (int64_t)s * mt.stride[side];
-      const float2 y = ml[-at];
-      j.add(y.x, y.y, *reinterpret_cast<const f32x4*>(po + at * D));
+    for (int k = 0; k < kAtOnce; ++k) {
+      const int s = min(s0 + k, all - 1), t = s - mt.pieces[0];
+      const int64_t at = t < 0 ? first + (int64_t)s * mt.stride[0] : own + (int64_t)t * mt.stride[1];
+      y[k] = (reinterpret_cast<const float2*>(p.part) - 1)[-at];
+      o[k] = *reinterpret_cast<const f32x4*>(p.part + at * D + 4 * x);
     }
+#pragma unroll
+    for (int k = 0; k < kAtOnce; ++k)
+      if (s0 + k < all) j.add(y[k].x, y[k].y, o[k]);
   }
   const int r = mt.r0 + rr, tok = r / p.G;
   const int64_t at = ((mt.q0 + (int64_t)tok) * (p.Hkv * p.G) + kvh * p.G + (r - tok * p.G)) * D + 4 * x;
