@@ -12,14 +12,15 @@
 //
 // What bounds it (calls in a row): latency and launches where it is small, a wave's
 // instructions where it is large, never HBM.
-//   one row of 32000 (fp32), top-k and top-p: 14 us, one kernel of 10: load and
-//     largest value 1.7, histogram 1.2, the list 2, its two orders and the sums 4.5.
-//   64 of them, all filters, the rows written (16 MB): 34 us, three kernels of 8, 12
-//     and 17 with 3.5 between their first and last work-groups' ends and starts;
+//   one row of 32000 (fp32), top-k and top-p: 9.6 us (10.9 with two barriers for each
+//     of the work-group's sums and searches), one kernel of 9: load and largest value
+//     1.7, histogram 1.2, the list 2, its two orders and the sums 3.5.
+//   64 of them, all filters, the rows written (16 MB): 33 us, three kernels of 8, 11
+//     and 18 with 3.5 between their first and last work-groups' ends and starts;
 //     rows with top-p alone are the last to end.
-//   128 of 128256 (bf16), top-p (33 MB, 5 us at HBM's rate): 52 us, three kernels of
-//     16, 21 and 14: 18 vector instructions and an LDS operation an element in the
-//     first, 22 in the second, on one work-group a compute unit (two of them
+//   128 of 128256 (bf16), top-p (33 MB, 5 us at HBM's rate): 49 us, three kernels of
+//     16, 21 and 13: 17 vector instructions and an LDS operation an element in the
+//     first, 23 in the second, on one work-group a compute unit (two of them
 //     with half the registers measured the same).
 #include "sv_sample.h"
 
