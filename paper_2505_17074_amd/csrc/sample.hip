@@ -247,6 +247,7 @@ struct Shared {
         } list;
         uint32_t values[kValues];      // how often a bf16 value comes
         unsigned long long runs[kThreads];       // of 64 keys in order
+        int ids[kList];                // of the entries in by_id
       };
     };
     double weights[kValues];           // a bf16 value's weight
@@ -1137,6 +1138,10 @@ struct Slices {
       }
       if (least > 0.0) stay = min(stay, max(1, count(y, n, [&](int, double w, double) { return w >= least; })));
       done.cut = {value_of(sh.keys[stay - 1]), (int)(uint32_t)sh.keys[stay - 1]};
+      if (stay > 128) {
+        pick(y, stay, u, done, token);
+        return true;
+      }
       // ids ascending: (id, place in the list)
       for (int i = t; i < stay; i += kThreads) sh.by_id[i] = (sh.keys[i] << 32) | (uint32_t)i;
       __syncthreads();
@@ -1179,6 +1184,57 @@ struct Slices {
     }
     by_runs(ONE ? sh.slab : ws.slab, st.mode == kEdge, u, done, token);
     return true;
+  }
+
+  // The total, and the token, of more than 128 list entries that stay, whose weights are
+  // y's: which run of ids has it by the runs' sums (fixed point, whose order does not
+  // matter), then which of the run's entries.  (Sorted by their ids instead, 400 of
+  // them: 2 us longer.)
+  __device__ __forceinline__ void pick(const Two& y, int stay, double u, RowDone& done, int& token) {
+    const int t = threadIdx.x;
+    auto run_of = [&](int id) { return (id + row.head) / VEC / p.slab_units; };
+    static_assert(kSlabs == kThreads, "a run a thread");
+    sh.add[t] = 0;
+    if (t == 0) sh.n = 0;
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < 2; ++k)
+      if (2 * t + k < stay) atomicAdd(&sh.add[run_of((int)(uint32_t)sh.keys[2 * t + k])], fixed(k ? y.w1 : y.w0, kListUnit));
+    __syncthreads();
+    const unsigned long long mine = sh.add[t], upto = block_scan(sh, turn, mine);
+    if (t == kThreads - 1) sh.out[0] = upto;
+    __syncthreads();
+    const double all = (double)sh.out[0], mark = u * all;
+    done.total = all * (1.0 / kListUnit);
+    // the first whose sum exceeds the mark (none: the last that has weight)
+    int best = block_reduce(sh, turn, mine && (double)upto > mark ? t : 0x7fffffff, 0x7fffffff, Least{});
+    best = min(best, block_reduce(sh, turn, mine ? t : 0, 0, Most{}));
+    if (t == best) sh.out[0] = upto - mine;
+#pragma unroll
+    for (int k = 0; k < 2; ++k)
+      if (2 * t + k < stay) {
+        const int id = (int)(uint32_t)sh.keys[2 * t + k];
+        const unsigned long long w = fixed(k ? y.w1 : y.w0, kListUnit);
+        if (w && run_of(id) == best) {
+          const int at = atomicAdd(&sh.n, 1);
+          sh.by_id[at] = w;
+          sh.ids[at] = id;
+        }
+      }
+    __syncthreads();
+    const int m = sh.n;
+    const unsigned long long before = sh.out[0];
+    int first = 0x7fffffff, last = -1;
+    for (int i = t; i < m; i += kThreads) {
+      const int id = sh.ids[i];
+      unsigned long long s = before;
+      for (int j = 0; j < m; ++j) s += sh.ids[j] <= id ? sh.by_id[j] : 0;
+      if ((double)s > mark) first = min(first, id);
+      last = max(last, id);
+    }
+    first = block_reduce(sh, turn, first, 0x7fffffff, Least{});
+    last = block_reduce(sh, turn, last, -1, Most{});
+    token = min(first, last);
   }
 
   // The total, and the token, of what stays by the sums of its runs of ids (`list`: and
