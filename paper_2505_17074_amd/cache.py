@@ -37,6 +37,8 @@ def _current_raw_stream(index: int) -> int:
 
 # torch's own short way to the handle, where it has it (2 us less a call)
 _current_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", _current_raw_stream)
+# and to the current device, asked for only where tensors are on one
+_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 
 
 def _let_go() -> None:
@@ -184,7 +186,7 @@ class PagedCache:
         """The pools' device made current for a call (a context)."""
         if self._index is None:
             raise ValueError("the pools are not in device memory")
-        return _HERE if torch.cuda.current_device() == self._index else torch.cuda.device(self._index)
+        return _HERE if _current_device() == self._index else torch.cuda.device(self._index)
 
     def _stream(self, stream) -> int:
         h = _current_raw_stream(self._index) if stream is None else stream.cuda_stream

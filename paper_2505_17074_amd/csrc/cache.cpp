@@ -409,26 +409,29 @@ sv::CachePools pools(const spec_cache_t* c, int layer, bool one_run) {
 sv::MoveLaunch move_launch(const sv::CachePools& p, int layers, int64_t rows) {
   return {layers, rows * p.heads * p.row_units * 16 * 2 * layers >= sv::kMoveStream};
 }
-// The new rows as segments of at most `parts` blocks of `rows` rows, in launches
+// The new rows as segments of at most `parts` blocks of 2^log rows, in launches
 // of up to kMoveSegments of them: as few blocks as keep the batch in one launch's
 // table, so that ragged batches leave few work-groups without rows; a single
 // request's rows are one segment.
 template <typename P, typename F>
-spec_status_t in_segments(const spec_chunks_t* chunks, int rows, P& p, F&& launch) {
+spec_status_t in_segments(const spec_chunks_t* chunks, int log, P& p, F&& launch) {
   auto blocks = [&](int i) -> int64_t {
     const int64_t lo = chunks->ctx_len[i], n = chunks->new_len[i];
-    return n ? (lo + n - 1) / rows - lo / rows + 1 : 0;
+    return n ? ((lo + n - 1) >> log) - (lo >> log) + 1 : 0;
   };
   int64_t longest = 0, all = 0;
   for (int i = 0; i < chunks->num_requests; ++i) {
     longest = std::max(longest, blocks(i));
     all += blocks(i);
   }
-  int64_t parts = longest == all && all < 1 << 16 ? std::max<int64_t>(longest, 1) : 1;
-  for (;; parts *= 2) {
-    int64_t segs = 0;
-    for (int i = 0; i < chunks->num_requests; ++i) segs += (blocks(i) + parts - 1) / parts;
-    if (segs <= sv::kMoveSegments || parts >= longest) break;
+  int64_t parts = std::max<int64_t>(longest, 1);
+  if (longest != all || all >= 1 << 16) {
+    for (int more = 0;; ++more) {
+      parts = (int64_t)1 << more;
+      int64_t segs = 0;
+      for (int i = 0; i < chunks->num_requests; ++i) segs += (blocks(i) + parts - 1) >> more;
+      if (segs <= sv::kMoveSegments || parts >= longest) break;
+    }
   }
   int64_t row = 0;
   int n_seg = 0;
@@ -436,7 +439,7 @@ spec_status_t in_segments(const spec_chunks_t* chunks, int rows, P& p, F&& launc
     int32_t pos = chunks->ctx_len[i];
     const int32_t end = pos + chunks->new_len[i];
     while (pos < end) {
-      const int32_t stop = (int32_t)std::min<int64_t>(end, (pos / rows + parts) * rows);
+      const int32_t stop = (int32_t)std::min<int64_t>(end, ((pos >> log) + parts) << log);
       p.seg[n_seg++] = {i, pos, (int32_t)row, stop - pos};
       row += stop - pos;
       pos = stop;
@@ -616,7 +619,7 @@ spec_status_t spec_cache_append(const spec_chunks_t* chunks, const spec_cache_t*
   p.bt_stride = cache->block_stride;
   p.bt = cache->block_table;
   hipStream_t s = static_cast<hipStream_t>(stream);
-  return in_segments(chunks, sv::kMoveRows, p, [&](int n, int parts) { return sv::launch_append(p, n, parts, l, s); });
+  return in_segments(chunks, sv::kMoveLog, p, [&](int n, int parts) { return sv::launch_append(p, n, parts, l, s); });
 }
 
 spec_status_t spec_cache_append_rotated(const spec_chunks_t* chunks, const spec_cache_t* cache,
@@ -674,8 +677,9 @@ spec_status_t spec_cache_append_rotated(const spec_chunks_t* chunks, const spec_
   p.bt = cache->block_table;
   p.bt_stride = cache->block_stride;
   hipStream_t s = static_cast<hipStream_t>(stream);
-  p.rows = nq >= sv::kManyTurned ? sv::kTurnRows : sv::kTurnRows / 2;
-  return in_segments(chunks, p.rows, p, [&](int n, int parts) {
+  const int log = nq >= sv::kManyTurned ? sv::kTurnLog : sv::kTurnLog - 1;
+  p.rows = 1 << log;
+  return in_segments(chunks, log, p, [&](int n, int parts) {
     return sv::launch_rotate(p, n, parts, l, cache->dtype == SPEC_F32, rot->interleaved != 0, s);
   });
 }

@@ -147,8 +147,8 @@ constexpr int64_t kTurnStream = (int64_t)128 << 20;
 struct AppendSegment {
   int32_t req, pos, row, n;
 };
-constexpr int kMoveRows = 16;          // rows of one work-group (divides a page)
-constexpr int kTurnRows = 4;           // of one that rotates them, at most (two in small batches)
+constexpr int kMoveLog = 4, kMoveRows = 1 << kMoveLog;       // rows of one work-group (divides a page)
+constexpr int kTurnLog = 2, kTurnRows = 1 << kTurnLog;       // of one that rotates them, at most (two in small batches)
 // Where four rows a work-group begin to pay: 960 rows of 24 KB 7.6 us with two
 // and 10.8 with four, 13300 of them 60.6 and 58.7.
 constexpr int64_t kManyTurned = 4096;

@@ -11,7 +11,7 @@ from typing import Optional
 import torch
 
 from . import binding as B
-from .cache import _current_raw_stream
+from .cache import _current_device, _current_raw_stream
 
 _DTYPE = {torch.bfloat16: B.SPEC_BF16, torch.float32: B.SPEC_F32}
 _HERE = contextlib.nullcontext()
@@ -106,7 +106,7 @@ class Sampler:
         if self.device.type != "cuda":
             raise ValueError("the logits are not in device memory")
         index = self.device.index
-        with _HERE if torch.cuda.current_device() == index else torch.cuda.device(self.device):
+        with _HERE if _current_device() == index else torch.cuda.device(self.device):
             h = _current_raw_stream(index) if stream is None else stream.cuda_stream
             if B.stream_capturing(h):
                 raise RuntimeError("a graph's calls need a workspace of their own: capture B.spec_sample")
