@@ -1007,6 +1007,7 @@ struct Slices {
       const int t = threadIdx.x, lane = t & 63, r0 = t - lane;
       unsigned long long mine = ~0ull;
       int at = 0;
+      constexpr int kAtOnce = 8;       // runs: their steps wait for memory together
       if (r0 < n) {
         mine = t < n ? keys[t] : ~0ull;
         const int m = min(64, n - r0);
@@ -1016,13 +1017,18 @@ struct Slices {
       }
       __syncthreads();
       if (t < n) {
-#pragma unroll 8
-        for (int r = 0; r < n; r += 64) {
-          if (r == r0) continue;
-          int k = 0;
+        at = 0;
+        for (int r = 0; r < n; r += 64 * kAtOnce) {
+          int k[kAtOnce];                                  // of the last run again where there are fewer
 #pragma unroll
-          for (int step = 32; step > 0; step /= 2) k += runs[r + k + step - 1] < mine ? step : 0;
-          at += k + (runs[r + k] < mine);
+          for (int j = 0; j < kAtOnce; ++j) k[j] = min(r + 64 * j, (n - 1) & ~63);
+#pragma unroll
+          for (int step = 32; step > 0; step /= 2)
+#pragma unroll
+            for (int j = 0; j < kAtOnce; ++j) k[j] += runs[k[j] + step - 1] < mine ? step : 0;
+#pragma unroll
+          for (int j = 0; j < kAtOnce; ++j)
+            if (r + 64 * j < n) at += k[j] - (r + 64 * j) + (runs[k[j]] < mine);
         }
         keys[at] = mine;
       }
