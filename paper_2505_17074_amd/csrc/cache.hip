@@ -125,7 +125,7 @@ struct Turned {                        // a 16-byte unit's elements in fp32
 // row to row, the queries' heads first, then K's and V's.  Bound by HBM where it is
 // large (6 prompts' 13300 rows of 32 + 2 x 8 heads of 128, 327 MB: 60 us, 5.5 TB/s
 // with torch's copy at 5.1) and by the launch and one round of loads where it is
-// small (one row 4.0 us, 64 trees of 15 nodes, 24 MB, 8; a call 8 and 10 on the
+// small (one row 4.0 us, 64 trees of 15 nodes, 24 MB, 8; a call 8 and 9 on the
 // host).
 template <bool F32, bool INTER, bool STREAM, int N>
 __global__ __launch_bounds__(256) void cache_append_rotated(RotateParams<N> p) {
