@@ -52,10 +52,11 @@ class Sampler:
         st, need = B.spec_sample_workspace_bytes(self._args)
         B.check(st, "spec_sample_workspace_bytes")
         # the last one goes back to torch's allocator, which knows the streams it was used on
-        self._ws_bytes = need + need // 4
+        size = need + need // 4
         with torch.cuda.stream(self._last):    # a block that no other stream's pending work has
-            self._ws = torch.empty(self._ws_bytes + 256, dtype=torch.uint8, device=self.device)
-        self._ws_ptr = (self._ws.data_ptr() + 255) // 256 * 256
+            ws = torch.empty(size + 256, dtype=torch.uint8, device=self.device)
+        # nothing raises from here on: the size is that of the memory at the address
+        self._ws, self._ws_ptr, self._ws_bytes = ws, (ws.data_ptr() + 255) // 256 * 256, size
 
     def _per_row(self, t: Optional[torch.Tensor], name: str, dtype: torch.dtype, rows: int) -> Optional[int]:
         if t is None:
