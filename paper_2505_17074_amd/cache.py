@@ -372,17 +372,19 @@ class ChunkAttention(StagingRing):
         if dev > self.ws_bytes:
             if self.ws_bytes:
                 stream.synchronize()          # earlier calls' workspace goes back to the allocator
-            self.ws_bytes = dev + dev // 4
+            size = dev + dev // 4
             with torch.cuda.stream(stream):       # a block that no other stream's pending work has
-                self._ws = torch.empty(self.ws_bytes + 256, dtype=torch.uint8, device=self.cache.device)
-            self.ws_ptr = (self._ws.data_ptr() + 255) // 256 * 256
+                ws = torch.empty(size + 256, dtype=torch.uint8, device=self.cache.device)
+            # nothing raises from here on: the size is that of the memory at the address
+            self._ws, self.ws_ptr, self.ws_bytes = ws, (ws.data_ptr() + 255) // 256 * 256, size
         if host > self.staging_bytes:
             if self.staging_bytes:
                 stream.synchronize()          # and their staging
-            self.staging_bytes = host + host // 4
-            size = (self.staging_bytes + 255) // 256 * 256
-            self._pinned = torch.empty(size * len(self._staging), dtype=torch.uint8, pin_memory=True)
-            self._staging = [self._pinned.data_ptr() + i * size for i in range(len(self._staging))]
+            slots, size = len(self._staging), host + host // 4
+            apart = (size + 255) // 256 * 256
+            pinned = torch.empty(apart * slots, dtype=torch.uint8, pin_memory=True)
+            places = [pinned.data_ptr() + i * apart for i in range(slots)]
+            self._pinned, self._staging, self.staging_bytes = pinned, places, size
 
     def run(self, chunks: B.SpecChunks, q: torch.Tensor, out: torch.Tensor, layer: int = 0,
             stream: Optional[torch.cuda.Stream] = None, prefixes: Optional[B.SpecPrefixes] = None) -> None:
