@@ -61,8 +61,8 @@ class _Stream:
         pass
 
 
-def _prefixes(kind):
-    return B.make_prefixes([2], [256]) if kind == "prefixes" else None
+def _prefixes(kind, n):
+    return B.make_prefixes([n], [256]) if kind == "prefixes" else None
 
 
 def _attention(kind):
@@ -88,7 +88,8 @@ def _consistent(a):
 @pytest.mark.parametrize("fails", ["workspace", "staging"])
 @pytest.mark.parametrize("kind", ["plain", "window", "prefixes"])
 def test_an_attention_that_cannot_grow(monkeypatch, kind, fails):
-    small, large = B.make_chunks([300, 300], [1, 1]), B.make_chunks([90000] * 2, [900] * 2)
+    small = B.make_chunks([300, 300], [1, 1])
+    large = B.make_chunks([90000] * 40, [900] * 40)        # its plan alone outgrows the first workspace
     empty = torch.empty
     broken = []
 
@@ -99,18 +100,18 @@ def test_an_attention_that_cannot_grow(monkeypatch, kind, fails):
 
     monkeypatch.setattr(torch, "empty", allocate)
     a = _attention(kind)
-    a._grow(small, _Stream(), _prefixes(kind))
+    a._grow(small, _Stream(), _prefixes(kind, 2))
     _consistent(a)
     was = _state(a)
     broken.append(True)
     with pytest.raises(torch.OutOfMemoryError):
-        a._grow(large, _Stream(), _prefixes(kind))
+        a._grow(large, _Stream(), _prefixes(kind, 40))
     now = _state(a)
     assert now[2:] == was[2:]
     if fails == "workspace":
         assert now == was
     _consistent(a)
     broken.clear()
-    a._grow(large, _Stream(), _prefixes(kind))
+    a._grow(large, _Stream(), _prefixes(kind, 40))
     assert a.ws_bytes > was[1] and a.staging_bytes > was[2]
     _consistent(a)
