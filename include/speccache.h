@@ -246,7 +246,9 @@ SPEC_API spec_status_t spec_cache_append(const spec_chunks_t* chunks, const spec
  *                rows are right where spec_cache_commit moves them.  NULL: the
  *                row's place in its request, ctx_len[i] + r.
  *   q, q_out     [Nq, num_q_heads, d] in the cache's dtype, strides in elements,
- *                last dim contiguous, 16-byte aligned rows.  q_out is q itself
+ *                last dim contiguous, 16-byte aligned rows.  q_out's tokens lie
+ *                behind each other with all their heads, or its heads with all
+ *                their tokens (either order, any gaps).  q_out is q itself
  *                (with the same strides) or overlaps nothing that the call reads
  *                or writes.  num_q_heads 0: no queries (the four strides are
  *                ignored).  With queries num_layers is 1.

@@ -642,10 +642,11 @@ spec_status_t spec_cache_append_rotated(const spec_chunks_t* chunks, const spec_
     if (!aligned16(rot->q) || !aligned16(rot->q_out)) return SPEC_ERR_INVALID_ARG;
     for (const int64_t x : {rot->q_stride_tok, rot->q_stride_head, rot->out_stride_tok, rot->out_stride_head})
       if (x < 1 || x % vec) return SPEC_ERR_INVALID_ARG;
-    // rows that are written do not overlap
-    if (rot->num_q_heads > 1 && rot->out_stride_head < cache->head_dim) return SPEC_ERR_INVALID_ARG;
-    if (nq > 1 && rot->out_stride_tok < (rot->num_q_heads - 1) * rot->out_stride_head + cache->head_dim)
-      return SPEC_ERR_INVALID_ARG;
+    // rows that are written do not overlap: a token's heads lie before the next
+    // token's, or a head's tokens before the next head's
+    const int64_t d = cache->head_dim, h = rot->num_q_heads, by_row = rot->out_stride_tok, by_head = rot->out_stride_head;
+    if ((h > 1 && by_head < d) || (nq > 1 && by_row < d)) return SPEC_ERR_INVALID_ARG;
+    if (nq > 1 && h > 1 && (by_row - d) / by_head < h - 1 && (by_head - d) / by_row < nq - 1) return SPEC_ERR_INVALID_ARG;
     if (rot->q == rot->q_out && (rot->q_stride_tok != rot->out_stride_tok || rot->q_stride_head != rot->out_stride_head))
       return SPEC_ERR_INVALID_ARG;
     if (std::max(rot->q_stride_head, rot->out_stride_head) * eb / 16 > INT32_MAX) return SPEC_ERR_UNSUPPORTED;

@@ -199,3 +199,30 @@ def test_replayed_with_new_values(gpu_lib):
         p.cache.append_rotated(chunks, k, v, freq, q, q_out, positions=pos)
         torch.cuda.synchronize()
         assert torch.equal(got_q, q_out) and torch.equal(got_k, _rows(p)[0])
+
+
+@pytest.mark.parametrize("interleaved", [False, True], ids=["halves", "interleaved"])
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
+def test_heads_behind_each_other(gpu_lib, dtype, interleaved):
+    """Queries [Hq, rows, d] seen as [rows, Hq, d], into another tensor of that
+    order or of the usual one, and in place: the same values."""
+    print(f"[case] rotate heads first {dtype} {interleaved}", flush=True)
+    n, hq, d = 41, 6, 128
+    p = Paged([30, 0], [38, 3], 2, d, seed=7, dtype=dtype)
+    k, v = (x[0] for x in p.new_rows())
+    q = queries(n, hq, d, seed=7, dtype=dtype).cuda()
+    freq = _freq(d).cuda()
+    want = torch.empty_like(q)
+    p.cache.append_rotated(p.chunks(), k, v, freq, q, want, interleaved=interleaved)
+    heads = torch.full((hq, n + 1, d + 16), 7.0, dtype=dtype, device="cuda")          # gaps between rows and heads
+    view = heads[:, :n, :d].transpose(0, 1)
+    p.cache.append_rotated(p.chunks(), k, v, freq, q, view, interleaved=interleaved)
+    torch.cuda.synchronize()
+    assert torch.equal(view, want) and (heads[:, n:] == 7.0).all() and (heads[..., d:] == 7.0).all()
+    view.copy_(q)
+    back = torch.empty_like(q)
+    p.cache.append_rotated(p.chunks(), k, v, freq, view, back, interleaved=interleaved)
+    p.cache.append_rotated(p.chunks(), k, v, freq, view, view, interleaved=interleaved)
+    torch.cuda.synchronize()
+    assert torch.equal(back, want) and torch.equal(view, want)
+    assert (heads[:, n:] == 7.0).all() and (heads[..., d:] == 7.0).all()

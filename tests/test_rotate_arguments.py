@@ -100,3 +100,15 @@ def test_arguments_of_the_method():
     with pytest.raises(ValueError, match="device memory"):             # pools of the host
         c.append_rotated(chunks, new, new, freq, q, q)
     assert np.all(c.k.float().numpy() == 0)
+
+
+@pytest.mark.parametrize("kw,expect", [
+    # 70 tokens of 8 heads: heads behind each other are no overlap, so that what is refused is q's stride
+    (dict(out_stride_tok=128, out_stride_head=70 * 128), UNS), (dict(out_stride_tok=160, out_stride_head=69 * 160 + 128), UNS),
+    (dict(out_stride_tok=7 * 160 + 128, out_stride_head=160), UNS), (dict(out_stride_tok=1 << 33, out_stride_head=128), UNS),
+    (dict(out_stride_tok=120, out_stride_head=70 * 128), INV), (dict(out_stride_tok=128, out_stride_head=69 * 128), INV),
+    (dict(out_stride_tok=160, out_stride_head=69 * 160 + 120), INV), (dict(out_stride_tok=512, out_stride_head=128), INV),
+    (dict(out_stride_tok=7 * 160 + 120, out_stride_head=160), INV), (dict(out_stride_tok=1000, out_stride_head=1000), INV),
+])
+def test_orders_of_the_rotated_queries(kw, expect):
+    assert _call(_rotation(q=2 * FAKE, q_stride_head=1 << 36, **kw)) == expect
