@@ -146,3 +146,14 @@ def test_captured_and_repeated(gpu_lib):
         att.run(chunks, q, other, stream=None if i % 2 else stream, prefixes=groups)
         torch.cuda.synchronize()
         assert torch.equal(out, first) and torch.equal(other, first)
+
+
+@pytest.mark.parametrize("out", [BF16, F32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("sizes,prefixes", [([20], [1000]), ([12, 9, 1], [640, 1500, 300])])
+def test_single_tokens_of_small_heads(gpu_lib, sizes, prefixes, out):
+    """d = 64: a prefix's rows fill tall tiles, each request's own one row of one."""
+    print(f"[case] shared single d64 {sizes} {out}", flush=True)
+    n = sum(sizes)
+    p = make(sizes, prefixes, [(7 * i) % 150 for i in range(n)], [1] * n, 4, 64, 64, seed=n).write()
+    q = queries(n, 16, 64, seed=n)
+    check_close(_run(p, q, out, B.make_prefixes(sizes, prefixes)), *reference(p, q, causal_seen(p), out=out))
