@@ -232,8 +232,9 @@ SPEC_API spec_status_t spec_cache_append(const spec_chunks_t* chunks, const spec
  * the queries beside it, turned by its position, V as it is.  For pair i of
  * rotary_dim / 2, position p and the angle a = p freq[i] (radians),
  *   (x, y) -> (x cos a - y sin a, y cos a + x sin a),
- * the products and sums in fp32 (cos and sin off by 2^-23 at most, whatever p:
- * the angle and its turns are taken in 64 bits), each result rounded once.
+ * the products and sums in fp32 (cos and sin off by 2^-23 at most, whatever p,
+ * for frequencies up to 2^14: the angle and its turns are taken in two 64-bit
+ * numbers), each result rounded once.
  *   rotary_dim   the elements of a head that are turned, its first (an even
  *                number, up to head_dim and 512); the others are copied.  Pairs
  *                are elements i and i + rotary_dim / 2, or, with interleaved =

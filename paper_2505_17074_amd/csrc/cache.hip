@@ -72,13 +72,16 @@ __global__ __launch_bounds__(256) void cache_append(AppendParams<N> p) {
 }
 
 // cos and sin of p f, an angle in radians, for a whole number p and an fp32 f:
-// the product and its turns in 64 bits (p f has up to 55 bits, off by 2^-53 of
-// it; an angle of 2^20 turns is off by 2^-32 of one), the rest within an eighth of
-// a turn by the series, whose next terms are below 2^-28.
+// off by 2^-23 at most up to 2^45 radians (2^31 times an f of 2^14).  The product,
+// of up to 55 bits, is two 64-bit numbers and so is 2 / pi, so that what is left
+// of a quarter turn is off by 2^-53 of one, and by the angle's 2^-106; the rest
+// within an eighth of a turn by the series, whose next terms are below 2^-28.
 __device__ __forceinline__ float2 cos_sin(int32_t p, float f) {
-  const double turns4 = (double)p * (double)f * 0.63661977236758134308;      // quarter turns: 2 / pi
-  const double whole = __builtin_rint(turns4);
-  const float x = (float)((turns4 - whole) * 1.57079632679489661923);
+  constexpr double kQuarters = 0.63661977236758134308, kQuartersLow = -3.9357353350364970e-17;      // 2 / pi
+  const double angle = (double)p * (double)f, low = __builtin_fma((double)p, (double)f, -angle);
+  const double whole = __builtin_rint(angle * kQuarters);
+  const double part = __builtin_fma(angle, kQuarters, -whole) + __builtin_fma(angle, kQuartersLow, low * kQuarters);
+  const float x = (float)(part * 1.57079632679489661923);
   const float y = x * x;
   const float s = x + x * y * fmaf(y, fmaf(y, fmaf(y, 2.7557319e-6f, -1.9841270e-4f), 8.3333333e-3f), -1.6666667e-1f);
   const float c = fmaf(y, fmaf(y, fmaf(y, fmaf(y, fmaf(y, -2.7557319e-7f, 2.4801587e-5f), -1.3888889e-3f), 4.1666667e-2f), -0.5f), 1.f);

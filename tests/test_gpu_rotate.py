@@ -1,5 +1,8 @@
 """GPU: appended rows with the position rotation against its definition in 64
 bits.  The pools are NaN wherever no row was written."""
+import math
+from fractions import Fraction
+
 import numpy as np
 import pytest
 import torch
@@ -226,3 +229,36 @@ def test_heads_behind_each_other(gpu_lib, dtype, interleaved):
     torch.cuda.synchronize()
     assert torch.equal(back, want) and torch.equal(view, want)
     assert (heads[:, n:] == 7.0).all() and (heads[..., d:] == 7.0).all()
+
+
+PI = Fraction(31415926535897932384626433832795028841971693993751058209749445923, 10**64)     # 2^-212 off
+
+
+def _cos_sin(p, f):
+    """Of the exact product of a whole number and an fp32 number, to 2^-52 (the
+    product's turns are taken off in fractions: 2^46 of them are off by 2^-160)."""
+    a = Fraction(int(p)) * Fraction(float(f))
+    r = float(a - round(a / (2 * PI)) * 2 * PI)
+    return math.cos(r), math.sin(r)
+
+
+@pytest.mark.parametrize("largest", [1.0, 8.0, 1000.0, 16384.0])
+def test_cos_and_sin_of_any_angle(gpu_lib, largest):
+    """Rows of (1, 0) pairs turn into the angles' cos and sin themselves: off by
+    2^-23 at most, at all positions and frequencies up to 2^14."""
+    print(f"[case] rotate angles up to {largest}", flush=True)
+    rng = np.random.default_rng(int(largest))
+    n, pairs = 256, 64
+    pos = np.concatenate([rng.integers(-2**31, 2**31, 100), 2**31 - 1 - rng.integers(0, 1000, 50),
+                          -2**31 + rng.integers(0, 1000, 20), rng.integers(-2**24, 2**24, 50), np.arange(-18, 18)])
+    freq = (rng.random(pairs) * largest).astype(np.float32)
+    freq[:3] = largest, -largest, np.nextafter(np.float32(largest), np.float32(0))
+    p = Paged([0], [n], 1, 2 * pairs, dtype=F32, seed=8)
+    k = torch.zeros((n, 1, 2 * pairs), dtype=F32, device="cuda")
+    k[..., :pairs] = 1.0
+    p.cache.append_rotated(p.chunks(), k, k, torch.from_numpy(freq).cuda(),
+                           positions=torch.from_numpy(pos.astype(np.int32)).cuda())
+    torch.cuda.synchronize()
+    got = _rows(p)[0][:, 0].double().cpu().numpy()
+    want = np.array([[_cos_sin(x, f) for f in freq] for x in pos]).transpose(0, 2, 1).reshape(n, 2 * pairs)
+    assert np.abs(got - want).max() <= 2.0 ** -23, float(np.abs(got - want).max() * 2.0 ** 23)
