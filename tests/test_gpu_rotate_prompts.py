@@ -16,8 +16,8 @@ CASES = {
     "many_rows": ([0, 37, 1000, 3, 64], [1501, 7, 2002, 63, 650], 4, 2, 64, 64, 64, BF16),
     "many_rows_f32": ([5, 0, 31], [1502, 2001, 801], 5, 1, 96, 32, 64, F32),
     "one_prompt": ([7], [4099], 3, 3, 128, 96, 128, BF16),
-    "many_bytes": ([0, 100, 31, 7], [4001, 3, 3500, 3400], 32, 8, 128, 64, 128, BF16),      # 268 MB moved
-    "many_bytes_f32": ([9, 2], [4321, 1111], 32, 8, 128, 64, 128, F32),
+    "many_bytes": ([0, 100, 31, 7], [4001, 3, 3600, 3400], 32, 8, 128, 64, 128, BF16),      # 135 MB read and written
+    "many_bytes_f32": ([9, 2], [4321, 1211], 32, 8, 128, 64, 128, F32),
 }
 
 
