@@ -22,7 +22,8 @@ class Sampler:
     the batches.  Calls are serialised: one on another stream than the last waits
     for it.  A graph is captured from B.spec_sample with a workspace of its own: a
     replay would write this one beside later calls, so a call on a capturing stream
-    is refused.  An object is used by one thread at a time.
+    is refused, and one on another stream while the last call's captures.  An object
+    is used by one thread at a time.
 
     A call runs on `stream`, or the current one, after what is on it already; its
     tensors are its caller's to order and to keep, as for any work on a stream
@@ -43,6 +44,9 @@ class Sampler:
         """The next call runs on another stream than the last, whose use of the
         workspace it waits for."""
         if self._last is not None:
+            if B.stream_capturing(self._last_h):
+                # an event there belongs to the graph, and who waits for it does so too
+                raise RuntimeError("the last call's stream is capturing a graph, which would take this call in")
             stream.wait_event(self._last.record_event())
         if self._ws is not None:
             self._ws.record_stream(stream)
