@@ -98,8 +98,8 @@ class StagingRing:
 
     Calls are serialised: before a call on a stream other than the previous
     call's, that stream waits on an event recorded on the previous call's
-    stream after that call.  Calls that should run concurrently need objects
-    of their own.
+    stream after that call (refused while that stream captures a graph).  Calls
+    that should run concurrently need objects of their own.
     """
 
     def _ring(self, slots: list, event_every: int) -> None:
@@ -116,6 +116,9 @@ class StagingRing:
         another stream: the two share the workspace."""
         last = self._last_stream
         if last is not None and stream != last:
+            if B.stream_capturing(last.cuda_stream) and not B.stream_capturing(stream.cuda_stream):
+                # an event there belongs to the graph, and who waits for it does so too
+                raise RuntimeError("the last call's stream is capturing a graph, which would take this call in")
             ev = torch.cuda.Event()
             ev.record(last)
             stream.wait_event(ev)
@@ -177,8 +180,8 @@ class Verifier(StagingRing):
 
     def run(self, which: str = "verify", stream: Optional[torch.cuda.Stream] = None) -> None:
         stream = stream or torch.cuda.current_stream(self.batch.device)
-        s = self._slot(stream)
         self._order(stream)
+        s = self._slot(stream)
         stg = self._staging[s].data_ptr()
         h = stream.cuda_stream
         try:

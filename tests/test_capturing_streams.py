@@ -7,6 +7,7 @@ import pytest
 import torch
 
 from paper_2505_17074_amd import binding as B
+from paper_2505_17074_amd.batch import StagingRing
 from paper_2505_17074_amd.sample import Sampler
 
 
@@ -50,3 +51,40 @@ def test_a_sampler():
     CAPTURING[1] = False
     s._move(2, b)
     assert a.events == b.events == 1 and (s._last, s._last_h) == (b, 2)
+
+
+class _Event:
+    def record(self, stream):
+        stream.record_event()
+
+
+def test_a_staging_ring(monkeypatch):
+    monkeypatch.setattr(torch.cuda, "Event", _Event)
+    r, a, b = StagingRing(), _Stream(1), _Stream(2)
+    r._ring([None] * 4, 2)
+    r._order(a)
+    r._done(r._slot(a), a)
+    CAPTURING[1] = True
+    with pytest.raises(RuntimeError, match="captur"):
+        r._order(b)
+    assert a.events == b.events == 0 and r._last_stream is a and r._i == 1
+    CAPTURING[2] = True                        # both in one graph: it orders them
+    r._order(b)
+    assert a.events == b.events == 1
+    CAPTURING.clear()
+    r._order(a)
+    assert r._last_stream is a and a.events == b.events == 2
+
+
+def test_a_verifier_orders_before_it_takes_a_slot(monkeypatch):
+    """So that a refused call records nothing for the slots used before either."""
+    from paper_2505_17074_amd.batch import Verifier
+    monkeypatch.setattr(torch.cuda, "Event", _Event)
+    v, a, b = Verifier.__new__(Verifier), _Stream(1), _Stream(2)
+    v._ring([None] * 4, 2)
+    v._order(a)
+    v._done(v._slot(a), a)
+    CAPTURING[1] = True
+    with pytest.raises(RuntimeError, match="captur"):
+        v.run(stream=b)
+    assert a.events == b.events == 0 and v._pending == [0]
