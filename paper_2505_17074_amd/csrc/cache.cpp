@@ -105,8 +105,7 @@ struct ChunkPlan {
   std::vector<ChunkItem> items;
   std::vector<ChunkJoin> joins;
   std::vector<ChunkMeet> meets;
-  int32_t n_tall = 0;                      // the first items, of tall tiles; the others are low
-  bool two_parts = false;
+  bool tall = false, two_parts = false;
   sv::Keys keys = sv::kEvery;
   int32_t join_rows = 0, join_pieces = 0, meet_rows = 0, turn0 = 0, turn1 = 0;
   int32_t window = sv::kNoWindow, sinks = 0;
@@ -123,7 +122,6 @@ struct RowTile {
   int32_t len = 0, pieces = 0;
   int64_t part = -1;
   bool meets = false;       // joined with another tile's keys, whether cut or not
-  bool tall = false;
 };
 
 // A group of requests behind a shared prefix: its tiles of the prefix, and each
@@ -175,9 +173,9 @@ spec_status_t plan_chunk(const spec_chunks_t* r, const spec_cache_t* c, const sp
   // rows are those of all its group's requests, and go by themselves.
   int64_t most = 0;
   for (int i = 0; i < r->num_requests; ++i) most = std::max<int64_t>(most, (int64_t)r->new_len[i] * G);
-  bool tall = most > sv::kChunkLowRows;
-  int RT = tall ? sv::kChunkTallRows : sv::kChunkLowRows;
-  P.two_parts = !tall;                     // for a bf16 output: as without the prefixes
+  P.tall = most > sv::kChunkLowRows;
+  int RT = P.tall ? sv::kChunkTallRows : sv::kChunkLowRows;
+  P.two_parts = !P.tall;                   // for a bf16 output: as without the prefixes
   // Groups whose prefix is read once: whole 64-key tiles of it, what is left goes
   // with each request's own keys; where it saves more steps than the two partial
   // outputs of each row cost.  (32 requests of 10-200 tokens behind 4 prefixes of
@@ -205,8 +203,10 @@ spec_status_t plan_chunk(const spec_chunks_t* r, const spec_cache_t* c, const sp
       many |= rows > sv::kChunkLowRows;
       for (int i = at; i < at + groups->group_size[x]; ++i) prefix_of[i] = prefix;
     }
-    tall |= many;
-    if (tall) RT = sv::kChunkTallRows;
+    // the requests' own tiles are as tall as the prefixes' (their few rows are spread
+    // over the waves for d = 128, and leave three of four without any for d = 64)
+    P.tall |= many;
+    if (P.tall) RT = sv::kChunkTallRows;
   }
   P.keys = win ? sv::kWindowed : shared.empty() ? sv::kEvery : sv::kBehind;
   if (win) {
@@ -214,13 +214,12 @@ spec_status_t plan_chunk(const spec_chunks_t* r, const spec_cache_t* c, const sp
     P.sinks = std::min(win->sinks, sv::kNoWindow);
   }
   std::vector<RowTile> tiles;
-  // by height: low tiles, tall ones
-  int64_t q0 = 0, total[2] = {0, 0}, longest[2] = {0, 0}, cap[2], n_items[2] = {0, 0};
+  int64_t q0 = 0, total = 0, longest = 0;
   auto place = [&](const RowTile& t) {
     tiles.push_back(t);
     const int64_t kt = (t.keys + sv::kChunkTile - 1) / sv::kChunkTile;
-    total[t.tall] += kt * Hkv;
-    longest[t.tall] = std::max(longest[t.tall], kt);
+    total += kt * Hkv;
+    longest = std::max(longest, kt);
   };
   size_t next = 0;
   std::vector<size_t> own0;                // each request's first tile of its own, where a prefix is shared
@@ -234,7 +233,6 @@ spec_status_t plan_chunk(const spec_chunks_t* r, const spec_cache_t* c, const sp
       for (int r0 = 0; r0 < rows; r0 += RT) {
         RowTile t{i, r0, std::min(RT, rows - r0), x.prefix, (int32_t)q0, x.prefix, 0, r->num_requests + (int32_t)next};
         t.meets = true;
-        t.tall = tall;
         place(t);
       }
       ++next;
@@ -252,14 +250,14 @@ spec_status_t plan_chunk(const spec_chunks_t* r, const spec_cache_t* c, const sp
       }
       RowTile t{i, r0, nr, r->ctx_len[i] + (r0 + nr - 1) / G + 1 - skip, (int32_t)q0, r->ctx_len[i] - skip, skip, i};
       t.meets = prefix > 0;
-      t.tall = tall;
       place(t);
     }
     q0 += n;
   }
   const int cus = compute_units();
   // A row tile's keys in equal pieces of at most so many 64-key tiles.
-  {
+  int64_t cap;
+  if (!P.tall) {
     // Few rows: the keys stream past them at HBM's rate whatever the pieces, so
     // they are cut to 16 / 3 of them a compute unit, about what runs there at once
     // for d = 128 (five, by their 32 KB of LDS), where the last ones to end lose
@@ -269,14 +267,13 @@ spec_status_t plan_chunk(const spec_chunks_t* r, const spec_cache_t* c, const sp
     // 15.2 and 14.6.  All at d = 128; d = 64 goes by the same rule, though ten would
     // fit: 64 single tokens over 4000 rows of 8 KV heads (524 MB) 86 us, 6.1 TB/s.
     const int64_t slots = 4 * (int64_t)cus;
-    cap[0] = std::max<int64_t>(total[0] <= cus ? 1 : 2, (3 * total[0] + 4 * slots - 1) / (4 * slots));
+    cap = std::max<int64_t>(total <= cus ? 1 : 2, (3 * total + 4 * slots - 1) / (4 * slots));
     // Windows make them about equally long, and two of those a compute unit leave
     // nothing to balance that a join would be paid for (64 single tokens, windows of
     // 1024: pieces of 7 tiles 58 us, whole 55).
     const int64_t n = (int64_t)tiles.size() * Hkv;
-    if (win && n >= 2 * (int64_t)cus && 4 * longest[0] * n <= 5 * total[0]) cap[0] = longest[0];
-  }
-  {
+    if (win && n >= 2 * (int64_t)cus && 4 * longest * n <= 5 * total) cap = longest;
+  } else {
     // Many rows: a compute unit takes a 64-key tile in about a microsecond,
     // whether one work-group runs on it or two (1.1-1.2 and 0.94), so the longest
     // item bounds the kernel only where it is longer than a unit's mean share.
@@ -289,21 +286,22 @@ spec_status_t plan_chunk(const spec_chunks_t* r, const spec_cache_t* c, const sp
     // 4 17.  Decoding requests beside a chunk run in the same launch (beside 8
     // chunks of 33-700 tokens, 16 single ones: 181 us, in a launch of their own
     // before it 198).
-    const int64_t mean = (total[1] + cus - 1) / cus;
-    cap[1] = longest[1] <= mean + 7 ? longest[1] : std::max<int64_t>(4, mean);
+    const int64_t mean = (total + cus - 1) / cus;
+    cap = longest <= mean + 7 ? longest : std::max<int64_t>(4, mean);
     // A prefix's tiles are long beside the requests' own, which fill the other
     // halves of their units (64 single tokens behind 8000 rows: pieces of 12 tiles
     // 37.9 us, of the mean, 15, 39.3, of 10 39.3, of 8 43.8).
-    if (P.keys == sv::kBehind && longest[1] > mean + 7) cap[1] = std::max<int64_t>(4, 4 * mean / 5);
+    if (P.keys == sv::kBehind && longest > mean + 7) cap = std::max<int64_t>(4, 4 * mean / 5);
   }
+  int64_t n_items = 0;
   for (RowTile& t : tiles) {
     const int64_t kt = (t.keys + sv::kChunkTile - 1) / sv::kChunkTile;
-    const int64_t pieces = (kt + cap[t.tall] - 1) / cap[t.tall];
+    const int64_t pieces = (kt + cap - 1) / cap;
     t.len = (int32_t)((kt + pieces - 1) / pieces);
     t.pieces = (int32_t)((kt + t.len - 1) / t.len);
-    n_items[t.tall] += t.pieces;
+    n_items += t.pieces;
   }
-  if ((n_items[0] + n_items[1]) * Hkv >= (int64_t)1 << 24) return SPEC_ERR_UNSUPPORTED;      // a launch's work-items are 32 bits
+  if (n_items * Hkv >= (int64_t)1 << 24) return SPEC_ERR_UNSUPPORTED;      // a launch's work-items are 32 bits
   // The longest first, so that the last to start are the shortest; after each,
   // its request's neighbouring row tiles down to 7 / 8 of its length, which
   // read the same keys at the same time.  With the heads innermost they also
@@ -315,9 +313,7 @@ spec_status_t plan_chunk(const spec_chunks_t* r, const spec_cache_t* c, const sp
   std::vector<int32_t> order, sorted(tiles.size());
   order.reserve(tiles.size());
   for (size_t i = 0; i < tiles.size(); ++i) sorted[i] = (int32_t)i;
-  std::stable_sort(sorted.begin(), sorted.end(), [&](int32_t x, int32_t y) {
-    return tiles[x].tall != tiles[y].tall ? tiles[x].tall : tiles[x].len > tiles[y].len;
-  });
+  std::stable_sort(sorted.begin(), sorted.end(), [&](int32_t x, int32_t y) { return tiles[x].len > tiles[y].len; });
   std::vector<bool> placed(tiles.size(), false);
   for (const int32_t x : sorted) {
     if (placed[x]) continue;
@@ -334,8 +330,7 @@ spec_status_t plan_chunk(const spec_chunks_t* r, const spec_cache_t* c, const sp
         order.push_back((int32_t)y);
       }
   }
-  P.items.reserve((size_t)(n_items[0] + n_items[1]));
-  P.n_tall = (int32_t)n_items[1];
+  P.items.reserve((size_t)n_items);
   for (const int32_t x : order) {
     RowTile& t = tiles[x];
     const int32_t len = t.len * sv::kChunkTile;
@@ -372,9 +367,9 @@ spec_status_t plan_chunk(const spec_chunks_t* r, const spec_cache_t* c, const sp
   // work-groups b and b + cus of the tall kernel share a compute unit at first
   // (d = 128; with d = 64 a third joins them): the longest with the shortest of
   // the first two rounds
-  if (n_items[1] * Hkv > cus) {
+  if (P.tall && n_items * Hkv > cus) {
     P.turn0 = cus;
-    P.turn1 = (int32_t)std::min<int64_t>(n_items[1] * Hkv, 2 * (int64_t)cus);
+    P.turn1 = (int32_t)std::min<int64_t>(n_items * Hkv, 2 * (int64_t)cus);
   }
 
   P.off_joins = align_up(sizeof(ChunkItem) * P.items.size());
@@ -546,9 +541,8 @@ spec_status_t chunk_attn(const spec_chunks_t* chunks, const spec_cache_t* cache,
     if (P.joins.size() == 1) j.one = P.joins[0];
     else j.joins = reinterpret_cast<const ChunkJoin*>(plan + P.off_joins);
     const sv::MeetParams m = {p.out, p.part, reinterpret_cast<const ChunkMeet*>(plan + P.off_meets), p.Hkv, p.G};
-    const sv::ChunkLaunch l = {P.n_tall, (int32_t)P.items.size() - P.n_tall, (int32_t)P.joins.size(), cache->head_dim,
-                               args->out_dtype == SPEC_F32, P.two_parts, P.join_rows, P.join_pieces, P.keys,
-                               (int32_t)P.meets.size(), P.meet_rows};
+    const sv::ChunkLaunch l = {(int32_t)P.items.size(), (int32_t)P.joins.size(), cache->head_dim, args->out_dtype == SPEC_F32,
+                               P.tall, P.two_parts, P.join_rows, P.join_pieces, P.keys, (int32_t)P.meets.size(), P.meet_rows};
     return sv::launch_chunk(p, j, m, l, s) == hipSuccess ? SPEC_OK : SPEC_ERR_HIP;
   });
 }

@@ -945,22 +945,17 @@ __global__ __launch_bounds__(256) void chunk_meet(MeetParams p) {
 template <int D, bool F32, Keys KEYS>
 static hipError_t launch_d(const ChunkParams& p, const JoinParams& j, const MeetParams& m, const ChunkLaunch& l,
                            hipStream_t s) {
-  // a prefix's tall tiles beside low ones of the requests' own: P as in these
-  constexpr int TALL = F32 ? 3 : 1, BESIDE = F32 ? 3 : KEYS == kBehind ? 2 : 1, NG = 1024 / D;
-  hipError_t e = hipSuccess;
-  if (l.n_tall > 0) {
-    const dim3 g(l.n_tall * p.Hkv);
-    if (l.two_parts) chunk_attn<D, 4, 64, 2, BESIDE, F32, KEYS><<<g, dim3(256), 0, s>>>(p);
-    else chunk_attn<D, 4, 64, 2, TALL, F32, KEYS><<<g, dim3(256), 0, s>>>(p);
-    e = hipGetLastError();
+  constexpr int NG = 1024 / D;
+  const dim3 g(l.n_items * p.Hkv);
+  if (!l.tall) {
+    chunk_attn<D, 1, 32, 2, F32 ? 3 : 2, F32, KEYS><<<g, dim3(64), 0, s>>>(p);
+  } else if (KEYS == kBehind && l.two_parts) {
+    // a group's rows fill tall tiles where its requests' own would not: P as in theirs
+    chunk_attn<D, 4, 64, 2, F32 ? 3 : KEYS == kBehind ? 2 : 1, F32, KEYS><<<g, dim3(256), 0, s>>>(p);
+  } else {
+    chunk_attn<D, 4, 64, 2, F32 ? 3 : 1, F32, KEYS><<<g, dim3(256), 0, s>>>(p);
   }
-  if (e == hipSuccess && l.n_low > 0) {
-    ChunkParams low = p;
-    low.items += l.n_tall;
-    low.turn0 = low.turn1 = 0;
-    chunk_attn<D, 1, 32, 2, F32 ? 3 : 2, F32, KEYS><<<dim3(l.n_low * p.Hkv), dim3(64), 0, s>>>(low);
-    e = hipGetLastError();
-  }
+  hipError_t e = hipGetLastError();
   if (e == hipSuccess && KEYS == kBehind && l.n_meets > 0) {
     chunk_meet<D, F32><<<dim3(l.n_meets * p.Hkv, (l.meet_rows + NG - 1) / NG), dim3(256), 0, s>>>(m);
     e = hipGetLastError();

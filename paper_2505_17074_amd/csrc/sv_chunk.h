@@ -99,12 +99,11 @@ static_assert(sizeof(ChunkParams) <= kSmallArgs && sizeof(JoinParams) <= kSmallA
 
 // What the launches go by.
 struct ChunkLaunch {
-  int32_t n_tall, n_low;               // items of one KV head: up to kChunkTallRows rows on four
-                                       // waves, then up to kChunkLowRows on one
-  int32_t n_joins;
+  int32_t n_items, n_joins;            // of one KV head
   int32_t D;
   bool out_f32;
-  bool two_parts;       // a bf16 output: P in two bf16 parts in tall tiles too
+  bool tall;            // items of up to kChunkTallRows rows on four waves, else kChunkLowRows on one
+  bool two_parts;       // a bf16 output: P in two bf16 parts, in tall items (kBehind) too
   int32_t join_rows;    // rows of the tallest joined tile
   int32_t join_pieces;  // pieces of the longest
   Keys keys;            // what the items leave out
