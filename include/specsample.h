@@ -68,11 +68,25 @@ typedef enum spec_sample_rows {
  * 64 bits, top-p's in fixed point: n weights to n^2 2^-61 of the largest (7e-9 for
  * 128256 of them) at the worst.  Tokens and the sets that stay are those of the
  * definition unless a sum is that near to its border.  Results are deterministic.
- * A row costs two reads of its logits and of some of them a third; one whose top-p
- * cut lies among more than 2048 tokens within T / 64 of each other's logits (logits
- * that are nearly all the same), or behind a top-k of more than 512 that leaves more
- * than 2048 near its own cut, is searched by one work-group alone: 0.2-0.45 ms for
- * 32000-128256 tokens.
+ * A row costs two reads of its logits and of some of them a third.  These rows are
+ * searched by one work-group alone instead, 0.06-0.45 ms for 32000-128256 tokens
+ * where others take 0.01-0.06:
+ *   top-k from 1025 on with a top-p below one, whatever the logits, and from 513 on
+ *     with one where no more than top_k tokens are not masked out;
+ *   top-k whose last token has others within 1/32 of its logit (whatever T), equal
+ *     ones among them, so that they, and for a top_k of up to 1024 all tokens before
+ *     them, are more than 2048; or whose last token is more than 62 below the
+ *     largest logit;
+ *   a top_k of up to 512 where the large logits, or all that a mask leaves, have
+ *     neighbouring ids: its last token is looked for among the largest of each of
+ *     1024 threads, which read 16 bytes of a row in turn, and then more than 2048
+ *     tokens may be above what they have (3000 neighbours in bf16 are 375 threads',
+ *     for a top_k of 400);
+ *   top-p alone with its cut among more than 2048 tokens within T / 64 of each
+ *     other's logits (logits that are nearly all the same), or so near one that
+ *     tokens below e^-31 of the largest weight make it up (rows of millions);
+ *   a largest logit of 2^18 and above in magnitude with top-k, of 2^17 T with top-p
+ *     alone (T very small, or infinite).
  */
 typedef struct spec_sample_args {
   int32_t num_rows;

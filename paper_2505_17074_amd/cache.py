@@ -325,8 +325,9 @@ class ChunkAttention(StagingRing):
     grows with the batches, and `ring` pinned staging buffers (StagingRing).  A
     graph is captured from B.spec_chunk_attn with a workspace and staging of its
     own: a replay reads the staging it was captured with, and here the ring
-    reuses its slots, so a call on a capturing stream is refused.  An object is
-    used by one thread at a time."""
+    reuses its slots, so a call on a capturing stream is refused, and one on
+    another stream while the last call's captures.  An object is used by one
+    thread at a time."""
 
     def __init__(self, cache: PagedCache, num_q_heads: int, scale: float = 0.0, ring: int = 32, event_every: int = 8,
                  window: Optional[int] = None, sinks: int = 0):

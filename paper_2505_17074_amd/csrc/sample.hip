@@ -11,17 +11,19 @@
 // that no sum depends on the order of its terms.
 //
 // What bounds it (calls in a row): latency and launches where it is small, a wave's
-// instructions where it is large, never HBM.
-//   one row of 32000 (fp32), top-k and top-p: 9.1 us (10.9 with two barriers for each
-//     of the work-group's sums and searches), one kernel of 8.4: load and largest value
-//     1.7, histogram 1.2, the list 2, its two orders and the sums 3.
+// instructions and its waits for LDS and barriers, about half each, where it is
+// large, never HBM.
+//   one row of 32000 (fp32), top-k and top-p: 9-12 us by the logits; where 9.1 (10.9
+//     with two barriers for each of the work-group's sums and searches), one kernel of
+//     8.4: load and largest value 1.7, histogram 1.2, the list 2, its two orders and the
+//     sums 3.
 //   64 of them, all filters, the rows written (16 MB): 32 us, three kernels of 8, 11
 //     and 15.5 with 3.5 between their first and last work-groups' ends and starts;
 //     rows with top-p alone, and those of 400 tokens, are the last to end.
 //   128 of 128256 (bf16), top-p (33 MB, 5 us at HBM's rate): 49 us, three kernels of
 //     16, 21 and 13: 17 vector instructions and an LDS operation an element in the
-//     first, 23 in the second, on one work-group a compute unit (two of them
-//     with half the registers measured the same).
+//     first, 23 in the second (8.5 and 11 us at four cycles each), on one work-group a
+//     compute unit (two of them with half the registers measured the same).
 #include "sv_sample.h"
 
 #include <type_traits>
