@@ -111,14 +111,20 @@ class StagingRing:
         self._i = 0                        # calls issued
         self._last_stream = None           # stream of the previous call (workspace owner)
 
+    def _not_into_a_graph(self, stream):
+        """Refuses a call that would have to wait for an event of a stream that
+        captures a graph: the event belongs to the graph, and who waits for it
+        does so too."""
+        last = self._last_stream
+        if last is not None and stream != last and B.stream_capturing(last.cuda_stream) and \
+                not B.stream_capturing(stream.cuda_stream):
+            raise RuntimeError("the last call's stream is capturing a graph, which would take this call in")
+
     def _order(self, stream):
         """Make `stream` wait for the previous call when that call ran on
         another stream: the two share the workspace."""
         last = self._last_stream
         if last is not None and stream != last:
-            if B.stream_capturing(last.cuda_stream) and not B.stream_capturing(stream.cuda_stream):
-                # an event there belongs to the graph, and who waits for it does so too
-                raise RuntimeError("the last call's stream is capturing a graph, which would take this call in")
             ev = torch.cuda.Event()
             ev.record(last)
             stream.wait_event(ev)
@@ -180,8 +186,9 @@ class Verifier(StagingRing):
 
     def run(self, which: str = "verify", stream: Optional[torch.cuda.Stream] = None) -> None:
         stream = stream or torch.cuda.current_stream(self.batch.device)
-        self._order(stream)
+        self._not_into_a_graph(stream)
         s = self._slot(stream)
+        self._order(stream)
         stg = self._staging[s].data_ptr()
         h = stream.cuda_stream
         try:

@@ -413,6 +413,7 @@ class ChunkAttention(StagingRing):
             if B.stream_capturing(h):
                 raise RuntimeError("a graph's calls need a workspace and staging of their own: capture B.spec_chunk_attn")
             stream = stream or cache._streams[h]
+            self._not_into_a_graph(stream)
             self._order(stream)
             for grown in (False, True):
                 s = self._slot(stream)
